@@ -63,7 +63,9 @@ enum {
                              lay outside the fp16 range +-65504 (or was not a number) and was saturated to the nearest
                              finite value.  Nothing is disabled: no infinity or NaN is produced, the call completes, but
                              the affected rows no longer follow the arithmetic stated at mn_verify_forward */
-  MN_DEV_CTX = 32         /* ctx_b + k_b + 1 exceeds the max_ctx the host passed (the sequence is a no-op) */
+  MN_DEV_CTX = 32,        /* ctx_b + k_b + 1 exceeds the max_ctx the host passed (the sequence is a no-op) */
+  MN_DEV_POOL = 64,       /* mn_kv_reserve: not enough free blocks */
+  MN_DEV_SEQ = 128        /* page pool: a slot out of range, a child's slot that is in use, or one filled twice by a call */
 };
 
 /* Limits (checked; MN_EINVAL / MN_EUNSUPPORTED beyond them). */
@@ -321,6 +323,57 @@ void mn_selector_destroy(mn_selector *sel);
 mn_status mn_selector_observe(mn_selector *sel, double t_llm, double vl, int *s_out, double *slope_out);
 int mn_selector_current(const mn_selector *sel);   /* -1 when sel is NULL */
 long mn_selector_adjustments(const mn_selector *sel); /* decisions taken so far; -1 when sel is NULL */
+
+/* ---- the page pool (section 4: blocks behind the table, and their release) --------------------------
+ * Which slot (row of the block table) holds which physical blocks, kept on the device beside the table so that no step
+ * waits for the host.  A block may be in several rows: requests forked from one prompt share its pages (block_refs > 1) until
+ * one of them is about to write.  All of it is the caller's memory:
+ *   block_tables dev [max_seqs][max_blocks_per_seq], the array that mn_kv.block_tables points at
+ *   block_refs   dev [num_blocks]: rows holding the block, 0 = free.  Start: zeros, or 1 for every block in a table.
+ *   seq_blocks   dev [max_seqs]: blocks that the slot holds, the first entries of its row.  Start: zeros, or what the rows hold.
+ *   ctx_lens     is mn_kv.ctx_lens, dev [max_seqs]; an empty slot has 0 blocks and 0 tokens.
+ * Decisions follow from this state alone (lowest free block first, in the order of slot and position), so equal calls give equal
+ * tables.  Whatever a call cannot do it leaves as it was and reports in *dev_status (or NULL): a damaged row (an id out of
+ * range, a context longer than its blocks) is MN_DEV_BLOCK_TABLE.
+ * n <= max_seqs <= MN_MAX_BATCH and B <= max_seqs; n = 0 and B = 0 are no-ops. */
+typedef struct {
+  int32_t *block_tables, *block_refs, *seq_blocks;
+  int max_seqs;
+} mn_pool;
+
+/* Bytes of workspace that mn_kv_reserve and mn_kv_compact need (256-byte aligned; nothing is kept in it between calls).
+ * 0 on invalid arguments. */
+size_t mn_kv_workspace_bytes(int num_blocks, int max_seqs);
+
+/* Room for the next step: afterwards slot b < B may be written up to position tokens[b] - 1 (ctx_b + k_b + 1 tokens ahead of a
+ * step; a slot with tokens[b] <= ctx_lens[b] is left alone).  Blocks that the row lacks are added, and shared blocks at
+ * positions from ctx_lens[b] on are replaced by blocks of its own, the one that holds tokens already with a copy of its page in
+ * every layer.  All sharers of a block that write in this call get one (the old block is free when none is left).  Slots are
+ * served in order; the first one whose blocks the pool does not have, and every one behind it that needs a block, is left as it
+ * was (MN_DEV_POOL), and so is one whose tokens exceed the table (MN_DEV_BLOCK_TABLE).
+ *   tokens dev [B] */
+mn_status mn_kv_reserve(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, const int32_t *tokens, int B, void *workspace,
+                        size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* Slot dst[i] becomes a copy of slot src[i]: the blocks of its ctx_lens tokens, shared, and its context.  No page moves; the
+ * child's own tokens get their pages from mn_kv_reserve.  Pairs are judged by the state at entry; one whose slots are out of
+ * range or the same, whose dst is in use or is filled by an earlier pair, or whose src is filled by this call, is left out
+ * (MN_DEV_SEQ).
+ *   src, dst dev [n] */
+mn_status mn_kv_fork(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, const int32_t *src, const int32_t *dst, int n,
+                     int32_t *dev_status, void *stream);
+
+/* Slots seqs[i] are emptied: one reference less on each of their blocks, table entries -1, no tokens.  An empty slot, or one
+ * listed twice, is fine.
+ *   seqs dev [n] */
+mn_status mn_kv_free(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, const int32_t *seqs, int n, int32_t *dev_status, void *stream);
+
+/* Packs the pool: afterwards the live blocks are exactly the ids below their number, *n_live.  The live blocks from that id on, in
+ * ascending order, move to the free ids below it, in ascending order, their pages in every layer and every table entry with
+ * them (shared blocks stay shared; the vacated pages keep their bytes).
+ *   n_live dev [1] (out) or NULL */
+mn_status mn_kv_compact(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, int32_t *n_live, void *workspace, size_t workspace_bytes,
+                        int32_t *dev_status, void *stream);
 
 /* ---- measuring sticks (no part of the method) ---------------------------------------------------
  * For callers who cannot bring their own microbenchmarks: what a plain streaming read and a dense fp16

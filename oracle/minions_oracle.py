@@ -569,3 +569,99 @@ class Selector:
             self.samples = []
             self.adjustments += 1
         return self.s
+
+
+# --------------------------------------------------------------------------
+# the page pool: blocks behind the table (section 4, block manager)
+# --------------------------------------------------------------------------
+
+class PagePool:
+    """Block tables as lists, one decision after the other.  ``pages`` are arrays whose first axis is the physical block (any
+    number of them: every layer's K and V); they move with the blocks.  Status bits: 1 damaged row or table too short, 64 not enough free blocks,
+    128 slots that do not fit together."""
+
+    TABLE, EMPTY, SLOT = 1, 64, 128
+
+    def __init__(self, tables, refs, held, ctx, block_size, pages=()):
+        self.width, self.bs = tables.shape[1], block_size
+        self.table = np.array(tables, np.int64)
+        self.refs, self.held, self.ctx = (np.array(a, np.int64) for a in (refs, held, ctx))
+        self.pages = [np.array(p) for p in pages]
+        self.status = 0
+
+    def _row_ok(self, s):
+        c, h = self.ctx[s], self.held[s]
+        return c >= 0 and 0 <= h <= self.width and -(-c // self.bs) <= h
+
+    def reserve(self, tokens):
+        before, free = self.refs.copy(), [i for i, r in enumerate(self.refs) if r == 0]
+        demand = 0
+        for b, t in enumerate(tokens):
+            if t <= max(self.ctx[b], 0):
+                continue
+            first, need = self.ctx[b] // self.bs, -(-t // self.bs)
+            if not self._row_ok(b) or need > self.width or any(not 0 <= i < len(before) for i in self.table[b, first:min(need, self.held[b])]):
+                self.status |= self.TABLE
+                continue
+            want = [at for at in range(first, need) if at >= self.held[b] or before[self.table[b, at]] > 1]
+            if not want:
+                continue
+            demand += len(want)
+            if demand > len(free):
+                self.status |= self.EMPTY
+                continue
+            for at, new in zip(want, free[demand - len(want):demand]):
+                self.refs[new] = 1
+                if at < self.held[b]:
+                    old = self.table[b, at]
+                    self.refs[old] -= 1
+                    if at * self.bs < self.ctx[b]:
+                        for p in self.pages:
+                            p[new] = p[old]
+                self.table[b, at] = new
+            self.held[b] = max(self.held[b], need)
+
+    def fork(self, src, dst):
+        slots = range(len(self.held))
+        for i, (s, d) in enumerate(zip(src, dst)):
+            if s not in slots or d not in slots or s == d or d in dst[:i] or s in dst or self.held[d] or self.ctx[d]:
+                self.status |= self.SLOT
+                continue
+            n = -(-self.ctx[s] // self.bs)
+            row = self.table[s, :max(n, 0)]
+            if self.ctx[s] < 0 or n > self.held[s] or n > self.width or any(not 0 <= k < len(self.refs) for k in row):
+                self.status |= self.TABLE
+                continue
+            self.table[d, :n] = row
+            self.refs[row] += 1
+            self.held[d], self.ctx[d] = n, self.ctx[s]
+
+    def free(self, seqs):
+        for s in seqs:
+            if not 0 <= s < len(self.held):
+                self.status |= self.SLOT
+                continue
+            n = int(np.clip(self.held[s], 0, self.width))
+            if n != self.held[s]:
+                self.status |= self.TABLE
+            for k in range(n):
+                i = self.table[s, k]
+                if 0 <= i < len(self.refs) and self.refs[i] > 0:
+                    self.refs[i] -= 1
+                else:
+                    self.status |= self.TABLE
+                self.table[s, k] = -1
+            self.held[s] = self.ctx[s] = 0
+
+    def compact(self):
+        live = [i for i, r in enumerate(self.refs) if r > 0]
+        n = len(live)
+        move = dict(zip([i for i in live if i >= n], [i for i in range(n) if self.refs[i] <= 0]))
+        for a, b in move.items():
+            self.refs[b], self.refs[a] = self.refs[a], 0
+            for p in self.pages:
+                p[b] = p[a]
+        for s in range(len(self.held)):
+            for k in range(int(np.clip(self.held[s], 0, self.width))):
+                self.table[s, k] = move.get(self.table[s, k], self.table[s, k])
+        return n

@@ -18,6 +18,7 @@ MN_ARCH_OPT, MN_ARCH_LLAMA = 0, 1
 MN_DT_F32, MN_DT_BF16 = 0, 1
 MN_VOTE_TREE, MN_VOTE_COLUMN = 0, 1
 MN_DEV_BLOCK_TABLE, MN_DEV_SPEC_LEN, MN_DEV_TOKEN, MN_DEV_DRAFTS, MN_DEV_RANGE, MN_DEV_CTX = 1, 2, 4, 8, 16, 32
+MN_DEV_POOL, MN_DEV_SEQ = 64, 128
 MN_MAX_DRAFTS, MN_MAX_BATCH, MN_MAX_SPLIT_K = 64, 4096, 16
 MN_NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -27,6 +28,7 @@ EXPORTS = ("mn_create", "mn_destroy", "mn_last_error", "mn_status_str", "mn_work
            "mn_profile_collect", "mn_packed_weight_bytes", "mn_pack_weight", "mn_acr_update",
            "mn_verify_sample", "mn_draft_sample",
            "mn_selector_create", "mn_selector_destroy", "mn_selector_observe", "mn_selector_current",
+           "mn_kv_workspace_bytes", "mn_kv_reserve", "mn_kv_fork", "mn_kv_free", "mn_kv_compact",
            "mn_selector_adjustments", "mn_probe_stream_read", "mn_probe_mfma", "mn_probe_mfma_data")
 PROF_KINDS = ("prepare", "norm", "gemm", "rope_append", "attention", "act", "argmax", "vote", "accept")
 
@@ -50,6 +52,10 @@ class Weights(C.Structure):
 class KV(C.Structure):
     _fields_ = [("k_layers", _PP), ("v_layers", _PP), ("block_size", C.c_int), ("num_blocks", C.c_int),
                 ("max_blocks_per_seq", C.c_int), ("block_tables", C.c_void_p), ("ctx_lens", C.c_void_p)]
+
+
+class Pool(C.Structure):
+    _fields_ = [("block_tables", C.c_void_p), ("block_refs", C.c_void_p), ("seq_blocks", C.c_void_p), ("max_seqs", C.c_int)]
 
 
 def _load() -> C.CDLL:
@@ -92,6 +98,16 @@ def _load() -> C.CDLL:
                                     C.c_long, vp]
     lib.mn_acr_update.restype = i32
     lib.mn_acr_update.argtypes = [vp, vp, vp, vp, vp, i32, i32, C.c_double, C.c_double, C.c_float, C.c_float, vp, vp, vp]
+    lib.mn_kv_workspace_bytes.restype = sz
+    lib.mn_kv_workspace_bytes.argtypes = [i32, i32]
+    lib.mn_kv_reserve.restype = i32
+    lib.mn_kv_reserve.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, i32, vp, sz, vp, vp]
+    lib.mn_kv_fork.restype = i32
+    lib.mn_kv_fork.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, vp, i32, vp, vp]
+    lib.mn_kv_free.restype = i32
+    lib.mn_kv_free.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, i32, vp, vp]
+    lib.mn_kv_compact.restype = i32
+    lib.mn_kv_compact.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, vp, sz, vp, vp]
     lib.mn_selector_create.restype = i32
     lib.mn_selector_create.argtypes = [C.POINTER(vp), i32, i32, i32, i32, i32, i32]
     lib.mn_selector_destroy.restype = None
@@ -225,6 +241,26 @@ def mn_acr_update(ctx, voted_ssm, accepted_len, spec_len, n_out, B, n, reward_th
                   reward_factor, punish_factor, ssm_w, acr=None, stream=None) -> None:
     _check(lib.mn_acr_update(ctx, voted_ssm, accepted_len, spec_len, n_out, B, n, reward_threshold, punish_threshold,
                              reward_factor, punish_factor, ssm_w, acr, stream), ctx)
+
+
+def mn_kv_workspace_bytes(num_blocks: int, max_seqs: int) -> int:
+    return int(lib.mn_kv_workspace_bytes(num_blocks, max_seqs))
+
+
+def mn_kv_reserve(ctx, kv: KV, pool: Pool, tokens, B, workspace, workspace_bytes, dev_status=None, stream=None) -> None:
+    _check(lib.mn_kv_reserve(ctx, C.byref(kv), C.byref(pool), tokens, B, workspace, workspace_bytes, dev_status, stream), ctx)
+
+
+def mn_kv_fork(ctx, kv: KV, pool: Pool, src, dst, n, dev_status=None, stream=None) -> None:
+    _check(lib.mn_kv_fork(ctx, C.byref(kv), C.byref(pool), src, dst, n, dev_status, stream), ctx)
+
+
+def mn_kv_free(ctx, kv: KV, pool: Pool, seqs, n, dev_status=None, stream=None) -> None:
+    _check(lib.mn_kv_free(ctx, C.byref(kv), C.byref(pool), seqs, n, dev_status, stream), ctx)
+
+
+def mn_kv_compact(ctx, kv: KV, pool: Pool, n_live, workspace, workspace_bytes, dev_status=None, stream=None) -> None:
+    _check(lib.mn_kv_compact(ctx, C.byref(kv), C.byref(pool), n_live, workspace, workspace_bytes, dev_status, stream), ctx)
 
 
 def mn_selector_create(s_init: int, s_min: int, s_max: int, decision_threshold: int, s_penalty: int,

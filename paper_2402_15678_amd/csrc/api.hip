@@ -747,6 +747,101 @@ extern "C" mn_status mn_attention(mn_ctx* c, const void* q, const int32_t* spec_
   return hip_check(c, who);
 }
 
+// ---- page pool ----------------------------------------------------------------------------------------
+static mn_status check_pool(mn_ctx* c, const mn_kv* kv, const mn_pool* pool, int n, int32_t* status, bool pages, const char* who, PoolView* out) {
+  if (!kv || !pool) return fail(c, MN_ENULL, "%s: kv or pool is NULL", who);
+  if (!kv->block_tables || !kv->ctx_lens || !pool->block_tables || !pool->block_refs || !pool->seq_blocks)
+    return fail(c, MN_ENULL, "%s: a member of kv or pool is NULL", who);
+  if (kv->block_tables != pool->block_tables) return fail(c, MN_EINVAL, "%s: kv and pool have different block tables", who);
+  if (kv->block_size <= 0 || kv->num_blocks <= 0 || kv->max_blocks_per_seq <= 0)
+    return fail(c, MN_EINVAL, "%s: block_size/num_blocks/max_blocks_per_seq", who);
+  if (pool->max_seqs < 1 || pool->max_seqs > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: max_seqs = %d outside [1, %d]", who, pool->max_seqs, MN_MAX_BATCH);
+  if (n < 0 || n > pool->max_seqs) return fail(c, MN_EINVAL, "%s: %d sequences of %d slots", who, n, pool->max_seqs);
+  if (pages) {
+    if (!kv->k_layers || !kv->v_layers) return fail(c, MN_ENULL, "%s: k_layers or v_layers is NULL", who);
+    for (int l = 0; l < c->d.n_layers; ++l)
+      if (!kv->k_layers[l] || !kv->v_layers[l]) return fail(c, MN_ENULL, "%s: kv layer %d pointer is NULL", who, l);
+    if (((uint64_t)kv->block_size * c->d.n_kv_heads * c->d.head_dim * 4) >> 34) return fail(c, MN_EUNSUPPORTED, "%s: blocks of %d tokens", who, kv->block_size);
+  }
+  *out = PoolView{pool->block_tables, pool->block_refs, pool->seq_blocks, kv->ctx_lens, pool->max_seqs, kv->max_blocks_per_seq, kv->num_blocks,
+                  kv->block_size, status};
+  return MN_OK;
+}
+
+static mn_status check_pool_workspace(mn_ctx* c, const PoolView& p, const void* workspace, size_t bytes, const char* who) {
+  if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
+  if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
+  const size_t need = pool_work_bytes(p.num_blocks, p.max_seqs);
+  if (bytes < need) return fail(c, MN_EWORKSPACE, "%s: workspace %zu bytes, need %zu", who, bytes, need);
+  return MN_OK;
+}
+
+static size_t page_bytes(const mn_ctx* c, const mn_kv* kv) {
+  return (size_t)kv->block_size * c->d.n_kv_heads * c->d.head_dim * (c->d.dtype == MN_DT_BF16 ? 2 : 4);
+}
+
+extern "C" size_t mn_kv_workspace_bytes(int num_blocks, int max_seqs) {
+  if (num_blocks < 1 || max_seqs < 1 || max_seqs > MN_MAX_BATCH) return 0;
+  return pool_work_bytes(num_blocks, max_seqs);
+}
+
+extern "C" mn_status mn_kv_reserve(mn_ctx* c, mn_kv* kv, const mn_pool* pool, const int32_t* tokens, int B, void* workspace,
+                                   size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  const char* who = "mn_kv_reserve";
+  if (!c) return MN_ENULL;
+  PoolView p;
+  if (mn_status s = check_pool(c, kv, pool, B, dev_status, true, who, &p)) return s;
+  if (mn_status s = check_pool_workspace(c, p, workspace, workspace_bytes, who)) return s;
+  if (B == 0) return MN_OK;
+  if (!tokens) return fail(c, MN_ENULL, "%s: tokens is NULL", who);
+  {
+    Tap t(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
+    launch_reserve(p, tokens, B, kv->k_layers, kv->v_layers, c->d.n_layers, page_bytes(c, kv), workspace, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
+extern "C" mn_status mn_kv_fork(mn_ctx* c, mn_kv* kv, const mn_pool* pool, const int32_t* src, const int32_t* dst, int n,
+                                int32_t* dev_status, void* stream) {
+  const char* who = "mn_kv_fork";
+  PoolView p;
+  if (mn_status s = check_pool(c, kv, pool, n, dev_status, false, who, &p)) return s;
+  if (n == 0) return MN_OK;
+  if (!src || !dst) return fail(c, MN_ENULL, "%s: src or dst is NULL", who);
+  {
+    Tap t(c ? &c->prof : nullptr, MN_PROF_ACCEPT, (hipStream_t)stream);
+    launch_fork(p, src, dst, n, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
+extern "C" mn_status mn_kv_free(mn_ctx* c, mn_kv* kv, const mn_pool* pool, const int32_t* seqs, int n, int32_t* dev_status, void* stream) {
+  const char* who = "mn_kv_free";
+  PoolView p;
+  if (mn_status s = check_pool(c, kv, pool, n, dev_status, false, who, &p)) return s;
+  if (n == 0) return MN_OK;
+  if (!seqs) return fail(c, MN_ENULL, "%s: seqs is NULL", who);
+  {
+    Tap t(c ? &c->prof : nullptr, MN_PROF_ACCEPT, (hipStream_t)stream);
+    launch_free(p, seqs, n, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
+extern "C" mn_status mn_kv_compact(mn_ctx* c, mn_kv* kv, const mn_pool* pool, int32_t* n_live, void* workspace, size_t workspace_bytes,
+                                   int32_t* dev_status, void* stream) {
+  const char* who = "mn_kv_compact";
+  if (!c) return MN_ENULL;
+  PoolView p;
+  if (mn_status s = check_pool(c, kv, pool, 0, dev_status, true, who, &p)) return s;
+  if (mn_status s = check_pool_workspace(c, p, workspace, workspace_bytes, who)) return s;
+  {
+    Tap t(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
+    launch_compact(p, n_live, kv->k_layers, kv->v_layers, c->d.n_layers, page_bytes(c, kv), workspace, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
 // ---- timing taps ------------------------------------------------------------------------------------
 extern "C" mn_status mn_profile_enable(mn_ctx* c, int on) {
   if (!c) return MN_ENULL;

@@ -178,4 +178,29 @@ AttnPlan attention_plan(const AttnArgs& a);  // what the kernels that will run n
 // hipSuccess, or the error of a one-time kernel attribute setting that failed (nothing is launched then)
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 
+// ---- pool.hip ----
+struct PoolView {
+  int32_t *tables, *refs, *seq_blocks, *ctx_lens;  // [max_seqs][width], [num_blocks], [max_seqs], [max_seqs]
+  int max_seqs, width, num_blocks, block_size;
+  int32_t* status;
+};
+struct PoolWork {  // in the caller's workspace
+  int32_t *n_pairs, *n_live;
+  int32_t *from, *to;  // pairs of blocks to copy
+  int32_t* list;       // blocks handed over between the parts of a plan
+  int32_t* map;        // where a block went
+};
+constexpr int LAYERS_PER_LAUNCH = 96;  // (their pointers are kernel arguments)
+struct LayerPages {
+  void *k[LAYERS_PER_LAUNCH], *v[LAYERS_PER_LAUNCH];
+};
+size_t pool_work_bytes(int num_blocks, int max_seqs);
+void launch_fork(const PoolView& p, const int32_t* src, const int32_t* dst, int n, hipStream_t st);
+void launch_free(const PoolView& p, const int32_t* seqs, int n, hipStream_t st);
+// page_bytes: one K (or V) block of one layer, a multiple of 16
+void launch_reserve(const PoolView& p, const int32_t* tokens, int B, void* const* k, void* const* v, int n_layers, size_t page_bytes,
+                    void* workspace, hipStream_t st);
+void launch_compact(const PoolView& p, int32_t* n_live, void* const* k, void* const* v, int n_layers, size_t page_bytes, void* workspace,
+                    hipStream_t st);
+
 }  // namespace mn

@@ -201,6 +201,57 @@ class DeviceKV:
         return (self.k_pages[layer].float().cpu().numpy(), self.v_pages[layer].float().cpu().numpy())
 
 
+class KVPool:
+    """Which slot of a DeviceKV's table holds which blocks (mn_kv_*): forked requests share pages, every slot gets room ahead of
+    its next tokens, finished ones give their blocks back, and the pool can be packed.  The whole mapping (table, references,
+    blocks per slot, context lengths) moves into one tensor, ``state``, which one copy saves or puts back; the DeviceKV's table and
+    context lengths become views of it."""
+
+    def __init__(self, model: DeviceModel, kv: DeviceKV, block_refs: torch.Tensor, seq_blocks: torch.Tensor):
+        self.model, self.kv, self.max_seqs = model, kv, int(kv.block_tables.shape[0])
+        assert block_refs.numel() == kv.num_blocks and seq_blocks.numel() == self.max_seqs == kv.ctx_lens.numel()
+        parts = [kv.block_tables, block_refs, seq_blocks, kv.ctx_lens]
+        self.state = torch.cat([t.to(torch.int32).reshape(-1) for t in parts])
+        table, self.block_refs, self.seq_blocks, kv.ctx_lens = self.state.split([t.numel() for t in parts])
+        kv.block_tables = table.view(self.max_seqs, kv.max_blocks_per_seq)
+        kv.c.block_tables, kv.c.ctx_lens = kv.block_tables.data_ptr(), kv.ctx_lens.data_ptr()
+        self.c = B.Pool(kv.block_tables.data_ptr(), self.block_refs.data_ptr(), self.seq_blocks.data_ptr(), self.max_seqs)
+        self.n_live = torch.zeros((1,), dtype=torch.int32, device=self.state.device)
+        self.dev_status = torch.zeros((1,), dtype=torch.int32, device=self.state.device)
+        self.ws_bytes = B.mn_kv_workspace_bytes(kv.num_blocks, self.max_seqs)
+        if self.ws_bytes == 0:
+            raise RuntimeError("mn_kv_workspace_bytes rejected the shape")
+        self.workspace = torch.empty((self.ws_bytes,), dtype=torch.uint8, device=self.state.device)
+
+    @classmethod
+    def from_tables(cls, model: DeviceModel, kv: DeviceKV) -> "KVPool":
+        """Every non-negative entry at the start of a row is a block that the slot holds."""
+        held = (kv.block_tables >= 0).to(torch.int32).cumprod(dim=1)
+        ids = kv.block_tables[held.bool()].long()
+        refs = torch.bincount(ids, minlength=kv.num_blocks).to(torch.int32)
+        return cls(model, kv, refs, held.sum(dim=1).to(torch.int32))
+
+    def reserve(self, tokens: torch.Tensor) -> None:
+        """Room for tokens[b] positions in slots 0 .. len(tokens) - 1, none of it shared from the next token on."""
+        B.mn_kv_reserve(self.model.ctx, self.kv.c, self.c, tokens.data_ptr(), tokens.numel(), self.workspace.data_ptr(),
+                        self.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor) -> None:
+        """Slot dst[i] shares the blocks of slot src[i]'s tokens."""
+        assert src.numel() == dst.numel()
+        B.mn_kv_fork(self.model.ctx, self.kv.c, self.c, src.data_ptr(), dst.data_ptr(), src.numel(), self.dev_status.data_ptr(),
+                     stream_ptr())
+
+    def free(self, seqs: torch.Tensor) -> None:
+        B.mn_kv_free(self.model.ctx, self.kv.c, self.c, seqs.data_ptr(), seqs.numel(), self.dev_status.data_ptr(), stream_ptr())
+
+    def compact(self) -> torch.Tensor:
+        """Packs the live blocks into the lowest ids; returns their number (on the device)."""
+        B.mn_kv_compact(self.model.ctx, self.kv.c, self.c, self.n_live.data_ptr(), self.workspace.data_ptr(), self.ws_bytes,
+                        self.dev_status.data_ptr(), stream_ptr())
+        return self.n_live
+
+
 class VerifySession:
     """Output buffers + workspace for batches of up to B sequences / max_rows scored positions."""
 
