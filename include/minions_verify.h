@@ -431,6 +431,25 @@ mn_status mn_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, cons
                        int max_ctx, const mn_kv *kv, int layer, void *out, void *workspace, size_t workspace_bytes,
                        int32_t *dev_status, void *stream);
 
+/* Causal attention of one layer over whole prompts, on packed rows (no cache is read): sequence b has the rows
+ * seq_rows[b] .. seq_rows[b+1] - 1, its tokens 0, 1, ..., and row i sees the rows 0 .. i of its own sequence.
+ *   q        dev, row m at q + m * q_stride: [n_heads][head_dim], fp32 in fp32 models, fp16 in bf16 models
+ *   k, v     dev, likewise: [n_kv_heads][head_dim]
+ *            (strides in elements, so that the three may lie side by side in the rows of one QKV projection; addresses and row
+ *            strides are multiples of 16 bytes)
+ *   seq_rows dev [B+1], ascending from 0 or more; h_seq_rows HOST [B+1], the same values: they size the launch.  Sequences without
+ *            rows are fine.  Values on the device that do not fit the launch leave the call undone (MN_DEV_SPEC_LEN).
+ *   out      dev [h_seq_rows[B]][n_heads * head_dim], same type as q; only rows that belong to a sequence are written
+ *   kv       NULL, or the cache that the prompts enter: the rows of k and v are also written into layer `layer`'s pages, token i
+ *            of sequence b at position i of table row b (tokens whose block id is out of range are left out: MN_DEV_BLOCK_TABLE).
+ *            ctx_lens is neither read nor written.
+ * Elements of q, k and v must be finite (fp16: within +-65504); one that is not leaves its sequence's rows undefined, no other's.
+ * The scores, the statistics and the sums are fp32; fp16 probabilities are rounded to fp16 for the second product, in the sum of
+ * the outputs and of the probabilities alike.  No workspace. */
+mn_status mn_prompt_attention(mn_ctx *ctx, const void *q, long q_stride, const void *k, long k_stride, const void *v,
+                              long v_stride, const int32_t *seq_rows, const int32_t *h_seq_rows, int B, const mn_kv *kv,
+                              int layer, void *out, int32_t *dev_status, void *stream);
+
 /* ---- timing taps (for benchmarks; off by default) --------------------------------------------- */
 
 /* Kernel families of the step, as indexed in mn_profile_collect's arrays. */

@@ -28,7 +28,7 @@ EXPORTS = ("mn_create", "mn_destroy", "mn_last_error", "mn_status_str", "mn_work
            "mn_profile_collect", "mn_packed_weight_bytes", "mn_pack_weight", "mn_acr_update",
            "mn_verify_sample", "mn_draft_sample",
            "mn_selector_create", "mn_selector_destroy", "mn_selector_observe", "mn_selector_current",
-           "mn_kv_workspace_bytes", "mn_kv_reserve", "mn_kv_fork", "mn_kv_free", "mn_kv_compact",
+           "mn_prompt_attention", "mn_kv_workspace_bytes", "mn_kv_reserve", "mn_kv_fork", "mn_kv_free", "mn_kv_compact",
            "mn_selector_adjustments", "mn_probe_stream_read", "mn_probe_mfma", "mn_probe_mfma_data")
 PROF_KINDS = ("prepare", "norm", "gemm", "rope_append", "attention", "act", "argmax", "vote", "accept")
 
@@ -98,6 +98,9 @@ def _load() -> C.CDLL:
                                     C.c_long, vp]
     lib.mn_acr_update.restype = i32
     lib.mn_acr_update.argtypes = [vp, vp, vp, vp, vp, i32, i32, C.c_double, C.c_double, C.c_float, C.c_float, vp, vp, vp]
+    lib.mn_prompt_attention.restype = i32
+    lib.mn_prompt_attention.argtypes = [vp, vp, C.c_long, vp, C.c_long, vp, C.c_long, vp, C.POINTER(C.c_int32), i32,
+                                        C.POINTER(KV), i32, vp, vp, vp]
     lib.mn_kv_workspace_bytes.restype = sz
     lib.mn_kv_workspace_bytes.argtypes = [i32, i32]
     lib.mn_kv_reserve.restype = i32
@@ -241,6 +244,12 @@ def mn_acr_update(ctx, voted_ssm, accepted_len, spec_len, n_out, B, n, reward_th
                   reward_factor, punish_factor, ssm_w, acr=None, stream=None) -> None:
     _check(lib.mn_acr_update(ctx, voted_ssm, accepted_len, spec_len, n_out, B, n, reward_threshold, punish_threshold,
                              reward_factor, punish_factor, ssm_w, acr, stream), ctx)
+
+
+def mn_prompt_attention(ctx, q, q_stride, k, k_stride, v, v_stride, seq_rows, h_seq_rows, B, out, kv: Optional[KV] = None,
+                        layer=0, dev_status=None, stream=None) -> None:
+    _check(lib.mn_prompt_attention(ctx, q, q_stride, k, k_stride, v, v_stride, seq_rows, h_seq_rows, B,
+                                   C.byref(kv) if kv is not None else None, layer, out, dev_status, stream), ctx)
 
 
 def mn_kv_workspace_bytes(num_blocks: int, max_seqs: int) -> int:

@@ -747,6 +747,56 @@ extern "C" mn_status mn_attention(mn_ctx* c, const void* q, const int32_t* spec_
   return hip_check(c, who);
 }
 
+// ---- attention over whole prompts -------------------------------------------------------------------
+extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride, const void* k, long k_stride, const void* v,
+                                         long v_stride, const int32_t* seq_rows, const int32_t* h_seq_rows, int B, const mn_kv* kv,
+                                         int layer, void* out, int32_t* dev_status, void* stream) {
+  const char* who = "mn_prompt_attention";
+  if (!c) return MN_ENULL;
+  if (B < 0 || B > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: B = %d outside [0, %d]", who, B, MN_MAX_BATCH);
+  if (B == 0) return MN_OK;
+  if (!q || !k || !v || !seq_rows || !h_seq_rows || !out) return fail(c, MN_ENULL, "%s: a required pointer is NULL", who);
+  const mn_model_desc& d = c->d;
+  const int G = d.n_heads / d.n_kv_heads, es = d.dtype == MN_DT_BF16 ? 2 : 4;
+  int longest = 0;
+  if (h_seq_rows[0] < 0) return fail(c, MN_EINVAL, "%s: h_seq_rows[0] = %d", who, h_seq_rows[0]);
+  for (int b = 0; b < B; ++b) {
+    const long n = (long)h_seq_rows[b + 1] - h_seq_rows[b];
+    if (n < 0) return fail(c, MN_EINVAL, "%s: h_seq_rows[%d] = %d below h_seq_rows[%d] = %d", who, b + 1, h_seq_rows[b + 1], b, h_seq_rows[b]);
+    if (n > longest) longest = (int)n;
+  }
+  const int M = h_seq_rows[B];
+  if (M > (1 << 20)) return fail(c, MN_EINVAL, "%s: %d rows", who, M);
+  if ((long)M * G >= (1l << 30)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d heads per KV head", who, M, G);
+  if (q_stride < (long)d.n_heads * d.head_dim || k_stride < (long)d.n_kv_heads * d.head_dim || v_stride < (long)d.n_kv_heads * d.head_dim)
+    return fail(c, MN_EINVAL, "%s: a row stride is shorter than its row", who);
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out | (uintptr_t)(q_stride * es) | (uintptr_t)(k_stride * es) | (uintptr_t)(v_stride * es)) & 15)
+    return fail(c, MN_EINVAL, "%s: addresses and row strides must be multiples of 16 bytes", who);
+  TileArgs t{};
+  if (kv) {
+    if (mn_status s = check_kv(c, kv, longest, who)) return s;
+    if (layer < 0 || layer >= (d.n_layers > 0 ? d.n_layers : 1)) return fail(c, MN_EINVAL, "%s: layer %d", who, layer);
+    if (!kv->k_layers[layer] || !kv->v_layers[layer]) return fail(c, MN_ENULL, "%s: kv layer pointer is NULL", who);
+    t.kv = KvView{kv->k_layers[layer], kv->v_layers[layer], kv->block_tables, kv->block_size, kv->num_blocks, kv->max_blocks_per_seq};
+  }
+  t.q = q; t.k = k; t.v = v; t.q_stride = q_stride; t.k_stride = k_stride; t.v_stride = v_stride; t.out = out;
+  t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.B = B;
+  t.seq_rows = seq_rows; t.status = dev_status;
+  const int rows = prompt_tile_rows(d.n_heads, d.n_kv_heads, d.head_dim, d.dtype, (long)(M - h_seq_rows[0]) * G);
+  long tiles = 0;
+  for (int b = 0; b < B; ++b) tiles += ((long)(h_seq_rows[b + 1] - h_seq_rows[b]) * G + rows - 1) / rows;
+  if (tiles * d.n_kv_heads >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
+  t.n_tiles = (int)tiles;
+  t.max_tiles = (int)(((long)longest * G + rows - 1) / rows);
+  hipError_t lerr;
+  {
+    Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);
+    lerr = launch_prompt(t, rows, (hipStream_t)stream);
+  }
+  if (lerr != hipSuccess) return fail(c, MN_EHIP, "%s: kernel attribute: %s", who, hipGetErrorString(lerr));
+  return hip_check(c, who);
+}
+
 // ---- page pool ----------------------------------------------------------------------------------------
 static mn_status check_pool(mn_ctx* c, const mn_kv* kv, const mn_pool* pool, int n, int32_t* status, bool pages, const char* who, PoolView* out) {
   if (!kv || !pool) return fail(c, MN_ENULL, "%s: kv or pool is NULL", who);

@@ -178,6 +178,23 @@ AttnPlan attention_plan(const AttnArgs& a);  // what the kernels that will run n
 // hipSuccess, or the error of a one-time kernel attribute setting that failed (nothing is launched then)
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 
+// ---- tile_attention.hip ----
+struct TileArgs {
+  const void *q, *k, *v;  // rows [M][H][hd] and [M][Hkv][hd] in the activation type, strides in elements (k, v: dense keys only)
+  long q_stride, k_stride, v_stride;
+  void* out;              // [M][H * hd]
+  int M, H, Hkv, hd, dtype, B;
+  int n_tiles;            // workgroups per KV head
+  int max_tiles;          // most tiles of a sequence
+  const int32_t* seq_rows;  // [B + 1] (dense keys)
+  const int32_t* items;     // work list, 8 int32 per record (pages)
+  KvView kv;                // pages to read, or (dense keys, k non-null) to write the rows to
+  float *o_part, *ml_part;
+  int32_t* status;
+};
+int prompt_tile_rows(int H, int Hkv, int hd, int dtype, long stack_rows);
+hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st);
+
 // ---- pool.hip ----
 struct PoolView {
   int32_t *tables, *refs, *seq_blocks, *ctx_lens;  // [max_seqs][width], [num_blocks], [max_seqs], [max_seqs]

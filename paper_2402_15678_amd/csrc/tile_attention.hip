@@ -1,0 +1,558 @@
+// Attention of many query rows over the same keys, as tiles of a dense product: whole prompts (packed rows, causal) and batches whose
+// sequences share a prefix of the paged cache.
+//
+// o_r = sum_j p_rj v_j / sum_j p_rj with p_rj = 2^(c s_rj - m_r), s_rj = q_r . k_j, c = log2(e) / sqrt(head_dim), in one pass over the
+// keys with a running reference m_r.  The G query heads of a KV head are stacked: row r of the stack is query head r % G of token
+// r / G, so a tile of rows reads the keys of its KV head once for all of them.
+//
+//  * tile_mfma_kernel   fp16, head_dim 64 or 128, dense rows or pages of 16 tokens: 16x16x32 matrix instructions, keys staged in
+//    LDS for all the waves of a workgroup.
+//  * tile_f32_kernel    every other type, head_dim and block size: 16x16x4 fp32 matrix instructions.
+//  * prefix_plan_kernel, prefix_merge_kernel   the work list of a shared-prefix call, and the sum of its parts.
+#include "launch.h"
+#include "../../include/minions_verify.h"
+
+#include <mutex>
+
+namespace mn {
+
+constexpr float LOG2E_T = 1.4426950408889634f;
+constexpr int TKEYS = 64;              // keys per staged tile of the MFMA kernel
+constexpr int PAGE = 16;               // tokens per block that it reads
+constexpr int NO_LIMIT = 1 << 29;      // an item whose rows all see every key of its range
+constexpr float LAZY = 6.f;            // the reference moves when a score exceeds it by 2^6
+
+// One tile of work: stack rows [rbase, R) (as many as a workgroup holds) of the tokens from m0 on against the keys [key0, key_end).
+// Row r sees the keys up to ctx + r / G.
+struct Item {
+  int m0, R, rbase, key0, key_end, ctx, seq, slot;
+};
+
+// Sum over the lanes of max(0, n(b) - level) for b < B.
+template <typename F>
+__device__ __forceinline__ int tiles_from(int level, int B, F n) {
+  int s = 0;
+  for (int b = threadIdx.x & 63; b < B; b += 64) s += max(0, n(b) - level);
+  return __builtin_amdgcn_readfirstlane(wave_sum_i(s));
+}
+
+// Tile t of a packed batch whose sequence b has n(b) tiles.  Order: last tiles first (a causal tile's work grows with its number),
+// so the longest ones start first and the short ones fill the gaps.  Level `tile` and the sequence are found by counting how
+// many tiles lie at or above a level; `total` is the number of all tiles.
+template <typename F>
+__device__ __forceinline__ void find_tile(int t, int B, int max_tiles, F n, int total, int& seq, int& tile) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = max_tiles, above = 0;         // tiles at levels >= lo: more than t; >= hi: `above`, t at most
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1, c = tiles_from(mid, B, n);
+    if (c > t) lo = mid;
+    else { hi = mid; above = c; }
+  }
+  tile = lo;
+  int ord = t - above;
+  seq = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const bool has = b0 + lane < B && n(b0 + lane) > lo;
+    const uint64_t ballot = __ballot(has);
+    const int c = __popcll(ballot);
+    if (ord < c) {
+      seq = b0 + __ffsll((unsigned long long)__ballot(has && __popcll(ballot & ((1ull << lane) - 1)) == ord)) - 1;
+      break;
+    }
+    ord -= c;
+  }
+}
+
+// The prompt's item of this workgroup.  Lengths come from the device; those that do not fit the launch (which the host's sized)
+// leave the whole call undone.  s_n: room for a number per sequence.
+template <int ROWS>
+__device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, int G, int32_t* s_n, Item& it) {
+  const int lane = threadIdx.x & 63;
+  bool bad = false;
+  auto tiles = [&](int b) {
+    const int r0 = a.seq_rows[b], r1 = a.seq_rows[b + 1];
+    const bool fits = r0 >= 0 && r1 >= r0 && r1 <= a.M;
+    const int n = fits ? (int)(((long)(r1 - r0) * G + ROWS - 1) / ROWS) : 0;
+    bad |= !fits || n > a.max_tiles;
+    return min(n, a.max_tiles);
+  };
+  int own = 0;
+  if (a.B <= 64) {
+    if (lane < a.B) own = tiles(lane);
+  } else {
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) s_n[b] = tiles(b);
+    __syncthreads();
+  }
+  auto n = [&](int b) { return a.B <= 64 ? own : s_n[b]; };
+  const int total = tiles_from(0, a.B, n);
+  if (__syncthreads_or(bad) || total != a.n_tiles) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, MN_DEV_SPEC_LEN);
+    return false;
+  }
+  int seq, tile;
+  find_tile(t, a.B, a.max_tiles, n, total, seq, tile);
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  tile = __builtin_amdgcn_readfirstlane(tile);
+  const int row0 = a.seq_rows[seq], len = a.seq_rows[seq + 1] - row0;
+  it.m0 = row0; it.R = len * G; it.rbase = tile * ROWS; it.key0 = 0; it.ctx = 0; it.seq = seq; it.slot = -1;
+  it.key_end = min(len, (min(it.R, it.rbase + ROWS) - 1) / G + 1);
+  return true;
+}
+
+__device__ __forceinline__ bool list_item(const TileArgs& a, int t, Item& it) {
+  const int4 x = reinterpret_cast<const int4*>(a.items)[2 * t], y = reinterpret_cast<const int4*>(a.items)[2 * t + 1];
+  it = Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  return it.R > 0;
+}
+
+// Rows of K and V of the tokens whose first stack row lies in this tile, into the pages (position = token of the sequence).
+template <typename T, int ROWS>
+__device__ __forceinline__ void append_rows(const TileArgs& a, const Item& it, int G, int kvh) {
+  const int j0 = (it.rbase + G - 1) / G, j1 = (min(it.R, it.rbase + ROWS) + G - 1) / G;
+  const int hd = a.hd, bs = a.kv.block_size;
+  const int32_t* bt = a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq;
+  bool bad = false;
+  // 8 consecutive head-dim elements of one token: 16 bytes (fp32: 32) of a K page, a column of a V page
+  for (int i = threadIdx.x; i < (j1 - j0) * (hd / 8); i += blockDim.x) {
+    const int j = j0 + i % (j1 - j0), c = i / (j1 - j0);
+    const int id = bt[j / bs], off = j % bs;
+    if ((uint32_t)id >= (uint32_t)a.kv.num_blocks) {
+      bad = true;
+      continue;
+    }
+    struct __attribute__((aligned(16))) Piece { T x[8]; };
+    const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.k) + (size_t)(it.m0 + j) * a.k_stride + (size_t)kvh * hd + 8 * c);
+    const Piece v = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.v) + (size_t)(it.m0 + j) * a.v_stride + (size_t)kvh * hd + 8 * c);
+    const size_t page = ((size_t)id * a.Hkv + kvh) * (size_t)(hd * bs);
+    *reinterpret_cast<Piece*>(static_cast<T*>(a.kv.k) + page + ((size_t)c * bs + off) * 8) = k;
+    T* to = static_cast<T*>(a.kv.v) + page + (size_t)(8 * c) * bs + off;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) to[(size_t)e * bs] = v.x[e];
+  }
+  if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+}
+
+// ------------------------------------------------------------------------------------------
+// fp16, head_dim 64 or 128
+// ------------------------------------------------------------------------------------------
+// A workgroup of NW waves holds 16 * CT * NW stack rows, wave w the rows from 16 * CT * w on, their queries in registers.  Both products
+// have the query row as the column index (S^T = K Q^T, O^T = V^T P^T): statistics are per-lane numbers, and with the K rows of a
+// half of 32 keys permuted (S^T row 4g + r of half t is key 8g + 4t + r) the probabilities leave the first product in the operand
+// order of the second.  A tile of 64 keys is staged by direct global -> LDS loads: K in operand order (the lane asks for the 16
+// bytes that belong at its place); V of pages likewise (a page keeps the block's tokens of one head-dim element together), V of dense
+// rows row by row, turned on the way to the registers by the transposing LDS read.
+template <int HDIM> struct TileStage {
+  static constexpr int HS = HDIM / 32, NU = HDIM / 16;
+  static constexpr int FRAGS = 4 * HS + 2 * NU;     // 1 KB pieces of a stage: K, then V
+  static constexpr int BYTES = FRAGS * 1024;
+};
+constexpr int STAGES = 3;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <int HDIM, int CT, int NW, bool PAGED>
+__global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(TileArgs a) {
+  using St = TileStage<HDIM>;
+  constexpr int HS = St::HS, NU = St::NU, LPW = St::FRAGS / NW, ROWS = 16 * CT * NW;
+  static_assert(St::FRAGS % NW == 0, "whole pieces per wave");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int G = a.H / a.Hkv;
+  const int t = blockIdx.x / a.Hkv, kvh = blockIdx.x % a.Hkv;
+  Item it;
+  if constexpr (PAGED) {
+    if (!list_item(a, t, it)) return;
+  } else {
+    if (!prompt_item<ROWS>(a, t, G, reinterpret_cast<int32_t*>(smem), it)) return;
+    if (a.kv.k) append_rows<f16_t, ROWS>(a, it, G, kvh);
+  }
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // this wave's rows, and the keys that its first and last row see
+  const int rw0 = it.rbase + wave * CT * 16;
+  const bool rows = rw0 < it.R;
+  const int min_lim = min(it.key_end - 1, it.ctx + rw0 / G);
+  const int max_lim = rows ? min(it.key_end - 1, it.ctx + (min(it.R, rw0 + CT * 16) - 1) / G) : -1;
+  f16x8 qf[CT][HS];
+  int lim[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int r = min(rw0 + 16 * ct + l16, it.R - 1), j = r / G;
+    lim[ct] = min(it.key_end - 1, it.ctx + j);
+    const f16_t* q = static_cast<const f16_t*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * HDIM;
+#pragma unroll
+    for (int s = 0; s < HS; ++s) qf[ct][s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
+  }
+  f32x4 O[CT][NU], L[CT];
+  float run_m[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    run_m[ct] = -INFINITY;
+    L[ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < NU; ++u) O[ct][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+  const float c = rsqrtf((float)HDIM) * LOG2E_T;
+
+  // ---- staging ----
+  const int n_tiles = (it.key_end - it.key0 + TKEYS - 1) / TKEYS;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
+  const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
+  const int last_key = it.key_end - 1, last_blk = last_key / PAGE;
+  const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u;
+  auto stage = [&](int tile) {
+    const int k0 = it.key0 + min(tile, n_tiles - 1) * TKEYS;     // (stages past the end repeat the last one)
+    const uint32_t to = lds0 + (uint32_t)(tile % STAGES) * St::BYTES;
+    uint32_t id[TKEYS / PAGE];
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int i = 0; i < TKEYS / PAGE; ++i) id[i] = min((uint32_t)bt[min(k0 / PAGE + i, last_blk)], (uint32_t)a.kv.num_blocks - 1u);
+    }
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+      const int f = wave * LPW + i;                              // (uniform)
+      const char* p;
+      if (f < 4 * HS) {
+        const int kb = f / (2 * HS), half = f / HS & 1, s = f % HS;
+        const int key = 32 * kb + 8 * (l16 >> 2) + 4 * half + (l16 & 3);
+        if constexpr (PAGED) {
+          const uint32_t lo = kb ? id[2] : id[0], hi = kb ? id[3] : id[1];
+          p = static_cast<const char*>(a.kv.k) + (uint64_t)((l16 >> 3) ? hi : lo) * blk_bytes +
+              ((size_t)kvh * (HDIM * PAGE) + ((4 * s + g) * PAGE + (key & (PAGE - 1))) * 8) * 2;
+        } else {
+          p = reinterpret_cast<const char*>(static_cast<const f16_t*>(a.k) + (size_t)(it.m0 + min(k0 + key, last_key)) * a.k_stride +
+                                            (size_t)kvh * HDIM + 32 * s + 8 * g);
+        }
+      } else {
+        const int w = f - 4 * HS;
+        if constexpr (PAGED) {
+          const int kb = w / NU, u = w % NU;
+          const uint32_t lo = kb ? id[2] : id[0], hi = kb ? id[3] : id[1];
+          p = static_cast<const char*>(a.kv.v) + (uint64_t)((g >> 1) ? hi : lo) * blk_bytes +
+              ((size_t)kvh * (HDIM * PAGE) + (16 * u + l16) * PAGE + 8 * (g & 1)) * 2;
+        } else {
+          // 512 / HDIM rows per piece; the 32-byte chunks of a row change places so that the transposing reads meet every bank
+          constexpr int CH = HDIM / 8;                           // 16-byte chunks per row
+          const int key = w * (64 / CH) + lane / CH, at = lane % CH;
+          const int swz = HDIM == 128 ? ((key & 3) | (key >> 1 & 4)) : ((key >> 1 & 1) | (key >> 2 & 2));
+          p = reinterpret_cast<const char*>(static_cast<const f16_t*>(a.v) + (size_t)(it.m0 + min(k0 + key, last_key)) * a.v_stride +
+                                            (size_t)kvh * HDIM + 8 * (at ^ (swz << 1)));
+        }
+      }
+      dma16<0, PAGED>(p, to + (uint32_t)f * 1024u);
+    }
+  };
+  __syncthreads();                                               // (the search is through with its part of the LDS)
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) stage(i);
+
+  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+  // transposing reads: lanes 4k .. 4k + 3 of a group of 16 address 32 bytes of key 8g + k, lane i receives column i
+  const uint32_t v_lane = (uint32_t)((8 * g + (l16 >> 2)) * (2 * HDIM) + (HDIM == 128 ? ((l16 >> 2) | (g & 1) << 2) : ((l16 >> 3) | (g & 1) << 1)) * 32 +
+                                     (l16 & 3) * 8);
+
+  for (int i = 0; i < n_tiles; ++i) {
+    wait_vm<(STAGES - 2) * LPW>();                               // this wave's part of tile i has landed ...
+    __syncthreads();                                             // ... and everybody's; tile i - 1 has been read by all
+    stage(i + STAGES - 1);
+    const int k0 = it.key0 + i * TKEYS;
+    if (k0 > max_lim) continue;                                  // (no row of the wave sees the tile)
+    const unsigned char* st = smem + (i % STAGES) * St::BYTES;
+    const bool masked = k0 + TKEYS - 1 > min_lim;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f16x8 kf[2 * HS];
+#pragma unroll
+      for (int f = 0; f < 2 * HS; ++f) kf[f] = *reinterpret_cast<const f16x8*>(st + ((kb * 2 * HS + f) * 64 + lane) * 16);
+      f16x8 P[CT];
+      const int keyg = k0 + 32 * kb + 8 * g;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        f32x4 S0 = {0.f, 0.f, 0.f, 0.f}, S1 = S0;
+#pragma unroll
+        for (int s = 0; s < HS; ++s) {
+          S0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[s], qf[ct][s], S0, 0, 0, 0);
+          S1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[HS + s], qf[ct][s], S1, 0, 0, 0);
+        }
+        float sc[8] = {S0[0], S0[1], S0[2], S0[3], S1[0], S1[1], S1[2], S1[3]};
+        if (masked) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sc[e] = keyg + e > lim[ct] ? -INFINITY : sc[e];
+        }
+        float tm = sc[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) tm = __builtin_fmaxf(tm, sc[e]);
+        tm *= c;
+        if (__any(tm > run_m[ct] + LAZY)) {
+          uint32_t x, y;
+          lane_pair<16>(__float_as_uint(tm), x, y);
+          tm = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
+          lane_pair<32>(__float_as_uint(tm), x, y);
+          tm = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
+          const float nm = __builtin_fmaxf(run_m[ct], tm);
+          const float alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m[ct] - nm);
+          run_m[ct] = nm;
+#pragma unroll
+          for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
+          L[ct] *= alpha;
+        }
+        const float nm = run_m[ct] == -INFINITY ? 0.f : -run_m[ct];
+        union { f16x8 v; uint32_t u[4]; } pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          pf.u[e] = pack2h(__builtin_amdgcn_exp2f(fmaf(sc[2 * e], c, nm)), __builtin_amdgcn_exp2f(fmaf(sc[2 * e + 1], c, nm)));
+        P[ct] = pf.v;
+      }
+      f16x8 vf[NU];
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        if constexpr (PAGED) {
+          vf[u] = *reinterpret_cast<const f16x8*>(st + ((4 * HS + kb * NU + u) * 64 + lane) * 16);
+        } else {
+          union { f16x8 v; s16x4 h[2]; } x;
+          const uint32_t at = (v_lane ^ (uint32_t)(u * 32)) + (uint32_t)(4 * HS * 1024 + kb * 32 * 2 * HDIM);
+          x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
+          x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
+          vf[u] = x.v;
+        }
+      }
+      if (PAGED && masked) {
+        // slots past the last key may hold anything, and 0 times anything has to stay 0
+        const int past = keyg + 8 - it.key_end;
+        if (past > 0) {
+#pragma unroll
+          for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e >= 8 - past) vf[u][e] = (f16_t)0.f;
+        }
+      }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) O[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[u], P[ct], O[ct][u], 0, 0, 0);
+        L[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, P[ct], L[ct], 0, 0, 0);
+      }
+    }
+  }
+  wait_vm<0>();                                                  // (stages past the end land before the LDS is given back)
+
+  // ---- output: lane holds O^T[16u + 4g + i][row l16], and its row's sum ----
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int r = rw0 + 16 * ct + l16;
+    if (r >= it.R) continue;
+    const int j = r / G, m = it.m0 + j, h = kvh * G + r - j * G;
+    const float l = L[ct][0];
+    if constexpr (PAGED) {
+      float* o = a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * HDIM + 4 * g;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) *reinterpret_cast<f32x4*>(o + 16 * u) = O[ct][u];
+      if (g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m[ct], l);
+    } else {
+      const float inv = 1.f / l;
+      f16_t* o = static_cast<f16_t*>(a.out) + ((size_t)m * a.H + h) * HDIM + 4 * g;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        const f32x4 v = O[ct][u];
+        *reinterpret_cast<uint2*>(o + 16 * u) = make_uint2(pack2h(v[0] * inv, v[1] * inv), pack2h(v[2] * inv, v[3] * inv));
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// every other type, head_dim and block size
+// ------------------------------------------------------------------------------------------
+// Four waves of 16 stack rows; 32 keys at a time, widened to fp32 in LDS.  Products as above on the 16x16x4 fp32 instruction: lane
+// (row l16, g) holds of the first product's operands the elements 16 * step + 4g .. 4g + 3 of a row (four instructions take one each), and
+// of the second's the keys 4g + r that the first leaves in its registers.  HDP: head_dim padded to a multiple of 16 with zeros.
+constexpr int FKEYS = 32, FROWS = 64;
+
+template <typename T, int HDP, bool PAGED>
+__global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
+  constexpr int LD = HDP + 4, NU = HDP / 16;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  float* s_k = reinterpret_cast<float*>(smem);                   // [FKEYS][LD]
+  float* s_v = s_k + FKEYS * LD;
+  const int G = a.H / a.Hkv;
+  const int t = blockIdx.x / a.Hkv, kvh = blockIdx.x % a.Hkv;
+  Item it;
+  if constexpr (PAGED) {
+    if (!list_item(a, t, it)) return;
+  } else {
+    if (!prompt_item<FROWS>(a, t, G, reinterpret_cast<int32_t*>(smem), it)) return;
+    if (a.kv.k) append_rows<T, FROWS>(a, it, G, kvh);
+  }
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, wave = tid >> 6;
+  const int hd = a.hd;
+  const int rw = it.rbase + wave * 16 + l16, r = min(rw, it.R - 1), j = r / G;
+  const int lim = min(it.key_end - 1, it.ctx + j);
+  const float c = rsqrtf((float)hd) * LOG2E_T;
+  f32x4 q[NU], O[NU];
+  const T* Q = static_cast<const T*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * hd;
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    O[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[u][e] = 16 * u + 4 * g + e < hd ? (float)Q[16 * u + 4 * g + e] * c : 0.f;
+  }
+  float run_m = -INFINITY, run_l = 0.f;
+  const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
+  const int bs = PAGED ? a.kv.block_size : 1;
+  __syncthreads();                                               // (the search is through with its part of the LDS)
+  for (int k0 = it.key0; k0 < it.key_end; k0 += FKEYS) {
+    // the keys' rows, 8 elements at a time; past the last key and past head_dim zeros
+    for (int i = tid; i < FKEYS * (HDP / 8); i += 256) {
+      const int key = i % FKEYS, p8 = i / FKEYS, pos = k0 + key;
+      struct __attribute__((aligned(16))) Piece { T x[8]; };
+      float kx[8], vx[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
+      if (pos < it.key_end && 8 * p8 < hd) {
+        if constexpr (PAGED) {
+          const uint32_t id = min((uint32_t)bt[pos / bs], (uint32_t)a.kv.num_blocks - 1u);
+          const size_t page = ((size_t)id * a.Hkv + kvh) * (size_t)(hd * bs);
+          const int off = pos % bs;
+          const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.kv.k) + page + ((size_t)p8 * bs + off) * 8);
+          const T* v = static_cast<const T*>(a.kv.v) + page + (size_t)(8 * p8) * bs + off;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v[(size_t)e * bs]; }
+        } else {
+          const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.k) + (size_t)(it.m0 + pos) * a.k_stride + (size_t)kvh * hd + 8 * p8);
+          const Piece v = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.v) + (size_t)(it.m0 + pos) * a.v_stride + (size_t)kvh * hd + 8 * p8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v.x[e]; }
+        }
+      }
+      f32x4 *dk = reinterpret_cast<f32x4*>(s_k + key * LD + 8 * p8), *dv = reinterpret_cast<f32x4*>(s_v + key * LD + 8 * p8);
+      dk[0] = (f32x4){kx[0], kx[1], kx[2], kx[3]}; dk[1] = (f32x4){kx[4], kx[5], kx[6], kx[7]};
+      dv[0] = (f32x4){vx[0], vx[1], vx[2], vx[3]}; dv[1] = (f32x4){vx[4], vx[5], vx[6], vx[7]};
+    }
+    __syncthreads();
+    f32x4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 k = *reinterpret_cast<const f32x4*>(s_k + (16 * h + l16) * LD + 16 * u + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[u][e], S[h], 0, 0, 0);
+      }
+    float tm = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (k0 + 16 * h + 4 * g + e > lim) S[h][e] = -INFINITY;
+        tm = fmaxf(tm, S[h][e]);
+      }
+    uint32_t x, y;
+    lane_pair<16>(__float_as_uint(tm), x, y);
+    tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
+    lane_pair<32>(__float_as_uint(tm), x, y);
+    tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
+    const float nm = fmaxf(run_m, tm), ref = nm == -INFINITY ? 0.f : nm;
+    const float alpha = __builtin_amdgcn_exp2f(run_m - ref);
+    run_m = nm;
+    run_l *= alpha;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) O[u] *= alpha;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(S[h][e] - ref);
+        run_l += p;
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+          O[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(s_v[(16 * h + 4 * g + e) * LD + 16 * u + l16], p, O[u], 0, 0, 0);
+      }
+    __syncthreads();
+  }
+  // the row's sum over the four lane groups
+  uint32_t x, y;
+  lane_pair<16>(__float_as_uint(run_l), x, y);
+  run_l = __uint_as_float(x) + __uint_as_float(y);
+  lane_pair<32>(__float_as_uint(run_l), x, y);
+  run_l = __uint_as_float(x) + __uint_as_float(y);
+  if (rw >= it.R) return;
+  const int m = it.m0 + j, h = kvh * G + r - j * G;
+  const float inv = 1.f / run_l;
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    if (16 * u + 4 * g >= hd) continue;
+    if constexpr (PAGED) {
+      *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + 16 * u + 4 * g) = O[u];
+    } else {
+      T* o = static_cast<T*>(a.out) + ((size_t)m * a.H + h) * hd + 16 * u + 4 * g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (T)(O[u][e] * inv);
+    }
+  }
+  if (PAGED && g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m, run_l);
+}
+
+// ------------------------------------------------------------------------------------------
+// launch
+// ------------------------------------------------------------------------------------------
+static bool tile_mfma(const TileArgs& a, bool paged) {
+  return a.dtype == MN_DT_BF16 && (a.hd == 64 || a.hd == 128) && (!paged || a.kv.block_size == PAGE);
+}
+
+// Rows of a workgroup's tile for a call whose longest stack and number of stack rows per KV head are given.
+int prompt_tile_rows(int H, int Hkv, int hd, int dtype, long stack_rows) {
+  TileArgs a{};
+  a.dtype = dtype; a.hd = hd;
+  if (!tile_mfma(a, false)) return FROWS;
+  // 256 rows where that leaves a workgroup per CU, 64 otherwise
+  return stack_rows * Hkv >= 256 * 256 ? 256 : 64;
+}
+
+template <typename K>
+static hipError_t allow_lds(K kernel, size_t bytes) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <int HDIM, int CT, int NW, bool PAGED>
+static hipError_t launch_mfma(const TileArgs& a, hipStream_t st) {
+  static std::once_flag once;
+  static hipError_t err = hipSuccess;
+  std::call_once(once, [] { err = allow_lds(tile_mfma_kernel<HDIM, CT, NW, PAGED>, STAGES * TileStage<HDIM>::BYTES); });
+  if (err != hipSuccess) return err;
+  tile_mfma_kernel<HDIM, CT, NW, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv, NW * 64, STAGES * TileStage<HDIM>::BYTES, st>>>(a);
+  return hipSuccess;
+}
+
+template <typename T, int HDP, bool PAGED>
+static hipError_t launch_f32(const TileArgs& a, hipStream_t st) {
+  constexpr size_t need = 2 * (size_t)FKEYS * (HDP + 4) * 4;
+  static std::once_flag once;
+  static hipError_t err = hipSuccess;
+  std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED>, need); });
+  if (err != hipSuccess) return err;
+  const size_t list = PAGED || a.B <= 64 ? 0 : (size_t)a.B * 4;  // (the search's numbers)
+  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv, 256, need > list ? need : list, st>>>(a);
+  return hipSuccess;
+}
+
+template <typename T, bool PAGED>
+static hipError_t launch_f32_hd(const TileArgs& a, hipStream_t st) {
+  switch (a.hd) {
+    case 8: case 16: return launch_f32<T, 16, PAGED>(a, st);
+    case 32: return launch_f32<T, 32, PAGED>(a, st);
+    case 64: return launch_f32<T, 64, PAGED>(a, st);
+    case 128: return launch_f32<T, 128, PAGED>(a, st);
+    default: return launch_f32<T, 256, PAGED>(a, st);
+  }
+}
+
+hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st) {
+  if (a.n_tiles <= 0) return hipSuccess;
+  if (!tile_mfma(a, false)) return a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, false>(a, st) : launch_f32_hd<float, false>(a, st);
+  if (a.hd == 128) return tile_rows == 256 ? launch_mfma<128, 2, 8, false>(a, st) : launch_mfma<128, 1, 4, false>(a, st);
+  return tile_rows == 256 ? launch_mfma<64, 2, 8, false>(a, st) : launch_mfma<64, 1, 4, false>(a, st);
+}
+
+}  // namespace mn

@@ -201,6 +201,26 @@ class DeviceKV:
         return (self.k_pages[layer].float().cpu().numpy(), self.v_pages[layer].float().cpu().numpy())
 
 
+class PromptRows:
+    """The host's copy of a packed batch's row offsets (they size the launch)."""
+
+    def __init__(self, row0: Sequence[int]):
+        self.B, self.h = len(row0) - 1, B.host_i32(row0)
+
+
+def prompt_attention(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_rows: torch.Tensor, plan: PromptRows,
+                     out: torch.Tensor, kv: Optional[DeviceKV] = None, layer: int = 0, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention over the packed rows of whole prompts; with `kv` the rows of k and v also enter the cache.
+    q [M][H][hd], k and v [M][Hkv][hd]: views with any row stride (a QKV projection's rows)."""
+    for t in (q, k, v):
+        assert t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2]
+    assert out.is_contiguous() and out.dtype == q.dtype
+    B.mn_prompt_attention(model.ctx, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                          seq_rows.data_ptr(), plan.h, plan.B, out.data_ptr(), kv.c if kv is not None else None, layer,
+                          dev_status.data_ptr() if dev_status is not None else None, stream_ptr())
+    return out
+
+
 class KVPool:
     """Which slot of a DeviceKV's table holds which blocks (mn_kv_*): forked requests share pages, every slot gets room ahead of
     its next tokens, finished ones give their blocks back, and the pool can be packed.  The whole mapping (table, references,

@@ -1,0 +1,221 @@
+"""Attention over whole prompts (mn_prompt_attention) against the definition in 64 bits, every element within the bound that the
+roundings of its inputs' type allow (attention_bounds.py)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2402_15678_amd import synth
+from tests.attention_bounds import attend, check
+
+pytestmark = pytest.mark.gpu
+DT = {"f16": torch.float16, "f32": torch.float32}
+
+
+def _model(H, Hkv, hd, kind, max_pos=1 << 16):
+    from paper_2402_15678_amd import harness
+    d = synth.ModelDesc(synth.ARCH_LLAMA, synth.DT_BF16 if kind == "f16" else synth.DT_F32, 1, 128, H, Hkv, hd, 128, 8, max_pos)
+    return d, harness.DeviceModel.random_on_device(d, 1)
+
+
+def _rows(H, Hkv, hd, kind, lens, seed, scale=1.0, lead=0, tail=0, pad=0):
+    """A QKV projection's rows; what lies in front of the first sequence and behind the last is not a number."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    M = lead + sum(lens)
+    x = torch.randn((M + tail, (H + 2 * Hkv) * hd + pad), generator=g, device="cuda")
+    x[:, :H * hd] *= scale
+    x[:lead] = float("nan")
+    x[M:] = float("nan")
+    x[:, (H + 2 * Hkv) * hd:] = float("nan")
+    x = x.to(DT[kind])
+    q = x[:, :H * hd].view(-1, H, hd) if not pad else x[:, :H * hd].unflatten(1, (H, hd))
+    k = x[:, H * hd:(H + Hkv) * hd].unflatten(1, (Hkv, hd))
+    v = x[:, (H + Hkv) * hd:(H + 2 * Hkv) * hd].unflatten(1, (Hkv, hd))
+    row0 = (lead + np.concatenate(([0], np.cumsum(lens)))).astype(np.int32)
+    return q, k, v, row0
+
+
+def _call(model, q, k, v, row0, out, kv=None, h_row0=None):
+    from paper_2402_15678_amd import harness
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    harness.prompt_attention(model, q, k, v, torch.from_numpy(row0).cuda(), harness.PromptRows((row0 if h_row0 is None else h_row0).tolist()),
+                             out, kv, 0, status)
+    torch.cuda.synchronize()
+    return status.item()
+
+
+def _compare(q, k, v, row0, out, kind):
+    for a, b in zip(row0[:-1].tolist(), row0[1:].tolist()):
+        if a < b:
+            want, bound = attend(q[a:b], k[a:b], v[a:b], torch.arange(b - a, device="cuda"), kind == "f16")
+            check(out[a:b], want, bound)
+
+
+GEOMETRIES = [(64, 8, 128, "f16"), (4, 4, 128, "f16"), (12, 12, 64, "f16"), (6, 2, 64, "f16"), (5, 1, 128, "f16"), (128, 2, 64, "f16"),
+              (4, 4, 64, "f32"), (8, 2, 128, "f32"), (6, 2, 32, "f32"), (8, 8, 8, "f32"), (4, 1, 16, "f32"), (2, 2, 256, "f32"),
+              (8, 8, 32, "f16"), (8, 2, 256, "f16"), (16, 4, 8, "f16"), (8, 8, 16, "f16")]
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", GEOMETRIES)
+@pytest.mark.parametrize("lens", [[1], [2, 0, 1, 33], [15, 16, 17, 31, 32, 65], [130, 0, 257]], ids=str)
+def test_prompt_matches_the_definition(H, Hkv, hd, kind, lens):
+    d, model = _model(H, Hkv, hd, kind)
+    q, k, v, row0 = _rows(H, Hkv, hd, kind, lens, sum(lens) + H + hd)
+    out = torch.full((len(q), H * hd), -7.0, dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    _compare(q, k, v, row0, out, kind)
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind,lens", [
+    (64, 8, 128, "f16", [700, 1, 1153, 64]), (8, 8, 128, "f16", [2100, 300, 3]), (12, 12, 64, "f16", [1500, 77, 512, 513]),
+    (64, 8, 128, "f16", [5]), (40, 40, 128, "f16", [300, 900, 60, 777]), (8, 1, 64, "f16", [4099]), (4, 4, 64, "f32", [1000, 31]), (24, 2, 64, "f16", [1, 4000, 2])])
+def test_long_and_ragged_prompts(H, Hkv, hd, kind, lens):
+    d, model = _model(H, Hkv, hd, kind)
+    q, k, v, row0 = _rows(H, Hkv, hd, kind, lens, 5)
+    out = torch.full((len(q), H * hd), -7.0, dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    _compare(q, k, v, row0, out, kind)
+
+
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f16", 64), ("f32", 64)])
+@pytest.mark.parametrize("count", [64, 65, 300, 4096])
+def test_many_sequences(kind, hd, count):
+    g = np.random.default_rng(count)
+    lens = [int(x) for x in (g.integers(0, 9, count) if count > 300 else g.integers(0, 120, count))]
+    d, model = _model(4, 2, hd, kind)
+    q, k, v, row0 = _rows(4, 2, hd, kind, lens, 6)
+    out = torch.full((len(q), 4 * hd), -7.0, dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    # (a sample of the sequences: the definition goes one by one)
+    for b in sorted(set(g.integers(0, count, 60).tolist())):
+        a, z = int(row0[b]), int(row0[b + 1])
+        if a < z:
+            check(out[a:z], *attend(q[a:z], k[a:z], v[a:z], torch.arange(z - a, device="cuda"), kind == "f16"))
+    assert not (out == -7.0).all(dim=1).any()
+
+
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f16", 64), ("f32", 32), ("f16", 32)])
+def test_rows_outside_the_sequences_are_neither_read_nor_written(kind, hd):
+    lens, lead, tail = [70, 5, 129], 3, 9
+    d, model = _model(8, 4, hd, kind)
+    q, k, v, row0 = _rows(8, 4, hd, kind, lens, 7, lead=lead, tail=tail, pad=16)
+    out = torch.full((len(q), 8 * hd), -7.0, dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    _compare(q, k, v, row0, out, kind)
+    assert (out[:lead] == -7.0).all() and (out[lead + sum(lens):] == -7.0).all()
+
+
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f16", 64), ("f32", 64)])
+@pytest.mark.parametrize("shape", ["peaked", "rising", "falling", "flat", "late"])
+def test_scores_far_apart(kind, hd, shape):
+    """The running reference: scores of +-200 and more, ascending and descending along the keys, all equal, one large one late."""
+    n = 300
+    d, model = _model(4, 2, hd, kind)
+    q, k, v, row0 = _rows(4, 2, hd, kind, [n], 8)
+    q, k = q.clone(), k.clone()
+    if shape == "peaked":
+        q *= 20
+    elif shape in ("rising", "falling"):
+        q[:] = 1.0
+        ramp = torch.arange(n, device="cuda") / n * 40 - 20
+        k[:] = (ramp if shape == "rising" else ramp.flip(0)).view(-1, 1, 1).to(k.dtype)
+    elif shape == "flat":
+        k[:] = 0.0
+    else:
+        q[:] = 4.0
+        k *= 0.1
+        k[n - 70] = 8.0
+    out = torch.zeros((n, 4 * hd), dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    _compare(q, k, v, row0, out, kind)
+
+
+def test_values_of_the_whole_fp16_range():
+    for hd in (64, 128, 32):
+        d, model = _model(4, 4, hd, "f16")
+        q, k, v, row0 = _rows(4, 4, hd, "f16", [100], 9)
+        v = torch.where(v > 0, 65504.0, -65504.0).to(torch.float16)
+        v[:, 1] = 6e-8
+        out = torch.zeros((100, 4 * hd), dtype=torch.float16, device="cuda")
+        assert _call(model, q, k, v, row0, out) == 0
+        _compare(q, k, v, row0, out, "f16")
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind,bs", [(64, 8, 128, "f16", 16), (6, 2, 64, "f16", 16), (4, 4, 64, "f32", 16), (4, 2, 128, "f16", 8),
+                                              (6, 2, 32, "f32", 5), (8, 8, 8, "f32", 1), (5, 1, 128, "f16", 16)])
+def test_prompts_enter_the_cache(H, Hkv, hd, kind, bs):
+    from paper_2402_15678_amd import harness
+    lens = [37, 1, 0, 64, 130]
+    d, model = _model(H, Hkv, hd, kind)
+    q, k, v, row0 = _rows(H, Hkv, hd, kind, lens, 10)
+    need = [-(-n // bs) for n in lens]
+    g = np.random.default_rng(3)
+    ids = g.permutation(sum(need) + 3).astype(np.int32)
+    table = np.full((len(lens), max(need) + 1), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = ids[at:at + n]
+        at += n
+    blocks = len(ids)
+    kp = torch.full((blocks, Hkv, hd // 8, bs, 8), -3.0, dtype=DT[kind], device="cuda")
+    vp = torch.full((blocks, Hkv, hd, bs), -3.0, dtype=DT[kind], device="cuda")
+    wk, wv = kp.clone(), vp.clone()
+    for b, n in enumerate(lens):
+        for i in range(n):
+            r, blk, off = int(row0[b]) + i, int(table[b, i // bs]), i % bs
+            wk[blk, :, :, off] = k[r].view(Hkv, -1, 8)
+            wv[blk, :, :, off] = v[r]
+    kv = harness.DeviceKV(d, bs, blocks, table, [9] * len(lens), [kp], [vp])
+    out = torch.zeros((len(q), H * hd), dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out, kv) == 0
+    _compare(q, k, v, row0, out, kind)
+    assert torch.equal(kp, wk) and torch.equal(vp, wv)
+    assert kv.ctx_lens.tolist() == [9] * len(lens)
+    # a block id out of range: its tokens stay out of the cache, everything else is as before
+    from paper_2402_15678_amd import binding
+    hit = int(table[4, 2 if bs > 1 else 100])
+    table[4, 2 if bs > 1 else 100] = blocks + 5
+    kp.fill_(-3.0)
+    vp.fill_(-3.0)
+    wk[hit], wv[hit] = -3.0, -3.0
+    kv = harness.DeviceKV(d, bs, blocks, table, [9] * len(lens), [kp], [vp])
+    again = torch.zeros_like(out)
+    assert _call(model, q, k, v, row0, again, kv) == binding.MN_DEV_BLOCK_TABLE
+    assert torch.equal(again, out) and torch.equal(kp, wk) and torch.equal(vp, wv)
+
+
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f32", 32)])
+def test_lengths_that_do_not_fit_the_launch_leave_the_call_undone(kind, hd):
+    from paper_2402_15678_amd import binding
+    lens = [70, 40, 300]
+    d, model = _model(4, 4, hd, kind)
+    q, k, v, row0 = _rows(4, 4, hd, kind, lens, 11)
+    for wrong in ([0, 70, 110, 411], [0, 70, 60, 410], [-1, 70, 110, 410], [0, 10, 20, 30], [0, 0, 0, 410], [0, 70, 110, 1 << 30]):
+        out = torch.full((len(q), 4 * hd), -7.0, dtype=DT[kind], device="cuda")
+        assert _call(model, q, k, v, np.array(wrong, np.int32), out, h_row0=row0) == binding.MN_DEV_SPEC_LEN
+        assert (out == -7.0).all()
+
+
+def test_same_numbers_on_another_stream_and_from_a_graph():
+    from paper_2402_15678_amd import harness
+    d, model = _model(64, 8, 128, "f16")
+    q, k, v, row0 = _rows(64, 8, 128, "f16", [300, 41, 800], 12)
+    rows, plan = torch.from_numpy(row0).cuda(), harness.PromptRows(row0.tolist())
+    want = torch.zeros((len(q), 64 * 128), dtype=torch.float16, device="cuda")
+    harness.prompt_attention(model, q, k, v, rows, plan, want)
+    out = torch.zeros_like(want)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        harness.prompt_attention(model, q, k, v, rows, plan, out)
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        harness.prompt_attention(model, q, k, v, rows, plan, out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        harness.prompt_attention(model, q, k, v, rows, plan, want)
