@@ -786,6 +786,7 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   long tiles = 0;
   for (int b = 0; b < B; ++b) tiles += ((long)(h_seq_rows[b + 1] - h_seq_rows[b]) * G + rows - 1) / rows;
   if (tiles * d.n_kv_heads >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
+  if (tiles == 0) return MN_OK;
   t.n_tiles = (int)tiles;
   t.max_tiles = (int)(((long)longest * G + rows - 1) / rows);
   hipError_t lerr;

@@ -549,7 +549,6 @@ static hipError_t launch_f32_hd(const TileArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st) {
-  if (a.n_tiles <= 0) return hipSuccess;
   if (!tile_mfma(a, false)) return a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, false>(a, st) : launch_f32_hd<float, false>(a, st);
   if (a.hd == 128) return tile_rows == 256 ? launch_mfma<128, 2, 8, false>(a, st) : launch_mfma<128, 1, 4, false>(a, st);
   return tile_rows == 256 ? launch_mfma<64, 2, 8, false>(a, st) : launch_mfma<64, 1, 4, false>(a, st);
