@@ -450,6 +450,17 @@ mn_status mn_prompt_attention(mn_ctx *ctx, const void *q, long q_stride, const v
                               long v_stride, const int32_t *seq_rows, const int32_t *h_seq_rows, int B, const mn_kv *kv,
                               int layer, void *out, int32_t *dev_status, void *stream);
 
+/* Multi-token paged attention of one layer for a batch whose sequences share their first prefix_len cached tokens (mn_kv_fork
+ * leaves them so): what mn_attention computes, with the shared keys read once for all sequences instead of once for each.
+ * Arguments as there; prefix_len is a multiple of the block size, 0 included, and smaller than max_ctx.  The first
+ * prefix_len / block_size entries of every table row are the same blocks and ctx_lens[b] >= prefix_len; a sequence for which
+ * either does not hold (MN_DEV_BLOCK_TABLE, MN_DEV_CTX), or whose row holds an id out of range, gets zeros.
+ * workspace: mn_prefix_workspace_bytes(ctx, B, sum_b q_b or more, prefix_len, max_ctx or more) bytes, 256-byte aligned. */
+size_t mn_prefix_workspace_bytes(const mn_ctx *ctx, int B, int max_rows, int prefix_len, int max_ctx);
+mn_status mn_prefix_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, const int32_t *h_spec_len, int B,
+                              int prefix_len, int max_ctx, const mn_kv *kv, int layer, void *out, void *workspace,
+                              size_t workspace_bytes, int32_t *dev_status, void *stream);
+
 /* ---- timing taps (for benchmarks; off by default) --------------------------------------------- */
 
 /* Kernel families of the step, as indexed in mn_profile_collect's arrays. */

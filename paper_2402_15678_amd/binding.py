@@ -28,7 +28,8 @@ EXPORTS = ("mn_create", "mn_destroy", "mn_last_error", "mn_status_str", "mn_work
            "mn_profile_collect", "mn_packed_weight_bytes", "mn_pack_weight", "mn_acr_update",
            "mn_verify_sample", "mn_draft_sample",
            "mn_selector_create", "mn_selector_destroy", "mn_selector_observe", "mn_selector_current",
-           "mn_prompt_attention", "mn_kv_workspace_bytes", "mn_kv_reserve", "mn_kv_fork", "mn_kv_free", "mn_kv_compact",
+           "mn_prompt_attention", "mn_prefix_workspace_bytes", "mn_prefix_attention",
+           "mn_kv_workspace_bytes", "mn_kv_reserve", "mn_kv_fork", "mn_kv_free", "mn_kv_compact",
            "mn_selector_adjustments", "mn_probe_stream_read", "mn_probe_mfma", "mn_probe_mfma_data")
 PROF_KINDS = ("prepare", "norm", "gemm", "rope_append", "attention", "act", "argmax", "vote", "accept")
 
@@ -101,6 +102,10 @@ def _load() -> C.CDLL:
     lib.mn_prompt_attention.restype = i32
     lib.mn_prompt_attention.argtypes = [vp, vp, C.c_long, vp, C.c_long, vp, C.c_long, vp, C.POINTER(C.c_int32), i32,
                                         C.POINTER(KV), i32, vp, vp, vp]
+    lib.mn_prefix_workspace_bytes.restype = sz
+    lib.mn_prefix_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.mn_prefix_attention.restype = i32
+    lib.mn_prefix_attention.argtypes = [vp, vp, vp, C.POINTER(C.c_int32), i32, i32, i32, C.POINTER(KV), i32, vp, vp, sz, vp, vp]
     lib.mn_kv_workspace_bytes.restype = sz
     lib.mn_kv_workspace_bytes.argtypes = [i32, i32]
     lib.mn_kv_reserve.restype = i32
@@ -250,6 +255,16 @@ def mn_prompt_attention(ctx, q, q_stride, k, k_stride, v, v_stride, seq_rows, h_
                         layer=0, dev_status=None, stream=None) -> None:
     _check(lib.mn_prompt_attention(ctx, q, q_stride, k, k_stride, v, v_stride, seq_rows, h_seq_rows, B,
                                    C.byref(kv) if kv is not None else None, layer, out, dev_status, stream), ctx)
+
+
+def mn_prefix_workspace_bytes(ctx, B: int, max_rows: int, prefix_len: int, max_ctx: int) -> int:
+    return int(lib.mn_prefix_workspace_bytes(ctx, B, max_rows, prefix_len, max_ctx))
+
+
+def mn_prefix_attention(ctx, q, spec_len, h_spec_len, B, prefix_len, max_ctx, kv: KV, layer, out, workspace, workspace_bytes,
+                        dev_status=None, stream=None) -> None:
+    _check(lib.mn_prefix_attention(ctx, q, spec_len, h_spec_len, B, prefix_len, max_ctx, C.byref(kv), layer, out, workspace,
+                                   workspace_bytes, dev_status, stream), ctx)
 
 
 def mn_kv_workspace_bytes(num_blocks: int, max_seqs: int) -> int:

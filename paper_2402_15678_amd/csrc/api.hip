@@ -798,6 +798,53 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   return hip_check(c, who);
 }
 
+// ---- attention behind a shared prefix ------------------------------------------------------------------
+extern "C" size_t mn_prefix_workspace_bytes(const mn_ctx* c, int B, int max_rows, int prefix_len, int max_ctx) {
+  if (!c || B < 0 || B > MN_MAX_BATCH || max_rows < 0 || max_rows > (1 << 20) || prefix_len < 0 || max_ctx < prefix_len) return 0;
+  return prefix_workspace_bytes(B > 0 ? B : 1, max_rows > 0 ? max_rows : 1, c->d.n_heads, c->d.n_kv_heads, c->d.head_dim, prefix_len, max_ctx);
+}
+
+extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t* spec_len, const int32_t* h_spec_len, int B,
+                                         int prefix_len, int max_ctx, const mn_kv* kv, int layer, void* out, void* workspace,
+                                         size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  const char* who = "mn_prefix_attention";
+  if (!c) return MN_ENULL;
+  if (B < 0 || B > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: B = %d outside [0, %d]", who, B, MN_MAX_BATCH);
+  if (max_ctx < 0) return fail(c, MN_EINVAL, "%s: max_ctx = %d", who, max_ctx);
+  if (B == 0) return MN_OK;
+  if (!q || !spec_len || !h_spec_len || !out) return fail(c, MN_ENULL, "%s: a required pointer is NULL", who);
+  if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(c, MN_EINVAL, "%s: q and out must be 16-byte aligned", who);
+  if (mn_status s = check_kv(c, kv, max_ctx, who)) return s;
+  const mn_model_desc& d = c->d;
+  if (layer < 0 || layer >= (d.n_layers > 0 ? d.n_layers : 1)) return fail(c, MN_EINVAL, "%s: layer %d", who, layer);
+  if (!kv->k_layers[layer] || !kv->v_layers[layer]) return fail(c, MN_ENULL, "%s: kv layer pointer is NULL", who);
+  if (prefix_len < 0 || prefix_len % kv->block_size) return fail(c, MN_EINVAL, "%s: prefix_len = %d is no multiple of the block size %d", who, prefix_len, kv->block_size);
+  int k_max = 0;
+  for (int b = 0; b < B; ++b) if (h_spec_len[b] > k_max) k_max = h_spec_len[b];
+  int M = 0, max_q = 0;
+  if (mn_status s = count_rows(c, h_spec_len, B, k_max, &M, &max_q, who)) return s;
+  if ((long)max_ctx < (long)prefix_len + max_q)
+    return fail(c, MN_EINVAL, "%s: max_ctx %d smaller than the prefix of %d and the longest scored run %d", who, max_ctx, prefix_len, max_q);
+  if ((long)M * (d.n_heads / d.n_kv_heads) >= (1l << 29)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d heads", who, M, d.n_heads);
+  if (max_ctx >= (1 << 28)) return fail(c, MN_EUNSUPPORTED, "%s: max_ctx = %d", who, max_ctx);
+  if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
+  if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
+  const size_t need = prefix_workspace_bytes(B, M, d.n_heads, d.n_kv_heads, d.head_dim, prefix_len, max_ctx);
+  if (workspace_bytes < need) return fail(c, MN_EWORKSPACE, "%s: workspace %zu bytes, need %zu", who, workspace_bytes, need);
+  TileArgs t{};
+  t.kv = KvView{kv->k_layers[layer], kv->v_layers[layer], kv->block_tables, kv->block_size, kv->num_blocks, kv->max_blocks_per_seq};
+  t.q = q; t.q_stride = (long)d.n_heads * d.head_dim; t.out = out;
+  t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.B = B;
+  t.prefix_len = prefix_len; t.status = dev_status;
+  hipError_t lerr;
+  {
+    Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);
+    lerr = launch_prefix(t, spec_len, kv->ctx_lens, max_q, max_ctx, workspace, (hipStream_t)stream);
+  }
+  if (lerr != hipSuccess) return fail(c, MN_EHIP, "%s: kernel attribute: %s", who, hipGetErrorString(lerr));
+  return hip_check(c, who);
+}
+
 // ---- page pool ----------------------------------------------------------------------------------------
 static mn_status check_pool(mn_ctx* c, const mn_kv* kv, const mn_pool* pool, int n, int32_t* status, bool pages, const char* who, PoolView* out) {
   if (!kv || !pool) return fail(c, MN_ENULL, "%s: kv or pool is NULL", who);

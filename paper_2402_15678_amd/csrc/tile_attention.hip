@@ -105,6 +105,20 @@ __device__ __forceinline__ bool list_item(const TileArgs& a, int t, Item& it) {
   return it.R > 0;
 }
 
+// A sequence's table row, looked at by one workgroup of its items: every block id in range, and the prefix's entries those of the first
+// row (what the call reads for all of them).  Rows of a sequence that fails are zeros (prefix_merge_kernel).
+__device__ __forceinline__ void check_table(const TileArgs& a, const Item& it, int kvh) {
+  if (it.slot != a.prefix_splits || it.rbase != 0 || kvh != 0) return;
+  const int32_t *first = a.kv.block_tables, *row = first + (size_t)it.seq * a.kv.max_blocks_per_seq;
+  const int shared = a.prefix_len / a.kv.block_size, all = (int)(((long)it.ctx + it.R / (a.H / a.Hkv) + a.kv.block_size - 1) / a.kv.block_size);
+  bool bad = false;
+  for (int i = threadIdx.x; i < all; i += blockDim.x) bad |= (uint32_t)row[i] >= (uint32_t)a.kv.num_blocks || (i < shared && row[i] != first[i]);
+  if (bad) {
+    a.seq_bad[it.seq] = 1;
+    if (a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+  }
+}
+
 // Rows of K and V of the tokens whose first stack row lies in this tile, into the pages (position = token of the sequence).
 template <typename T, int ROWS>
 __device__ __forceinline__ void append_rows(const TileArgs& a, const Item& it, int G, int kvh) {
@@ -162,6 +176,7 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(Til
   Item it;
   if constexpr (PAGED) {
     if (!list_item(a, t, it)) return;
+    check_table(a, it, kvh);
   } else {
     if (!prompt_item<ROWS>(a, t, G, reinterpret_cast<int32_t*>(smem), it)) return;
     if (a.kv.k) append_rows<f16_t, ROWS>(a, it, G, kvh);
@@ -381,6 +396,7 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
   Item it;
   if constexpr (PAGED) {
     if (!list_item(a, t, it)) return;
+    check_table(a, it, kvh);
   } else {
     if (!prompt_item<FROWS>(a, t, G, reinterpret_cast<int32_t*>(smem), it)) return;
     if (a.kv.k) append_rows<T, FROWS>(a, it, G, kvh);
@@ -495,6 +511,116 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
+// a batch that shares a prefix
+// ------------------------------------------------------------------------------------------
+// Every row sees the shared keys [0, P) and its own sequence's from P on.  The shared part is one dense product: all rows of the batch,
+// stacked, against keys that are read once per tile of rows, in `prefix_splits` ranges of keys when the rows alone do not fill the
+// chip.  The rest goes sequence by sequence, in ranges of `chunk` keys.  Each range leaves an unnormalised output with its
+// reference and sum per row in a slot of its own, and a row's slots are put together at the end.
+//
+// prefix_plan_kernel (one workgroup): the rows' sequences, who takes part, and the list of items.
+__global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
+  __shared__ int s_rows[16], s_items[16], s_bad;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  int flags = 0;
+  const auto length = [&](int b) {
+    const int k = p.spec_len[b];
+    return k >= 0 && k < p.max_q ? k + 1 : -1;
+  };
+  // lengths first: rows that do not add up to the host's, or a run longer than its longest, disable the batch
+  int rows = 0;
+  bool off = false;
+  for (int b = tid; b < p.B; b += 1024) {
+    const int q = length(b);
+    off |= q < 0;
+    rows += max(q, 0);
+  }
+  rows = wave_sum_i(rows);
+  if (lane == 0) s_rows[wave] = rows;
+  if (off) s_bad = 1;
+  __syncthreads();
+  int total = 0;
+  for (int w = 0; w < 16; ++w) total += s_rows[w];
+  const bool batch = s_bad == 0 && total == p.M;
+  if (!batch) flags |= MN_DEV_SPEC_LEN;
+  int4* items = reinterpret_cast<int4*>(p.items);
+  const int R = p.G * p.M, shared = batch ? p.row_tiles * p.prefix_splits : 0;
+  const int tiles = (p.prefix_len + TKEYS - 1) / TKEYS;
+  for (int i = tid; i < shared; i += 1024) {
+    const int rt = i / p.prefix_splits, s = i % p.prefix_splits;
+    const int k0 = (int)((long)tiles * s / p.prefix_splits) * TKEYS, k1 = min(p.prefix_len, (int)((long)tiles * (s + 1) / p.prefix_splits) * TKEYS);
+    items[2 * i] = make_int4(0, R, rt * p.tile_rows, k0);
+    items[2 * i + 1] = make_int4(k1, NO_LIMIT, 0, s);
+  }
+  int row_at = 0, item_at = shared;
+  for (int b0 = 0; b0 < p.B; b0 += 1024) {
+    const int b = b0 + tid, q = batch && b < p.B ? length(b) : 0;
+    int ctx = 0, ranges = 0, rts = 0;
+    if (q > 0) {
+      ctx = p.ctx_lens[b];
+      if (ctx < p.prefix_len || (long)ctx + q > p.max_ctx) {
+        flags |= MN_DEV_CTX;
+      } else {
+        ranges = (ctx + q - p.prefix_len + p.chunk - 1) / p.chunk;
+        rts = (p.G * q + p.tile_rows - 1) / p.tile_rows;
+      }
+    }
+    const int rows_incl = wave_scan_i(q), items_incl = wave_scan_i(ranges * rts);
+    __syncthreads();
+    if (lane == 63) { s_rows[wave] = rows_incl; s_items[wave] = items_incl; }
+    __syncthreads();
+    int row0 = row_at + rows_incl - q, at = item_at + items_incl - ranges * rts;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) { row0 += s_rows[w]; at += s_items[w]; }
+      row_at += s_rows[w];
+      item_at += s_items[w];
+    }
+    if (b < p.B) p.seq_bad[b] = 0;
+    for (int j = 0; j < q; ++j) p.row_meta[row0 + j] = make_int2(b, ranges);
+    for (int rt = 0; rt < rts; ++rt)
+      for (int s = 0; s < ranges; ++s, ++at) {
+        const int k0 = p.prefix_len + s * p.chunk;
+        items[2 * at] = make_int4(row0, p.G * q, rt * p.tile_rows, k0);
+        items[2 * at + 1] = make_int4(min(k0 + p.chunk, ctx + q), ctx, b, p.prefix_splits + s);
+      }
+  }
+  if (!batch)
+    for (int m = tid; m < p.M; m += 1024) p.row_meta[m] = make_int2(0, 0);
+  for (int i = item_at + tid; i < p.max_items; i += 1024) items[2 * i] = make_int4(0, 0, 0, 0);
+  if (flags && p.status) atomicOr(p.status, flags);
+}
+
+// Four elements of a row of one head per thread.
+template <typename T>
+__global__ void __launch_bounds__(256) prefix_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ ml_part,
+                                                           const int2* __restrict__ row_meta, const int32_t* __restrict__ seq_bad,
+                                                           int prefix_splits, int M, int H, int hd, T* __restrict__ out) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, heads = (size_t)M * H;
+  const int per = hd / 4;
+  if (i >= heads * per) return;
+  const size_t mh = i / per;
+  const int2 meta = row_meta[mh / H];
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  if (meta.y > 0 && !seq_bad[meta.x]) {
+    const int n = prefix_splits + meta.y;
+    float top = -INFINITY;
+    for (int s = 0; s < n; ++s) top = fmaxf(top, ml_part[(s * heads + mh) * 2]);
+    for (int s = 0; s < n; ++s) {
+      const float2 ml = *reinterpret_cast<const float2*>(ml_part + (s * heads + mh) * 2);
+      const float w = __builtin_amdgcn_exp2f(ml.x - top);
+      l += ml.y * w;
+      o += *reinterpret_cast<const f32x4*>(o_part + s * heads * hd + 4 * i) * w;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[4 * i + e] = (T)(o[e] * inv);
+}
+
+// ------------------------------------------------------------------------------------------
 // launch
 // ------------------------------------------------------------------------------------------
 static bool tile_mfma(const TileArgs& a, bool paged) {
@@ -552,6 +678,88 @@ hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st) {
   if (!tile_mfma(a, false)) return a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, false>(a, st) : launch_f32_hd<float, false>(a, st);
   if (a.hd == 128) return tile_rows == 256 ? launch_mfma<128, 2, 8, false>(a, st) : launch_mfma<128, 1, 4, false>(a, st);
   return tile_rows == 256 ? launch_mfma<64, 2, 8, false>(a, st) : launch_mfma<64, 1, 4, false>(a, st);
+}
+
+
+// Shape of a shared-prefix launch, from what the host knows.
+constexpr int MAX_PREFIX_SPLITS = 32, MAX_RANGES = 16, TARGET_WGS = 512, PREFIX_TILE_ROWS = 256;
+struct PrefixShape {
+  int tile_rows, row_tiles, prefix_splits, chunk, ranges;
+};
+static int prefix_tile_rows(const TileArgs& a, int M) {
+  if (!tile_mfma(a, true)) return FROWS;
+  return (long)M * (a.H / a.Hkv) > 64 ? PREFIX_TILE_ROWS : 64;
+}
+static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
+  PrefixShape s;
+  const int G = a.H / a.Hkv;
+  s.tile_rows = prefix_tile_rows(a, M);
+  s.row_tiles = (int)(((long)M * G + s.tile_rows - 1) / s.tile_rows);
+  const int tiles = (a.prefix_len + TKEYS - 1) / TKEYS, by_keys = tiles / 4 > 1 ? tiles / 4 : 1;
+  const long wgs = (long)s.row_tiles * a.Hkv;
+  int n = (int)((TARGET_WGS + wgs - 1) / wgs);
+  if (n > by_keys) n = by_keys;
+  if (n > MAX_PREFIX_SPLITS) n = MAX_PREFIX_SPLITS;
+  s.prefix_splits = a.prefix_len > 0 ? n : 0;
+  const int rest = max_ctx - a.prefix_len, want = (long)a.B * a.Hkv >= 256 ? 1024 : 256;
+  s.ranges = (rest + want - 1) / want;
+  if (s.ranges > MAX_RANGES) s.ranges = MAX_RANGES;
+  if (s.ranges < 1) s.ranges = 1;
+  s.chunk = ((rest + s.ranges - 1) / s.ranges + TKEYS - 1) / TKEYS * TKEYS;
+  return s;
+}
+struct PrefixLayout {
+  size_t meta, bad, items, o_part, ml_part, total;
+  size_t max_items, slot_rows;
+};
+// (everything here grows with B, M and max_ctx: a workspace for the largest batch serves every smaller one)
+static PrefixLayout prefix_layout(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx) {
+  PrefixLayout L;
+  const long G = H / Hkv;
+  // prefix_splits * row tiles is at most the target (per KV head) and one per row tile more, or MAX_PREFIX_SPLITS
+  const long tiles = (G * M + 63) / 64, ranges = max_ctx - prefix_len > 256 ? MAX_RANGES : 1;
+  const long splits_rows_a = (long)MAX_PREFIX_SPLITS * M, splits_rows_b = (long)TARGET_WGS * PREFIX_TILE_ROWS / H + 2l * M;
+  L.slot_rows = (size_t)((splits_rows_a < splits_rows_b ? splits_rows_a : splits_rows_b) + ranges * M);
+  L.max_items = (size_t)((tiles + B) * ranges + tiles + TARGET_WGS + MAX_PREFIX_SPLITS);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 4095) & ~(size_t)4095; return o; };
+  L.meta = take((size_t)M * 8); L.bad = take((size_t)B * 4); L.items = take(L.max_items * 32);
+  L.ml_part = take(L.slot_rows * H * 2 * 4);
+  L.o_part = take(L.slot_rows * H * hd * 4);
+  L.total = at;
+  return L;
+}
+size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx) {
+  return prefix_layout(B, M, H, Hkv, hd, prefix_len, max_ctx).total;
+}
+
+// max_q: the longest run of rows; sum_tiles(rows): row tiles of all sequences
+hipError_t launch_prefix(TileArgs a, const int32_t* spec_len, const int32_t* ctx_lens, int max_q, int max_ctx, void* workspace, hipStream_t st) {
+  const PrefixLayout L = prefix_layout(a.B, a.M, a.H, a.Hkv, a.hd, a.prefix_len, max_ctx);
+  const PrefixShape s = prefix_shape(a, a.M, max_ctx);
+  unsigned char* w = static_cast<unsigned char*>(workspace);
+  PrefixPlan p{};
+  p.spec_len = spec_len; p.ctx_lens = ctx_lens; p.status = a.status;
+  p.B = a.B; p.M = a.M; p.G = a.H / a.Hkv; p.max_q = max_q; p.max_ctx = max_ctx; p.prefix_len = a.prefix_len;
+  p.prefix_splits = s.prefix_splits; p.row_tiles = s.row_tiles; p.tile_rows = s.tile_rows; p.chunk = s.chunk;
+  p.items = reinterpret_cast<int32_t*>(w + L.items); p.row_meta = reinterpret_cast<int2*>(w + L.meta);
+  p.seq_bad = reinterpret_cast<int32_t*>(w + L.bad);
+  const long rest = ((long)a.M * p.G / s.tile_rows + a.B) * s.ranges;
+  p.max_items = (int)(s.row_tiles * s.prefix_splits + rest);
+  a.items = p.items; a.seq_bad = p.seq_bad; a.prefix_splits = s.prefix_splits; a.n_tiles = p.max_items;
+  a.o_part = reinterpret_cast<float*>(w + L.o_part); a.ml_part = reinterpret_cast<float*>(w + L.ml_part);
+  prefix_plan_kernel<<<1, 1024, 0, st>>>(p);
+  hipError_t e;
+  if (!tile_mfma(a, true)) e = a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, true>(a, st) : launch_f32_hd<float, true>(a, st);
+  else if (a.hd == 128) e = s.tile_rows == 64 ? launch_mfma<128, 1, 4, true>(a, st) : launch_mfma<128, 2, 8, true>(a, st);
+  else e = s.tile_rows == 64 ? launch_mfma<64, 1, 4, true>(a, st) : launch_mfma<64, 2, 8, true>(a, st);
+  if (e != hipSuccess) return e;
+  const unsigned grid = (unsigned)(((size_t)a.M * a.H * (a.hd / 4) + 255) / 256);
+  if (a.dtype == MN_DT_BF16)
+    prefix_merge_kernel<<<grid, 256, 0, st>>>(a.o_part, a.ml_part, p.row_meta, p.seq_bad, s.prefix_splits, a.M, a.H, a.hd, static_cast<f16_t*>(a.out));
+  else
+    prefix_merge_kernel<<<grid, 256, 0, st>>>(a.o_part, a.ml_part, p.row_meta, p.seq_bad, s.prefix_splits, a.M, a.H, a.hd, static_cast<float*>(a.out));
+  return hipSuccess;
 }
 
 }  // namespace mn

@@ -221,6 +221,27 @@ def prompt_attention(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: to
     return out
 
 
+class PrefixSession:
+    """Workspace for the attention of batches of up to B sequences / max_rows rows that share their first prefix_len tokens."""
+
+    def __init__(self, model: DeviceModel, kv: DeviceKV, B_: int, max_rows: int, prefix_len: int, max_ctx: int):
+        self.model, self.kv, self.prefix_len, self.max_ctx = model, kv, prefix_len, max_ctx
+        self.ws_bytes = B.mn_prefix_workspace_bytes(model.ctx, B_, max_rows, prefix_len, max_ctx)
+        if self.ws_bytes == 0:
+            raise RuntimeError("mn_prefix_workspace_bytes rejected the shape")
+        dev = kv.block_tables.device
+        self.workspace = torch.empty((self.ws_bytes,), dtype=torch.uint8, device=dev)
+        self.dev_status = torch.zeros((1,), dtype=torch.int32, device=dev)
+
+    def attention(self, q: torch.Tensor, spec_len: torch.Tensor, h_spec_len: Sequence[int], out: torch.Tensor, layer: int = 0) -> torch.Tensor:
+        """q [rows][H][hd] at positions ctx_b .. ctx_b + spec_len[b], whose keys are in the cache; out [rows][H * hd]."""
+        assert q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype
+        B.mn_prefix_attention(self.model.ctx, q.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len),
+                              self.prefix_len, self.max_ctx, self.kv.c, layer, out.data_ptr(), self.workspace.data_ptr(),
+                              self.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
+        return out
+
+
 class KVPool:
     """Which slot of a DeviceKV's table holds which blocks (mn_kv_*): forked requests share pages, every slot gets room ahead of
     its next tokens, finished ones give their blocks back, and the pool can be packed.  The whole mapping (table, references,
