@@ -436,7 +436,7 @@ mn_status mn_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, cons
  *   q        dev, row m at q + m * q_stride: [n_heads][head_dim], fp32 in fp32 models, fp16 in bf16 models
  *   k, v     dev, likewise: [n_kv_heads][head_dim]
  *            (strides in elements, so that the three may lie side by side in the rows of one QKV projection; addresses and row
- *            strides are multiples of 16 bytes)
+ *            strides are multiples of 16 bytes, strides below 2^24)
  *   seq_rows dev [B+1], ascending from 0 or more; h_seq_rows HOST [B+1], the same values: they size the launch.  Sequences without
  *            rows are fine.  Values on the device that do not fit the launch leave the call undone (MN_DEV_SPEC_LEN).
  *   out      dev [h_seq_rows[B]][n_heads * head_dim], same type as q; only rows that belong to a sequence are written

@@ -770,6 +770,7 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   if ((long)M * G >= (1l << 30)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d heads per KV head", who, M, G);
   if (q_stride < (long)d.n_heads * d.head_dim || k_stride < (long)d.n_kv_heads * d.head_dim || v_stride < (long)d.n_kv_heads * d.head_dim)
     return fail(c, MN_EINVAL, "%s: a row stride is shorter than its row", who);
+  if (q_stride >= (1l << 24) || k_stride >= (1l << 24) || v_stride >= (1l << 24)) return fail(c, MN_EUNSUPPORTED, "%s: a row stride of 2^24 elements or more", who);
   if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out | (uintptr_t)(q_stride * es) | (uintptr_t)(k_stride * es) | (uintptr_t)(v_stride * es)) & 15)
     return fail(c, MN_EINVAL, "%s: addresses and row strides must be multiples of 16 bytes", who);
   TileArgs t{};

@@ -160,10 +160,30 @@ template <int HDIM> struct TileStage {
   static constexpr int FRAGS = 4 * HS + 2 * NU;     // 1 KB pieces of a stage: K, then V
   static constexpr int BYTES = FRAGS * 1024;
 };
-constexpr int STAGES = 3;
+constexpr int STAGES = 4;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(4))) int32_t typed_const_i32;  // (scalar loads)
+template <int N> struct PieceC { static constexpr int value = N; };
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void pieces(F f) {
+  if constexpr (I < N) {
+    f(PieceC<I>{});
+    pieces<N, I + 1>(f);
+  }
+}
+// dma16 from a scalar base and a 32-bit offset per lane
+template <int OFFSET>
+__device__ __forceinline__ void dma16s(const char* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
+}
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// the largest of a lane's eight scores (`maximum` takes a NaN as it is, and so needs no instruction to quiet one first)
+__device__ __forceinline__ float top(const f32x4 (&S)[2]) {
+  const auto m = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
+  return m(m(m(m(S[0][0], S[0][1]), S[0][2]), m(m(S[0][3], S[1][0]), S[1][1])), m(S[1][2], S[1][3]));
+}
 
 template <int HDIM, int CT, int NW, bool PAGED>
 __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(TileArgs a) {
@@ -199,140 +219,142 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(Til
 #pragma unroll
     for (int s = 0; s < HS; ++s) qf[ct][s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
   }
-  f32x4 O[CT][NU], L[CT];
-  float run_m[CT];
+  f32x4 O[CT][NU];
+  float run_m[CT], neg_m[CT], thr[CT], L[CT];                    // reference, its negative (0: none yet), scores that move it, sum of this lane
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    run_m[ct] = -INFINITY;
-    L[ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    run_m[ct] = thr[ct] = -INFINITY;
+    neg_m[ct] = L[ct] = 0.f;
 #pragma unroll
     for (int u = 0; u < NU; ++u) O[ct][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
-  const float c = rsqrtf((float)HDIM) * LOG2E_T;
+  const float c = rsqrtf((float)HDIM) * LOG2E_T, inv_c = 1.f / c;
 
-  // ---- staging ----
+  // ---- staging: the first half of the waves fetches K, the second V; a wave's pieces share one address (per tile) ----
   const int n_tiles = (it.key_end - it.key0 + TKEYS - 1) / TKEYS;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
-  const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
-  const int last_key = it.key_end - 1, last_blk = last_key / PAGE;
-  const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u;
-  auto stage = [&](int tile) {
+  const int last_key = it.key_end - 1;
+  const bool k_wave = wave < NW / 2;
+  const int p0 = (k_wave ? wave : wave - NW / 2) * LPW;          // first piece of the wave, of K or of V
+  const uint32_t to0 = lds0 + (uint32_t)((k_wave ? 0 : 4 * HS) + p0) * 1024u;
+  // pages: the two blocks that the wave's pieces lie in
+  const int kb_w = k_wave ? p0 / (2 * HS) : p0 / NU;
+  const typed_const_i32* bt = PAGED ? reinterpret_cast<const typed_const_i32*>(reinterpret_cast<uintptr_t>(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq)) : nullptr;
+  const int last_blk = last_key / PAGE;
+  const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u, blk_max = (uint32_t)a.kv.num_blocks - 1u;
+  int id0 = 0, id1 = 0;
+  const char* page = nullptr;
+  const auto ask_ids = [&](int tile) {
+    const int blk = (it.key0 + min(tile, n_tiles - 1) * TKEYS) / PAGE + 2 * kb_w;
+    id0 = bt[min(blk, last_blk)];
+    id1 = bt[min(blk + 1, last_blk)];
+  };
+  if constexpr (PAGED) {
+    const size_t head = (size_t)kvh * (HDIM * PAGE);
+    const int half = p0 / HS & 1, s0 = p0 % HS, u0 = p0 % NU;
+    page = k_wave ? static_cast<const char*>(a.kv.k) + (head + ((4 * s0 + g) * PAGE + 8 * (l16 >> 2 & 1) + 4 * half + (l16 & 3)) * 8) * 2
+                  : static_cast<const char*>(a.kv.v) + (head + (16 * u0 + l16) * PAGE + 8 * (g & 1)) * 2;
+    ask_ids(0);
+  }
+  // dense rows: byte offset of the lane's 16 bytes from the tile's first row, for tiles that lie wholly inside the sequence
+  constexpr int CH = HDIM / 8, KPP = 64 / CH;                    // 16-byte chunks per row, rows per piece of V
+  const uint32_t stride = (uint32_t)(k_wave ? a.k_stride : a.v_stride) * 2u;
+  const char* dense = PAGED ? nullptr : (k_wave ? static_cast<const char*>(a.k) : static_cast<const char*>(a.v)) + ((size_t)it.m0 * stride + (size_t)kvh * HDIM * 2);
+  const int k_key = 32 * kb_w + 8 * (l16 >> 2) + 4 * (p0 / HS & 1) + (l16 & 3);  // K: the lane's key, head-dim chunk 4s + g
+  const int v_key = p0 * KPP + lane / CH;                        // V: of the first piece
+  // the 32-byte chunks of a row of V change places, so that the transposing reads meet every bank
+  const auto v_chunk = [&](int key) {
+    const int swz = HDIM == 128 ? ((key & 3) | (key >> 1 & 4)) : ((key >> 1 & 1) | (key >> 2 & 2));
+    return (uint32_t)((lane % CH) ^ (swz << 1)) * 16u;
+  };
+  const uint32_t k_off = (uint32_t)k_key * stride + (uint32_t)g * 16u;
+  constexpr int FLIP = HDIM == 128 ? 2 : 1;                      // every FLIP pieces the other half of the row comes first
+  const uint32_t v_off[2] = {(uint32_t)v_key * stride + v_chunk(v_key), (uint32_t)v_key * stride + (v_chunk(v_key) ^ HDIM)};
+  const auto stage = [&](int tile) {
     const int k0 = it.key0 + min(tile, n_tiles - 1) * TKEYS;     // (stages past the end repeat the last one)
-    const uint32_t to = lds0 + (uint32_t)(tile % STAGES) * St::BYTES;
-    uint32_t id[TKEYS / PAGE];
+    const uint32_t to = to0 + (uint32_t)(tile % STAGES) * St::BYTES;
     if constexpr (PAGED) {
-#pragma unroll
-      for (int i = 0; i < TKEYS / PAGE; ++i) id[i] = min((uint32_t)bt[min(k0 / PAGE + i, last_blk)], (uint32_t)a.kv.num_blocks - 1u);
-    }
-#pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-      const int f = wave * LPW + i;                              // (uniform)
-      const char* p;
-      if (f < 4 * HS) {
-        const int kb = f / (2 * HS), half = f / HS & 1, s = f % HS;
-        const int key = 32 * kb + 8 * (l16 >> 2) + 4 * half + (l16 & 3);
-        if constexpr (PAGED) {
-          const uint32_t lo = kb ? id[2] : id[0], hi = kb ? id[3] : id[1];
-          p = static_cast<const char*>(a.kv.k) + (uint64_t)((l16 >> 3) ? hi : lo) * blk_bytes +
-              ((size_t)kvh * (HDIM * PAGE) + ((4 * s + g) * PAGE + (key & (PAGE - 1))) * 8) * 2;
-        } else {
-          p = reinterpret_cast<const char*>(static_cast<const f16_t*>(a.k) + (size_t)(it.m0 + min(k0 + key, last_key)) * a.k_stride +
-                                            (size_t)kvh * HDIM + 32 * s + 8 * g);
-        }
+      const uint32_t sel = k_wave ? l16 >> 3 : g >> 1;
+      const char* p = page + (uint64_t)min((uint32_t)(sel ? id1 : id0), blk_max) * blk_bytes;
+      if (k_wave) {
+        pieces<LPW>([&](auto i) { dma16<(i.value / HS) * 64 + (i.value % HS) * 1024, true>(p, to + i.value * 1024u); });
       } else {
-        const int w = f - 4 * HS;
-        if constexpr (PAGED) {
-          const int kb = w / NU, u = w % NU;
-          const uint32_t lo = kb ? id[2] : id[0], hi = kb ? id[3] : id[1];
-          p = static_cast<const char*>(a.kv.v) + (uint64_t)((g >> 1) ? hi : lo) * blk_bytes +
-              ((size_t)kvh * (HDIM * PAGE) + (16 * u + l16) * PAGE + 8 * (g & 1)) * 2;
+        pieces<LPW>([&](auto i) { dma16<i.value * 512, true>(p, to + i.value * 1024u); });
+      }
+      ask_ids(tile + 1);
+    } else {
+      const char* row = dense + (uint64_t)(uint32_t)k0 * stride;
+      if (k0 + TKEYS - 1 <= last_key) {
+        if (k_wave) {
+          pieces<LPW>([&](auto i) { dma16s<(i.value % HS) * 64>(row + (i.value / HS) * 4 * (uint64_t)stride, k_off, to + i.value * 1024u); });
         } else {
-          // 512 / HDIM rows per piece; the 32-byte chunks of a row change places so that the transposing reads meet every bank
-          constexpr int CH = HDIM / 8;                           // 16-byte chunks per row
-          const int key = w * (64 / CH) + lane / CH, at = lane % CH;
-          const int swz = HDIM == 128 ? ((key & 3) | (key >> 1 & 4)) : ((key >> 1 & 1) | (key >> 2 & 2));
-          p = reinterpret_cast<const char*>(static_cast<const f16_t*>(a.v) + (size_t)(it.m0 + min(k0 + key, last_key)) * a.v_stride +
-                                            (size_t)kvh * HDIM + 8 * (at ^ (swz << 1)));
+          pieces<LPW>([&](auto i) { dma16s<0>(row + i.value * KPP * (uint64_t)stride, v_off[i.value / FLIP & 1], to + i.value * 1024u); });
+        }
+      } else {                                                   // rows past the end repeat the last one
+        if (k_wave) {
+          pieces<LPW>([&](auto i) {
+            dma16s<(i.value % HS) * 64>(row, (uint32_t)min(k_key + 4 * (i.value / HS), last_key - k0) * stride + g * 16u, to + i.value * 1024u);
+          });
+        } else {
+          pieces<LPW>([&](auto i) {
+            const int key = v_key + i.value * KPP;
+            dma16s<0>(row, (uint32_t)min(key, last_key - k0) * stride + v_chunk(key), to + i.value * 1024u);
+          });
         }
       }
-      dma16<0, PAGED>(p, to + (uint32_t)f * 1024u);
     }
   };
-  __syncthreads();                                               // (the search is through with its part of the LDS)
-#pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i) stage(i);
-
-  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
   // transposing reads: lanes 4k .. 4k + 3 of a group of 16 address 32 bytes of key 8g + k, lane i receives column i
   const uint32_t v_lane = (uint32_t)((8 * g + (l16 >> 2)) * (2 * HDIM) + (HDIM == 128 ? ((l16 >> 2) | (g & 1) << 2) : ((l16 >> 3) | (g & 1) << 1)) * 32 +
                                      (l16 & 3) * 8);
+  const auto slot = [&](int tile) { return smem + (tile % STAGES) * St::BYTES; };
+  const auto load_k = [&](const unsigned char* st, int kb, f16x8 (&kf)[2 * HS]) {
+#pragma unroll
+    for (int f = 0; f < 2 * HS; ++f) kf[f] = *reinterpret_cast<const f16x8*>(st + ((kb * 2 * HS + f) * 64 + lane) * 16);
+  };
+  const auto load_v = [&](const unsigned char* st, int kb, f16x8 (&vf)[NU]) {
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      if constexpr (PAGED) {
+        vf[u] = *reinterpret_cast<const f16x8*>(st + ((4 * HS + kb * NU + u) * 64 + lane) * 16);
+      } else {
+        union { f16x8 v; s16x4 h[2]; } x;
+        const uint32_t at = (v_lane ^ (uint32_t)(u * 32)) + (uint32_t)(4 * HS * 1024 + kb * 32 * 2 * HDIM);
+        x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
+        x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
+        vf[u] = x.v;
+      }
+    }
+  };
+  const auto scores = [&](const f16x8 (&kf)[2 * HS], f32x4 (&S)[CT][2], float (&tm)[CT]) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      S[ct][0] = S[ct][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < HS; ++h) {
+        S[ct][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h], qf[ct][h], S[ct][0], 0, 0, 0);
+        S[ct][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[HS + h], qf[ct][h], S[ct][1], 0, 0, 0);
+      }
+      tm[ct] = top(S[ct]);
+    }
+  };
 
-  for (int i = 0; i < n_tiles; ++i) {
-    wait_vm<(STAGES - 2) * LPW>();                               // this wave's part of tile i has landed ...
-    __syncthreads();                                             // ... and everybody's; tile i - 1 has been read by all
-    stage(i + STAGES - 1);
-    const int k0 = it.key0 + i * TKEYS;
-    if (k0 > max_lim) continue;                                  // (no row of the wave sees the tile)
-    const unsigned char* st = smem + (i % STAGES) * St::BYTES;
-    const bool masked = k0 + TKEYS - 1 > min_lim;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f16x8 kf[2 * HS];
-#pragma unroll
-      for (int f = 0; f < 2 * HS; ++f) kf[f] = *reinterpret_cast<const f16x8*>(st + ((kb * 2 * HS + f) * 64 + lane) * 16);
-      f16x8 P[CT];
-      const int keyg = k0 + 32 * kb + 8 * g;
+  // One half tile (32 keys) after the other.  Its scores are there when its turn comes (S, their maximum of this lane tm); those of the
+  // next one are worked out beside its probabilities (first part), and its second product (second part) runs while the keys of
+  // the half behind the next and the values of the next are on their way from the LDS: the matrix pipe and the vector unit both
+  // have work, and neither waits for the LDS.
+  f16x8 kf[2 * HS], vf[NU], P[CT];
+  const auto first = [&](int k0, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
+    const int keyg = k0 + 8 * g;
+    if (k0 + 31 > min_lim) {                                     // (uniform) a key that some row does not see
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        f32x4 S0 = {0.f, 0.f, 0.f, 0.f}, S1 = S0;
 #pragma unroll
-        for (int s = 0; s < HS; ++s) {
-          S0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[s], qf[ct][s], S0, 0, 0, 0);
-          S1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[HS + s], qf[ct][s], S1, 0, 0, 0);
-        }
-        float sc[8] = {S0[0], S0[1], S0[2], S0[3], S1[0], S1[1], S1[2], S1[3]};
-        if (masked) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sc[e] = keyg + e > lim[ct] ? -INFINITY : sc[e];
-        }
-        float tm = sc[0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) tm = __builtin_fmaxf(tm, sc[e]);
-        tm *= c;
-        if (__any(tm > run_m[ct] + LAZY)) {
-          uint32_t x, y;
-          lane_pair<16>(__float_as_uint(tm), x, y);
-          tm = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
-          lane_pair<32>(__float_as_uint(tm), x, y);
-          tm = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
-          const float nm = __builtin_fmaxf(run_m[ct], tm);
-          const float alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m[ct] - nm);
-          run_m[ct] = nm;
-#pragma unroll
-          for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
-          L[ct] *= alpha;
-        }
-        const float nm = run_m[ct] == -INFINITY ? 0.f : -run_m[ct];
-        union { f16x8 v; uint32_t u[4]; } pf;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          pf.u[e] = pack2h(__builtin_amdgcn_exp2f(fmaf(sc[2 * e], c, nm)), __builtin_amdgcn_exp2f(fmaf(sc[2 * e + 1], c, nm)));
-        P[ct] = pf.v;
+        for (int e = 0; e < 8; ++e)
+          if (keyg + e > lim[ct]) S[ct][e >> 2][e & 3] = -INFINITY;
+        tm[ct] = top(S[ct]);
       }
-      f16x8 vf[NU];
-#pragma unroll
-      for (int u = 0; u < NU; ++u) {
-        if constexpr (PAGED) {
-          vf[u] = *reinterpret_cast<const f16x8*>(st + ((4 * HS + kb * NU + u) * 64 + lane) * 16);
-        } else {
-          union { f16x8 v; s16x4 h[2]; } x;
-          const uint32_t at = (v_lane ^ (uint32_t)(u * 32)) + (uint32_t)(4 * HS * 1024 + kb * 32 * 2 * HDIM);
-          x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
-          x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
-          vf[u] = x.v;
-        }
-      }
-      if (PAGED && masked) {
+      if constexpr (PAGED) {
         // slots past the last key may hold anything, and 0 times anything has to stay 0
         const int past = keyg + 8 - it.key_end;
         if (past > 0) {
@@ -343,12 +365,78 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(Til
               if (e >= 8 - past) vf[u][e] = (f16_t)0.f;
         }
       }
+    }
+    bool move = false;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) move |= tm[ct] > thr[ct];
+    if (__any(move)) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
+        uint32_t x, y;
+        float t2 = tm[ct];
+        lane_pair<16>(__float_as_uint(t2), x, y);
+        t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
+        lane_pair<32>(__float_as_uint(t2), x, y);
+        t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y)) * c;
+        const float nm = __builtin_fmaxf(run_m[ct], t2);
+        const float alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m[ct] - nm);
+        run_m[ct] = nm;
+        thr[ct] = nm == -INFINITY ? -INFINITY : (nm + LAZY) * inv_c;
+        neg_m[ct] = nm == -INFINITY ? 0.f : -nm;
 #pragma unroll
-        for (int u = 0; u < NU; ++u) O[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[u], P[ct], O[ct][u], 0, 0, 0);
-        L[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, P[ct], L[ct], 0, 0, 0);
+        for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
+        L[ct] *= alpha;
       }
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      union { f16x8 v; uint32_t u[4]; f16x2 h[4]; } pf;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        pf.u[e] = pack2h(__builtin_amdgcn_exp2f(fmaf(S[ct][e >> 1][2 * (e & 1)], c, neg_m[ct])),
+                         __builtin_amdgcn_exp2f(fmaf(S[ct][e >> 1][2 * (e & 1) + 1], c, neg_m[ct])));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) L[ct] = __builtin_amdgcn_fdot2(pf.h[e], (f16x2){(f16_t)1.f, (f16_t)1.f}, L[ct], false);
+      P[ct] = pf.v;
+    }
+    scores(kf, Sn, tn);
+  };
+  const auto second = [&](const unsigned char* k_slot, int k_kb, const unsigned char* v_slot, int v_kb) {
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(k_slot, k_kb, kf);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int u = 0; u < NU; ++u) O[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[u], P[ct], O[ct][u], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(v_slot, v_kb, vf);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  const int n_wave = min(n_tiles, max(0, max_lim + TKEYS - it.key0) / TKEYS);  // tiles that a row of the wave sees
+  __syncthreads();                                               // (the search is through with its part of the LDS)
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) stage(i);
+  wait_vm<(STAGES - 2) * LPW>();
+  __syncthreads();
+  f32x4 Sa[CT][2], Sb[CT][2];
+  float ta[CT], tb[CT];
+  load_k(slot(0), 0, kf);
+  scores(kf, Sa, ta);
+  load_k(slot(0), 1, kf);
+  load_v(slot(0), 0, vf);
+  for (int i = 0; i < n_tiles; ++i) {
+    const int k0 = it.key0 + i * TKEYS;
+    const bool on = i < n_wave;                                  // (uniform)
+    if (on) first(k0, Sa, ta, Sb, tb);
+    wait_vm<(STAGES - 3) * LPW>();                               // this wave's part of tile i + 1 has landed ...
+    __syncthreads();                                             // ... and everybody's; tile i - 1 has been read by all
+    stage(i + STAGES - 1);
+    if (on) {
+      second(slot(i + 1), 0, slot(i), 1);
+      first(k0 + 32, Sb, tb, Sa, ta);
+      second(slot(i + 1), 1, slot(i + 1), 0);
     }
   }
   wait_vm<0>();                                                  // (stages past the end land before the LDS is given back)
@@ -356,10 +444,15 @@ __global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(Til
   // ---- output: lane holds O^T[16u + 4g + i][row l16], and its row's sum ----
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
+    uint32_t x, y;                                               // the row's sum over the four lane groups
+    lane_pair<16>(__float_as_uint(L[ct]), x, y);
+    L[ct] = __uint_as_float(x) + __uint_as_float(y);
+    lane_pair<32>(__float_as_uint(L[ct]), x, y);
+    L[ct] = __uint_as_float(x) + __uint_as_float(y);
     const int r = rw0 + 16 * ct + l16;
     if (r >= it.R) continue;
     const int j = r / G, m = it.m0 + j, h = kvh * G + r - j * G;
-    const float l = L[ct][0];
+    const float l = L[ct];
     if constexpr (PAGED) {
       float* o = a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * HDIM + 4 * g;
 #pragma unroll
