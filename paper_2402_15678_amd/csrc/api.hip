@@ -783,7 +783,7 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   t.q = q; t.k = k; t.v = v; t.q_stride = q_stride; t.k_stride = k_stride; t.v_stride = v_stride; t.out = out;
   t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.B = B;
   t.seq_rows = seq_rows; t.status = dev_status;
-  const int rows = prompt_tile_rows(d.n_heads, d.n_kv_heads, d.head_dim, d.dtype, (long)(M - h_seq_rows[0]) * G);
+  const int rows = prompt_tile_rows(t, (long)(M - h_seq_rows[0]) * G);
   long tiles = 0;
   for (int b = 0; b < B; ++b) tiles += ((long)(h_seq_rows[b + 1] - h_seq_rows[b]) * G + rows - 1) / rows;
   if (tiles * d.n_kv_heads >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
@@ -827,6 +827,7 @@ extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t
   if ((long)max_ctx < (long)prefix_len + max_q)
     return fail(c, MN_EINVAL, "%s: max_ctx %d smaller than the prefix of %d and the longest scored run %d", who, max_ctx, prefix_len, max_q);
   if ((long)M * (d.n_heads / d.n_kv_heads) >= (1l << 29)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d heads", who, M, d.n_heads);
+  if (!prefix_fits(M, d.n_heads, d.n_kv_heads, prefix_len)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows behind %d tokens", who, M, prefix_len);
   if (max_ctx >= (1 << 28)) return fail(c, MN_EUNSUPPORTED, "%s: max_ctx = %d", who, max_ctx);
   if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
   if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);

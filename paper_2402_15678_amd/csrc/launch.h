@@ -190,20 +190,27 @@ struct TileArgs {
   const int32_t* items;     // work list, 8 int32 per record (pages)
   KvView kv;                // pages to read, or (dense keys, k non-null) to write the rows to
   float *o_part, *ml_part;  // [slot][M][H][hd] and [slot][M][H][2]: outputs, (reference, sum)
-  int prefix_len, prefix_splits;
+  int prefix_len, prefix_units, n_units, share, n_streams, prefix_slots, row_tiles, tile_rows;  // the shared part (stream_item)
   int32_t* seq_bad;         // [B] set where a table row is damaged
   int32_t* status;
 };
 struct PrefixPlan {
   const int32_t *spec_len, *ctx_lens;
-  int B, M, G, max_q, max_ctx, prefix_len, prefix_splits, row_tiles, tile_rows, chunk, max_items;
+  int B, M, G, max_q, max_ctx, prefix_len, prefix_slots, tile_rows, chunk, max_items;
   int32_t* items;
   int2* row_meta;           // [M] (sequence, its ranges of own keys: 0 where it takes no part)
   int32_t *seq_bad, *status;
 };
+struct PrefixMerge {
+  const float *o_part, *ml_part;
+  const int2* row_meta;
+  const int32_t* seq_bad;
+  int M, H, Hkv, hd, prefix_slots, prefix_units, n_units, share, row_tiles, tile_rows;
+};
+bool prefix_fits(int M, int H, int Hkv, int prefix_len);
 size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx);
 hipError_t launch_prefix(TileArgs a, const int32_t* spec_len, const int32_t* ctx_lens, int max_q, int max_ctx, void* workspace, hipStream_t st);
-int prompt_tile_rows(int H, int Hkv, int hd, int dtype, long stack_rows);
+int prompt_tile_rows(const TileArgs& a, long stack_rows);
 hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st);
 
 // ---- pool.hip ----

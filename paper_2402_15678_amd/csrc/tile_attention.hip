@@ -10,6 +10,7 @@
 //  * tile_f32_kernel    every other type, head_dim and block size: 16x16x4 fp32 matrix instructions.
 //  * prefix_plan_kernel, prefix_merge_kernel   the work list of a shared-prefix call, and the sum of its parts.
 #include "launch.h"
+#include "tune.h"
 #include "../../include/minions_verify.h"
 
 #include <mutex>
@@ -17,7 +18,7 @@
 namespace mn {
 
 constexpr float LOG2E_T = 1.4426950408889634f;
-constexpr int TKEYS = 64;              // keys per staged tile of the MFMA kernel
+constexpr int TKEYS = 64;              // ranges of keys begin at multiples of it
 constexpr int PAGE = 16;               // tokens per block that it reads
 constexpr int NO_LIMIT = 1 << 29;      // an item whose rows all see every key of its range
 constexpr float LAZY = 6.f;            // the reference moves when a score exceeds it by 2^6
@@ -105,10 +106,32 @@ __device__ __forceinline__ bool list_item(const TileArgs& a, int t, Item& it) {
   return it.R > 0;
 }
 
+// The shared part, as streams.  Its work is a line of units: 64 keys of the prefix for one tile of rows of one KV head, the keys of a tile
+// one after the other, the tiles of a KV head one after the other.  Stream s takes the units [s * share, (s + 1) * share), which
+// are a piece of one tile or the end of one and the beginning of others; every piece is an item, and leaves its part in the
+// slot that counts the streams of its tile.  With as many streams as workgroups fit the chip at once all of them end together,
+// whatever the number of tiles: 64 x 9 rows of 64/8 heads behind 8192 keys are 36 tiles x 8 heads for 512 workgroups.
+// Consecutive streams run on one XCD (ids are dealt round-robin), so an XCD's L2 holds the keys of few KV heads.
+__device__ __forceinline__ int stream_of(const TileArgs& a, int wg) {
+  const int per = a.n_streams >> 3;
+  return wg < 8 * per ? (wg & 7) * per + (wg >> 3) : wg;
+}
+__device__ __forceinline__ bool stream_item(const TileArgs& a, int stream, int& unit, int& kvh, Item& it) {
+  const int end = min((stream + 1) * a.share, a.n_units);
+  if (unit >= end) return false;
+  const int tile = unit / a.prefix_units, from = unit - tile * a.prefix_units, n = min(end - unit, a.prefix_units - from);
+  unit += n;
+  kvh = tile / a.row_tiles;
+  it.m0 = 0; it.R = a.H / a.Hkv * a.M; it.rbase = (tile - kvh * a.row_tiles) * a.tile_rows;
+  it.key0 = from * TKEYS; it.key_end = min(a.prefix_len, (from + n) * TKEYS);
+  it.ctx = NO_LIMIT; it.seq = 0; it.slot = stream - tile * a.prefix_units / a.share;
+  return true;
+}
+
 // A sequence's table row, looked at by one workgroup of its items: every block id in range, and the prefix's entries those of the first
 // row (what the call reads for all of them).  Rows of a sequence that fails are zeros (prefix_merge_kernel).
 __device__ __forceinline__ void check_table(const TileArgs& a, const Item& it, int kvh) {
-  if (it.slot != a.prefix_splits || it.rbase != 0 || kvh != 0) return;
+  if (it.slot != a.prefix_slots || it.rbase != 0 || kvh != 0) return;
   const int32_t *first = a.kv.block_tables, *row = first + (size_t)it.seq * a.kv.max_blocks_per_seq;
   const int shared = a.prefix_len / a.kv.block_size, all = (int)(((long)it.ctx + it.R / (a.H / a.Hkv) + a.kv.block_size - 1) / a.kv.block_size);
   bool bad = false;
@@ -155,9 +178,11 @@ __device__ __forceinline__ void append_rows(const TileArgs& a, const Item& it, i
 // order of the second.  A tile of 64 keys is staged by direct global -> LDS loads: K in operand order (the lane asks for the 16
 // bytes that belong at its place); V of pages likewise (a page keeps the block's tokens of one head-dim element together), V of dense
 // rows row by row, turned on the way to the registers by the transposing LDS read.
+constexpr int TK = 32;                              // keys per stage
 template <int HDIM> struct TileStage {
   static constexpr int HS = HDIM / 32, NU = HDIM / 16;
-  static constexpr int FRAGS = 4 * HS + 2 * NU;     // 1 KB pieces of a stage: K, then V
+  static constexpr int KP = TK / 16 * HS;           // 1 KB pieces of K in a stage, and as many of V
+  static constexpr int FRAGS = 2 * KP;
   static constexpr int BYTES = FRAGS * 1024;
 };
 constexpr int STAGES = 4;
@@ -186,288 +211,355 @@ __device__ __forceinline__ float top(const f32x4 (&S)[2]) {
 }
 
 template <int HDIM, int CT, int NW, bool PAGED>
-__global__ void __launch_bounds__(NW * 64, NW == 8 ? 2 : 1) tile_mfma_kernel(TileArgs a) {
+__global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
   using St = TileStage<HDIM>;
-  constexpr int HS = St::HS, NU = St::NU, LPW = St::FRAGS / NW, ROWS = 16 * CT * NW;
+  constexpr int HS = St::HS, NU = St::NU, KP = St::KP, LPW = St::FRAGS / NW, ROWS = 16 * CT * NW;
   static_assert(St::FRAGS % NW == 0, "whole pieces per wave");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int G = a.H / a.Hkv;
-  const int t = blockIdx.x / a.Hkv, kvh = blockIdx.x % a.Hkv;
+  int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
   Item it;
+  bool more = false;
   if constexpr (PAGED) {
-    if (!list_item(a, t, it)) return;
-    check_table(a, it, kvh);
+    const int own = a.n_tiles * a.Hkv;                           // workgroups of the sequences' own keys; the streams come behind
+    if ((int)blockIdx.x < own) {
+      if (!list_item(a, blockIdx.x / a.Hkv, it)) return;
+      check_table(a, it, kvh);
+    } else {
+      stream = stream_of(a, blockIdx.x - own);
+      unit = stream * a.share;
+      if (!stream_item(a, stream, unit, kvh, it)) return;
+      more = true;
+    }
   } else {
-    if (!prompt_item<ROWS>(a, t, G, reinterpret_cast<int32_t*>(smem), it)) return;
-    if (a.kv.k) append_rows<f16_t, ROWS>(a, it, G, kvh);
+    if (!prompt_item<ROWS>(a, blockIdx.x / a.Hkv, G, reinterpret_cast<int32_t*>(smem), it)) return;
   }
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // this wave's rows, and the keys that its first and last row see
-  const int rw0 = it.rbase + wave * CT * 16;
-  const bool rows = rw0 < it.R;
-  const int min_lim = min(it.key_end - 1, it.ctx + rw0 / G);
-  const int max_lim = rows ? min(it.key_end - 1, it.ctx + (min(it.R, rw0 + CT * 16) - 1) / G) : -1;
-  f16x8 qf[CT][HS];
-  int lim[CT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int r = min(rw0 + 16 * ct + l16, it.R - 1), j = r / G;
-    lim[ct] = min(it.key_end - 1, it.ctx + j);
-    const f16_t* q = static_cast<const f16_t*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * HDIM;
-#pragma unroll
-    for (int s = 0; s < HS; ++s) qf[ct][s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
-  }
-  f32x4 O[CT][NU];
-  float run_m[CT], neg_m[CT], thr[CT], L[CT];                    // reference, its negative (0: none yet), scores that move it, sum of this lane
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    run_m[ct] = thr[ct] = -INFINITY;
-    neg_m[ct] = L[ct] = 0.f;
-#pragma unroll
-    for (int u = 0; u < NU; ++u) O[ct][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  }
-  const float c = rsqrtf((float)HDIM) * LOG2E_T, inv_c = 1.f / c;
-
-  // ---- staging: the first half of the waves fetches K, the second V; a wave's pieces share one address (per tile) ----
-  const int n_tiles = (it.key_end - it.key0 + TKEYS - 1) / TKEYS;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
-  const int last_key = it.key_end - 1;
-  const bool k_wave = wave < NW / 2;
-  const int p0 = (k_wave ? wave : wave - NW / 2) * LPW;          // first piece of the wave, of K or of V
-  const uint32_t to0 = lds0 + (uint32_t)((k_wave ? 0 : 4 * HS) + p0) * 1024u;
-  // pages: the two blocks that the wave's pieces lie in
-  const int kb_w = k_wave ? p0 / (2 * HS) : p0 / NU;
-  const typed_const_i32* bt = PAGED ? reinterpret_cast<const typed_const_i32*>(reinterpret_cast<uintptr_t>(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq)) : nullptr;
-  const int last_blk = last_key / PAGE;
-  const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u, blk_max = (uint32_t)a.kv.num_blocks - 1u;
-  int id0 = 0, id1 = 0;
-  const char* page = nullptr;
-  const auto ask_ids = [&](int tile) {
-    const int blk = (it.key0 + min(tile, n_tiles - 1) * TKEYS) / PAGE + 2 * kb_w;
-    id0 = bt[min(blk, last_blk)];
-    id1 = bt[min(blk + 1, last_blk)];
-  };
-  if constexpr (PAGED) {
-    const size_t head = (size_t)kvh * (HDIM * PAGE);
-    const int half = p0 / HS & 1, s0 = p0 % HS, u0 = p0 % NU;
-    page = k_wave ? static_cast<const char*>(a.kv.k) + (head + ((4 * s0 + g) * PAGE + 8 * (l16 >> 2 & 1) + 4 * half + (l16 & 3)) * 8) * 2
-                  : static_cast<const char*>(a.kv.v) + (head + (16 * u0 + l16) * PAGE + 8 * (g & 1)) * 2;
-    ask_ids(0);
-  }
-  // dense rows: byte offset of the lane's 16 bytes from the tile's first row, for tiles that lie wholly inside the sequence
-  constexpr int CH = HDIM / 8, KPP = 64 / CH;                    // 16-byte chunks per row, rows per piece of V
-  const uint32_t stride = (uint32_t)(k_wave ? a.k_stride : a.v_stride) * 2u;
-  const char* dense = PAGED ? nullptr : (k_wave ? static_cast<const char*>(a.k) : static_cast<const char*>(a.v)) + ((size_t)it.m0 * stride + (size_t)kvh * HDIM * 2);
-  const int k_key = 32 * kb_w + 8 * (l16 >> 2) + 4 * (p0 / HS & 1) + (l16 & 3);  // K: the lane's key, head-dim chunk 4s + g
-  const int v_key = p0 * KPP + lane / CH;                        // V: of the first piece
-  // the 32-byte chunks of a row of V change places, so that the transposing reads meet every bank
-  const auto v_chunk = [&](int key) {
-    const int swz = HDIM == 128 ? ((key & 3) | (key >> 1 & 4)) : ((key >> 1 & 1) | (key >> 2 & 2));
-    return (uint32_t)((lane % CH) ^ (swz << 1)) * 16u;
-  };
-  const uint32_t k_off = (uint32_t)k_key * stride + (uint32_t)g * 16u;
-  constexpr int FLIP = HDIM == 128 ? 2 : 1;                      // every FLIP pieces the other half of the row comes first
-  const uint32_t v_off[2] = {(uint32_t)v_key * stride + v_chunk(v_key), (uint32_t)v_key * stride + (v_chunk(v_key) ^ HDIM)};
-  const auto stage = [&](int tile) {
-    const int k0 = it.key0 + min(tile, n_tiles - 1) * TKEYS;     // (stages past the end repeat the last one)
-    const uint32_t to = to0 + (uint32_t)(tile % STAGES) * St::BYTES;
-    if constexpr (PAGED) {
-      const uint32_t sel = k_wave ? l16 >> 3 : g >> 1;
-      const char* p = page + (uint64_t)min((uint32_t)(sel ? id1 : id0), blk_max) * blk_bytes;
-      if (k_wave) {
-        pieces<LPW>([&](auto i) { dma16<(i.value / HS) * 64 + (i.value % HS) * 1024, true>(p, to + i.value * 1024u); });
-      } else {
-        pieces<LPW>([&](auto i) { dma16<i.value * 512, true>(p, to + i.value * 1024u); });
-      }
-      ask_ids(tile + 1);
-    } else {
-      const char* row = dense + (uint64_t)(uint32_t)k0 * stride;
-      if (k0 + TKEYS - 1 <= last_key) {
-        if (k_wave) {
-          pieces<LPW>([&](auto i) { dma16s<(i.value % HS) * 64>(row + (i.value / HS) * 4 * (uint64_t)stride, k_off, to + i.value * 1024u); });
-        } else {
-          pieces<LPW>([&](auto i) { dma16s<0>(row + i.value * KPP * (uint64_t)stride, v_off[i.value / FLIP & 1], to + i.value * 1024u); });
-        }
-      } else {                                                   // rows past the end repeat the last one
-        if (k_wave) {
-          pieces<LPW>([&](auto i) {
-            dma16s<(i.value % HS) * 64>(row, (uint32_t)min(k_key + 4 * (i.value / HS), last_key - k0) * stride + g * 16u, to + i.value * 1024u);
-          });
-        } else {
-          pieces<LPW>([&](auto i) {
-            const int key = v_key + i.value * KPP;
-            dma16s<0>(row, (uint32_t)min(key, last_key - k0) * stride + v_chunk(key), to + i.value * 1024u);
-          });
-        }
-      }
-    }
-  };
-  // transposing reads: lanes 4k .. 4k + 3 of a group of 16 address 32 bytes of key 8g + k, lane i receives column i
-  const uint32_t v_lane = (uint32_t)((8 * g + (l16 >> 2)) * (2 * HDIM) + (HDIM == 128 ? ((l16 >> 2) | (g & 1) << 2) : ((l16 >> 3) | (g & 1) << 1)) * 32 +
-                                     (l16 & 3) * 8);
-  const auto slot = [&](int tile) { return smem + (tile % STAGES) * St::BYTES; };
-  const auto load_k = [&](const unsigned char* st, int kb, f16x8 (&kf)[2 * HS]) {
-#pragma unroll
-    for (int f = 0; f < 2 * HS; ++f) kf[f] = *reinterpret_cast<const f16x8*>(st + ((kb * 2 * HS + f) * 64 + lane) * 16);
-  };
-  const auto load_v = [&](const unsigned char* st, int kb, f16x8 (&vf)[NU]) {
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      if constexpr (PAGED) {
-        vf[u] = *reinterpret_cast<const f16x8*>(st + ((4 * HS + kb * NU + u) * 64 + lane) * 16);
-      } else {
-        union { f16x8 v; s16x4 h[2]; } x;
-        const uint32_t at = (v_lane ^ (uint32_t)(u * 32)) + (uint32_t)(4 * HS * 1024 + kb * 32 * 2 * HDIM);
-        x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
-        x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
-        vf[u] = x.v;
-      }
-    }
-  };
-  const auto scores = [&](const f16x8 (&kf)[2 * HS], f32x4 (&S)[CT][2], float (&tm)[CT]) {
+  do {
+    // this wave's rows, and the keys that its first and last row see
+    const int rw0 = it.rbase + wave * CT * 16;
+    const bool rows = rw0 < it.R;
+    const int min_lim = min(it.key_end - 1, it.ctx + rw0 / G);
+    const int max_lim = rows ? min(it.key_end - 1, it.ctx + (min(it.R, rw0 + CT * 16) - 1) / G) : -1;
+    f16x8 qf[CT][HS];
+    int lim[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      S[ct][0] = S[ct][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      const int r = min(rw0 + 16 * ct + l16, it.R - 1), j = r / G;
+      lim[ct] = min(it.key_end - 1, it.ctx + j);
+      const f16_t* q = static_cast<const f16_t*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * HDIM;
 #pragma unroll
-      for (int h = 0; h < HS; ++h) {
-        S[ct][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h], qf[ct][h], S[ct][0], 0, 0, 0);
-        S[ct][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[HS + h], qf[ct][h], S[ct][1], 0, 0, 0);
-      }
-      tm[ct] = top(S[ct]);
+      for (int s = 0; s < HS; ++s) qf[ct][s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
     }
-  };
-
-  // One half tile (32 keys) after the other.  Its scores are there when its turn comes (S, their maximum of this lane tm); those of the
-  // next one are worked out beside its probabilities (first part), and its second product (second part) runs while the keys of
-  // the half behind the next and the values of the next are on their way from the LDS: the matrix pipe and the vector unit both
-  // have work, and neither waits for the LDS.
-  f16x8 kf[2 * HS], vf[NU], P[CT];
-  const auto first = [&](int k0, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
-    const int keyg = k0 + 8 * g;
-    if (k0 + 31 > min_lim) {                                     // (uniform) a key that some row does not see
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (keyg + e > lim[ct]) S[ct][e >> 2][e & 3] = -INFINITY;
-        tm[ct] = top(S[ct]);
-      }
-      if constexpr (PAGED) {
-        // slots past the last key may hold anything, and 0 times anything has to stay 0
-        const int past = keyg + 8 - it.key_end;
-        if (past > 0) {
-#pragma unroll
-          for (int u = 0; u < NU; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e >= 8 - past) vf[u][e] = (f16_t)0.f;
-        }
-      }
-    }
-    bool move = false;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) move |= tm[ct] > thr[ct];
-    if (__any(move)) {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        uint32_t x, y;
-        float t2 = tm[ct];
-        lane_pair<16>(__float_as_uint(t2), x, y);
-        t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
-        lane_pair<32>(__float_as_uint(t2), x, y);
-        t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y)) * c;
-        const float nm = __builtin_fmaxf(run_m[ct], t2);
-        const float alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m[ct] - nm);
-        run_m[ct] = nm;
-        thr[ct] = nm == -INFINITY ? -INFINITY : (nm + LAZY) * inv_c;
-        neg_m[ct] = nm == -INFINITY ? 0.f : -nm;
-#pragma unroll
-        for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
-        L[ct] *= alpha;
-      }
-    }
+    f32x4 O[CT][NU];
+    float run_m[CT], neg_m[CT], thr[CT], L[CT];                    // reference, its negative (0: none yet), scores that move it, sum of this lane
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      union { f16x8 v; uint32_t u[4]; f16x2 h[4]; } pf;
+      run_m[ct] = thr[ct] = -INFINITY;
+      neg_m[ct] = L[ct] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        pf.u[e] = pack2h(__builtin_amdgcn_exp2f(fmaf(S[ct][e >> 1][2 * (e & 1)], c, neg_m[ct])),
-                         __builtin_amdgcn_exp2f(fmaf(S[ct][e >> 1][2 * (e & 1) + 1], c, neg_m[ct])));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) L[ct] = __builtin_amdgcn_fdot2(pf.h[e], (f16x2){(f16_t)1.f, (f16_t)1.f}, L[ct], false);
-      P[ct] = pf.v;
+      for (int u = 0; u < NU; ++u) O[ct][u] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-    scores(kf, Sn, tn);
-  };
-  const auto second = [&](const unsigned char* k_slot, int k_kb, const unsigned char* v_slot, int v_kb) {
-    __builtin_amdgcn_sched_barrier(0);
-    load_k(k_slot, k_kb, kf);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int u = 0; u < NU; ++u) O[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[u], P[ct], O[ct][u], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(v_slot, v_kb, vf);
-    __builtin_amdgcn_sched_barrier(0);
-  };
+    const float c = rsqrtf((float)HDIM) * LOG2E_T, inv_c = 1.f / c;
 
-  const int n_wave = min(n_tiles, max(0, max_lim + TKEYS - it.key0) / TKEYS);  // tiles that a row of the wave sees
-  __syncthreads();                                               // (the search is through with its part of the LDS)
-#pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i) stage(i);
-  wait_vm<(STAGES - 2) * LPW>();
-  __syncthreads();
-  f32x4 Sa[CT][2], Sb[CT][2];
-  float ta[CT], tb[CT];
-  load_k(slot(0), 0, kf);
-  scores(kf, Sa, ta);
-  load_k(slot(0), 1, kf);
-  load_v(slot(0), 0, vf);
-  for (int i = 0; i < n_tiles; ++i) {
-    const int k0 = it.key0 + i * TKEYS;
-    const bool on = i < n_wave;                                  // (uniform)
-    if (on) first(k0, Sa, ta, Sb, tb);
-    wait_vm<(STAGES - 3) * LPW>();                               // this wave's part of tile i + 1 has landed ...
-    __syncthreads();                                             // ... and everybody's; tile i - 1 has been read by all
-    stage(i + STAGES - 1);
-    if (on) {
-      second(slot(i + 1), 0, slot(i), 1);
-      first(k0 + 32, Sb, tb, Sa, ta);
-      second(slot(i + 1), 1, slot(i + 1), 0);
-    }
-  }
-  wait_vm<0>();                                                  // (stages past the end land before the LDS is given back)
-
-  // ---- output: lane holds O^T[16u + 4g + i][row l16], and its row's sum ----
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    uint32_t x, y;                                               // the row's sum over the four lane groups
-    lane_pair<16>(__float_as_uint(L[ct]), x, y);
-    L[ct] = __uint_as_float(x) + __uint_as_float(y);
-    lane_pair<32>(__float_as_uint(L[ct]), x, y);
-    L[ct] = __uint_as_float(x) + __uint_as_float(y);
-    const int r = rw0 + 16 * ct + l16;
-    if (r >= it.R) continue;
-    const int j = r / G, m = it.m0 + j, h = kvh * G + r - j * G;
-    const float l = L[ct];
+    // ---- staging: the first half of the waves fetches K, the second V; a wave's pieces share one address (per tile) ----
+    const int n_tiles = (it.key_end - it.key0 + TK - 1) / TK;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
+    const int last_key = it.key_end - 1;
+    const bool k_wave = wave < NW / 2;
+    const int p0 = (k_wave ? wave : wave - NW / 2) * LPW;          // first piece of the wave, of K or of V
+    const uint32_t to0 = lds0 + (uint32_t)((k_wave ? 0 : KP) + p0) * 1024u;
+    // pages: the two blocks that the wave's pieces lie in
+    const int kb_w = k_wave ? p0 / (2 * HS) : p0 / NU;
+    const typed_const_i32* bt = PAGED ? reinterpret_cast<const typed_const_i32*>(reinterpret_cast<uintptr_t>(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq)) : nullptr;
+    const int last_blk = last_key / PAGE;
+    const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u, blk_max = (uint32_t)a.kv.num_blocks - 1u;
+    int id0 = 0, id1 = 0;
+    const char* page = nullptr;
+    const auto ask_ids = [&](int tile) {
+      const int blk = (it.key0 + min(tile, n_tiles - 1) * TK) / PAGE + 2 * kb_w;
+      id0 = bt[min(blk, last_blk)];
+      id1 = bt[min(blk + 1, last_blk)];
+    };
     if constexpr (PAGED) {
-      float* o = a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * HDIM + 4 * g;
+      const size_t head = (size_t)kvh * (HDIM * PAGE);
+      const int half = p0 / HS & 1, s0 = p0 % HS, u0 = p0 % NU;
+      page = k_wave ? static_cast<const char*>(a.kv.k) + (head + ((4 * s0 + g) * PAGE + 8 * (l16 >> 2 & 1) + 4 * half + (l16 & 3)) * 8) * 2
+                    : static_cast<const char*>(a.kv.v) + (head + (16 * u0 + l16) * PAGE + 8 * (g & 1)) * 2;
+      ask_ids(0);
+    }
+    // dense rows: byte offset of the lane's 16 bytes from the tile's first row, for tiles that lie wholly inside the sequence
+    constexpr int CH = HDIM / 8, KPP = 64 / CH;                    // 16-byte chunks per row, rows per piece of V
+    const uint32_t stride = (uint32_t)(k_wave ? a.k_stride : a.v_stride) * 2u;
+    const char* dense = PAGED ? nullptr : (k_wave ? static_cast<const char*>(a.k) : static_cast<const char*>(a.v)) + ((size_t)it.m0 * stride + (size_t)kvh * HDIM * 2);
+    // the lane's row in its first piece: of K (head-dim chunk 4s + g) the key in operand order, of V the row as it comes; the 32-byte chunks
+    // of a row of V change places, so that the transposing reads meet every bank
+    const int key_lane = k_wave ? 8 * (l16 >> 2) + 4 * (p0 / HS & 1) + (l16 & 3) : p0 * KPP + lane / CH;
+    const auto v_chunk = [&](int key) {
+      const int swz = HDIM == 128 ? ((key & 3) | (key >> 1 & 4)) : ((key >> 1 & 1) | (key >> 2 & 2));
+      return (uint32_t)((lane % CH) ^ (swz << 1)) * 16u;
+    };
+    constexpr int FLIP = HDIM == 128 ? 2 : 1;                      // every FLIP pieces of V the other half of the row comes first
+    const uint32_t off0 = (uint32_t)key_lane * stride + (k_wave ? (uint32_t)g * 16u : v_chunk(key_lane));
+    const uint32_t off1 = (uint32_t)key_lane * stride + (v_chunk(key_lane) ^ HDIM);
+    const auto stage = [&](int tile) {
+      const int k0 = it.key0 + min(tile, n_tiles - 1) * TK;     // (stages past the end repeat the last one)
+      const uint32_t to = to0 + (uint32_t)(tile % STAGES) * St::BYTES;
+      if constexpr (PAGED) {
+        const uint32_t sel = k_wave ? l16 >> 3 : g >> 1;
+        const char* p = page + (uint64_t)min((uint32_t)(sel ? id1 : id0), blk_max) * blk_bytes;
+        // (keys that no other tile of rows reads are not kept in the L2)
+        const auto fetch = [&](auto once) {
+          constexpr bool ONCE = decltype(once)::value;
+          if (k_wave) {
+            pieces<LPW>([&](auto i) { dma16<(i.value / HS) * 64 + (i.value % HS) * 1024, ONCE>(p, to + i.value * 1024u); });
+          } else {
+            pieces<LPW>([&](auto i) { dma16<i.value * 512, ONCE>(p, to + i.value * 1024u); });
+          }
+        };
+        if (more && a.row_tiles > 1) fetch(BoolC<false>{});
+        else fetch(BoolC<true>{});
+        ask_ids(tile + 1);
+      } else {
+        const char* row = dense + (uint64_t)(uint32_t)k0 * stride;
+        if (k0 + TK - 1 <= last_key) {
+          if (k_wave) {
+            pieces<LPW>([&](auto i) { dma16s<(i.value % HS) * 64>(row + (i.value / HS) * 4 * (uint64_t)stride, off0, to + i.value * 1024u); });
+          } else {
+            pieces<LPW>([&](auto i) { dma16s<0>(row + i.value * KPP * (uint64_t)stride, (i.value / FLIP & 1) ? off1 : off0, to + i.value * 1024u); });
+          }
+        } else {                                                   // rows past the end repeat the last one
+          if (k_wave) {
+            pieces<LPW>([&](auto i) {
+              dma16s<(i.value % HS) * 64>(row, (uint32_t)min(key_lane + 4 * (i.value / HS), last_key - k0) * stride + g * 16u, to + i.value * 1024u);
+            });
+          } else {
+            pieces<LPW>([&](auto i) {
+              const int key = key_lane + i.value * KPP;
+              dma16s<0>(row, (uint32_t)min(key, last_key - k0) * stride + v_chunk(key), to + i.value * 1024u);
+            });
+          }
+        }
+      }
+    };
+    // transposing reads: lanes 4k .. 4k + 3 of a group of 16 address 32 bytes of key 8g + k, lane i receives column i
+    const uint32_t v_lane = (uint32_t)((8 * g + (l16 >> 2)) * (2 * HDIM) + (HDIM == 128 ? ((l16 >> 2) | (g & 1) << 2) : ((l16 >> 3) | (g & 1) << 1)) * 32 +
+                                       (l16 & 3) * 8);
+    const auto slot = [&](int tile) { return smem + (tile % STAGES) * St::BYTES; };
+    const auto load_k = [&](const unsigned char* st, f16x8 (&kf)[2 * HS]) {
 #pragma unroll
-      for (int u = 0; u < NU; ++u) *reinterpret_cast<f32x4*>(o + 16 * u) = O[ct][u];
-      if (g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m[ct], l);
-    } else {
-      const float inv = 1.f / l;
-      f16_t* o = static_cast<f16_t*>(a.out) + ((size_t)m * a.H + h) * HDIM + 4 * g;
+      for (int f = 0; f < 2 * HS; ++f) kf[f] = *reinterpret_cast<const f16x8*>(st + (f * 64 + lane) * 16);
+    };
+    const auto load_v = [&](const unsigned char* st, f16x8 (&vf)[NU]) {
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
-        const f32x4 v = O[ct][u];
-        *reinterpret_cast<uint2*>(o + 16 * u) = make_uint2(pack2h(v[0] * inv, v[1] * inv), pack2h(v[2] * inv, v[3] * inv));
+        if constexpr (PAGED) {
+          vf[u] = *reinterpret_cast<const f16x8*>(st + ((KP + u) * 64 + lane) * 16);
+        } else {
+          union { f16x8 v; s16x4 h[2]; } x;
+          const uint32_t at = (v_lane ^ (uint32_t)(u * 32)) + (uint32_t)(KP * 1024);
+          x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
+          x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
+          vf[u] = x.v;
+        }
+      }
+    };
+    const auto scores = [&](const f16x8 (&kf)[2 * HS], f32x4 (&S)[CT][2], float (&tm)[CT]) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        S[ct][0] = S[ct][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < HS; ++h) {
+          S[ct][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h], qf[ct][h], S[ct][0], 0, 0, 0);
+          S[ct][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[HS + h], qf[ct][h], S[ct][1], 0, 0, 0);
+        }
+        tm[ct] = top(S[ct]);
+      }
+    };
+
+    // One half tile (32 keys) after the other.  Its scores are there when its turn comes (S, their maximum of this lane tm); those of the
+    // next one are worked out beside its probabilities (first part), and its second product (second part) runs while the keys of
+    // the half behind the next and the values of the next are on their way from the LDS: the matrix pipe and the vector unit both
+    // have work, and neither waits for the LDS.
+    f16x8 kf[2 * HS], vf[NU], P[CT];
+    const auto first = [&](int k0, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
+      const int keyg = k0 + 8 * g;
+      if (k0 + 31 > min_lim) {                                     // (uniform) a key that some row does not see
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (keyg + e > lim[ct]) S[ct][e >> 2][e & 3] = -INFINITY;
+          tm[ct] = top(S[ct]);
+        }
+        if constexpr (PAGED) {
+          // slots past the last key may hold anything, and 0 times anything has to stay 0
+          const int past = keyg + 8 - it.key_end;
+          if (past > 0) {
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (e >= 8 - past) vf[u][e] = (f16_t)0.f;
+          }
+        }
+      }
+      bool move = false;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) move |= tm[ct] > thr[ct];
+      if (__any(move)) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          uint32_t x, y;
+          float t2 = tm[ct];
+          lane_pair<16>(__float_as_uint(t2), x, y);
+          t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y));
+          lane_pair<32>(__float_as_uint(t2), x, y);
+          t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y)) * c;
+          const float nm = __builtin_fmaxf(run_m[ct], t2);
+          const float alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m[ct] - nm);
+          run_m[ct] = nm;
+          thr[ct] = nm == -INFINITY ? -INFINITY : (nm + LAZY) * inv_c;
+          neg_m[ct] = nm == -INFINITY ? 0.f : -nm;
+#pragma unroll
+          for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
+          L[ct] *= alpha;
+        }
+      }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        union { f16x8 v; uint32_t u[4]; f16x2 h[4]; } pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          pf.u[e] = pack2h(__builtin_amdgcn_exp2f(fmaf(S[ct][e >> 1][2 * (e & 1)], c, neg_m[ct])),
+                           __builtin_amdgcn_exp2f(fmaf(S[ct][e >> 1][2 * (e & 1) + 1], c, neg_m[ct])));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) L[ct] = __builtin_amdgcn_fdot2(pf.h[e], (f16x2){(f16_t)1.f, (f16_t)1.f}, L[ct], false);
+        P[ct] = pf.v;
+      }
+      scores(kf, Sn, tn);
+    };
+    const auto second = [&](const unsigned char* k_slot, const unsigned char* v_slot) {
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(k_slot, kf);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int u = 0; u < NU; ++u) O[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[u], P[ct], O[ct][u], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(v_slot, vf);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+
+    const int n_wave = min(n_tiles, max(0, max_lim + TK - it.key0) / TK);  // tiles that a row of the wave sees
+    __syncthreads();                                               // (the search, or the piece before, is through with the LDS)
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) stage(i);
+    wait_vm<(STAGES - 3) * LPW>();
+    __syncthreads();
+    f32x4 Sa[CT][2], Sb[CT][2];
+    float ta[CT], tb[CT];
+    load_k(slot(0), kf);
+    scores(kf, Sa, ta);
+    load_k(slot(1), kf);
+    load_v(slot(0), vf);
+    // Tile i: its first part, then the hand-over: this wave's share of tile i + 2 has landed, then everybody's; tile i - 1 has been read
+    // by all, and its place is filled again.
+    const auto tile = [&](int i, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
+      const bool on = i < n_wave;                                  // (uniform)
+      if (on) first(it.key0 + i * TK, S, tm, Sn, tn);
+      wait_vm<(STAGES - 4) * LPW>();
+      __syncthreads();
+      stage(i + STAGES - 1);
+      if (on) second(slot(i + 2), slot(i + 1));
+    };
+    for (int i = 0; i < n_tiles; i += 2) {                         // (behind an odd last tile comes one that no wave works on)
+      tile(i, Sa, ta, Sb, tb);
+      tile(i + 1, Sb, tb, Sa, ta);
+    }
+    wait_vm<0>();                                                  // (stages past the end land before the LDS is given back)
+
+    // ---- output: lane holds O^T[16u + 4g + i][row l16], and its row's sum ----
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      uint32_t x, y;                                               // the row's sum over the four lane groups
+      lane_pair<16>(__float_as_uint(L[ct]), x, y);
+      L[ct] = __uint_as_float(x) + __uint_as_float(y);
+      lane_pair<32>(__float_as_uint(L[ct]), x, y);
+      L[ct] = __uint_as_float(x) + __uint_as_float(y);
+      const int r = rw0 + 16 * ct + l16;
+      if (r >= it.R) continue;
+      const int j = r / G, m = it.m0 + j, h = kvh * G + r - j * G;
+      const float l = L[ct];
+      if constexpr (PAGED) {
+        float* o = a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * HDIM + 4 * g;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) *reinterpret_cast<f32x4*>(o + 16 * u) = O[ct][u];
+        if (g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m[ct], l);
+      } else {
+        const float inv = 1.f / l;
+        f16_t* o = static_cast<f16_t*>(a.out) + ((size_t)m * a.H + h) * HDIM + 4 * g;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          const f32x4 v = O[ct][u];
+          *reinterpret_cast<uint2*>(o + 16 * u) = make_uint2(pack2h(v[0] * inv, v[1] * inv), pack2h(v[2] * inv, v[3] * inv));
+        }
       }
     }
-  }
+    // Rows that enter the cache: those whose first stack row lies in this workgroup's tile, out of the stages (they are the last keys it read:
+    // every stage holds the last tile now, earlier ones are fetched again).  A lane's piece of K is 8 elements of one token, and of V
+    // 8 tokens of one element: 16 bytes of a page each way.  7800 rows of 40 KV heads of 128, 161 us without: written as they come
+    // by the rows at the start 221 us, by a kernel of its own 253, like this 208, where 160 MB of pages are worth about 35.
+    if (!PAGED && a.kv.k) {
+      const int put0 = (it.rbase + G - 1) / G, put1 = (min(it.R, it.rbase + ROWS) + G - 1) / G;
+      __syncthreads();                                             // (everybody is through with the stages, and the last tile is there)
+      if (put0 / TK < n_tiles - 1) {                               // (at most ROWS / TK stages, and one more if ROWS / G is no multiple of TK)
+        static_assert(ROWS / TK <= STAGES && ROWS / 2 / TK + 1 <= STAGES, "the rows of a tile fit the stages");
+        for (int i = put0 / TK; i * TK < put1; ++i) stage(i);
+        wait_vm<0>();
+        __syncthreads();
+      }
+      bool bad = false;
+      for (int i = put0 / TK; i * TK < put1; ++i) {
+        const unsigned char* st = slot(i);
+        const int key = i * TK + (k_wave ? key_lane : 8 * g);
+        if (key >= put1 || key + (k_wave ? 0 : 7) < put0) continue;
+        const uint32_t id = (uint32_t)a.kv.block_tables[(size_t)it.seq * a.kv.max_blocks_per_seq + key / PAGE];
+        if (id >= (uint32_t)a.kv.num_blocks) {
+          bad = true;
+          continue;
+        }
+        const size_t page = ((size_t)id * a.Hkv + kvh) * (HDIM * PAGE);
+        if (k_wave) {
+          f16_t* to = static_cast<f16_t*>(a.kv.k) + page + (g * PAGE + (key & (PAGE - 1))) * 8;
+#pragma unroll
+          for (int n = 0; n < LPW; ++n)
+            *reinterpret_cast<f16x8*>(to + ((p0 + n) % HS) * (4 * PAGE * 8)) = *reinterpret_cast<const f16x8*>(st + ((p0 + n) * 64 + lane) * 16);
+        } else {
+          f16_t* to = static_cast<f16_t*>(a.kv.v) + page + (16 * p0 + l16) * PAGE + (key & (PAGE - 1));
+          const bool all = key >= put0 && key + 8 <= put1;
+#pragma unroll
+          for (int n = 0; n < LPW; ++n) {
+            union { f16x8 v; s16x4 h[2]; } x;
+            const uint32_t at = (v_lane ^ (uint32_t)((p0 + n) * 32)) + (uint32_t)(KP * 1024);
+            x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
+            x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
+            if (all) {
+              *reinterpret_cast<f16x8*>(to + n * 16 * PAGE) = x.v;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (key + e >= put0 && key + e < put1) to[n * 16 * PAGE + e] = x.v[e];
+            }
+          }
+        }
+      }
+      if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+    }
+  } while (more && stream_item(a, stream, unit, kvh, it));
 }
 
 // ------------------------------------------------------------------------------------------
@@ -485,131 +577,142 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
   float* s_k = reinterpret_cast<float*>(smem);                   // [FKEYS][LD]
   float* s_v = s_k + FKEYS * LD;
   const int G = a.H / a.Hkv;
-  const int t = blockIdx.x / a.Hkv, kvh = blockIdx.x % a.Hkv;
+  int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
   Item it;
+  bool more = false;
   if constexpr (PAGED) {
-    if (!list_item(a, t, it)) return;
-    check_table(a, it, kvh);
+    const int own = a.n_tiles * a.Hkv;                           // workgroups of the sequences' own keys; the streams come behind
+    if ((int)blockIdx.x < own) {
+      if (!list_item(a, blockIdx.x / a.Hkv, it)) return;
+      check_table(a, it, kvh);
+    } else {
+      stream = stream_of(a, blockIdx.x - own);
+      unit = stream * a.share;
+      if (!stream_item(a, stream, unit, kvh, it)) return;
+      more = true;
+    }
   } else {
-    if (!prompt_item<FROWS>(a, t, G, reinterpret_cast<int32_t*>(smem), it)) return;
+    if (!prompt_item<FROWS>(a, blockIdx.x / a.Hkv, G, reinterpret_cast<int32_t*>(smem), it)) return;
     if (a.kv.k) append_rows<T, FROWS>(a, it, G, kvh);
   }
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, wave = tid >> 6;
   const int hd = a.hd;
-  const int rw = it.rbase + wave * 16 + l16, r = min(rw, it.R - 1), j = r / G;
-  const int lim = min(it.key_end - 1, it.ctx + j);
-  const float c = rsqrtf((float)hd) * LOG2E_T;
-  f32x4 q[NU], O[NU];
-  const T* Q = static_cast<const T*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * hd;
+  do {
+    const int rw = it.rbase + wave * 16 + l16, r = min(rw, it.R - 1), j = r / G;
+    const int lim = min(it.key_end - 1, it.ctx + j);
+    const float c = rsqrtf((float)hd) * LOG2E_T;
+    f32x4 q[NU], O[NU];
+    const T* Q = static_cast<const T*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * hd;
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    O[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < NU; ++u) {
+      O[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) q[u][e] = 16 * u + 4 * g + e < hd ? (float)Q[16 * u + 4 * g + e] * c : 0.f;
-  }
-  float run_m = -INFINITY, run_l = 0.f;
-  const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
-  const int bs = PAGED ? a.kv.block_size : 1;
-  __syncthreads();                                               // (the search is through with its part of the LDS)
-  for (int k0 = it.key0; k0 < it.key_end; k0 += FKEYS) {
-    // the keys' rows, 8 elements at a time; past the last key and past head_dim zeros
-    for (int i = tid; i < FKEYS * (HDP / 8); i += 256) {
-      const int key = i % FKEYS, p8 = i / FKEYS, pos = k0 + key;
-      struct __attribute__((aligned(16))) Piece { T x[8]; };
-      float kx[8], vx[8];
+      for (int e = 0; e < 4; ++e) q[u][e] = 16 * u + 4 * g + e < hd ? (float)Q[16 * u + 4 * g + e] * c : 0.f;
+    }
+    float run_m = -INFINITY, run_l = 0.f;
+    const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
+    const int bs = PAGED ? a.kv.block_size : 1;
+    __syncthreads();                                               // (the search is through with its part of the LDS)
+    for (int k0 = it.key0; k0 < it.key_end; k0 += FKEYS) {
+      // the keys' rows, 8 elements at a time; past the last key and past head_dim zeros
+      for (int i = tid; i < FKEYS * (HDP / 8); i += 256) {
+        const int key = i % FKEYS, p8 = i / FKEYS, pos = k0 + key;
+        struct __attribute__((aligned(16))) Piece { T x[8]; };
+        float kx[8], vx[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
-      if (pos < it.key_end && 8 * p8 < hd) {
-        if constexpr (PAGED) {
-          const uint32_t id = min((uint32_t)bt[pos / bs], (uint32_t)a.kv.num_blocks - 1u);
-          const size_t page = ((size_t)id * a.Hkv + kvh) * (size_t)(hd * bs);
-          const int off = pos % bs;
-          const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.kv.k) + page + ((size_t)p8 * bs + off) * 8);
-          const T* v = static_cast<const T*>(a.kv.v) + page + (size_t)(8 * p8) * bs + off;
+        for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
+        if (pos < it.key_end && 8 * p8 < hd) {
+          if constexpr (PAGED) {
+            const uint32_t id = min((uint32_t)bt[pos / bs], (uint32_t)a.kv.num_blocks - 1u);
+            const size_t page = ((size_t)id * a.Hkv + kvh) * (size_t)(hd * bs);
+            const int off = pos % bs;
+            const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.kv.k) + page + ((size_t)p8 * bs + off) * 8);
+            const T* v = static_cast<const T*>(a.kv.v) + page + (size_t)(8 * p8) * bs + off;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v[(size_t)e * bs]; }
-        } else {
-          const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.k) + (size_t)(it.m0 + pos) * a.k_stride + (size_t)kvh * hd + 8 * p8);
-          const Piece v = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.v) + (size_t)(it.m0 + pos) * a.v_stride + (size_t)kvh * hd + 8 * p8);
+            for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v[(size_t)e * bs]; }
+          } else {
+            const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.k) + (size_t)(it.m0 + pos) * a.k_stride + (size_t)kvh * hd + 8 * p8);
+            const Piece v = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.v) + (size_t)(it.m0 + pos) * a.v_stride + (size_t)kvh * hd + 8 * p8);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v.x[e]; }
+            for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v.x[e]; }
+          }
         }
+        f32x4 *dk = reinterpret_cast<f32x4*>(s_k + key * LD + 8 * p8), *dv = reinterpret_cast<f32x4*>(s_v + key * LD + 8 * p8);
+        dk[0] = (f32x4){kx[0], kx[1], kx[2], kx[3]}; dk[1] = (f32x4){kx[4], kx[5], kx[6], kx[7]};
+        dv[0] = (f32x4){vx[0], vx[1], vx[2], vx[3]}; dv[1] = (f32x4){vx[4], vx[5], vx[6], vx[7]};
       }
-      f32x4 *dk = reinterpret_cast<f32x4*>(s_k + key * LD + 8 * p8), *dv = reinterpret_cast<f32x4*>(s_v + key * LD + 8 * p8);
-      dk[0] = (f32x4){kx[0], kx[1], kx[2], kx[3]}; dk[1] = (f32x4){kx[4], kx[5], kx[6], kx[7]};
-      dv[0] = (f32x4){vx[0], vx[1], vx[2], vx[3]}; dv[1] = (f32x4){vx[4], vx[5], vx[6], vx[7]};
+      __syncthreads();
+      f32x4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 k = *reinterpret_cast<const f32x4*>(s_k + (16 * h + l16) * LD + 16 * u + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[u][e], S[h], 0, 0, 0);
+        }
+      float tm = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (k0 + 16 * h + 4 * g + e > lim) S[h][e] = -INFINITY;
+          tm = fmaxf(tm, S[h][e]);
+        }
+      uint32_t x, y;
+      lane_pair<16>(__float_as_uint(tm), x, y);
+      tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
+      lane_pair<32>(__float_as_uint(tm), x, y);
+      tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
+      const float nm = fmaxf(run_m, tm), ref = nm == -INFINITY ? 0.f : nm;
+      const float alpha = __builtin_amdgcn_exp2f(run_m - ref);
+      run_m = nm;
+      run_l *= alpha;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) O[u] *= alpha;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(S[h][e] - ref);
+          run_l += p;
+#pragma unroll
+          for (int u = 0; u < NU; ++u)
+            O[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(s_v[(16 * h + 4 * g + e) * LD + 16 * u + l16], p, O[u], 0, 0, 0);
+        }
+      __syncthreads();
     }
-    __syncthreads();
-    f32x4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-    for (int u = 0; u < NU; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 k = *reinterpret_cast<const f32x4*>(s_k + (16 * h + l16) * LD + 16 * u + 4 * g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) S[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[u][e], S[h], 0, 0, 0);
-      }
-    float tm = -INFINITY;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (k0 + 16 * h + 4 * g + e > lim) S[h][e] = -INFINITY;
-        tm = fmaxf(tm, S[h][e]);
-      }
+    // the row's sum over the four lane groups
     uint32_t x, y;
-    lane_pair<16>(__float_as_uint(tm), x, y);
-    tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
-    lane_pair<32>(__float_as_uint(tm), x, y);
-    tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
-    const float nm = fmaxf(run_m, tm), ref = nm == -INFINITY ? 0.f : nm;
-    const float alpha = __builtin_amdgcn_exp2f(run_m - ref);
-    run_m = nm;
-    run_l *= alpha;
+    lane_pair<16>(__float_as_uint(run_l), x, y);
+    run_l = __uint_as_float(x) + __uint_as_float(y);
+    lane_pair<32>(__float_as_uint(run_l), x, y);
+    run_l = __uint_as_float(x) + __uint_as_float(y);
+    if (rw >= it.R) continue;
+    const int m = it.m0 + j, h = kvh * G + r - j * G;
+    const float inv = 1.f / run_l;
 #pragma unroll
-    for (int u = 0; u < NU; ++u) O[u] *= alpha;
+    for (int u = 0; u < NU; ++u) {
+      if (16 * u + 4 * g >= hd) continue;
+      if constexpr (PAGED) {
+        *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + 16 * u + 4 * g) = O[u];
+      } else {
+        T* o = static_cast<T*>(a.out) + ((size_t)m * a.H + h) * hd + 16 * u + 4 * g;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(S[h][e] - ref);
-        run_l += p;
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-          O[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(s_v[(16 * h + 4 * g + e) * LD + 16 * u + l16], p, O[u], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) o[e] = (T)(O[u][e] * inv);
       }
-    __syncthreads();
-  }
-  // the row's sum over the four lane groups
-  uint32_t x, y;
-  lane_pair<16>(__float_as_uint(run_l), x, y);
-  run_l = __uint_as_float(x) + __uint_as_float(y);
-  lane_pair<32>(__float_as_uint(run_l), x, y);
-  run_l = __uint_as_float(x) + __uint_as_float(y);
-  if (rw >= it.R) return;
-  const int m = it.m0 + j, h = kvh * G + r - j * G;
-  const float inv = 1.f / run_l;
-#pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    if (16 * u + 4 * g >= hd) continue;
-    if constexpr (PAGED) {
-      *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + 16 * u + 4 * g) = O[u];
-    } else {
-      T* o = static_cast<T*>(a.out) + ((size_t)m * a.H + h) * hd + 16 * u + 4 * g;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = (T)(O[u][e] * inv);
     }
-  }
-  if (PAGED && g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m, run_l);
+    if (PAGED && g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m, run_l);
+  } while (more && stream_item(a, stream, unit, kvh, it));
 }
 
 // ------------------------------------------------------------------------------------------
 // a batch that shares a prefix
 // ------------------------------------------------------------------------------------------
 // Every row sees the shared keys [0, P) and its own sequence's from P on.  The shared part is one dense product: all rows of the batch,
-// stacked, against keys that are read once per tile of rows, in `prefix_splits` ranges of keys when the rows alone do not fill the
-// chip.  The rest goes sequence by sequence, in ranges of `chunk` keys.  Each range leaves an unnormalised output with its
-// reference and sum per row in a slot of its own, and a row's slots are put together at the end.
+// stacked, against keys that are read once per tile of rows (stream_item).  The rest goes sequence by sequence, in ranges of `chunk`
+// keys, from a work list.  Each piece leaves an unnormalised output with its reference and sum per row in a slot of its own,
+// and a row's slots are put together at the end.
 //
 // prefix_plan_kernel (one workgroup): the rows' sequences, who takes part, and the list of items.
 __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
@@ -639,15 +742,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   const bool batch = s_bad == 0 && total == p.M;
   if (!batch) flags |= MN_DEV_SPEC_LEN;
   int4* items = reinterpret_cast<int4*>(p.items);
-  const int R = p.G * p.M, shared = batch ? p.row_tiles * p.prefix_splits : 0;
-  const int tiles = (p.prefix_len + TKEYS - 1) / TKEYS;
-  for (int i = tid; i < shared; i += 1024) {
-    const int rt = i / p.prefix_splits, s = i % p.prefix_splits;
-    const int k0 = (int)((long)tiles * s / p.prefix_splits) * TKEYS, k1 = min(p.prefix_len, (int)((long)tiles * (s + 1) / p.prefix_splits) * TKEYS);
-    items[2 * i] = make_int4(0, R, rt * p.tile_rows, k0);
-    items[2 * i + 1] = make_int4(k1, NO_LIMIT, 0, s);
-  }
-  int row_at = 0, item_at = shared;
+  int row_at = 0, item_at = 0;
   for (int b0 = 0; b0 < p.B; b0 += 1024) {
     const int b = b0 + tid, q = batch && b < p.B ? length(b) : 0;
     int ctx = 0, ranges = 0, rts = 0;
@@ -676,7 +771,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
       for (int s = 0; s < ranges; ++s, ++at) {
         const int k0 = p.prefix_len + s * p.chunk;
         items[2 * at] = make_int4(row0, p.G * q, rt * p.tile_rows, k0);
-        items[2 * at + 1] = make_int4(min(k0 + p.chunk, ctx + q), ctx, b, p.prefix_splits + s);
+        items[2 * at + 1] = make_int4(min(k0 + p.chunk, ctx + q), ctx, b, p.prefix_slots + s);
       }
   }
   if (!batch)
@@ -685,27 +780,46 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   if (flags && p.status) atomicOr(p.status, flags);
 }
 
-// Four elements of a row of one head per thread.
+// Four elements of a row of one head per thread; four slots are asked for at once.
 template <typename T>
-__global__ void __launch_bounds__(256) prefix_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ ml_part,
-                                                           const int2* __restrict__ row_meta, const int32_t* __restrict__ seq_bad,
-                                                           int prefix_splits, int M, int H, int hd, T* __restrict__ out) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, heads = (size_t)M * H;
-  const int per = hd / 4;
+__global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, heads = (size_t)p.M * p.H;
+  const int per = p.hd / 4;
   if (i >= heads * per) return;
   const size_t mh = i / per;
-  const int2 meta = row_meta[mh / H];
+  const int m = (int)(mh / p.H), h = (int)(mh - (size_t)m * p.H), G = p.H / p.Hkv, kvh = h / G;
+  const int2 meta = p.row_meta[m];
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  if (meta.y > 0 && !seq_bad[meta.x]) {
-    const int n = prefix_splits + meta.y;
-    float top = -INFINITY;
-    for (int s = 0; s < n; ++s) top = fmaxf(top, ml_part[(s * heads + mh) * 2]);
-    for (int s = 0; s < n; ++s) {
-      const float2 ml = *reinterpret_cast<const float2*>(ml_part + (s * heads + mh) * 2);
-      const float w = __builtin_amdgcn_exp2f(ml.x - top);
-      l += ml.y * w;
-      o += *reinterpret_cast<const f32x4*>(o_part + s * heads * hd + 4 * i) * w;
+  float l = 0.f, top = -INFINITY;
+  if (meta.y > 0 && !p.seq_bad[meta.x]) {
+    int shared = 0;                                              // streams that met the row's tile
+    if (p.n_units > 0) {
+      const int first = (kvh * p.row_tiles + (m * G + h - kvh * G) / p.tile_rows) * p.prefix_units;
+      shared = (first + p.prefix_units - 1) / p.share - first / p.share + 1;
+    }
+    const int n = shared + meta.y;
+    for (int s0 = 0; s0 < n; s0 += 4) {
+      float2 ml[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int s = min(s0 + u, n - 1), at = s < shared ? s : p.prefix_slots + s - shared;
+        ml[u] = *reinterpret_cast<const float2*>(p.ml_part + (at * heads + mh) * 2);
+        v[u] = *reinterpret_cast<const f32x4*>(p.o_part + at * heads * p.hd + 4 * i);
+      }
+      float nm = top;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) nm = fmaxf(nm, ml[u].x);
+      const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
+      l *= keep;
+      o *= keep;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float w = s0 + u < n ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
+        l += ml[u].y * w;
+        o += v[u] * w;
+      }
+      top = nm;
     }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -721,12 +835,13 @@ static bool tile_mfma(const TileArgs& a, bool paged) {
 }
 
 // Rows of a workgroup's tile for a call whose longest stack and number of stack rows per KV head are given.
-int prompt_tile_rows(int H, int Hkv, int hd, int dtype, long stack_rows) {
-  TileArgs a{};
-  a.dtype = dtype; a.hd = hd;
-  if (!tile_mfma(a, false)) return FROWS;
-  // 256 rows where that leaves a workgroup per CU, 64 otherwise
-  return stack_rows * Hkv >= 256 * 256 ? 256 : 64;
+int prompt_tile_rows(const TileArgs& a, long stack_rows) {
+  if (!tile_mfma(a, a.kv.k != nullptr)) return FROWS;
+  if (const int f = MN_TUNE("MN_TILE", 0)) return f;
+  // 128 rows where that fills the chip (two workgroups per CU), 64 otherwise.  Measured, 128 against 64 rows: 8192 tokens of 64/8 heads of
+  // 128 1086 and 1446 us, 8 prompts of 60 to 1500 tokens of 40 heads 162 and 203; 300 tokens of 12 heads of 64 10.1 and 8.5, 8 such
+  // prompts of 300 to 1200 (562 workgroups) 22.8 and 21.9.
+  return stack_rows * a.Hkv >= 512 * 128 ? 128 : 64;
 }
 
 template <typename K>
@@ -734,14 +849,20 @@ static hipError_t allow_lds(K kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <int HDIM, int CT, int NW, bool PAGED>
-static hipError_t launch_mfma(const TileArgs& a, hipStream_t st) {
+template <int HDIM, int CT, bool PAGED>
+static hipError_t launch_mfma_as(const TileArgs& a, hipStream_t st) {
+  constexpr size_t lds = STAGES * TileStage<HDIM>::BYTES;
   static std::once_flag once;
   static hipError_t err = hipSuccess;
-  std::call_once(once, [] { err = allow_lds(tile_mfma_kernel<HDIM, CT, NW, PAGED>, STAGES * TileStage<HDIM>::BYTES); });
+  std::call_once(once, [] { err = allow_lds(tile_mfma_kernel<HDIM, CT, 4, PAGED>, lds); });
   if (err != hipSuccess) return err;
-  tile_mfma_kernel<HDIM, CT, NW, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv, NW * 64, STAGES * TileStage<HDIM>::BYTES, st>>>(a);
+  tile_mfma_kernel<HDIM, CT, 4, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (unsigned)a.n_streams, 256, lds, st>>>(a);
   return hipSuccess;
+}
+template <bool PAGED>
+static hipError_t launch_mfma(const TileArgs& a, int tile_rows, hipStream_t st) {
+  if (a.hd == 128) return tile_rows == 128 ? launch_mfma_as<128, 2, PAGED>(a, st) : launch_mfma_as<128, 1, PAGED>(a, st);
+  return tile_rows == 128 ? launch_mfma_as<64, 2, PAGED>(a, st) : launch_mfma_as<64, 1, PAGED>(a, st);
 }
 
 template <typename T, int HDP, bool PAGED>
@@ -752,7 +873,7 @@ static hipError_t launch_f32(const TileArgs& a, hipStream_t st) {
   std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED>, need); });
   if (err != hipSuccess) return err;
   const size_t list = PAGED || a.B <= 64 ? 0 : (size_t)a.B * 4;  // (the search's numbers)
-  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv, 256, need > list ? need : list, st>>>(a);
+  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (unsigned)a.n_streams, 256, need > list ? need : list, st>>>(a);
   return hipSuccess;
 }
 
@@ -768,32 +889,33 @@ static hipError_t launch_f32_hd(const TileArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st) {
-  if (!tile_mfma(a, false)) return a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, false>(a, st) : launch_f32_hd<float, false>(a, st);
-  if (a.hd == 128) return tile_rows == 256 ? launch_mfma<128, 2, 8, false>(a, st) : launch_mfma<128, 1, 4, false>(a, st);
-  return tile_rows == 256 ? launch_mfma<64, 2, 8, false>(a, st) : launch_mfma<64, 1, 4, false>(a, st);
+  if (!tile_mfma(a, a.kv.k != nullptr)) return a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, false>(a, st) : launch_f32_hd<float, false>(a, st);
+  return launch_mfma<false>(a, tile_rows, st);
 }
 
 
 // Shape of a shared-prefix launch, from what the host knows.
-constexpr int MAX_PREFIX_SPLITS = 32, MAX_RANGES = 16, TARGET_WGS = 512, PREFIX_TILE_ROWS = 256;
+constexpr int STREAMS = 512;          // two workgroups per CU
+constexpr int MIN_SHARE = 4;          // units of a stream at least: a workgroup's lead-in is worth about as much
+constexpr int MAX_SLOTS = 33;         // of a tile of rows
+constexpr int MAX_RANGES = 16;        // of a sequence's own keys
 struct PrefixShape {
-  int tile_rows, row_tiles, prefix_splits, chunk, ranges;
+  int tile_rows, row_tiles, units, n_units, share, n_streams, slots, chunk, ranges;
 };
-static int prefix_tile_rows(const TileArgs& a, int M) {
-  if (!tile_mfma(a, true)) return FROWS;
-  return (long)M * (a.H / a.Hkv) > 64 ? PREFIX_TILE_ROWS : 64;
-}
 static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
-  PrefixShape s;
-  const int G = a.H / a.Hkv;
-  s.tile_rows = prefix_tile_rows(a, M);
-  s.row_tiles = (int)(((long)M * G + s.tile_rows - 1) / s.tile_rows);
-  const int tiles = (a.prefix_len + TKEYS - 1) / TKEYS, by_keys = tiles / 4 > 1 ? tiles / 4 : 1;
-  const long wgs = (long)s.row_tiles * a.Hkv;
-  int n = (int)((TARGET_WGS + wgs - 1) / wgs);
-  if (n > by_keys) n = by_keys;
-  if (n > MAX_PREFIX_SPLITS) n = MAX_PREFIX_SPLITS;
-  s.prefix_splits = a.prefix_len > 0 ? n : 0;
+  PrefixShape s{};
+  const long G = a.H / a.Hkv;
+  s.tile_rows = !tile_mfma(a, true) ? FROWS : MN_TUNE("MN_TILE", 0) ? MN_TUNE("MN_TILE", 0) : (M * G > 64 ? 128 : 64);
+  s.row_tiles = (int)((M * G + s.tile_rows - 1) / s.tile_rows);
+  s.units = (a.prefix_len + TKEYS - 1) / TKEYS;
+  s.n_units = s.row_tiles * a.Hkv * s.units;
+  s.share = (s.n_units + STREAMS - 1) / STREAMS;
+  const int by_slots = (s.units + MAX_SLOTS - 3) / (MAX_SLOTS - 2);
+  const int least = s.units < 1 ? 1 : (s.units < MIN_SHARE ? s.units : MIN_SHARE);  // (a stream of several short tiles would only be longer)
+  if (s.share < least) s.share = least;
+  if (s.share < by_slots) s.share = by_slots;
+  s.n_streams = (s.n_units + s.share - 1) / s.share;
+  s.slots = s.units > 0 ? (s.units - 1) / s.share + 2 : 0;
   const int rest = max_ctx - a.prefix_len, want = (long)a.B * a.Hkv >= 256 ? 1024 : 256;
   s.ranges = (rest + want - 1) / want;
   if (s.ranges > MAX_RANGES) s.ranges = MAX_RANGES;
@@ -808,12 +930,11 @@ struct PrefixLayout {
 // (everything here grows with B, M and max_ctx: a workspace for the largest batch serves every smaller one)
 static PrefixLayout prefix_layout(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx) {
   PrefixLayout L;
-  const long G = H / Hkv;
-  // prefix_splits * row tiles is at most the target (per KV head) and one per row tile more, or MAX_PREFIX_SPLITS
-  const long tiles = (G * M + 63) / 64, ranges = max_ctx - prefix_len > 256 ? MAX_RANGES : 1;
-  const long splits_rows_a = (long)MAX_PREFIX_SPLITS * M, splits_rows_b = (long)TARGET_WGS * PREFIX_TILE_ROWS / H + 2l * M;
-  L.slot_rows = (size_t)((splits_rows_a < splits_rows_b ? splits_rows_a : splits_rows_b) + ranges * M);
-  L.max_items = (size_t)((tiles + B) * ranges + tiles + TARGET_WGS + MAX_PREFIX_SPLITS);
+  const long G = H / Hkv, ranges = max_ctx - prefix_len > 256 ? MAX_RANGES : 1;
+  // slots of a tile: units / share + 2 with share >= row tiles * KV heads * units / STREAMS, and MAX_SLOTS; row tiles >= M G / 128
+  const long slots_a = (long)MAX_SLOTS * M, slots_b = (long)STREAMS * 128 / H + 3l * M;
+  L.slot_rows = (size_t)((slots_a < slots_b ? slots_a : slots_b) + ranges * M);
+  L.max_items = (size_t)(((G * M + 63) / 64 + B) * ranges);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 4095) & ~(size_t)4095; return o; };
   L.meta = take((size_t)M * 8); L.bad = take((size_t)B * 4); L.items = take(L.max_items * 32);
@@ -825,8 +946,11 @@ static PrefixLayout prefix_layout(int B, int M, int H, int Hkv, int hd, int pref
 size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx) {
   return prefix_layout(B, M, H, Hkv, hd, prefix_len, max_ctx).total;
 }
+bool prefix_fits(int M, int H, int Hkv, int prefix_len) {
+  return (((long)M * (H / Hkv) + 63) / 64) * Hkv * (((long)prefix_len + TKEYS - 1) / TKEYS) < (1l << 30);
+}
 
-// max_q: the longest run of rows; sum_tiles(rows): row tiles of all sequences
+// max_q: the longest run of rows
 hipError_t launch_prefix(TileArgs a, const int32_t* spec_len, const int32_t* ctx_lens, int max_q, int max_ctx, void* workspace, hipStream_t st) {
   const PrefixLayout L = prefix_layout(a.B, a.M, a.H, a.Hkv, a.hd, a.prefix_len, max_ctx);
   const PrefixShape s = prefix_shape(a, a.M, max_ctx);
@@ -834,24 +958,23 @@ hipError_t launch_prefix(TileArgs a, const int32_t* spec_len, const int32_t* ctx
   PrefixPlan p{};
   p.spec_len = spec_len; p.ctx_lens = ctx_lens; p.status = a.status;
   p.B = a.B; p.M = a.M; p.G = a.H / a.Hkv; p.max_q = max_q; p.max_ctx = max_ctx; p.prefix_len = a.prefix_len;
-  p.prefix_splits = s.prefix_splits; p.row_tiles = s.row_tiles; p.tile_rows = s.tile_rows; p.chunk = s.chunk;
+  p.prefix_slots = s.slots; p.tile_rows = s.tile_rows; p.chunk = s.chunk;
   p.items = reinterpret_cast<int32_t*>(w + L.items); p.row_meta = reinterpret_cast<int2*>(w + L.meta);
   p.seq_bad = reinterpret_cast<int32_t*>(w + L.bad);
-  const long rest = ((long)a.M * p.G / s.tile_rows + a.B) * s.ranges;
-  p.max_items = (int)(s.row_tiles * s.prefix_splits + rest);
-  a.items = p.items; a.seq_bad = p.seq_bad; a.prefix_splits = s.prefix_splits; a.n_tiles = p.max_items;
+  p.max_items = (int)(((long)a.M * p.G / s.tile_rows + a.B) * s.ranges);
+  a.items = p.items; a.seq_bad = p.seq_bad; a.n_tiles = p.max_items;
+  a.prefix_slots = s.slots; a.prefix_units = s.units; a.n_units = s.n_units; a.share = s.share; a.n_streams = s.n_streams;
+  a.row_tiles = s.row_tiles; a.tile_rows = s.tile_rows;
   a.o_part = reinterpret_cast<float*>(w + L.o_part); a.ml_part = reinterpret_cast<float*>(w + L.ml_part);
   prefix_plan_kernel<<<1, 1024, 0, st>>>(p);
   hipError_t e;
   if (!tile_mfma(a, true)) e = a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, true>(a, st) : launch_f32_hd<float, true>(a, st);
-  else if (a.hd == 128) e = s.tile_rows == 64 ? launch_mfma<128, 1, 4, true>(a, st) : launch_mfma<128, 2, 8, true>(a, st);
-  else e = s.tile_rows == 64 ? launch_mfma<64, 1, 4, true>(a, st) : launch_mfma<64, 2, 8, true>(a, st);
+  else e = launch_mfma<true>(a, s.tile_rows, st);
   if (e != hipSuccess) return e;
+  const PrefixMerge g{a.o_part, a.ml_part, p.row_meta, p.seq_bad, a.M, a.H, a.Hkv, a.hd, s.slots, s.units, s.n_units, s.share, s.row_tiles, s.tile_rows};
   const unsigned grid = (unsigned)(((size_t)a.M * a.H * (a.hd / 4) + 255) / 256);
-  if (a.dtype == MN_DT_BF16)
-    prefix_merge_kernel<<<grid, 256, 0, st>>>(a.o_part, a.ml_part, p.row_meta, p.seq_bad, s.prefix_splits, a.M, a.H, a.hd, static_cast<f16_t*>(a.out));
-  else
-    prefix_merge_kernel<<<grid, 256, 0, st>>>(a.o_part, a.ml_part, p.row_meta, p.seq_bad, s.prefix_splits, a.M, a.H, a.hd, static_cast<float*>(a.out));
+  if (a.dtype == MN_DT_BF16) prefix_merge_kernel<<<grid, 256, 0, st>>>(g, static_cast<f16_t*>(a.out));
+  else prefix_merge_kernel<<<grid, 256, 0, st>>>(g, static_cast<float*>(a.out));
   return hipSuccess;
 }
 
