@@ -69,13 +69,11 @@ __device__ __forceinline__ void find_tile(int t, int B, int max_tiles, F n, int 
 template <int ROWS>
 __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, int G, int32_t* s_n, Item& it) {
   const int lane = threadIdx.x & 63;
-  bool bad = false;
-  auto tiles = [&](int b) {
+  auto tiles = [&](int b) {                      // -1: does not fit
     const int r0 = a.seq_rows[b], r1 = a.seq_rows[b + 1];
-    const bool fits = r0 >= 0 && r1 >= r0 && r1 <= a.M;
-    const int n = fits ? (int)(((long)(r1 - r0) * G + ROWS - 1) / ROWS) : 0;
-    bad |= !fits || n > a.max_tiles;
-    return min(n, a.max_tiles);
+    if (r0 < 0 || r1 < r0 || r1 > a.M) return -1;
+    const int n = (int)(((long)(r1 - r0) * G + ROWS - 1) / ROWS);
+    return n > a.max_tiles ? -1 : n;
   };
   int own = 0;
   if (a.B <= 64) {
@@ -85,8 +83,10 @@ __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, int G, int
     __syncthreads();
   }
   auto n = [&](int b) { return a.B <= 64 ? own : s_n[b]; };
+  bool bad = false;
+  for (int b = lane; b < a.B; b += 64) bad |= n(b) < 0;
   const int total = tiles_from(0, a.B, n);
-  if (__syncthreads_or(bad) || total != a.n_tiles) {
+  if (__any(bad) || total != a.n_tiles) {
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, MN_DEV_SPEC_LEN);
     return false;
   }
@@ -188,7 +188,7 @@ template <int HDIM> struct TileStage {
 constexpr int STAGES = 4;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(4))) int32_t typed_const_i32;  // (scalar loads)
+typedef __attribute__((address_space(4))) int32_t const_i32;  // (scalar loads)
 template <int N> struct PieceC { static constexpr int value = N; };
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void pieces(F f) {
@@ -197,12 +197,15 @@ __device__ __forceinline__ void pieces(F f) {
     pieces<N, I + 1>(f);
   }
 }
-// dma16 from a scalar base and a 32-bit offset per lane
-template <int OFFSET>
-__device__ __forceinline__ void dma16s(const char* base, uint32_t off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
-}
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+// dma16 from a scalar base and a 32-bit offset per lane
+template <int OFFSET, bool STREAM>
+__device__ __forceinline__ void dma16s(const char* base, uint32_t off, uint32_t lds_base) {
+  if constexpr (STREAM)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3 nt" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
+}
 
 // the largest of a lane's eight scores (`maximum` takes a NaN as it is, and so needs no instruction to quiet one first)
 __device__ __forceinline__ float top(const f32x4 (&S)[2]) {
@@ -264,99 +267,88 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     }
     const float c = rsqrtf((float)HDIM) * LOG2E_T, inv_c = 1.f / c;
 
-    // ---- staging: the first half of the waves fetches K, the second V; a wave's pieces share one address (per tile) ----
+    // ---- staging: waves 0 and 1 fetch K, 2 and 3 V, each the 16 keys (the block) that its parity names, 1 KB of whole rows or of a whole
+    // page per load.  The 16-byte chunks of a row, and of a page, change places inside 256 bytes on the way, so that the reads of
+    // the operands meet every bank (`turn`). ----
     const int n_tiles = (it.key_end - it.key0 + TK - 1) / TK;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
     const int last_key = it.key_end - 1;
     const bool k_wave = wave < NW / 2;
-    const int p0 = (k_wave ? wave : wave - NW / 2) * LPW;          // first piece of the wave, of K or of V
-    const uint32_t to0 = lds0 + (uint32_t)((k_wave ? 0 : KP) + p0) * 1024u;
-    // pages: the two blocks that the wave's pieces lie in
-    const int kb_w = k_wave ? p0 / (2 * HS) : p0 / NU;
-    const typed_const_i32* bt = PAGED ? reinterpret_cast<const typed_const_i32*>(reinterpret_cast<uintptr_t>(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq)) : nullptr;
-    const int last_blk = last_key / PAGE;
-    const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u, blk_max = (uint32_t)a.kv.num_blocks - 1u;
-    int id0 = 0, id1 = 0;
-    const char* page = nullptr;
-    const auto ask_ids = [&](int tile) {
-      const int blk = (it.key0 + min(tile, n_tiles - 1) * TK) / PAGE + 2 * kb_w;
-      id0 = bt[min(blk, last_blk)];
-      id1 = bt[min(blk + 1, last_blk)];
-    };
-    if constexpr (PAGED) {
-      const size_t head = (size_t)kvh * (HDIM * PAGE);
-      const int half = p0 / HS & 1, s0 = p0 % HS, u0 = p0 % NU;
-      page = k_wave ? static_cast<const char*>(a.kv.k) + (head + ((4 * s0 + g) * PAGE + 8 * (l16 >> 2 & 1) + 4 * half + (l16 & 3)) * 8) * 2
-                    : static_cast<const char*>(a.kv.v) + (head + (16 * u0 + l16) * PAGE + 8 * (g & 1)) * 2;
-      ask_ids(0);
-    }
-    // dense rows: byte offset of the lane's 16 bytes from the tile's first row, for tiles that lie wholly inside the sequence
-    constexpr int CH = HDIM / 8, KPP = 64 / CH;                    // 16-byte chunks per row, rows per piece of V
+    const int side = wave & 1;
+    const uint32_t to0 = lds0 + (uint32_t)((k_wave ? 0 : KP) + side * LPW) * 1024u;
+    // pages
+    const const_i32* bt = PAGED ? reinterpret_cast<const const_i32*>(reinterpret_cast<uintptr_t>(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq)) : nullptr;
+    const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u;
+    int next_id = 0;
+    const auto ask_id = [&](int tile) { next_id = bt[min((it.key0 + min(tile, n_tiles - 1) * TK) / PAGE + side, last_key / PAGE)]; };
+    // dense rows
+    constexpr int CH = HDIM / 8, KPP = 64 / CH;                    // 16-byte chunks per row, rows per piece
     const uint32_t stride = (uint32_t)(k_wave ? a.k_stride : a.v_stride) * 2u;
-    const char* dense = PAGED ? nullptr : (k_wave ? static_cast<const char*>(a.k) : static_cast<const char*>(a.v)) + ((size_t)it.m0 * stride + (size_t)kvh * HDIM * 2);
-    // the lane's row in its first piece: of K (head-dim chunk 4s + g) the key in operand order, of V the row as it comes; the 32-byte chunks
-    // of a row of V change places, so that the transposing reads meet every bank
-    const int key_lane = k_wave ? 8 * (l16 >> 2) + 4 * (p0 / HS & 1) + (l16 & 3) : p0 * KPP + lane / CH;
-    const auto v_chunk = [&](int key) {
-      const int swz = HDIM == 128 ? ((key & 3) | (key >> 1 & 4)) : ((key >> 1 & 1) | (key >> 2 & 2));
-      return (uint32_t)((lane % CH) ^ (swz << 1)) * 16u;
+    const int key_lane = 16 * side + lane / CH;                    // the lane's row in its first piece
+    // K: the 16 keys of a half in as many places.  V: 32 bytes stay together (the transposing reads take as much of a row)
+    const auto turn = [&](int key) {
+      if (k_wave) return HDIM == 128 ? ((key >> 1 & 12) | (key & 3)) : ((key >> 2 & 6) | (key >> 1 & 1));
+      return HDIM == 128 ? ((key & 3) << 1 | (key & 8)) : ((key & 2) | (key >> 1 & 4));
     };
-    constexpr int FLIP = HDIM == 128 ? 2 : 1;                      // every FLIP pieces of V the other half of the row comes first
-    const uint32_t off0 = (uint32_t)key_lane * stride + (k_wave ? (uint32_t)g * 16u : v_chunk(key_lane));
-    const uint32_t off1 = (uint32_t)key_lane * stride + (v_chunk(key_lane) ^ HDIM);
+    const char* base;                                              // of the wave's piece of the next tile (dense), or of its head (pages)
+    uint32_t off0, off1 = 0;                                       // the lane's bytes from it, in pieces whose keys agree in bit 3
+    if constexpr (PAGED) {
+      base = static_cast<const char*>(k_wave ? a.kv.k : a.kv.v) + (size_t)kvh * (HDIM * PAGE * 2);
+      off0 = 16u * (uint32_t)(k_wave ? lane ^ (side * 4) : lane ^ (lane >> 4 & 1));
+      ask_id(0);
+    } else {
+      base = static_cast<const char*>(k_wave ? a.k : a.v) + ((size_t)(it.m0 + it.key0) * stride + (size_t)kvh * HDIM * 2);
+      off0 = (uint32_t)key_lane * stride + 16u * (uint32_t)((lane % CH) ^ turn(key_lane));
+      off1 = (uint32_t)key_lane * stride + 16u * (uint32_t)((lane % CH) ^ turn(key_lane ^ 8));
+    }
     const auto stage = [&](int tile) {
-      const int k0 = it.key0 + min(tile, n_tiles - 1) * TK;     // (stages past the end repeat the last one)
-      const uint32_t to = to0 + (uint32_t)(tile % STAGES) * St::BYTES;
+      const uint32_t to = to0 + (uint32_t)(tile & (STAGES - 1)) * St::BYTES;
       if constexpr (PAGED) {
-        const uint32_t sel = k_wave ? l16 >> 3 : g >> 1;
-        const char* p = page + (uint64_t)min((uint32_t)(sel ? id1 : id0), blk_max) * blk_bytes;
+        const char* p = base + (uint64_t)min((uint32_t)next_id, (uint32_t)a.kv.num_blocks - 1u) * blk_bytes;
         // (keys that no other tile of rows reads are not kept in the L2)
-        const auto fetch = [&](auto once) {
-          constexpr bool ONCE = decltype(once)::value;
-          if (k_wave) {
-            pieces<LPW>([&](auto i) { dma16<(i.value / HS) * 64 + (i.value % HS) * 1024, ONCE>(p, to + i.value * 1024u); });
-          } else {
-            pieces<LPW>([&](auto i) { dma16<i.value * 512, ONCE>(p, to + i.value * 1024u); });
-          }
-        };
-        if (more && a.row_tiles > 1) fetch(BoolC<false>{});
-        else fetch(BoolC<true>{});
-        ask_ids(tile + 1);
+        if (more && a.row_tiles > 1) pieces<LPW>([&](auto i) { dma16s<i.value * 1024, false>(p, off0, to + i.value * 1024u); });
+        else pieces<LPW>([&](auto i) { dma16s<i.value * 1024, true>(p, off0, to + i.value * 1024u); });
+        ask_id(tile + 1);
       } else {
-        const char* row = dense + (uint64_t)(uint32_t)k0 * stride;
+        const int k0 = it.key0 + min(tile, n_tiles - 1) * TK;      // (stages past the end repeat the last one)
         if (k0 + TK - 1 <= last_key) {
-          if (k_wave) {
-            pieces<LPW>([&](auto i) { dma16s<(i.value % HS) * 64>(row + (i.value / HS) * 4 * (uint64_t)stride, off0, to + i.value * 1024u); });
-          } else {
-            pieces<LPW>([&](auto i) { dma16s<0>(row + i.value * KPP * (uint64_t)stride, (i.value / FLIP & 1) ? off1 : off0, to + i.value * 1024u); });
-          }
+          pieces<LPW>([&](auto i) { dma16s<0, false>(base + i.value * KPP * (uint64_t)stride, (i.value * KPP & 8) ? off1 : off0, to + i.value * 1024u); });
         } else {                                                   // rows past the end repeat the last one
-          if (k_wave) {
-            pieces<LPW>([&](auto i) {
-              dma16s<(i.value % HS) * 64>(row, (uint32_t)min(key_lane + 4 * (i.value / HS), last_key - k0) * stride + g * 16u, to + i.value * 1024u);
-            });
-          } else {
-            pieces<LPW>([&](auto i) {
-              const int key = key_lane + i.value * KPP;
-              dma16s<0>(row, (uint32_t)min(key, last_key - k0) * stride + v_chunk(key), to + i.value * 1024u);
-            });
-          }
+          pieces<LPW>([&](auto i) {
+            const int key = key_lane + i.value * KPP;
+            dma16s<0, false>(base, (uint32_t)min(key, last_key - k0) * stride + 16u * (uint32_t)((lane % CH) ^ turn(key)), to + i.value * 1024u);
+          });
         }
+        if (tile + 1 < n_tiles) base += TK * (uint64_t)stride;
       }
     };
-    // transposing reads: lanes 4k .. 4k + 3 of a group of 16 address 32 bytes of key 8g + k, lane i receives column i
-    const uint32_t v_lane = (uint32_t)((8 * g + (l16 >> 2)) * (2 * HDIM) + (HDIM == 128 ? ((l16 >> 2) | (g & 1) << 2) : ((l16 >> 3) | (g & 1) << 1)) * 32 +
-                                       (l16 & 3) * 8);
-    const auto slot = [&](int tile) { return smem + (tile % STAGES) * St::BYTES; };
+    // Operands of the first product: chunk 4s + g of key 8 (l16 >> 2) + 4 half + (l16 & 3).
+    uint32_t k_lane;
+    {
+      const int key = 8 * (l16 >> 2) + (l16 & 3);
+      if constexpr (PAGED) k_lane = (uint32_t)((l16 >> 3) * LPW * 1024 + g * 256 + ((key & 15) ^ (l16 >> 3) * 4) * 16);
+      else k_lane = (uint32_t)(key * (2 * HDIM) + 16 * (g ^ (HDIM == 128 ? l16 : (l16 >> 2 << 1 | (l16 >> 1 & 1)))));
+    }
+    // Of the second: 8 tokens of an element of a page, or by transposing reads: lanes 4k .. 4k + 3 of a group of 16 address 32 bytes of key
+    // 8g + k, lane i receives column i.
+    const uint32_t v_lane = PAGED ? (uint32_t)((g >> 1) * LPW * 1024 + l16 * 32 + ((g & 1) ^ (l16 >> 3)) * 16)
+                                  : (uint32_t)((8 * g + (l16 >> 2)) * (2 * HDIM) + (HDIM == 128 ? ((l16 >> 2) | (g & 1) << 2) : ((l16 >> 3) | (g & 1) << 1)) * 32 +
+                                               (l16 & 3) * 8);
+    const auto slot = [&](int tile) { return smem + (tile & (STAGES - 1)) * St::BYTES; };
     const auto load_k = [&](const unsigned char* st, f16x8 (&kf)[2 * HS]) {
 #pragma unroll
-      for (int f = 0; f < 2 * HS; ++f) kf[f] = *reinterpret_cast<const f16x8*>(st + (f * 64 + lane) * 16);
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int h = 0; h < HS; ++h) {
+          const uint32_t at = PAGED ? (k_lane ^ (uint32_t)(half * 64)) + (uint32_t)(h * 1024) : (k_lane ^ (uint32_t)(h * 64)) + (uint32_t)(half * 8 * HDIM);
+          kf[half * HS + h] = *reinterpret_cast<const f16x8*>(st + at);
+        }
     };
     const auto load_v = [&](const unsigned char* st, f16x8 (&vf)[NU]) {
 #pragma unroll
       for (int u = 0; u < NU; ++u) {
         if constexpr (PAGED) {
-          vf[u] = *reinterpret_cast<const f16x8*>(st + ((KP + u) * 64 + lane) * 16);
+          vf[u] = *reinterpret_cast<const f16x8*>(st + v_lane + (KP * 1024 + u * 512));
         } else {
           union { f16x8 v; s16x4 h[2]; } x;
           const uint32_t at = (v_lane ^ (uint32_t)(u * 32)) + (uint32_t)(KP * 1024);
@@ -366,7 +358,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
         }
       }
     };
-    const auto scores = [&](const f16x8 (&kf)[2 * HS], f32x4 (&S)[CT][2], float (&tm)[CT]) {
+    const auto scores = [&](const f16x8 (&kf)[2 * HS], f32x4 (&S)[CT][2]) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         S[ct][0] = S[ct][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -375,7 +367,6 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
           S[ct][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h], qf[ct][h], S[ct][0], 0, 0, 0);
           S[ct][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[HS + h], qf[ct][h], S[ct][1], 0, 0, 0);
         }
-        tm[ct] = top(S[ct]);
       }
     };
 
@@ -384,7 +375,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // the half behind the next and the values of the next are on their way from the LDS: the matrix pipe and the vector unit both
     // have work, and neither waits for the LDS.
     f16x8 kf[2 * HS], vf[NU], P[CT];
-    const auto first = [&](int k0, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
+    const auto first = [&](int k0, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2]) {
       const int keyg = k0 + 8 * g;
       if (k0 + 31 > min_lim) {                                     // (uniform) a key that some row does not see
 #pragma unroll
@@ -439,9 +430,9 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
         for (int e = 0; e < 4; ++e) L[ct] = __builtin_amdgcn_fdot2(pf.h[e], (f16x2){(f16_t)1.f, (f16_t)1.f}, L[ct], false);
         P[ct] = pf.v;
       }
-      scores(kf, Sn, tn);
+      scores(kf, Sn);
     };
-    const auto second = [&](const unsigned char* k_slot, const unsigned char* v_slot) {
+    const auto second = [&](const unsigned char* k_slot, const unsigned char* v_slot, const f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
       __builtin_amdgcn_sched_barrier(0);
       load_k(k_slot, kf);
       __builtin_amdgcn_sched_barrier(0);
@@ -449,6 +440,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int u = 0; u < NU; ++u) O[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[u], P[ct], O[ct][u], 0, 0, 0);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) tn[ct] = top(Sn[ct]);
       __builtin_amdgcn_sched_barrier(0);
       load_v(v_slot, vf);
       __builtin_amdgcn_sched_barrier(0);
@@ -463,18 +456,20 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     f32x4 Sa[CT][2], Sb[CT][2];
     float ta[CT], tb[CT];
     load_k(slot(0), kf);
-    scores(kf, Sa, ta);
+    scores(kf, Sa);
     load_k(slot(1), kf);
     load_v(slot(0), vf);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) ta[ct] = top(Sa[ct]);
     // Tile i: its first part, then the hand-over: this wave's share of tile i + 2 has landed, then everybody's; tile i - 1 has been read
     // by all, and its place is filled again.
     const auto tile = [&](int i, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
       const bool on = i < n_wave;                                  // (uniform)
-      if (on) first(it.key0 + i * TK, S, tm, Sn, tn);
+      if (on) first(it.key0 + i * TK, S, tm, Sn);
       wait_vm<(STAGES - 4) * LPW>();
       __syncthreads();
       stage(i + STAGES - 1);
-      if (on) second(slot(i + 2), slot(i + 1));
+      if (on) second(slot(i + 2), slot(i + 1), Sn, tn);
     };
     for (int i = 0; i < n_tiles; i += 2) {                         // (behind an odd last tile comes one that no wave works on)
       tile(i, Sa, ta, Sb, tb);
@@ -518,6 +513,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       __syncthreads();                                             // (everybody is through with the stages, and the last tile is there)
       if (put0 / TK < n_tiles - 1) {                               // (at most ROWS / TK stages, and one more if ROWS / G is no multiple of TK)
         static_assert(ROWS / TK <= STAGES && ROWS / 2 / TK + 1 <= STAGES, "the rows of a tile fit the stages");
+        base = static_cast<const char*>(k_wave ? a.k : a.v) + ((size_t)(it.m0 + put0 / TK * TK) * stride + (size_t)kvh * HDIM * 2);
         for (int i = put0 / TK; i * TK < put1; ++i) stage(i);
         wait_vm<0>();
         __syncthreads();
@@ -525,7 +521,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       bool bad = false;
       for (int i = put0 / TK; i * TK < put1; ++i) {
         const unsigned char* st = slot(i);
-        const int key = i * TK + (k_wave ? key_lane : 8 * g);
+        const int in_tile = k_wave ? 16 * side + l16 : 8 * g, key = i * TK + in_tile;
         if (key >= put1 || key + (k_wave ? 0 : 7) < put0) continue;
         const uint32_t id = (uint32_t)a.kv.block_tables[(size_t)it.seq * a.kv.max_blocks_per_seq + key / PAGE];
         if (id >= (uint32_t)a.kv.num_blocks) {
@@ -534,17 +530,18 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
         }
         const size_t page = ((size_t)id * a.Hkv + kvh) * (HDIM * PAGE);
         if (k_wave) {
-          f16_t* to = static_cast<f16_t*>(a.kv.k) + page + (g * PAGE + (key & (PAGE - 1))) * 8;
+          f16_t* to = static_cast<f16_t*>(a.kv.k) + page + (key & (PAGE - 1)) * 8;
 #pragma unroll
-          for (int n = 0; n < LPW; ++n)
-            *reinterpret_cast<f16x8*>(to + ((p0 + n) % HS) * (4 * PAGE * 8)) = *reinterpret_cast<const f16x8*>(st + ((p0 + n) * 64 + lane) * 16);
+          for (int n = 0; n < CH / 4; ++n)
+            *reinterpret_cast<f16x8*>(to + (4 * n + g) * (PAGE * 8)) =
+                *reinterpret_cast<const f16x8*>(st + in_tile * (2 * HDIM) + 16 * ((4 * n + g) ^ turn(in_tile)));
         } else {
-          f16_t* to = static_cast<f16_t*>(a.kv.v) + page + (16 * p0 + l16) * PAGE + (key & (PAGE - 1));
+          f16_t* to = static_cast<f16_t*>(a.kv.v) + page + (16 * side * LPW + l16) * PAGE + (key & (PAGE - 1));
           const bool all = key >= put0 && key + 8 <= put1;
 #pragma unroll
           for (int n = 0; n < LPW; ++n) {
             union { f16x8 v; s16x4 h[2]; } x;
-            const uint32_t at = (v_lane ^ (uint32_t)((p0 + n) * 32)) + (uint32_t)(KP * 1024);
+            const uint32_t at = (v_lane ^ (uint32_t)((side * LPW + n) * 32)) + (uint32_t)(KP * 1024);
             x.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at));
             x.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(st + at + 4 * 2 * HDIM));
             if (all) {
