@@ -789,11 +789,12 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   if (tiles * d.n_kv_heads >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
   if (tiles == 0) return MN_OK;
   t.n_tiles = (int)tiles;
+  t.tile_rows = rows;
   t.max_tiles = (int)(((long)longest * G + rows - 1) / rows);
   hipError_t lerr;
   {
     Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);
-    lerr = launch_prompt(t, rows, (hipStream_t)stream);
+    lerr = launch_prompt(t, (hipStream_t)stream);
   }
   if (lerr != hipSuccess) return fail(c, MN_EHIP, "%s: kernel attribute: %s", who, hipGetErrorString(lerr));
   return hip_check(c, who);
@@ -837,11 +838,12 @@ extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t
   t.kv = KvView{kv->k_layers[layer], kv->v_layers[layer], kv->block_tables, kv->block_size, kv->num_blocks, kv->max_blocks_per_seq};
   t.q = q; t.q_stride = (long)d.n_heads * d.head_dim; t.out = out;
   t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.B = B;
-  t.prefix_len = prefix_len; t.status = dev_status;
+  t.status = dev_status;
+  t.batch.spec_len = spec_len; t.batch.ctx_lens = kv->ctx_lens; t.batch.max_q = max_q; t.batch.max_ctx = max_ctx; t.batch.prefix_len = prefix_len;
   hipError_t lerr;
   {
     Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);
-    lerr = launch_prefix(t, spec_len, kv->ctx_lens, max_q, max_ctx, workspace, (hipStream_t)stream);
+    lerr = launch_prefix(t, workspace, (hipStream_t)stream);
   }
   if (lerr != hipSuccess) return fail(c, MN_EHIP, "%s: kernel attribute: %s", who, hipGetErrorString(lerr));
   return hip_check(c, who);

@@ -179,39 +179,49 @@ AttnPlan attention_plan(const AttnArgs& a);  // what the kernels that will run n
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st);
 
 // ---- tile_attention.hip ----
+// What a shared-prefix call's kernels need to tell the rows' sequences and ranges.
+struct PrefixBatch {
+  const int32_t *spec_len, *ctx_lens;
+  int B, M, G, max_q, max_ctx, prefix_len;
+  int tile_rows, chunk;   // rows of a workgroup's tile, own keys of a range
+};
 struct TileArgs {
   const void *q, *k, *v;  // rows [M][H][hd] and [M][Hkv][hd] in the activation type, strides in elements (k, v: dense keys only)
   long q_stride, k_stride, v_stride;
   void* out;              // [M][H * hd]
   int M, H, Hkv, hd, dtype, B;
-  int n_tiles;            // workgroups per KV head
+  int n_tiles;            // workgroups per KV head (shared prefix: for the sequences' own keys)
   int max_tiles;          // most tiles of a sequence
+  int tile_rows;
   const int32_t* seq_rows;  // [B + 1] (dense keys)
-  const int32_t* items;     // work list, 8 int32 per record (pages)
   KvView kv;                // pages to read, or (dense keys, k non-null) to write the rows to
-  float *o_part, *ml_part;  // [slot][M][H][hd] and [slot][M][H][2]: outputs, (reference, sum)
-  int prefix_len, prefix_units, n_units, share, n_streams, prefix_slots, row_tiles, tile_rows;  // the shared part (stream_item)
-  int32_t* seq_bad;         // [B] set where a table row is damaged
   int32_t* status;
+  // shared prefix
+  PrefixBatch batch;
+  const int32_t* items;     // work list of the own keys, 8 int32 per record, or null (at most 64 sequences)
+  float *o_part, *ml_part;  // [slot][M][H][hd] and [slot][M][H][2]: outputs, (reference, sum)
+  int prefix_units, n_units, share, n_streams, prefix_slots, row_tiles;  // the shared part (stream_item)
+  int32_t* seq_bad;         // [B] whether a table row is damaged
 };
 struct PrefixPlan {
-  const int32_t *spec_len, *ctx_lens;
-  int B, M, G, max_q, max_ctx, prefix_len, prefix_slots, tile_rows, chunk, max_items;
+  PrefixBatch batch;
+  int prefix_slots, max_items;
   int32_t* items;
   int2* row_meta;           // [M] (sequence, its ranges of own keys: 0 where it takes no part)
-  int32_t *seq_bad, *status;
+  int32_t* status;
 };
 struct PrefixMerge {
   const float *o_part, *ml_part;
-  const int2* row_meta;
+  const int2* row_meta;     // or null (at most 64 sequences)
   const int32_t* seq_bad;
-  int M, H, Hkv, hd, prefix_slots, prefix_units, n_units, share, row_tiles, tile_rows;
+  PrefixBatch batch;
+  int M, H, Hkv, hd, prefix_slots, prefix_units, n_units, share, row_tiles;
 };
 bool prefix_fits(int M, int H, int Hkv, int prefix_len);
 size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx);
-hipError_t launch_prefix(TileArgs a, const int32_t* spec_len, const int32_t* ctx_lens, int max_q, int max_ctx, void* workspace, hipStream_t st);
+hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st);
 int prompt_tile_rows(const TileArgs& a, long stack_rows);
-hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st);
+hipError_t launch_prompt(const TileArgs& a, hipStream_t st);
 
 // ---- pool.hip ----
 struct PoolView {

@@ -100,10 +100,57 @@ __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, int G, int
   return true;
 }
 
-__device__ __forceinline__ bool list_item(const TileArgs& a, int t, Item& it) {
-  const int4 x = reinterpret_cast<const int4*>(a.items)[2 * t], y = reinterpret_cast<const int4*>(a.items)[2 * t + 1];
-  it = Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-  return it.R > 0;
+// What takes part in a shared-prefix call, for up to 64 sequences: lane b has sequence b's rows, its first row, and the ranges and row
+// tiles of its own keys.  Lengths that do not add up to the host's rows, or a run longer than its longest one, disable the batch; a
+// context outside [prefix_len, max_ctx) its sequence.  (Larger batches: prefix_plan_kernel.)
+struct Share {
+  int q, row0, ctx, ranges, tiles, flags;
+};
+__device__ __forceinline__ Share lane_share(const PrefixBatch& p) {
+  const int b = threadIdx.x & 63;
+  Share s{0, 0, 0, 0, 0, 0};
+  bool off = false;
+  if (b < p.B) {
+    const int k = p.spec_len[b];
+    s.ctx = p.ctx_lens[b];
+    off = k < 0 || k >= p.max_q;
+    s.q = off ? 0 : k + 1;
+  }
+  const int incl = wave_scan_i(s.q);
+  s.row0 = incl - s.q;
+  if (__any(off) || __builtin_amdgcn_readlane(incl, 63) != p.M) {
+    s.q = 0;
+    s.flags = MN_DEV_SPEC_LEN;
+  } else if (s.q > 0) {
+    if (s.ctx < p.prefix_len || (long)s.ctx + s.q > p.max_ctx) {
+      s.flags = MN_DEV_CTX;
+    } else {
+      s.ranges = (s.ctx + s.q - p.prefix_len + p.chunk - 1) / p.chunk;
+      s.tiles = (p.G * s.q + p.tile_rows - 1) / p.tile_rows;
+    }
+  }
+  return s;
+}
+
+// Item t of the sequences' own keys.
+__device__ __forceinline__ bool own_item(const TileArgs& a, int t, Item& it) {
+  if (a.items) {
+    const int4 x = reinterpret_cast<const int4*>(a.items)[2 * t], y = reinterpret_cast<const int4*>(a.items)[2 * t + 1];
+    it = Item{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    return it.R > 0;
+  }
+  const Share s = lane_share(a.batch);
+  const int incl = wave_scan_i(s.ranges * s.tiles), first = incl - s.ranges * s.tiles;
+  if (t == 0 && threadIdx.x < 64 && blockIdx.x == 0 && s.flags && a.status) atomicOr(a.status, s.flags);
+  const uint64_t mine = __ballot(t >= first && t < incl);
+  if (mine == 0) return false;
+  const int b = __ffsll((unsigned long long)mine) - 1;
+  const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, b); };
+  const int at = t - of(first), ranges = of(s.ranges), rt = at / ranges, k0 = a.batch.prefix_len + (at - rt * ranges) * a.batch.chunk;
+  it.ctx = of(s.ctx);
+  it.m0 = of(s.row0); it.R = a.batch.G * of(s.q); it.rbase = rt * a.batch.tile_rows; it.key0 = k0;
+  it.key_end = min(k0 + a.batch.chunk, it.ctx + of(s.q)); it.seq = b; it.slot = a.prefix_slots + at - rt * ranges;
+  return true;
 }
 
 // The shared part, as streams.  Its work is a line of units: 64 keys of the prefix for one tile of rows of one KV head, the keys of a tile
@@ -122,8 +169,8 @@ __device__ __forceinline__ bool stream_item(const TileArgs& a, int stream, int& 
   const int tile = unit / a.prefix_units, from = unit - tile * a.prefix_units, n = min(end - unit, a.prefix_units - from);
   unit += n;
   kvh = tile / a.row_tiles;
-  it.m0 = 0; it.R = a.H / a.Hkv * a.M; it.rbase = (tile - kvh * a.row_tiles) * a.tile_rows;
-  it.key0 = from * TKEYS; it.key_end = min(a.prefix_len, (from + n) * TKEYS);
+  it.m0 = 0; it.R = a.H / a.Hkv * a.M; it.rbase = (tile - kvh * a.row_tiles) * a.batch.tile_rows;
+  it.key0 = from * TKEYS; it.key_end = min(a.batch.prefix_len, (from + n) * TKEYS);
   it.ctx = NO_LIMIT; it.seq = 0; it.slot = stream - tile * a.prefix_units / a.share;
   return true;
 }
@@ -133,12 +180,13 @@ __device__ __forceinline__ bool stream_item(const TileArgs& a, int stream, int& 
 __device__ __forceinline__ void check_table(const TileArgs& a, const Item& it, int kvh) {
   if (it.slot != a.prefix_slots || it.rbase != 0 || kvh != 0) return;
   const int32_t *first = a.kv.block_tables, *row = first + (size_t)it.seq * a.kv.max_blocks_per_seq;
-  const int shared = a.prefix_len / a.kv.block_size, all = (int)(((long)it.ctx + it.R / (a.H / a.Hkv) + a.kv.block_size - 1) / a.kv.block_size);
+  const int shared = a.batch.prefix_len / a.kv.block_size, all = (int)(((long)it.ctx + it.R / (a.H / a.Hkv) + a.kv.block_size - 1) / a.kv.block_size);
   bool bad = false;
   for (int i = threadIdx.x; i < all; i += blockDim.x) bad |= (uint32_t)row[i] >= (uint32_t)a.kv.num_blocks || (i < shared && row[i] != first[i]);
-  if (bad) {
-    a.seq_bad[it.seq] = 1;
-    if (a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) {
+    a.seq_bad[it.seq] = bad;
+    if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
   }
 }
 
@@ -226,7 +274,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
   if constexpr (PAGED) {
     const int own = a.n_tiles * a.Hkv;                           // workgroups of the sequences' own keys; the streams come behind
     if ((int)blockIdx.x < own) {
-      if (!list_item(a, blockIdx.x / a.Hkv, it)) return;
+      if (!own_item(a, blockIdx.x / a.Hkv, it)) return;
       check_table(a, it, kvh);
     } else {
       stream = stream_of(a, blockIdx.x - own);
@@ -562,17 +610,22 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
 // ------------------------------------------------------------------------------------------
 // every other type, head_dim and block size
 // ------------------------------------------------------------------------------------------
-// Four waves of 16 stack rows; 32 keys at a time, widened to fp32 in LDS.  Products as above on the 16x16x4 fp32 instruction: lane
-// (row l16, g) holds of the first product's operands the elements 16 * step + 4g .. 4g + 3 of a row (four instructions take one each), and
-// of the second's the keys 4g + r that the first leaves in its registers.  HDP: head_dim padded to a multiple of 16 with zeros.
-constexpr int FKEYS = 32, FROWS = 64;
+// Products in fp32 on the 16x16x4 instruction, 16 stack rows per wave.  Nothing is staged and the waves never wait for one another: a lane's
+// operands are 4 consecutive elements of a row of K (four instructions take one each), and of V 4 elements of one key (dense rows: row i of
+// instruction r is element VEC i + r of the group) or 4 tokens of one element (pages), read from memory in that shape and widened;
+// 16 rows per workgroup, every fourth 32 keys (heads of 256: 16) to a wave, their parts put together in LDS at the end.  Bound by the round
+// trips of a wave through its keys, and by the L1 beyond: 4 prompts of 33 to 700 tokens of 4 fp32 heads of 64 12.5 us (32.6 with 64 rows
+// and keys staged for all waves; 27.0 with 64 rows and every wave reading all keys), 4 of 1500 to 2500 154 us = 78 TFLOP/s
+// (211, 237), 4 fp16 prompts of 300 to 1500 of 8/2 heads of 256 115 us (245, 260).  HDP: head_dim padded to a multiple of 16.
+constexpr int FROWS = 16, KW = 4;                                // rows of a workgroup, its waves
+template <typename T> struct __attribute__((aligned(4 * sizeof(T)))) Four { T x[4]; };
 
 template <typename T, int HDP, bool PAGED>
 __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
-  constexpr int LD = HDP + 4, NU = HDP / 16;
+  constexpr int NU = HDP / 16, LD = HDP + 4, HALVES = HDP == 256 ? 1 : 2;  // (16 keys at a time: registers)
+  constexpr int KEYS = 16 * HALVES;
+  constexpr int VEC = PAGED ? 1 : (HDP >= 64 ? 4 : HDP / 16);    // consecutive elements of V that a lane takes from a dense row
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  float* s_k = reinterpret_cast<float*>(smem);                   // [FKEYS][LD]
-  float* s_v = s_k + FKEYS * LD;
   const int G = a.H / a.Hkv;
   int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
   Item it;
@@ -580,7 +633,7 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
   if constexpr (PAGED) {
     const int own = a.n_tiles * a.Hkv;                           // workgroups of the sequences' own keys; the streams come behind
     if ((int)blockIdx.x < own) {
-      if (!list_item(a, blockIdx.x / a.Hkv, it)) return;
+      if (!own_item(a, blockIdx.x / a.Hkv, it)) return;
       check_table(a, it, kvh);
     } else {
       stream = stream_of(a, blockIdx.x - own);
@@ -592,92 +645,130 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
     if (!prompt_item<FROWS>(a, blockIdx.x / a.Hkv, G, reinterpret_cast<int32_t*>(smem), it)) return;
     if (a.kv.k) append_rows<T, FROWS>(a, it, G, kvh);
   }
-  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int part = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hd = a.hd;
+  const float c = rsqrtf((float)hd) * LOG2E_T;
+  const int bs = PAGED ? a.kv.block_size : 1;
   do {
-    const int rw = it.rbase + wave * 16 + l16, r = min(rw, it.R - 1), j = r / G;
+    const int r = min(it.rbase + l16, it.R - 1), j = r / G;
     const int lim = min(it.key_end - 1, it.ctx + j);
-    const float c = rsqrtf((float)hd) * LOG2E_T;
+    const int max_lim = min(it.key_end - 1, it.ctx + (min(it.R, it.rbase + FROWS) - 1) / G);  // of all rows
     f32x4 q[NU], O[NU];
     const T* Q = static_cast<const T*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * hd;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       O[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      q[u] = O[u];
+      if (16 * u + 4 * g < hd) {
+        const Four<T> x = *reinterpret_cast<const Four<T>*>(Q + 16 * u + 4 * g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q[u][e] = 16 * u + 4 * g + e < hd ? (float)Q[16 * u + 4 * g + e] * c : 0.f;
+        for (int e = 0; e < 4; ++e) q[u][e] = (float)x.x[e] * c;
+      }
     }
     float run_m = -INFINITY, run_l = 0.f;
     const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
-    const int bs = PAGED ? a.kv.block_size : 1;
-    __syncthreads();                                               // (the search is through with its part of the LDS)
-    for (int k0 = it.key0; k0 < it.key_end; k0 += FKEYS) {
-      // the keys' rows, 8 elements at a time; past the last key and past head_dim zeros
-      for (int i = tid; i < FKEYS * (HDP / 8); i += 256) {
-        const int key = i % FKEYS, p8 = i / FKEYS, pos = k0 + key;
-        struct __attribute__((aligned(16))) Piece { T x[8]; };
-        float kx[8], vx[8];
+    const bool quads = PAGED && (bs & 3) == 0;                   // four tokens from a multiple of four lie in one block
+    const int shift = (bs & (bs - 1)) == 0 ? 31 - __clz(bs) : -1;
+    const auto block_of = [&](int key) { return shift >= 0 ? key >> shift : key / bs; };
+    const auto page_of = [&](int key) { return ((size_t)min((uint32_t)bt[block_of(key)], (uint32_t)a.kv.num_blocks - 1u) * a.Hkv + kvh) * (size_t)(hd * bs); };
+    for (int k0 = it.key0 + part * KEYS; k0 <= max_lim; k0 += KW * KEYS) {
+      const int last = it.key_end - 1;
+      // ---- scores ----
+      f32x4 S[HALVES];
+      const T* kr[HALVES];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
-        if (pos < it.key_end && 8 * p8 < hd) {
-          if constexpr (PAGED) {
-            const uint32_t id = min((uint32_t)bt[pos / bs], (uint32_t)a.kv.num_blocks - 1u);
-            const size_t page = ((size_t)id * a.Hkv + kvh) * (size_t)(hd * bs);
-            const int off = pos % bs;
-            const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.kv.k) + page + ((size_t)p8 * bs + off) * 8);
-            const T* v = static_cast<const T*>(a.kv.v) + page + (size_t)(8 * p8) * bs + off;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v[(size_t)e * bs]; }
-          } else {
-            const Piece k = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.k) + (size_t)(it.m0 + pos) * a.k_stride + (size_t)kvh * hd + 8 * p8);
-            const Piece v = *reinterpret_cast<const Piece*>(static_cast<const T*>(a.v) + (size_t)(it.m0 + pos) * a.v_stride + (size_t)kvh * hd + 8 * p8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { kx[e] = (float)k.x[e]; vx[e] = (float)v.x[e]; }
-          }
-        }
-        f32x4 *dk = reinterpret_cast<f32x4*>(s_k + key * LD + 8 * p8), *dv = reinterpret_cast<f32x4*>(s_v + key * LD + 8 * p8);
-        dk[0] = (f32x4){kx[0], kx[1], kx[2], kx[3]}; dk[1] = (f32x4){kx[4], kx[5], kx[6], kx[7]};
-        dv[0] = (f32x4){vx[0], vx[1], vx[2], vx[3]}; dv[1] = (f32x4){vx[4], vx[5], vx[6], vx[7]};
+      for (int h = 0; h < HALVES; ++h) {
+        S[h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        const int key = min(k0 + 16 * h + l16, last);
+        if constexpr (PAGED) kr[h] = static_cast<const T*>(a.kv.k) + page_of(key) + (size_t)(key - block_of(key) * bs) * 8;
+        else kr[h] = static_cast<const T*>(a.k) + (size_t)(it.m0 + key) * a.k_stride + (size_t)kvh * hd;
       }
-      __syncthreads();
-      f32x4 S[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      Four<T> kx[HALVES][NU];
 #pragma unroll
       for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 k = *reinterpret_cast<const f32x4*>(s_k + (16 * h + l16) * LD + 16 * u + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) S[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], q[u][e], S[h], 0, 0, 0);
+        for (int h = 0; h < HALVES; ++h) {
+          const int e0 = HDP == 16 ? min(4 * g, hd - 4) : 16 * u + 4 * g;  // (heads of 8: against zeros of the query)
+          kx[h][u] = *reinterpret_cast<const Four<T>*>(kr[h] + (PAGED ? (e0 >> 3) * (8 * bs) + (e0 & 7) : e0));
         }
+      // ---- values: asked for ahead of the products ----
+      Four<T> vx[HALVES][NU];
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        if constexpr (PAGED) {
+          const int key = k0 + 16 * h + 4 * g;
+          const size_t page = page_of(min(key, last));
+#pragma unroll
+          for (int u = 0; u < NU; ++u) {
+            const int el = HDP == 16 ? min(l16, hd - 1) : 16 * u + l16;
+            const T* v = static_cast<const T*>(a.kv.v) + page + el * bs;
+            if (quads) {
+              vx[h][u] = *reinterpret_cast<const Four<T>*>(v + (min(key, last & ~3) - block_of(min(key, last)) * bs));
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int ke = min(key + e, last);
+                vx[h][u].x[e] = static_cast<const T*>(a.kv.v)[page_of(ke) + (size_t)(el * bs + ke - block_of(ke) * bs)];
+              }
+            }
+            // slots past the last key may hold anything, and 0 times anything has to stay 0
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (key + e > last) vx[h][u].x[e] = (T)0.f;
+          }
+        } else {
+          // four keys: four instructions of VEC elements for each of the NU / VEC groups
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const T* v = static_cast<const T*>(a.v) + (size_t)(it.m0 + min(k0 + 16 * h + 4 * g + e, last)) * a.v_stride + (size_t)kvh * hd;
+#pragma unroll
+            for (int n = 0; n < NU / VEC; ++n) {
+              struct __attribute__((aligned(VEC * sizeof(T)))) Some { T x[VEC]; };
+              const int el = HDP == 16 ? min(l16, hd - 1) : n * (16 * VEC) + VEC * l16;
+              const Some x = *reinterpret_cast<const Some*>(v + el);
+#pragma unroll
+              for (int i = 0; i < VEC; ++i) vx[h][n * VEC + i].x[e] = x.x[i];
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h) S[h] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)kx[h][u].x[e], q[u][e], S[h], 0, 0, 0);
       float tm = -INFINITY;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < HALVES; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (k0 + 16 * h + 4 * g + e > lim) S[h][e] = -INFINITY;
           tm = fmaxf(tm, S[h][e]);
         }
-      uint32_t x, y;
-      lane_pair<16>(__float_as_uint(tm), x, y);
-      tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
-      lane_pair<32>(__float_as_uint(tm), x, y);
-      tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
-      const float nm = fmaxf(run_m, tm), ref = nm == -INFINITY ? 0.f : nm;
-      const float alpha = __builtin_amdgcn_exp2f(run_m - ref);
-      run_m = nm;
-      run_l *= alpha;
+      if (__any(tm > run_m)) {
+        uint32_t x, y;
+        lane_pair<16>(__float_as_uint(tm), x, y);
+        tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
+        lane_pair<32>(__float_as_uint(tm), x, y);
+        tm = fmaxf(__uint_as_float(x), __uint_as_float(y));
+        const float nm = fmaxf(run_m, tm), alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m - nm);
+        run_m = nm;
+        run_l *= alpha;
 #pragma unroll
-      for (int u = 0; u < NU; ++u) O[u] *= alpha;
+        for (int u = 0; u < NU; ++u) O[u] *= alpha;
+      }
+      const float ref = run_m == -INFINITY ? 0.f : run_m;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < HALVES; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float p = __builtin_amdgcn_exp2f(S[h][e] - ref);
           run_l += p;
 #pragma unroll
-          for (int u = 0; u < NU; ++u)
-            O[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(s_v[(16 * h + 4 * g + e) * LD + 16 * u + l16], p, O[u], 0, 0, 0);
+          for (int u = 0; u < NU; ++u) O[u] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)vx[h][u].x[e], p, O[u], 0, 0, 0);
         }
-      __syncthreads();
     }
     // the row's sum over the four lane groups
     uint32_t x, y;
@@ -685,21 +776,43 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
     run_l = __uint_as_float(x) + __uint_as_float(y);
     lane_pair<32>(__float_as_uint(run_l), x, y);
     run_l = __uint_as_float(x) + __uint_as_float(y);
-    if (rw >= it.R) continue;
-    const int m = it.m0 + j, h = kvh * G + r - j * G;
-    const float inv = 1.f / run_l;
+    // element of O[u][i] in this lane
+    const auto element = [&](int u, int i) { return u / VEC * (16 * VEC) + VEC * (4 * g + i) + u % VEC; };
+    float* s_o = reinterpret_cast<float*>(smem);               // [KW][16][LD]
+    float2* s_ml = reinterpret_cast<float2*>(smem + KW * 16 * LD * 4);
+    __syncthreads();                                           // (the search, or the piece before, is through with the LDS)
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      if (16 * u + 4 * g >= hd) continue;
+    for (int u = 0; u < NU; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_o[(part * 16 + l16) * LD + element(u, i)] = O[u][i];
+    if (g == 0) s_ml[part * 16 + l16] = make_float2(run_m, run_l);
+    __syncthreads();
+    for (int i = tid; i < 16 * (HDP / 4); i += 256) {
+      const int row = i / (HDP / 4), e0 = i % (HDP / 4) * 4, rr = it.rbase + row;
+      if (rr >= it.R || e0 >= hd) continue;
+      float top = -INFINITY, l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KW; ++w) top = fmaxf(top, s_ml[w * 16 + row].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float2 ml = s_ml[w * 16 + row];
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        l += ml.y * f;
+        o += *reinterpret_cast<const f32x4*>(s_o + (w * 16 + row) * LD + e0) * f;
+      }
+      const int jj = rr / G, m = it.m0 + jj, h = kvh * G + rr - jj * G;
       if constexpr (PAGED) {
-        *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + 16 * u + 4 * g) = O[u];
+        *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + e0) = o;
+        if (e0 == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(top, l);
       } else {
-        T* o = static_cast<T*>(a.out) + ((size_t)m * a.H + h) * hd + 16 * u + 4 * g;
+        Four<T> w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (T)(O[u][e] * inv);
+        for (int e = 0; e < 4; ++e) w.x[e] = (T)(o[e] / l);
+        *reinterpret_cast<Four<T>*>(static_cast<T*>(a.out) + ((size_t)m * a.H + h) * hd + e0) = w;
       }
     }
-    if (PAGED && g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m, run_l);
   } while (more && stream_item(a, stream, unit, kvh, it));
 }
 
@@ -711,21 +824,23 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
 // keys, from a work list.  Each piece leaves an unnormalised output with its reference and sum per row in a slot of its own,
 // and a row's slots are put together at the end.
 //
-// prefix_plan_kernel (one workgroup): the rows' sequences, who takes part, and the list of items.
+// prefix_plan_kernel (one workgroup; more than 64 sequences): the rows' sequences, who takes part, and the list of items.  Up to 64 every
+// workgroup finds its item by itself (own_item), and the merge its rows' sequences, which saves a launch: 5 us of 33 to 43.
 __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   __shared__ int s_rows[16], s_items[16], s_bad;
+  const PrefixBatch& c = p.batch;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (tid == 0) s_bad = 0;
   __syncthreads();
   int flags = 0;
   const auto length = [&](int b) {
-    const int k = p.spec_len[b];
-    return k >= 0 && k < p.max_q ? k + 1 : -1;
+    const int k = c.spec_len[b];
+    return k >= 0 && k < c.max_q ? k + 1 : -1;
   };
   // lengths first: rows that do not add up to the host's, or a run longer than its longest, disable the batch
   int rows = 0;
   bool off = false;
-  for (int b = tid; b < p.B; b += 1024) {
+  for (int b = tid; b < c.B; b += 1024) {
     const int q = length(b);
     off |= q < 0;
     rows += max(q, 0);
@@ -736,20 +851,20 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   __syncthreads();
   int total = 0;
   for (int w = 0; w < 16; ++w) total += s_rows[w];
-  const bool batch = s_bad == 0 && total == p.M;
+  const bool batch = s_bad == 0 && total == c.M;
   if (!batch) flags |= MN_DEV_SPEC_LEN;
   int4* items = reinterpret_cast<int4*>(p.items);
   int row_at = 0, item_at = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 1024) {
-    const int b = b0 + tid, q = batch && b < p.B ? length(b) : 0;
+  for (int b0 = 0; b0 < c.B; b0 += 1024) {
+    const int b = b0 + tid, q = batch && b < c.B ? length(b) : 0;
     int ctx = 0, ranges = 0, rts = 0;
     if (q > 0) {
-      ctx = p.ctx_lens[b];
-      if (ctx < p.prefix_len || (long)ctx + q > p.max_ctx) {
+      ctx = c.ctx_lens[b];
+      if (ctx < c.prefix_len || (long)ctx + q > c.max_ctx) {
         flags |= MN_DEV_CTX;
       } else {
-        ranges = (ctx + q - p.prefix_len + p.chunk - 1) / p.chunk;
-        rts = (p.G * q + p.tile_rows - 1) / p.tile_rows;
+        ranges = (ctx + q - c.prefix_len + c.chunk - 1) / c.chunk;
+        rts = (c.G * q + c.tile_rows - 1) / c.tile_rows;
       }
     }
     const int rows_incl = wave_scan_i(q), items_incl = wave_scan_i(ranges * rts);
@@ -762,61 +877,96 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
       row_at += s_rows[w];
       item_at += s_items[w];
     }
-    if (b < p.B) p.seq_bad[b] = 0;
     for (int j = 0; j < q; ++j) p.row_meta[row0 + j] = make_int2(b, ranges);
     for (int rt = 0; rt < rts; ++rt)
       for (int s = 0; s < ranges; ++s, ++at) {
-        const int k0 = p.prefix_len + s * p.chunk;
-        items[2 * at] = make_int4(row0, p.G * q, rt * p.tile_rows, k0);
-        items[2 * at + 1] = make_int4(min(k0 + p.chunk, ctx + q), ctx, b, p.prefix_slots + s);
+        const int k0 = c.prefix_len + s * c.chunk;
+        items[2 * at] = make_int4(row0, c.G * q, rt * c.tile_rows, k0);
+        items[2 * at + 1] = make_int4(min(k0 + c.chunk, ctx + q), ctx, b, p.prefix_slots + s);
       }
   }
   if (!batch)
-    for (int m = tid; m < p.M; m += 1024) p.row_meta[m] = make_int2(0, 0);
+    for (int m = tid; m < c.M; m += 1024) p.row_meta[m] = make_int2(0, 0);
   for (int i = item_at + tid; i < p.max_items; i += 1024) items[2 * i] = make_int4(0, 0, 0, 0);
   if (flags && p.status) atomicOr(p.status, flags);
 }
 
-// Four elements of a row of one head per thread; four slots are asked for at once.
-template <typename T>
+// Four elements of a row of one head per thread; several slots are asked for at once.  GROUPS threads share them where there are few rows
+// and many slots (6 rows of 64 heads, 33 slots: 10 us with one).
+constexpr int AT_ONCE = 4;
+template <typename T, int GROUPS>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, heads = (size_t)p.M * p.H;
-  const int per = p.hd / 4;
-  if (i >= heads * per) return;
-  const size_t mh = i / per;
+  constexpr int WIDE = 256 / GROUPS;
+  __shared__ float s_top[GROUPS][WIDE], s_l[GROUPS][WIDE];
+  __shared__ f32x4 s_o[GROUPS][WIDE];
+  const size_t heads = (size_t)p.M * p.H;
+  const int group = threadIdx.x / WIDE, lane_at = threadIdx.x % WIDE, per = p.hd / 4;
+  const size_t i = min((size_t)blockIdx.x * WIDE + lane_at, heads * per - 1), mh = i / per;  // (past the end: the last ones once more)
   const int m = (int)(mh / p.H), h = (int)(mh - (size_t)m * p.H), G = p.H / p.Hkv, kvh = h / G;
-  const int2 meta = p.row_meta[m];
+  int2 meta = make_int2(0, 0);                                   // sequence, ranges of its own keys
+  if (p.row_meta) {
+    meta = p.row_meta[m];
+  } else {
+    const Share s = lane_share(p.batch);
+    // (the rows of the wave, one after the other: few, and one unless a row is very short)
+    const int m0 = __builtin_amdgcn_readfirstlane(m), m1 = __builtin_amdgcn_readlane(m, 63);
+    for (int r = m0; r <= m1; ++r) {
+      const uint64_t has = __ballot(s.q > 0 && r >= s.row0 && r < s.row0 + s.q);
+      if (has == 0) continue;
+      const int b = __ffsll((unsigned long long)has) - 1, ranges = __builtin_amdgcn_readlane(s.ranges, b);
+      if (m == r) meta = make_int2(b, ranges);
+    }
+  }
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f, top = -INFINITY;
   if (meta.y > 0 && !p.seq_bad[meta.x]) {
     int shared = 0;                                              // streams that met the row's tile
     if (p.n_units > 0) {
-      const int first = (kvh * p.row_tiles + (m * G + h - kvh * G) / p.tile_rows) * p.prefix_units;
+      const int first = (kvh * p.row_tiles + (m * G + h - kvh * G) / p.batch.tile_rows) * p.prefix_units;
       shared = (first + p.prefix_units - 1) / p.share - first / p.share + 1;
     }
     const int n = shared + meta.y;
-    for (int s0 = 0; s0 < n; s0 += 4) {
-      float2 ml[4];
-      f32x4 v[4];
+    for (int s0 = group; s0 < n; s0 += AT_ONCE * GROUPS) {
+      float2 ml[AT_ONCE];
+      f32x4 v[AT_ONCE];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int s = min(s0 + u, n - 1), at = s < shared ? s : p.prefix_slots + s - shared;
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int s = min(s0 + u * GROUPS, n - 1), at = s < shared ? s : p.prefix_slots + s - shared;
         ml[u] = *reinterpret_cast<const float2*>(p.ml_part + (at * heads + mh) * 2);
         v[u] = *reinterpret_cast<const f32x4*>(p.o_part + at * heads * p.hd + 4 * i);
       }
       float nm = top;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) nm = fmaxf(nm, ml[u].x);
+      for (int u = 0; u < AT_ONCE; ++u) nm = fmaxf(nm, ml[u].x);
       const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
       l *= keep;
       o *= keep;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float w = s0 + u < n ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const float w = s0 + u * GROUPS < n ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
         l += ml[u].y * w;
         o += v[u] * w;
       }
       top = nm;
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    s_top[group][lane_at] = top;
+    s_l[group][lane_at] = l;
+    s_o[group][lane_at] = o;
+    __syncthreads();
+    if (group > 0) return;
+    float nm = top;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) nm = fmaxf(nm, s_top[g][lane_at]);
+    const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+      const float w = __builtin_amdgcn_exp2f(s_top[g][lane_at] - ref);
+      l += s_l[g][lane_at] * w;
+      o += s_o[g][lane_at] * w;
     }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -864,13 +1014,13 @@ static hipError_t launch_mfma(const TileArgs& a, int tile_rows, hipStream_t st) 
 
 template <typename T, int HDP, bool PAGED>
 static hipError_t launch_f32(const TileArgs& a, hipStream_t st) {
-  constexpr size_t need = 2 * (size_t)FKEYS * (HDP + 4) * 4;
+  constexpr size_t parts = (size_t)KW * 16 * ((HDP + 4) * 4 + 8);
   static std::once_flag once;
   static hipError_t err = hipSuccess;
-  std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED>, need); });
+  std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED>, parts); });
   if (err != hipSuccess) return err;
   const size_t list = PAGED || a.B <= 64 ? 0 : (size_t)a.B * 4;  // (the search's numbers)
-  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (unsigned)a.n_streams, 256, need > list ? need : list, st>>>(a);
+  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (unsigned)a.n_streams, 64 * KW, parts > list ? parts : list, st>>>(a);
   return hipSuccess;
 }
 
@@ -885,9 +1035,9 @@ static hipError_t launch_f32_hd(const TileArgs& a, hipStream_t st) {
   }
 }
 
-hipError_t launch_prompt(const TileArgs& a, int tile_rows, hipStream_t st) {
+hipError_t launch_prompt(const TileArgs& a, hipStream_t st) {
   if (!tile_mfma(a, a.kv.k != nullptr)) return a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, false>(a, st) : launch_f32_hd<float, false>(a, st);
-  return launch_mfma<false>(a, tile_rows, st);
+  return launch_mfma<false>(a, a.tile_rows, st);
 }
 
 
@@ -904,7 +1054,7 @@ static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
   const long G = a.H / a.Hkv;
   s.tile_rows = !tile_mfma(a, true) ? FROWS : MN_TUNE("MN_TILE", 0) ? MN_TUNE("MN_TILE", 0) : (M * G > 64 ? 128 : 64);
   s.row_tiles = (int)((M * G + s.tile_rows - 1) / s.tile_rows);
-  s.units = (a.prefix_len + TKEYS - 1) / TKEYS;
+  s.units = (a.batch.prefix_len + TKEYS - 1) / TKEYS;
   s.n_units = s.row_tiles * a.Hkv * s.units;
   s.share = (s.n_units + STREAMS - 1) / STREAMS;
   const int by_slots = (s.units + MAX_SLOTS - 3) / (MAX_SLOTS - 2);
@@ -913,7 +1063,7 @@ static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
   if (s.share < by_slots) s.share = by_slots;
   s.n_streams = (s.n_units + s.share - 1) / s.share;
   s.slots = s.units > 0 ? (s.units - 1) / s.share + 2 : 0;
-  const int rest = max_ctx - a.prefix_len, want = (long)a.B * a.Hkv >= 256 ? 1024 : 256;
+  const int rest = max_ctx - a.batch.prefix_len, want = (long)a.B * a.Hkv >= 256 ? 1024 : 256;
   s.ranges = (rest + want - 1) / want;
   if (s.ranges > MAX_RANGES) s.ranges = MAX_RANGES;
   if (s.ranges < 1) s.ranges = 1;
@@ -931,7 +1081,7 @@ static PrefixLayout prefix_layout(int B, int M, int H, int Hkv, int hd, int pref
   // slots of a tile: units / share + 2 with share >= row tiles * KV heads * units / STREAMS, and MAX_SLOTS; row tiles >= M G / 128
   const long slots_a = (long)MAX_SLOTS * M, slots_b = (long)STREAMS * 128 / H + 3l * M;
   L.slot_rows = (size_t)((slots_a < slots_b ? slots_a : slots_b) + ranges * M);
-  L.max_items = (size_t)(((G * M + 63) / 64 + B) * ranges);
+  L.max_items = (size_t)(((G * M + 15) / 16 + B) * ranges);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 4095) & ~(size_t)4095; return o; };
   L.meta = take((size_t)M * 8); L.bad = take((size_t)B * 4); L.items = take(L.max_items * 32);
@@ -944,34 +1094,43 @@ size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_l
   return prefix_layout(B, M, H, Hkv, hd, prefix_len, max_ctx).total;
 }
 bool prefix_fits(int M, int H, int Hkv, int prefix_len) {
-  return (((long)M * (H / Hkv) + 63) / 64) * Hkv * (((long)prefix_len + TKEYS - 1) / TKEYS) < (1l << 30);
+  return (((long)M * (H / Hkv) + 15) / 16) * Hkv * (((long)prefix_len + TKEYS - 1) / TKEYS) < (1l << 30);
 }
 
-// max_q: the longest run of rows
-hipError_t launch_prefix(TileArgs a, const int32_t* spec_len, const int32_t* ctx_lens, int max_q, int max_ctx, void* workspace, hipStream_t st) {
-  const PrefixLayout L = prefix_layout(a.B, a.M, a.H, a.Hkv, a.hd, a.prefix_len, max_ctx);
+template <typename T>
+static void launch_prefix_merge(const PrefixMerge& g, T* out, hipStream_t st) {
+  const size_t threads = (size_t)g.M * g.H * (g.hd / 4);
+  // (8 threads for the slots of a row where that still leaves no more than two workgroups per CU)
+  if (g.prefix_slots >= 8 && threads * 8 <= 512 * 256) prefix_merge_kernel<T, 8><<<(unsigned)((threads + 31) / 32), 256, 0, st>>>(g, out);
+  else prefix_merge_kernel<T, 1><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(g, out);
+}
+
+// a.batch: spec_len, ctx_lens, max_q (the longest run of rows), max_ctx and prefix_len are the caller's
+hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st) {
+  const int max_ctx = a.batch.max_ctx;
+  const PrefixLayout L = prefix_layout(a.B, a.M, a.H, a.Hkv, a.hd, a.batch.prefix_len, max_ctx);
   const PrefixShape s = prefix_shape(a, a.M, max_ctx);
   unsigned char* w = static_cast<unsigned char*>(workspace);
-  PrefixPlan p{};
-  p.spec_len = spec_len; p.ctx_lens = ctx_lens; p.status = a.status;
-  p.B = a.B; p.M = a.M; p.G = a.H / a.Hkv; p.max_q = max_q; p.max_ctx = max_ctx; p.prefix_len = a.prefix_len;
-  p.prefix_slots = s.slots; p.tile_rows = s.tile_rows; p.chunk = s.chunk;
-  p.items = reinterpret_cast<int32_t*>(w + L.items); p.row_meta = reinterpret_cast<int2*>(w + L.meta);
-  p.seq_bad = reinterpret_cast<int32_t*>(w + L.bad);
-  p.max_items = (int)(((long)a.M * p.G / s.tile_rows + a.B) * s.ranges);
-  a.items = p.items; a.seq_bad = p.seq_bad; a.n_tiles = p.max_items;
+  a.batch.B = a.B; a.batch.M = a.M; a.batch.G = a.H / a.Hkv; a.batch.tile_rows = s.tile_rows; a.batch.chunk = s.chunk;
+  a.seq_bad = reinterpret_cast<int32_t*>(w + L.bad);
+  a.n_tiles = (int)(((long)a.M * a.batch.G / s.tile_rows + a.B) * s.ranges);
   a.prefix_slots = s.slots; a.prefix_units = s.units; a.n_units = s.n_units; a.share = s.share; a.n_streams = s.n_streams;
   a.row_tiles = s.row_tiles; a.tile_rows = s.tile_rows;
   a.o_part = reinterpret_cast<float*>(w + L.o_part); a.ml_part = reinterpret_cast<float*>(w + L.ml_part);
-  prefix_plan_kernel<<<1, 1024, 0, st>>>(p);
+  int2* meta = nullptr;
+  if (a.B > 64) {
+    meta = reinterpret_cast<int2*>(w + L.meta);
+    int32_t* items = reinterpret_cast<int32_t*>(w + L.items);
+    a.items = items;
+    prefix_plan_kernel<<<1, 1024, 0, st>>>(PrefixPlan{a.batch, s.slots, a.n_tiles, items, meta, a.status});
+  }
   hipError_t e;
   if (!tile_mfma(a, true)) e = a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, true>(a, st) : launch_f32_hd<float, true>(a, st);
   else e = launch_mfma<true>(a, s.tile_rows, st);
   if (e != hipSuccess) return e;
-  const PrefixMerge g{a.o_part, a.ml_part, p.row_meta, p.seq_bad, a.M, a.H, a.Hkv, a.hd, s.slots, s.units, s.n_units, s.share, s.row_tiles, s.tile_rows};
-  const unsigned grid = (unsigned)(((size_t)a.M * a.H * (a.hd / 4) + 255) / 256);
-  if (a.dtype == MN_DT_BF16) prefix_merge_kernel<<<grid, 256, 0, st>>>(g, static_cast<f16_t*>(a.out));
-  else prefix_merge_kernel<<<grid, 256, 0, st>>>(g, static_cast<float*>(a.out));
+  const PrefixMerge g{a.o_part, a.ml_part, meta, a.seq_bad, a.batch, a.M, a.H, a.Hkv, a.hd, s.slots, s.units, s.n_units, s.share, s.row_tiles};
+  if (a.dtype == MN_DT_BF16) launch_prefix_merge(g, static_cast<f16_t*>(a.out), st);
+  else launch_prefix_merge(g, static_cast<float*>(a.out), st);
   return hipSuccess;
 }
 
