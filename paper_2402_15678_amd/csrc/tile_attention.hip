@@ -29,6 +29,13 @@ struct Item {
   int m0, R, rbase, key0, key_end, ctx, seq, slot;
 };
 
+// Division by a number that is mostly a power of two (a uniform branch in place of thirty instructions).
+struct Divide {
+  int d, shift;
+  __device__ __forceinline__ explicit Divide(int d_) : d(d_), shift((d_ & (d_ - 1)) == 0 ? 31 - __clz(d_) : -1) {}
+  __device__ __forceinline__ int operator()(int x) const { return shift >= 0 ? x >> shift : (int)((uint32_t)x / (uint32_t)d); }
+};
+
 // Sum over the lanes of max(0, n(b) - level) for b < B.
 template <typename F>
 __device__ __forceinline__ int tiles_from(int level, int B, F n) {
@@ -67,10 +74,12 @@ __device__ __forceinline__ void find_tile(int t, int B, int max_tiles, F n, int 
 // The prompt's item of this workgroup.  Lengths come from the device; those that do not fit the launch (which the host's sized)
 // leave the whole call undone.  s_n: room for a number per sequence.
 template <int ROWS>
-__device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, int G, int32_t* s_n, Item& it) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, const Divide& by, int32_t* s_n, Item& it) {
+  const int lane = threadIdx.x & 63, G = by.d;
+  int r0 = 0, r1 = 0;
   auto tiles = [&](int b) {                      // -1: does not fit
-    const int r0 = a.seq_rows[b], r1 = a.seq_rows[b + 1];
+    r0 = a.seq_rows[b];
+    r1 = a.seq_rows[b + 1];
     if (r0 < 0 || r1 < r0 || r1 > a.M) return -1;
     const int n = (int)(((long)(r1 - r0) * G + ROWS - 1) / ROWS);
     return n > a.max_tiles ? -1 : n;
@@ -94,9 +103,17 @@ __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, int G, int
   find_tile(t, a.B, a.max_tiles, n, total, seq, tile);
   seq = __builtin_amdgcn_readfirstlane(seq);
   tile = __builtin_amdgcn_readfirstlane(tile);
-  const int row0 = a.seq_rows[seq], len = a.seq_rows[seq + 1] - row0;
+  int row0, row1;
+  if (a.B <= 64) {                               // (the offsets are in the lanes)
+    row0 = __builtin_amdgcn_readlane(r0, seq);
+    row1 = __builtin_amdgcn_readlane(r1, seq);
+  } else {
+    row0 = a.seq_rows[seq];
+    row1 = a.seq_rows[seq + 1];
+  }
+  const int len = row1 - row0;
   it.m0 = row0; it.R = len * G; it.rbase = tile * ROWS; it.key0 = 0; it.ctx = 0; it.seq = seq; it.slot = -1;
-  it.key_end = min(len, (min(it.R, it.rbase + ROWS) - 1) / G + 1);
+  it.key_end = min(len, by(min(it.R, it.rbase + ROWS) - 1) + 1);
   return true;
 }
 
@@ -267,7 +284,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
   constexpr int HS = St::HS, NU = St::NU, KP = St::KP, LPW = St::FRAGS / NW, ROWS = 16 * CT * NW;
   static_assert(St::FRAGS % NW == 0, "whole pieces per wave");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  const int G = a.H / a.Hkv;
+  const Divide by(a.H / a.Hkv);                                  // (query heads per KV head)
+  const int G = by.d;
   int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
   Item it;
   bool more = false;
@@ -283,7 +301,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       more = true;
     }
   } else {
-    if (!prompt_item<ROWS>(a, blockIdx.x / a.Hkv, G, reinterpret_cast<int32_t*>(smem), it)) return;
+    if (!prompt_item<ROWS>(a, blockIdx.x / a.Hkv, by, reinterpret_cast<int32_t*>(smem), it)) return;
   }
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -292,13 +310,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // this wave's rows, and the keys that its first and last row see
     const int rw0 = it.rbase + wave * CT * 16;
     const bool rows = rw0 < it.R;
-    const int min_lim = min(it.key_end - 1, it.ctx + rw0 / G);
-    const int max_lim = rows ? min(it.key_end - 1, it.ctx + (min(it.R, rw0 + CT * 16) - 1) / G) : -1;
+    const int min_lim = min(it.key_end - 1, it.ctx + by(rw0));
+    const int max_lim = rows ? min(it.key_end - 1, it.ctx + by(min(it.R, rw0 + CT * 16) - 1)) : -1;
     f16x8 qf[CT][HS];
     int lim[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      const int r = min(rw0 + 16 * ct + l16, it.R - 1), j = r / G;
+      const int r = min(rw0 + 16 * ct + l16, it.R - 1), j = by(r);
       lim[ct] = min(it.key_end - 1, it.ctx + j);
       const f16_t* q = static_cast<const f16_t*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * HDIM;
 #pragma unroll
@@ -535,7 +553,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       L[ct] = __uint_as_float(x) + __uint_as_float(y);
       const int r = rw0 + 16 * ct + l16;
       if (r >= it.R) continue;
-      const int j = r / G, m = it.m0 + j, h = kvh * G + r - j * G;
+      const int j = by(r), m = it.m0 + j, h = kvh * G + r - j * G;
       const float l = L[ct];
       if constexpr (PAGED) {
         float* o = a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * HDIM + 4 * g;
@@ -626,7 +644,8 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
   constexpr int KEYS = 16 * HALVES;
   constexpr int VEC = PAGED ? 1 : (HDP >= 64 ? 4 : HDP / 16);    // consecutive elements of V that a lane takes from a dense row
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  const int G = a.H / a.Hkv;
+  const Divide by(a.H / a.Hkv);                                  // (query heads per KV head)
+  const int G = by.d;
   int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
   Item it;
   bool more = false;
@@ -642,7 +661,7 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
       more = true;
     }
   } else {
-    if (!prompt_item<FROWS>(a, blockIdx.x / a.Hkv, G, reinterpret_cast<int32_t*>(smem), it)) return;
+    if (!prompt_item<FROWS>(a, blockIdx.x / a.Hkv, by, reinterpret_cast<int32_t*>(smem), it)) return;
     if (a.kv.k) append_rows<T, FROWS>(a, it, G, kvh);
   }
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -651,9 +670,9 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
   const float c = rsqrtf((float)hd) * LOG2E_T;
   const int bs = PAGED ? a.kv.block_size : 1;
   do {
-    const int r = min(it.rbase + l16, it.R - 1), j = r / G;
+    const int r = min(it.rbase + l16, it.R - 1), j = by(r);
     const int lim = min(it.key_end - 1, it.ctx + j);
-    const int max_lim = min(it.key_end - 1, it.ctx + (min(it.R, it.rbase + FROWS) - 1) / G);  // of all rows
+    const int max_lim = min(it.key_end - 1, it.ctx + by(min(it.R, it.rbase + FROWS) - 1));  // of all rows
     f32x4 q[NU], O[NU];
     const T* Q = static_cast<const T*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * hd;
 #pragma unroll
@@ -802,7 +821,7 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
         l += ml.y * f;
         o += *reinterpret_cast<const f32x4*>(s_o + (w * 16 + row) * LD + e0) * f;
       }
-      const int jj = rr / G, m = it.m0 + jj, h = kvh * G + rr - jj * G;
+      const int jj = by(rr), m = it.m0 + jj, h = kvh * G + rr - jj * G;
       if constexpr (PAGED) {
         *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + e0) = o;
         if (e0 == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(top, l);
