@@ -212,10 +212,10 @@ def prompt_attention(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: to
                      out: torch.Tensor, kv: Optional[DeviceKV] = None, layer: int = 0, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Causal attention over the packed rows of whole prompts; with `kv` the rows of k and v also enter the cache.
     q [M][H][hd], k and v [M][Hkv][hd]: views with any row stride (a QKV projection's rows)."""
-    for t in (q, k, v):
-        assert t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2]
-    assert out.is_contiguous() and out.dtype == q.dtype
-    B.mn_prompt_attention(model.ctx, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+    hd = model.desc.head_dim
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    assert qs[1:] == ks[1:] == vs[1:] == (hd, 1) and out.is_contiguous() and out.dtype == q.dtype
+    B.mn_prompt_attention(model.ctx, q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0],
                           seq_rows.data_ptr(), plan.h, plan.B, out.data_ptr(), kv.c if kv is not None else None, layer,
                           dev_status.data_ptr() if dev_status is not None else None, stream_ptr())
     return out
