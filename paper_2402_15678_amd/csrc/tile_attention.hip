@@ -71,6 +71,27 @@ __device__ __forceinline__ void find_tile(int t, int B, int max_tiles, F n, int 
   }
 }
 
+// The same for up to 64 sequences, lane b holding sequence b's number: 64 levels are counted at once, one per lane.
+__device__ __forceinline__ void find_tile_lanes(int t, int B, int max_tiles, int own, int& seq, int& tile) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, above = 0, step = 1;
+  while ((long)step * 64 < max_tiles) step <<= 6;
+  for (;;) {                                     // level lo: more than t tiles at or above it; lo + 64 step: t at most
+    const int level = lo + lane * step;
+    int c = 0;
+    for (int b = 0; b < B; ++b) c += max(0, __builtin_amdgcn_readlane(own, b) - level);
+    const int at = 63 - __clzll((unsigned long long)__ballot(c > t));
+    lo += at * step;
+    if (at < 63) above = __builtin_amdgcn_readlane(c, at + 1);
+    if (step == 1) break;
+    step >>= 6;
+  }
+  tile = lo;
+  const bool has = own > lo;
+  const uint64_t ballot = __ballot(has);
+  seq = __ffsll((unsigned long long)__ballot(has && __popcll(ballot & ((1ull << lane) - 1)) == t - above)) - 1;
+}
+
 // The prompt's item of this workgroup.  Lengths come from the device; those that do not fit the launch (which the host's sized)
 // leave the whole call undone.  s_n: room for a number per sequence.
 template <int ROWS>
@@ -100,7 +121,8 @@ __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, const Divi
     return false;
   }
   int seq, tile;
-  find_tile(t, a.B, a.max_tiles, n, total, seq, tile);
+  if (a.B <= 64) find_tile_lanes(t, a.B, a.max_tiles, own, seq, tile);
+  else find_tile(t, a.B, a.max_tiles, n, total, seq, tile);
   seq = __builtin_amdgcn_readfirstlane(seq);
   tile = __builtin_amdgcn_readfirstlane(tile);
   int row0, row1;
