@@ -443,7 +443,7 @@ mn_status mn_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, cons
  *   kv       NULL, or the cache that the prompts enter: the rows of k and v are also written into layer `layer`'s pages, token i
  *            of sequence b at position i of table row b (tokens whose block id is out of range are left out: MN_DEV_BLOCK_TABLE).
  *            ctx_lens is neither read nor written.
- * Elements of q, k and v must be finite (fp16: within +-65504); one that is not leaves its sequence's rows undefined, no other's.
+ * An infinity or NaN in q stays with its row and head; in k and v it reaches the rows that see it, and no other.
  * The scores, the statistics and the sums are fp32; fp16 probabilities are rounded to fp16 for the second product, in the sum of
  * the outputs and of the probabilities alike.  No workspace. */
 mn_status mn_prompt_attention(mn_ctx *ctx, const void *q, long q_stride, const void *k, long k_stride, const void *v,
@@ -455,6 +455,7 @@ mn_status mn_prompt_attention(mn_ctx *ctx, const void *q, long q_stride, const v
  * Arguments as there; prefix_len is a multiple of the block size, 0 included, and smaller than max_ctx.  The first
  * prefix_len / block_size entries of every table row are the same blocks and ctx_lens[b] >= prefix_len; a sequence for which
  * either does not hold (MN_DEV_BLOCK_TABLE, MN_DEV_CTX), or whose row holds an id out of range, gets zeros.
+ * An infinity or NaN in q, k or v goes as far as in mn_prompt_attention; slots of the cache that hold no token may hold anything.
  * workspace: mn_prefix_workspace_bytes(ctx, B, sum_b q_b or more, prefix_len, max_ctx or more) bytes, 256-byte aligned. */
 size_t mn_prefix_workspace_bytes(const mn_ctx *ctx, int B, int max_rows, int prefix_len, int max_ctx);
 mn_status mn_prefix_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, const int32_t *h_spec_len, int B,

@@ -463,9 +463,10 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // the half behind the next and the values of the next are on their way from the LDS: the matrix pipe and the vector unit both
     // have work, and neither waits for the LDS.
     f16x8 kf[2 * HS], vf[NU], P[CT];
-    const auto first = [&](int k0, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2]) {
+    const auto first = [&](int k0, const unsigned char* next_keys, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2]) {
       const int keyg = k0 + 8 * g;
-      if (k0 + 31 > min_lim) {                                     // (uniform) a key that some row does not see
+      const bool masked = k0 + 31 > min_lim;                       // (uniform) a key that some row does not see
+      if (masked) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
@@ -505,6 +506,48 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
 #pragma unroll
           for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
           L[ct] *= alpha;
+        }
+      }
+      if (masked) {
+        // Values that are not finite reach the rows that see their key and no other (nor is 0 times them 0): they leave the product, and
+        // the rows that see +inf, -inf or NaN (as both) get what the sum would be.
+        f16x2 odd = {(f16_t)0.f, (f16_t)0.f};
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd = __builtin_elementwise_fma((f16x2){vf[u][2 * e], vf[u][2 * e + 1]}, (f16x2){(f16_t)0.f, (f16_t)0.f}, odd);
+        if (__any(odd[0] != odd[0] || odd[1] != odd[1])) {
+#pragma unroll
+          for (int u = 0; u < NU; ++u) {
+            union { f16x8 v; uint32_t u[4]; } w, at;
+            w.v = vf[u];
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {                 // +inf, -inf; NaN is both
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t x = w.u[e], sign = (side ? x : ~x) >> 15, nan = ((x & 0x03ff03ffu) + 0x03ff03ffu) >> 10;
+                at.u[e] = (((x & 0x7fff7fffu) + 0x04000400u) >> 15 & (sign | nan) & 0x00010001u) * 0x3c00u;  // 1.0 there
+              }
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) {
+                int ahead = lim[ct] - keyg;
+                asm volatile("" : "+v"(ahead));                    // (worked out anew each time: registers)
+                f16x8 sees;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sees[e] = e <= ahead ? (f16_t)1.f : (f16_t)0.f;
+                const f32x4 met = __builtin_amdgcn_mfma_f32_16x16x32_f16(at.v, sees, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (met[e] > 0.f) O[ct][u][e] += side ? -INFINITY : INFINITY;
+                __builtin_amdgcn_sched_barrier(0);
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w.u[e] &= ~((((w.u[e] & 0x7fff7fffu) + 0x04000400u) >> 15 & 0x00010001u) * 0xffffu);
+            vf[u] = w.v;
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          load_k(next_keys, kf);                                   // (their registers were needed)
         }
       }
 #pragma unroll
@@ -553,7 +596,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // by all, and its place is filled again.
     const auto tile = [&](int i, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
       const bool on = i < n_wave;                                  // (uniform)
-      if (on) first(it.key0 + i * TK, S, tm, Sn);
+      if (on) first(it.key0 + i * TK, slot(i + 1), S, tm, Sn);
       wait_vm<(STAGES - 4) * LPW>();
       __syncthreads();
       stage(i + STAGES - 1);
@@ -595,7 +638,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // Rows that enter the cache: those whose first stack row lies in this workgroup's tile, out of the stages (they are the last keys it read:
     // every stage holds the last tile now, earlier ones are fetched again).  A lane's piece of K is 8 elements of one token, and of V
     // 8 tokens of one element: 16 bytes of a page each way.  7800 rows of 40 KV heads of 128, 161 us without: written as they come
-    // by the rows at the start 221 us, by a kernel of its own 253, like this 208, where 160 MB of pages are worth about 35.
+    // by the rows at the start 221 us, by a kernel of its own 253, like this 208 (now 157 and 192), where 160 MB of pages are worth about 35.
     if (!PAGED && a.kv.k) {
       const int put0 = (it.rbase + G - 1) / G, put1 = (min(it.R, it.rbase + ROWS) + G - 1) / G;
       __syncthreads();                                             // (everybody is through with the stages, and the last tile is there)
@@ -654,14 +697,16 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
 // operands are 4 consecutive elements of a row of K (four instructions take one each), and of V 4 elements of one key (dense rows: row i of
 // instruction r is element VEC i + r of the group) or 4 tokens of one element (pages), read from memory in that shape and widened;
 // 16 rows per workgroup, every fourth 32 keys (heads of 256: 16) to a wave, their parts put together in LDS at the end.  Bound by the round
-// trips of a wave through its keys, and by the L1 beyond: 4 prompts of 33 to 700 tokens of 4 fp32 heads of 64 12.5 us (32.6 with 64 rows
-// and keys staged for all waves; 27.0 with 64 rows and every wave reading all keys), 4 of 1500 to 2500 154 us = 78 TFLOP/s
-// (211, 237), 4 fp16 prompts of 300 to 1500 of 8/2 heads of 256 115 us (245, 260).  HDP: head_dim padded to a multiple of 16.
+// trips of a wave through its keys, and by the L1 beyond: 4 prompts of 33 to 700 tokens of 4 fp32 heads of 64 11 us (32.6 with 64 rows
+// and keys staged for all waves; 27.0 with 64 rows and every wave reading all keys), 4 of 1500 to 2500 127 us = 95 TFLOP/s
+// (211, 237), 4 fp16 prompts of 300 to 1500 of 8/2 heads of 256 107 us (245, 260).  HDP: head_dim padded to a multiple of 16.
+// Two waves per SIMD are asked for where 256 registers hold a wave (not the pages of heads of 128 and more): left alone the
+// compiler takes more, and the last two take 140 and 152 us.
 constexpr int FROWS = 16, KW = 4;                                // rows of a workgroup, its waves
 template <typename T> struct __attribute__((aligned(4 * sizeof(T)))) Four { T x[4]; };
 
 template <typename T, int HDP, bool PAGED>
-__global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
+__global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_kernel(TileArgs a) {
   constexpr int NU = HDP / 16, LD = HDP + 4, HALVES = HDP == 256 ? 1 : 2;  // (16 keys at a time: registers)
   constexpr int KEYS = 16 * HALVES;
   constexpr int VEC = PAGED ? 1 : (HDP >= 64 ? 4 : HDP / 16);    // consecutive elements of V that a lane takes from a dense row
@@ -694,7 +739,8 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
   do {
     const int r = min(it.rbase + l16, it.R - 1), j = by(r);
     const int lim = min(it.key_end - 1, it.ctx + j);
-    const int max_lim = min(it.key_end - 1, it.ctx + by(min(it.R, it.rbase + FROWS) - 1));  // of all rows
+    const int min_lim = min(it.key_end - 1, it.ctx + by(it.rbase));  // of the rows
+    const int max_lim = min(it.key_end - 1, it.ctx + by(min(it.R, it.rbase + FROWS) - 1));
     f32x4 q[NU], O[NU];
     const T* Q = static_cast<const T*>(a.q) + (size_t)(it.m0 + j) * a.q_stride + (size_t)(kvh * G + r - j * G) * hd;
 #pragma unroll
@@ -799,6 +845,35 @@ __global__ void __launch_bounds__(256) tile_f32_kernel(TileArgs a) {
         run_l *= alpha;
 #pragma unroll
         for (int u = 0; u < NU; ++u) O[u] *= alpha;
+      }
+      if (k0 + KEYS - 1 > min_lim) {                             // values that are not finite, as above
+        float odd = 0.f;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+          for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = fmaf((float)vx[h][u].x[e], 0.f, odd);
+        if (__any(odd != odd)) {
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float v = (float)vx[h][u].x[e], sees = k0 + 16 * h + 4 * g + e <= lim ? 1.f : 0.f;
+                const bool up = !(v < INFINITY), down = !(v > -INFINITY);
+                const f32x4 a = __builtin_amdgcn_mfma_f32_16x16x4f32(up ? 1.f : 0.f, sees, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                const f32x4 b = __builtin_amdgcn_mfma_f32_16x16x4f32(down ? 1.f : 0.f, sees, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  if (a[i] > 0.f) O[u][i] += INFINITY;
+                  if (b[i] > 0.f) O[u][i] -= INFINITY;
+                }
+                if (up || down) vx[h][u].x[e] = (T)0.f;
+                __builtin_amdgcn_sched_barrier(0);
+              }
+        }
       }
       const float ref = run_m == -INFINITY ? 0.f : run_m;
 #pragma unroll
@@ -984,9 +1059,11 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __r
       o *= keep;
 #pragma unroll
       for (int u = 0; u < AT_ONCE; ++u) {
-        const float w = s0 + u * GROUPS < n ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
+        const bool in = s0 + u * GROUPS < n;                     // (what is not finite counts once, and not at all times 0)
+        const float w = in ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
         l += ml[u].y * w;
-        o += v[u] * w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += in ? v[u][e] * w : 0.f;
       }
       top = nm;
     }
@@ -1010,7 +1087,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __r
       o += s_o[g][lane_at] * w;
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < 4; ++e) out[4 * i + e] = (T)(o[e] * inv);
 }

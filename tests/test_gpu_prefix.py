@@ -287,3 +287,31 @@ def test_a_prompt_branches_steps_and_retires(H, Hkv, hd, kind):
     assert ses.dev_status.item() == 0 and ses2.dev_status.item() == 0 and pool.dev_status.item() == 0
     for i, b in enumerate((1, 3)):
         assert torch.equal(again[i * own:(i + 1) * own], got[b * own:(b + 1) * own])
+
+
+def _same(got, want):
+    """Bit for bit, NaN where there is NaN."""
+    off = ~((got == want) | (got.isnan() & want.isnan()))
+    assert not off.any().item(), f"{int(off.sum())} elements, the first (row, head, element) {off.nonzero()[0].tolist()}: {got[off][0].item()}, not {want[off][0].item()}"
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (4, 4, 128, "f16"), (12, 12, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 128, "f32"), (8, 8, 8, "f32"),
+                                           (2, 2, 256, "f32"), (8, 2, 256, "f16")])
+@pytest.mark.parametrize("at", [0, 2, 20])
+def test_what_is_not_finite_reaches_the_rows_that_see_it(H, Hkv, hd, kind, at):
+    """Infinities and NaN in the values of one scored token of one sequence: the rows before it, other elements, other KV heads and other
+    sequences keep their bits."""
+    x = Batch(H, Hkv, hd, kind, 64, [37, 5, 0], [2, 24, 4], 18)
+    plain, status = x.run()
+    assert status == 0
+    odd = {1: float("inf"), 3: float("-inf"), 6: float("nan"), hd - 1: float("inf")}
+    pos = x.ctx[1] + at
+    for e, y in odd.items():
+        x.vp[int(x.table[1, pos // x.bs]), Hkv - 1, e, pos % x.bs] = y
+    out, status = x.run()
+    assert status == 0
+    want = plain.clone().view(-1, H, hd)
+    r = x.rows(1)
+    for e, y in odd.items():
+        want[r.start + at:r.stop, (Hkv - 1) * (H // Hkv):, e] = y
+    _same(out.view_as(want), want)

@@ -219,3 +219,47 @@ def test_same_numbers_on_another_stream_and_from_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(out, want)
         harness.prompt_attention(model, q, k, v, rows, plan, want)
+
+
+def _same(got, want):
+    """Bit for bit, NaN where there is NaN."""
+    off = ~((got == want) | (got.isnan() & want.isnan()))
+    assert not off.any().item(), f"{int(off.sum())} elements, the first (row, head, element) {off.nonzero()[0].tolist()}: {got[off][0].item()}, not {want[off][0].item()}"
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (4, 4, 128, "f16"), (12, 12, 64, "f16"), (6, 2, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 128, "f32"),
+                                           (8, 8, 8, "f32"), (2, 2, 256, "f32"), (8, 2, 256, "f16"), (8, 8, 32, "f16")])
+@pytest.mark.parametrize("at", [0, 5, 40, 299])
+def test_what_is_not_finite_reaches_the_rows_that_see_it(H, Hkv, hd, kind, at):
+    """Infinities and NaN in a token's values: rows before it, other elements and other KV heads keep their bits, the rows from it on
+    get what the sum is.  In its key: the rows from it on are not numbers.  In a query: its own row and head."""
+    d, model = _model(H, Hkv, hd, kind)
+    q, k, v, row0 = _rows(H, Hkv, hd, kind, [300, 7], 17)
+    plain = torch.full((len(q), H * hd), -7.0, dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, plain) == 0
+    plain = plain.view(-1, H, hd)
+    G, h = H // Hkv, Hkv - 1
+    odd = {1: float("inf"), 3: float("-inf"), 6: float("nan"), hd - 1: float("inf")}
+    v2 = v.clone()
+    for e, x in odd.items():
+        v2[at, h, e] = x
+    out = torch.empty_like(plain).view(-1, H * hd)
+    assert _call(model, q, k, v2, row0, out) == 0
+    want = plain.clone()
+    for e, x in odd.items():
+        want[at:300, h * G:, e] = x
+    _same(out.view_as(want), want)
+
+    k2 = k.clone()
+    k2[at, h, 2] = float("nan")
+    assert _call(model, q, k2, v, row0, out) == 0
+    want = plain.clone()
+    want[at:300, h * G:] = float("nan")
+    _same(out.view_as(want), want)
+
+    q2 = q.clone()
+    q2[at, H - 1, 0] = float("nan")
+    assert _call(model, q2, k, v, row0, out) == 0
+    want = plain.clone()
+    want[at, H - 1] = float("nan")
+    _same(out.view_as(want), want)
