@@ -117,7 +117,8 @@ typedef struct {
  *                                                                  block's tokens together)
  * k_layers / v_layers are HOST arrays of n_layers device pointers, read at each call.
  * Rows at positions >= ctx_lens[b] are undefined; mn_verify_forward writes the k_b + 1 scored
- * tokens' rows there tentatively, only mn_accept_and_commit advances ctx_lens. */
+ * tokens' rows there tentatively, and of the steps only mn_accept_and_commit advances ctx_lens (the page pool's mn_kv_fork and
+ * mn_kv_free set those of the slots that they fill and empty). */
 typedef struct {
   void *const *k_layers;
   void *const *v_layers;
@@ -125,7 +126,7 @@ typedef struct {
   int num_blocks;              /* physical blocks per layer */
   int max_blocks_per_seq;      /* row length of block_tables */
   const int32_t *block_tables; /* dev [B][max_blocks_per_seq] */
-  int32_t *ctx_lens;           /* dev [B]; written only by mn_accept_and_commit */
+  int32_t *ctx_lens;           /* dev [B] */
 } mn_kv;
 
 /* ---- lifetime --------------------------------------------------------------------------- */
@@ -454,7 +455,8 @@ mn_status mn_prompt_attention(mn_ctx *ctx, const void *q, long q_stride, const v
  * leaves them so): what mn_attention computes, with the shared keys read once for all sequences instead of once for each.
  * Arguments as there; prefix_len is a multiple of the block size, 0 included, and smaller than max_ctx.  The first
  * prefix_len / block_size entries of every table row are the same blocks and ctx_lens[b] >= prefix_len; a sequence for which
- * either does not hold (MN_DEV_BLOCK_TABLE, MN_DEV_CTX), or whose row holds an id out of range, gets zeros.
+ * either does not hold (MN_DEV_BLOCK_TABLE, MN_DEV_CTX), or whose row holds an id out of range, gets zeros, an emptied slot among
+ * them.  The blocks are those of the first sequence with ctx_lens[b] >= prefix_len.
  * An infinity or NaN in q, k or v goes as far as in mn_prompt_attention; slots of the cache that hold no token may hold anything.
  * workspace: mn_prefix_workspace_bytes(ctx, B, sum_b q_b or more, prefix_len, max_ctx or more) bytes, 256-byte aligned. */
 size_t mn_prefix_workspace_bytes(const mn_ctx *ctx, int B, int max_rows, int prefix_len, int max_ctx);

@@ -201,13 +201,14 @@ struct TileArgs {
   const int32_t* items;     // work list of the own keys, 8 int32 per record, or null (at most 64 sequences)
   float *o_part, *ml_part;  // [slot][M][H][hd] and [slot][M][H][2]: outputs, (reference, sum)
   int prefix_units, n_units, share, n_streams, prefix_slots, row_tiles;  // the shared part (stream_item)
-  int32_t* seq_bad;         // [B] whether a table row is damaged
+  int32_t* seq_bad;         // [B] whether a table row is damaged; behind them the first sharer, if there is a work list
 };
 struct PrefixPlan {
   PrefixBatch batch;
   int prefix_slots, max_items;
   int32_t* items;
   int2* row_meta;           // [M] (sequence, its ranges of own keys: 0 where it takes no part)
+  int32_t* first;           // the first sequence whose context holds the prefix
   int32_t* status;
 };
 struct PrefixMerge {

@@ -214,11 +214,26 @@ __device__ __forceinline__ bool stream_item(const TileArgs& a, int stream, int& 
   return true;
 }
 
-// A sequence's table row, looked at by one workgroup of its items: every block id in range, and the prefix's entries those of the first
-// row (what the call reads for all of them).  Rows of a sequence that fails are zeros (prefix_merge_kernel).
+typedef __attribute__((address_space(4))) int32_t const_i32;  // (scalar loads)
+__device__ __forceinline__ const const_i32* scalar(const int32_t* p) { return reinterpret_cast<const const_i32*>(reinterpret_cast<uintptr_t>(p)); }
+
+// The sequence whose table row names the shared blocks: the first one whose context holds the prefix (slots emptied by then do not).
+__device__ __forceinline__ int first_sharer(const TileArgs& a) {
+  if (a.items) return scalar(a.seq_bad)[a.B];
+  if (scalar(a.batch.ctx_lens)[0] >= a.batch.prefix_len) return 0;
+  const int b = threadIdx.x & 63;
+  bool has = false;
+  if (b < a.B) has = a.batch.ctx_lens[b] >= a.batch.prefix_len;
+  const uint64_t all = __ballot(has);
+  return all ? __ffsll((unsigned long long)all) - 1 : 0;
+}
+
+// A sequence's table row, looked at by one workgroup of its items: every block id in range, and the prefix's entries those that the call
+// reads for all of them.  Rows of a sequence that fails are zeros (prefix_merge_kernel).
 __device__ __forceinline__ void check_table(const TileArgs& a, const Item& it, int kvh) {
   if (it.slot != a.prefix_slots || it.rbase != 0 || kvh != 0) return;
-  const int32_t *first = a.kv.block_tables, *row = first + (size_t)it.seq * a.kv.max_blocks_per_seq;
+  const int32_t *first = a.kv.block_tables + (size_t)first_sharer(a) * a.kv.max_blocks_per_seq;
+  const int32_t* row = a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq;
   const int shared = a.batch.prefix_len / a.kv.block_size, all = (int)(((long)it.ctx + it.R / (a.H / a.Hkv) + a.kv.block_size - 1) / a.kv.block_size);
   bool bad = false;
   for (int i = threadIdx.x; i < all; i += blockDim.x) bad |= (uint32_t)row[i] >= (uint32_t)a.kv.num_blocks || (i < shared && row[i] != first[i]);
@@ -275,7 +290,6 @@ template <int HDIM> struct TileStage {
 constexpr int STAGES = 4;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(4))) int32_t const_i32;  // (scalar loads)
 template <int N> struct PieceC { static constexpr int value = N; };
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void pieces(F f) {
@@ -365,7 +379,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     const int side = wave & 1;
     const uint32_t to0 = lds0 + (uint32_t)((k_wave ? 0 : KP) + side * LPW) * 1024u;
     // pages
-    const const_i32* bt = PAGED ? reinterpret_cast<const const_i32*>(reinterpret_cast<uintptr_t>(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq)) : nullptr;
+    const const_i32* bt = PAGED ? scalar(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq) : nullptr;
     const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u;
     int next_id = 0;
     const auto ask_id = [&](int tile) { next_id = bt[min((it.key0 + min(tile, n_tiles - 1) * TK) / PAGE + side, last_key / PAGE)]; };
@@ -384,6 +398,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       base = static_cast<const char*>(k_wave ? a.kv.k : a.kv.v) + (size_t)kvh * (HDIM * PAGE * 2);
       off0 = 16u * (uint32_t)(k_wave ? lane ^ (side * 4) : lane ^ (lane >> 4 & 1));
       ask_id(0);
+      if (more) {                                                  // (row 0 is mostly the one; its first id is on the way meanwhile)
+        const int seq = first_sharer(a);
+        if (seq > 0) {
+          bt = scalar(a.kv.block_tables + (size_t)seq * a.kv.max_blocks_per_seq);
+          ask_id(0);
+        }
+      }
     } else {
       base = static_cast<const char*>(k_wave ? a.k : a.v) + ((size_t)(it.m0 + it.key0) * stride + (size_t)kvh * HDIM * 2);
       off0 = (uint32_t)key_lane * stride + 16u * (uint32_t)((lane % CH) ^ turn(key_lane));
@@ -754,7 +775,7 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
       }
     }
     float run_m = -INFINITY, run_l = 0.f;
-    const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq : nullptr;
+    const int32_t* bt = PAGED ? a.kv.block_tables + (size_t)(more ? first_sharer(a) : it.seq) * a.kv.max_blocks_per_seq : nullptr;
     const bool quads = PAGED && (bs & 3) == 0;                   // four tokens from a multiple of four lie in one block
     const int shift = (bs & (bs - 1)) == 0 ? 31 - __clz(bs) : -1;
     const auto block_of = [&](int key) { return shift >= 0 ? key >> shift : key / bs; };
@@ -940,13 +961,13 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
 // keys, from a work list.  Each piece leaves an unnormalised output with its reference and sum per row in a slot of its own,
 // and a row's slots are put together at the end.
 //
-// prefix_plan_kernel (one workgroup; more than 64 sequences): the rows' sequences, who takes part, and the list of items.  Up to 64 every
+// prefix_plan_kernel (one workgroup; more than 64 sequences): the rows' sequences, who takes part, the first sharer, and the list of items.  Up to 64 every
 // workgroup finds its item by itself (own_item), and the merge its rows' sequences, which saves a launch: 5 us of 33 to 43.
 __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
-  __shared__ int s_rows[16], s_items[16], s_bad;
+  __shared__ int s_rows[16], s_items[16], s_bad, s_first;
   const PrefixBatch& c = p.batch;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (tid == 0) s_bad = 0;
+  if (tid == 0) { s_bad = 0; s_first = c.B; }
   __syncthreads();
   int flags = 0;
   const auto length = [&](int b) {
@@ -958,6 +979,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   bool off = false;
   for (int b = tid; b < c.B; b += 1024) {
     const int q = length(b);
+    if (c.ctx_lens[b] >= c.prefix_len) atomicMin(&s_first, b);
     off |= q < 0;
     rows += max(q, 0);
   }
@@ -967,6 +989,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   __syncthreads();
   int total = 0;
   for (int w = 0; w < 16; ++w) total += s_rows[w];
+  if (tid == 0) *p.first = s_first < c.B ? s_first : 0;
   const bool batch = s_bad == 0 && total == c.M;
   if (!batch) flags |= MN_DEV_SPEC_LEN;
   int4* items = reinterpret_cast<int4*>(p.items);
@@ -1202,7 +1225,7 @@ static PrefixLayout prefix_layout(int B, int M, int H, int Hkv, int hd, int pref
   L.max_items = (size_t)(((G * M + 15) / 16 + B) * ranges);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 4095) & ~(size_t)4095; return o; };
-  L.meta = take((size_t)M * 8); L.bad = take((size_t)B * 4); L.items = take(L.max_items * 32);
+  L.meta = take((size_t)M * 8); L.bad = take((size_t)(B + 1) * 4); L.items = take(L.max_items * 32);
   L.ml_part = take(L.slot_rows * H * 2 * 4);
   L.o_part = take(L.slot_rows * H * hd * 4);
   L.total = at;
@@ -1240,7 +1263,7 @@ hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st) {
     meta = reinterpret_cast<int2*>(w + L.meta);
     int32_t* items = reinterpret_cast<int32_t*>(w + L.items);
     a.items = items;
-    prefix_plan_kernel<<<1, 1024, 0, st>>>(PrefixPlan{a.batch, s.slots, a.n_tiles, items, meta, a.status});
+    prefix_plan_kernel<<<1, 1024, 0, st>>>(PrefixPlan{a.batch, s.slots, a.n_tiles, items, meta, a.seq_bad + a.B, a.status});
   }
   hipError_t e;
   if (!tile_mfma(a, true)) e = a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, true>(a, st) : launch_f32_hd<float, true>(a, st);

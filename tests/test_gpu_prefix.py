@@ -315,3 +315,69 @@ def test_what_is_not_finite_reaches_the_rows_that_see_it(H, Hkv, hd, kind, at):
     for e, y in odd.items():
         want[r.start + at:r.stop, (Hkv - 1) * (H // Hkv):, e] = y
     _same(out.view_as(want), want)
+
+
+@pytest.mark.parametrize("kind,hd,bs", [("f16", 128, 16), ("f16", 64, 16), ("f32", 32, 8)])
+@pytest.mark.parametrize("count", [5, 64, 65, 1030])
+def test_emptied_slots_in_a_batch(kind, hd, bs, count):
+    """Slots without tokens and blocks get zeros, the first ones among them, and nobody else notices."""
+    from paper_2402_15678_amd import binding
+    g = np.random.default_rng(count)
+    x = Batch(4, 2, hd, kind, 4 * bs, g.integers(0, 50, count).tolist(), g.integers(0, 4, count).tolist(), count, bs=bs)
+    whole, status = x.run()
+    assert status == 0
+    gone = [0, 1, count - 1]
+    for b in gone:
+        x.table[b] = -1
+        x.ctx[b] = 0
+    out, status = x.run(kv=x.kv())
+    assert status == binding.MN_DEV_CTX
+    rest = torch.ones(len(out), dtype=torch.bool, device="cuda")
+    for b in gone:
+        assert (out[x.rows(b)] == 0).all()
+        rest[x.rows(b)] = False
+    assert torch.equal(out[rest], whole[rest])
+    # nobody left
+    x.table[:] = -1
+    x.ctx = [0] * count
+    out, status = x.run(kv=x.kv())
+    assert status == binding.MN_DEV_CTX and (out == 0).all()
+
+
+@pytest.mark.parametrize("count", [6, 70])
+def test_two_batches_on_two_streams_at_once(count):
+    """Workspaces of their own: neither call sees the other, eager or replayed, step after step."""
+    from paper_2402_15678_amd import harness
+    xs = [Batch(16, 4, 128, "f16", 512, [30 + i] * count, [2] * count, 20 + i) for i in range(2)]
+    want = [x.run()[0] for x in xs]
+    sets = []
+    for x in xs:
+        kv = x.kv()
+        ses = harness.PrefixSession(x.model, kv, count, len(x.q), x.P, x.max_ctx)
+        spec = torch.tensor(x.ks, dtype=torch.int32, device="cuda")
+        out = torch.full((len(x.q), x.H * x.hd), -7.0, dtype=torch.float16, device="cuda")
+        sets.append((ses, spec, out, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, (ses, spec, out, st) in zip(xs, sets):
+            with torch.cuda.stream(st):
+                ses.attention(x.q, spec, x.ks, out)
+    torch.cuda.synchronize()
+    for w, (ses, spec, out, st) in zip(want, sets):
+        assert torch.equal(out, w) and ses.dev_status.item() == 0
+    graphs = []
+    for x, (ses, spec, out, st) in zip(xs, sets):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr, stream=st):
+            ses.attention(x.q, spec, x.ks, out)
+        graphs.append(gr)
+    for _ in range(5):
+        for s in sets:
+            s[2].zero_()
+        torch.cuda.synchronize()
+        for gr, (ses, spec, out, st) in zip(graphs, sets):
+            with torch.cuda.stream(st):
+                gr.replay()
+        torch.cuda.synchronize()
+        for w, s in zip(want, sets):
+            assert torch.equal(s[2], w)
