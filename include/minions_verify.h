@@ -358,8 +358,7 @@ mn_status mn_kv_reserve(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, const int32
 
 /* Slot dst[i] becomes a copy of slot src[i]: the blocks of its ctx_lens tokens, shared, and its context.  No page moves; the
  * child's own tokens get their pages from mn_kv_reserve.  Pairs are judged by the state at entry; one whose slots are out of
- * range or the same, whose dst is in use or is filled by an earlier pair, or whose src is filled by this call, is left out
- * (MN_DEV_SEQ).
+ * range or the same, whose dst is in use or an earlier pair's dst, or whose src is a dst of this call, is left out (MN_DEV_SEQ).
  *   src, dst dev [n] */
 mn_status mn_kv_fork(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, const int32_t *src, const int32_t *dst, int n,
                      int32_t *dev_status, void *stream);
