@@ -1126,10 +1126,12 @@ static bool tile_mfma(const TileArgs& a, bool paged) {
 int prompt_tile_rows(const TileArgs& a, long stack_rows) {
   if (!tile_mfma(a, a.kv.k != nullptr)) return FROWS;
   if (const int f = MN_TUNE("MN_TILE", 0)) return f;
-  // 128 rows where that fills the chip (two workgroups per CU), 64 otherwise.  Measured, 128 against 64 rows: 8192 tokens of 64/8 heads of
-  // 128 1086 and 1446 us, 8 prompts of 60 to 1500 tokens of 40 heads 162 and 203; 300 tokens of 12 heads of 64 10.1 and 8.5, 8 such
-  // prompts of 300 to 1200 (562 workgroups) 22.8 and 21.9.
-  return stack_rows * a.Hkv >= 512 * 128 ? 128 : 64;
+  // 128 rows where that fills the chip, 64 otherwise: two workgroups of 128 rows fit a CU, and three with heads of 64, where it pays
+  // from five sixths on.  Measured, 128 against 64 rows, heads of 128: 8192 tokens of 64/8 heads 1050 and 1390 us, 8 prompts of
+  // 60 to 1500 tokens of 40 heads 155 and 197, 1024 tokens of 64/8 heads (512 workgroups) 33 and 35, of 40 heads (320) 31 and
+  // 25.  12 heads of 64: 32 prompts of 1000 95 and 116, 8 of 1000 (750) 28 and 31, 8 of 300 to 1200 (562) 22 and 20, 300
+  // tokens 9.3 and 8.0.
+  return stack_rows * a.Hkv >= (a.hd == 64 ? 640 : 512) * 128 ? 128 : 64;
 }
 
 template <typename K>
@@ -1183,21 +1185,34 @@ hipError_t launch_prompt(const TileArgs& a, hipStream_t st) {
 
 
 // Shape of a shared-prefix launch, from what the host knows.
-constexpr int STREAMS = 512;          // two workgroups per CU
+constexpr int STREAMS = 512;          // two workgroups per CU (64 rows of heads of 64: four)
 constexpr int MIN_SHARE = 4;          // units of a stream at least: a workgroup's lead-in is worth about as much
 constexpr int MAX_SLOTS = 33;         // of a tile of rows
 constexpr int MAX_RANGES = 16;        // of a sequence's own keys
 struct PrefixShape {
   int tile_rows, row_tiles, units, n_units, share, n_streams, slots, chunk, ranges;
 };
+static int prefix_tile_rows(const TileArgs& a, int M, int units) {
+  if (!tile_mfma(a, true)) return FROWS;
+  if (const int f = MN_TUNE("MN_TILE", 0)) return f;
+  // 128 rows where a sequence's run fills most of them, and with heads of 128 where more than 64 rows meet enough of the prefix for
+  // seven units per stream; 64 otherwise.  Measured, 128 against 64 rows.  Runs of 17 x 8 rows behind 512 + 1000 keys, 8 sequences
+  // 36 and 39 us; of 131 x 8, 2 sequences 52 and 64, 32 sequences without a prefix 335 and 432; of 201 rows of 12 heads of 64, 8
+  // sequences 41 and 45; of 9 x 8 behind 2048 + 300, 16 sequences 44 and 41.  One row each, 64 x 8 rows behind 16384 keys
+  // 60 and 66; 16 sequences of 5 x 8 rows behind 4096 39 and 35; heads of 64, 128 sequences of 5 rows behind 8192 61 and 54.
+  const long G = a.H / a.Hkv;
+  if (G * a.batch.max_q >= 96) return 128;
+  return a.hd == 128 && M * G > 64 && (M * G + 127) / 128 * a.Hkv * units >= 7 * STREAMS ? 128 : 64;
+}
 static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
   PrefixShape s{};
   const long G = a.H / a.Hkv;
-  s.tile_rows = !tile_mfma(a, true) ? FROWS : MN_TUNE("MN_TILE", 0) ? MN_TUNE("MN_TILE", 0) : (M * G > 64 ? 128 : 64);
-  s.row_tiles = (int)((M * G + s.tile_rows - 1) / s.tile_rows);
   s.units = (a.batch.prefix_len + TKEYS - 1) / TKEYS;
+  s.tile_rows = prefix_tile_rows(a, M, s.units);
+  s.row_tiles = (int)((M * G + s.tile_rows - 1) / s.tile_rows);
   s.n_units = s.row_tiles * a.Hkv * s.units;
-  s.share = (s.n_units + STREAMS - 1) / STREAMS;
+  const int streams = s.tile_rows == 64 && a.hd == 64 ? 2 * STREAMS : STREAMS;
+  s.share = (s.n_units + streams - 1) / streams;
   const int by_slots = (s.units + MAX_SLOTS - 3) / (MAX_SLOTS - 2);
   const int least = s.units < 1 ? 1 : (s.units < MIN_SHARE ? s.units : MIN_SHARE);  // (a stream of several short tiles would only be longer)
   if (s.share < least) s.share = least;
@@ -1219,7 +1234,7 @@ struct PrefixLayout {
 static PrefixLayout prefix_layout(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx) {
   PrefixLayout L;
   const long G = H / Hkv, ranges = max_ctx - prefix_len > 256 ? MAX_RANGES : 1;
-  // slots of a tile: units / share + 2 with share >= row tiles * KV heads * units / STREAMS, and MAX_SLOTS; row tiles >= M G / 128
+  // slots of a tile: units / share + 2 with share >= row tiles * KV heads * units / streams, and MAX_SLOTS; row tiles >= M G / tile rows, streams * tile rows <= STREAMS * 128
   const long slots_a = (long)MAX_SLOTS * M, slots_b = (long)STREAMS * 128 / H + 3l * M;
   L.slot_rows = (size_t)((slots_a < slots_b ? slots_a : slots_b) + ranges * M);
   L.max_items = (size_t)(((G * M + 15) / 16 + B) * ranges);
