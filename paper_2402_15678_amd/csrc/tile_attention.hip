@@ -277,9 +277,14 @@ __device__ __forceinline__ void append_rows(const TileArgs& a, const Item& it, i
 // A workgroup of NW waves holds 16 * CT * NW stack rows, wave w the rows from 16 * CT * w on, their queries in registers.  Both products
 // have the query row as the column index (S^T = K Q^T, O^T = V^T P^T): statistics are per-lane numbers, and with the K rows of a
 // half of 32 keys permuted (S^T row 4g + r of half t is key 8g + 4t + r) the probabilities leave the first product in the operand
-// order of the second.  A tile of 64 keys is staged by direct global -> LDS loads: K in operand order (the lane asks for the 16
-// bytes that belong at its place); V of pages likewise (a page keeps the block's tokens of one head-dim element together), V of dense
-// rows row by row, turned on the way to the registers by the transposing LDS read.
+// order of the second.  Tiles of 32 keys are staged ahead by direct global -> LDS loads of whole rows, or of whole pages, their 16-byte
+// pieces in turned places so that the reads of the operands meet every bank; V of dense rows is turned on the way to the registers by
+// the transposing LDS read (a page keeps the block's tokens of one head-dim element together already).
+//
+// Bounds.  Long rows of keys: the matrix pipe.  8192 tokens of 64/8 heads of 128 take 1050 us = 1050 TFLOP/s (a library product of 8192^3
+// reaches 1133); without the staging 14 % less, without the exponentials 14 %, without the barriers 3 %.  Two workgroups of 128 rows per
+// CU, 251 registers a wave: a tile of 256 rows does not fit them, 64 rows read the stages twice as often (1390 us).  A shared prefix
+// behind few rows: HBM; 32000 keys of 8 heads of 128 in 34 us = 3.9 TB/s, lead-in included.
 constexpr int TK = 32;                              // keys per stage
 template <int HDIM> struct TileStage {
   static constexpr int HS = HDIM / 32, NU = HDIM / 16;
@@ -962,7 +967,7 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
 // and a row's slots are put together at the end.
 //
 // prefix_plan_kernel (one workgroup; more than 64 sequences): the rows' sequences, who takes part, the first sharer, and the list of items.  Up to 64 every
-// workgroup finds its item by itself (own_item), and the merge its rows' sequences, which saves a launch: 5 us of 33 to 43.
+// workgroup finds its item by itself (own_item), and the merge its rows' sequences, which saves a launch, 5 us.
 __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
   __shared__ int s_rows[16], s_items[16], s_bad, s_first;
   const PrefixBatch& c = p.batch;
@@ -1031,7 +1036,8 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
 }
 
 // Four elements of a row of one head per thread; several slots are asked for at once.  GROUPS threads share them where there are few rows
-// and many slots (6 rows of 64 heads, 33 slots: 10 us with one).
+// and many slots (6 rows of 64 heads, 33 slots: 4.6 us, with one 10).  Bound by
+// HBM where there are many rows: 576 rows of 64 heads of 128, 52 MB of parts, 17 us.
 constexpr int AT_ONCE = 4;
 template <typename T, int GROUPS>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
