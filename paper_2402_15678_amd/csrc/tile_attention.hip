@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
         else pieces<LPW>([&](auto i) { dma16s<i.value * 1024, true>(p, off0, to + i.value * 1024u); });
         ask_id(tile + 1);
       } else {
-        const int k0 = it.key0 + min(tile, n_tiles - 1) * TK;      // (stages past the end repeat the last one)
+        const int k0 = it.key0 + min(tile, n_tiles - 1) * TK;      // (of the first stages, those past the end repeat the last one)
         if (k0 + TK - 1 <= last_key) {
           pieces<LPW>([&](auto i) { dma16s<0, false>(base + i.value * KPP * (uint64_t)stride, (i.value * KPP & 8) ? off1 : off0, to + i.value * 1024u); });
         } else {                                                   // rows past the end repeat the last one
@@ -607,8 +607,10 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     const int n_wave = min(n_tiles, max(0, max_lim + TK - it.key0) / TK);  // tiles that a row of the wave sees
     __syncthreads();                                               // (the search, or the piece before, is through with the LDS)
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) stage(i);
-    wait_vm<(STAGES - 3) * LPW>();
+    for (int i = 0; i < STAGES - 1; ++i)
+      if (!PAGED || i < n_tiles) stage(i);                         // (dense rows: short ones are rare, and the test cost as much)
+    if (!PAGED || n_tiles >= STAGES - 1) wait_vm<(STAGES - 3) * LPW>();  // (tiles 0 and 1 are there)
+    else wait_vm<0>();
     __syncthreads();
     f32x4 Sa[CT][2], Sb[CT][2];
     float ta[CT], tb[CT];
@@ -625,14 +627,14 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       if (on) first(it.key0 + i * TK, slot(i + 1), S, tm, Sn);
       wait_vm<(STAGES - 4) * LPW>();
       __syncthreads();
-      stage(i + STAGES - 1);
+      if (i + STAGES - 1 < n_tiles) stage(i + STAGES - 1);
       if (on) second(slot(i + 2), slot(i + 1), Sn, tn);
     };
     for (int i = 0; i < n_tiles; i += 2) {                         // (behind an odd last tile comes one that no wave works on)
       tile(i, Sa, ta, Sb, tb);
       tile(i + 1, Sb, tb, Sa, ta);
     }
-    wait_vm<0>();                                                  // (stages past the end land before the LDS is given back)
+    wait_vm<0>();                                                  // (of a dense item's first stages, any past its end)
 
     // ---- output: lane holds O^T[16u + 4g + i][row l16], and its row's sum ----
 #pragma unroll
@@ -662,7 +664,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       }
     }
     // Rows that enter the cache: those whose first stack row lies in this workgroup's tile, out of the stages (they are the last keys it read:
-    // every stage holds the last tile now, earlier ones are fetched again).  A lane's piece of K is 8 elements of one token, and of V
+    // the last tile is still there, with others they are fetched again).  A lane's piece of K is 8 elements of one token, and of V
     // 8 tokens of one element: 16 bytes of a page each way.  7800 rows of 40 KV heads of 128, 161 us without: written as they come
     // by the rows at the start 221 us, by a kernel of its own 253, like this 208 (now 157 and 192), where 160 MB of pages are worth about 35.
     if (!PAGED && a.kv.k) {
@@ -1037,7 +1039,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
 
 // Four elements of a row of one head per thread; several slots are asked for at once.  GROUPS threads share them where there are few rows
 // and many slots (6 rows of 64 heads, 33 slots: 4.6 us, with one 10).  Bound by
-// HBM where there are many rows: 576 rows of 64 heads of 128, 52 MB of parts, 17 us.
+// HBM where there are many rows: 576 rows of 64 heads of 128, 71 MB of parts, 17 us.
 constexpr int AT_ONCE = 4;
 template <typename T, int GROUPS>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
