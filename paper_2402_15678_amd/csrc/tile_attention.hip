@@ -284,7 +284,7 @@ __device__ __forceinline__ void append_rows(const TileArgs& a, const Item& it, i
 // Bounds.  Long rows of keys: the matrix pipe.  8192 tokens of 64/8 heads of 128 take 1050 us = 1050 TFLOP/s (a library product of 8192^3
 // reaches 1133); without the staging 14 % less, without the exponentials 14 %, without the barriers 3 %.  Two workgroups of 128 rows per
 // CU, 251 registers a wave: a tile of 256 rows does not fit them, 64 rows read the stages twice as often (1390 us).  A shared prefix
-// behind few rows: HBM; 32000 keys of 8 heads of 128 in 34 us = 3.9 TB/s, lead-in included.
+// behind few rows: HBM; 32000 keys of 8 heads of 128 in 28 us = 4.7 TB/s, lead-in included.
 constexpr int TK = 32;                              // keys per stage
 template <int HDIM> struct TileStage {
   static constexpr int HS = HDIM / 32, NU = HDIM / 16;
@@ -324,6 +324,10 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
   using St = TileStage<HDIM>;
   constexpr int HS = St::HS, NU = St::NU, KP = St::KP, LPW = St::FRAGS / NW, ROWS = 16 * CT * NW;
   static_assert(St::FRAGS % NW == 0, "whole pieces per wave");
+  // Tiles asked for ahead of the one at hand.  Four keep two on their way between the hand-overs, where HBM is the bound (64 rows behind
+  // pages: 3 x 1 to 3 rows of 64/8 heads behind 32000 tokens 36.9 -> 31.4 us, 16 x 1 of 40 heads 29.3 -> 27.0); with the matrix
+  // pipe as the bound three are enough and 1 % faster.
+  constexpr int AHEAD = PAGED && CT == 1 ? STAGES : STAGES - 1;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const Divide by(a.H / a.Hkv);                                  // (query heads per KV head)
   const int G = by.d;
@@ -607,9 +611,9 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     const int n_wave = min(n_tiles, max(0, max_lim + TK - it.key0) / TK);  // tiles that a row of the wave sees
     __syncthreads();                                               // (the search, or the piece before, is through with the LDS)
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i)
+    for (int i = 0; i < AHEAD; ++i)
       if (!PAGED || i < n_tiles) stage(i);                         // (dense rows: short ones are rare, and the test cost as much)
-    if (!PAGED || n_tiles >= STAGES - 1) wait_vm<(STAGES - 3) * LPW>();  // (tiles 0 and 1 are there)
+    if (!PAGED || n_tiles >= AHEAD) wait_vm<(AHEAD - 2) * LPW>();  // (tiles 0 and 1 are there)
     else wait_vm<0>();
     __syncthreads();
     f32x4 Sa[CT][2], Sb[CT][2];
@@ -620,14 +624,15 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     load_v(slot(0), vf);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) ta[ct] = top(Sa[ct]);
-    // Tile i: its first part, then the hand-over: this wave's share of tile i + 2 has landed, then everybody's; tile i - 1 has been read
-    // by all, and its place is filled again.
+    // Tile i: its first part, then the hand-over: this wave's share of tile i + 2 has landed, then everybody's; tile i has been read by all
+    // (its values are in the registers), and its place, or that of tile i - 1, is filled again.
     const auto tile = [&](int i, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
       const bool on = i < n_wave;                                  // (uniform)
       if (on) first(it.key0 + i * TK, slot(i + 1), S, tm, Sn);
-      wait_vm<(STAGES - 4) * LPW>();
+      if (AHEAD > 3 && i + 3 < n_tiles) wait_vm<(AHEAD - 3) * LPW>();
+      else wait_vm<0>();
       __syncthreads();
-      if (i + STAGES - 1 < n_tiles) stage(i + STAGES - 1);
+      if (i + AHEAD < n_tiles) stage(i + AHEAD);
       if (on) second(slot(i + 2), slot(i + 1), Sn, tn);
     };
     for (int i = 0; i < n_tiles; i += 2) {                         // (behind an odd last tile comes one that no wave works on)
