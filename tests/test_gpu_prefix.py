@@ -381,3 +381,35 @@ def test_two_batches_on_two_streams_at_once(count):
         torch.cuda.synchronize()
         for w, s in zip(want, sets):
             assert torch.equal(s[2], w)
+
+
+def test_damaged_sequences_in_a_large_batch():
+    """More than 64 sequences (a work list): who fails gets zeros, the others their results; lengths that do not add up, everybody."""
+    from paper_2402_15678_amd import binding
+    count = 90
+    g = np.random.default_rng(3)
+    x = Batch(8, 2, 128, "f16", 64, g.integers(0, 90, count).tolist(), g.integers(0, 5, count).tolist(), 31, spare=1)
+    good, ctx = x.table.copy(), list(x.ctx)
+    whole, status = x.run()
+    assert status == 0
+    damages = [(lambda: x.table.__setitem__((66, 1), (x.table[66, 1] + 1) % x.kp.shape[0]), [66], binding.MN_DEV_BLOCK_TABLE),
+               (lambda: x.table.__setitem__((89, x.ctx[89] // 16), 1 << 30), [89], binding.MN_DEV_BLOCK_TABLE),
+               (lambda: (x.ctx.__setitem__(3, 63), x.ctx.__setitem__(70, 0)), [3, 70], binding.MN_DEV_CTX),
+               (lambda: x.ctx.__setitem__(80, 1 << 30), [80], binding.MN_DEV_CTX),
+               (lambda: x.ctx.__setitem__(0, -5), [0], binding.MN_DEV_CTX)]
+    for damage, gone, flag in damages:
+        damage()
+        out, status = x.run(kv=x.kv(), max_ctx=max(ctx) + 6)
+        x.table, x.ctx = good.copy(), list(ctx)
+        assert status == flag
+        rest = torch.ones(len(out), dtype=torch.bool, device="cuda")
+        for b in gone:
+            assert (out[x.rows(b)] == 0).all()
+            rest[x.rows(b)] = False
+        x.check(out, [b for b in (1, 2, 65, 67, 88) if b not in gone])
+        assert torch.equal(out[rest], x.run(max_ctx=max(ctx) + 6)[0][rest])
+    for at, by in ((5, 1), (89, -9), (70, 40)):
+        spec = list(x.ks)
+        spec[at] += by
+        out, status = x.run(spec=spec)
+        assert status == binding.MN_DEV_SPEC_LEN and (out == 0).all()

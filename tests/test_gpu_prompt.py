@@ -263,3 +263,19 @@ def test_what_is_not_finite_reaches_the_rows_that_see_it(H, Hkv, hd, kind, at):
     want = plain.clone()
     want[at, H - 1] = float("nan")
     _same(out.view_as(want), want)
+
+
+@pytest.mark.parametrize("kind,hd,M,row", [("f16", 64, 140000, 16384), ("f16", 128, 80000, 32768), ("f32", 64, 40000, 32768)])
+def test_rows_beyond_four_gigabytes(kind, hd, M, row):
+    """Offsets of rows pass 32 bits: a short sequence, and a long one behind it, checked at rows all over it."""
+    d, model = _model(2, 1, hd, kind)
+    q, k, v, row0 = _rows(2, 1, hd, kind, [5, M - 5], 8, pad=row - 4 * hd)
+    assert q.stride(0) == row and (M - 1) * row * q.element_size() > 1 << 32
+    out = torch.full((M, 2 * hd), -7.0, dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    kk, vv = k[5:].contiguous(), v[5:].contiguous()
+    for a in (0, 1, 31, 32, 127, 128, 1000, M // 2, M - 5 - 33, M - 6):
+        rows = torch.arange(a, min(a + 2, M - 5), device="cuda")
+        n = int(rows[-1]) + 1
+        want, bound = attend(q[5:][rows], kk[:n], vv[:n], rows, kind == "f16")
+        check(out[5:][rows], want, bound)
