@@ -730,7 +730,8 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
 // operands are 4 consecutive elements of a row of K (four instructions take one each), and of V 4 elements of one key (dense rows: row i of
 // instruction r is element VEC i + r of the group) or 4 tokens of one element (pages), read from memory in that shape and widened;
 // 16 rows per workgroup, every fourth 32 keys (heads of 256: 16) to a wave, their parts put together in LDS at the end.  Bound by the round
-// trips of a wave through its keys, and by the L1 beyond: 4 prompts of 33 to 700 tokens of 4 fp32 heads of 64 11 us (32.6 with 64 rows
+// trips of a wave through its keys, and beyond by the issue of its instructions (7000 tokens of 4 heads of 64 247 us = 102 TFLOP/s, a
+// library product of 8192^3 152; 32 rows per workgroup read half as much and take 283): 4 prompts of 33 to 700 tokens of 4 fp32 heads of 64 11 us (32.6 with 64 rows
 // and keys staged for all waves; 27.0 with 64 rows and every wave reading all keys), 4 of 1500 to 2500 127 us = 95 TFLOP/s
 // (211, 237), 4 fp16 prompts of 300 to 1500 of 8/2 heads of 256 107 us (245, 260).  HDP: head_dim padded to a multiple of 16.
 // Two waves per SIMD are asked for where 256 registers hold a wave (not the pages of heads of 128 and more): left alone the
