@@ -786,7 +786,7 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   const int rows = prompt_tile_rows(t, (long)(M - h_seq_rows[0]) * G);
   long tiles = 0;
   for (int b = 0; b < B; ++b) tiles += ((long)(h_seq_rows[b + 1] - h_seq_rows[b]) * G + rows - 1) / rows;
-  if (tiles * d.n_kv_heads >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
+  if (tiles * d.n_kv_heads > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
   if (tiles == 0) return MN_OK;
   t.n_tiles = (int)tiles;
   t.tile_rows = rows;
@@ -830,16 +830,17 @@ extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t
   if ((long)M * (d.n_heads / d.n_kv_heads) >= (1l << 29)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d heads", who, M, d.n_heads);
   if (!prefix_fits(M, d.n_heads, d.n_kv_heads, prefix_len)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows behind %d tokens", who, M, prefix_len);
   if (max_ctx >= (1 << 28)) return fail(c, MN_EUNSUPPORTED, "%s: max_ctx = %d", who, max_ctx);
-  if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
-  if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
-  const size_t need = prefix_workspace_bytes(B, M, d.n_heads, d.n_kv_heads, d.head_dim, prefix_len, max_ctx);
-  if (workspace_bytes < need) return fail(c, MN_EWORKSPACE, "%s: workspace %zu bytes, need %zu", who, workspace_bytes, need);
   TileArgs t{};
   t.kv = KvView{kv->k_layers[layer], kv->v_layers[layer], kv->block_tables, kv->block_size, kv->num_blocks, kv->max_blocks_per_seq};
   t.q = q; t.q_stride = (long)d.n_heads * d.head_dim; t.out = out;
   t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.B = B;
   t.status = dev_status;
   t.batch.spec_len = spec_len; t.batch.ctx_lens = kv->ctx_lens; t.batch.max_q = max_q; t.batch.max_ctx = max_ctx; t.batch.prefix_len = prefix_len;
+  if (const long wgs = prefix_workgroups(t); wgs > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %d rows take %ld workgroups", who, M, wgs);
+  if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
+  if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
+  const size_t need = prefix_workspace_bytes(B, M, d.n_heads, d.n_kv_heads, d.head_dim, prefix_len, max_ctx);
+  if (workspace_bytes < need) return fail(c, MN_EWORKSPACE, "%s: workspace %zu bytes, need %zu", who, workspace_bytes, need);
   hipError_t lerr;
   {
     Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);

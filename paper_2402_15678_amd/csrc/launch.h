@@ -218,11 +218,13 @@ struct PrefixMerge {
   PrefixBatch batch;
   int M, H, Hkv, hd, prefix_slots, prefix_units, n_units, share, row_tiles;
 };
+long prefix_workgroups(const TileArgs& a);
 bool prefix_fits(int M, int H, int Hkv, int prefix_len);
 size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx);
 hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st);
 int prompt_tile_rows(const TileArgs& a, long stack_rows);
 hipError_t launch_prompt(const TileArgs& a, hipStream_t st);
+constexpr long MAX_WORKGROUPS = (1l << 24) - 1;  // of 256 threads: a grid has fewer than 2^32
 
 // ---- pool.hip ----
 struct PoolView {

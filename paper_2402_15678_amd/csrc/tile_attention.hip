@@ -1240,6 +1240,12 @@ static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
   s.chunk = ((rest + s.ranges - 1) / s.ranges + TKEYS - 1) / TKEYS * TKEYS;
   return s;
 }
+// Workgroups of a call's largest launch.
+long prefix_workgroups(const TileArgs& a) {
+  const PrefixShape s = prefix_shape(a, a.M, a.batch.max_ctx);
+  const long tiles = ((long)a.M * (a.H / a.Hkv) / s.tile_rows + a.B) * s.ranges * a.Hkv + s.n_streams, merge = ((long)a.M * a.H * (a.hd / 4) + 255) / 256;
+  return tiles > merge ? tiles : merge;
+}
 struct PrefixLayout {
   size_t meta, bad, items, o_part, ml_part, total;
   size_t max_items, slot_rows;

@@ -1,6 +1,7 @@
 """No GPU needed: what the prompt attention refuses before anything is launched."""
 import pytest
 
+from tests.test_abi import _desc, _weights
 from tests.test_pool_refusals import P, _kv, _status, binding, ctx  # noqa: F401  (fixtures)
 
 
@@ -37,3 +38,25 @@ def test_the_cache_is_checked(binding, ctx):  # noqa: F811
     assert _status(binding, lambda: _call(binding, ctx, kv=_kv(binding), layer=1)) == binding.MN_EINVAL
     assert _status(binding, lambda: _call(binding, ctx, rows=(0, 3, 3, 68), kv=_kv(binding))) == binding.MN_ECAPACITY   # 65 tokens in 4 blocks
     assert _status(binding, lambda: _call(binding, ctx, rows=(0, 0, 0, 129), kv=_kv(binding, width=99))) == binding.MN_ECAPACITY   # max_pos
+
+
+@pytest.fixture(scope="module")
+def wide(binding):  # noqa: F811
+    """512 heads of 8."""
+    d = _desc(binding, d_model=4096, n_heads=512, n_kv_heads=512, head_dim=8, max_pos=1 << 21)
+    w, keep = _weights(binding)
+    c = binding.mn_create(d, w)
+    yield c
+    binding.mn_destroy(c)
+
+
+def test_more_workgroups_than_a_launch_holds(binding, wide):  # noqa: F811
+    kw = dict(qs=4096, ks=4096, vs=4096, B=1)
+    assert _status(binding, lambda: _call(binding, wide, rows=(0, 1 << 20), **kw)) == binding.MN_EUNSUPPORTED
+    assert _status(binding, lambda: _call(binding, wide, rows=(0, (1 << 19) + 1), **kw)) == binding.MN_EUNSUPPORTED
+
+
+def test_more_workgroups_than_a_launch_holds_behind_a_prefix(binding, wide):  # noqa: F811
+    ks, kv = binding.host_i32([255] * 4096), _kv(binding, width=1 << 16, nb=1 << 16)
+    for prefix in (0, 16):
+        assert _status(binding, lambda: binding.mn_prefix_attention(wide, P, P, ks, 4096, prefix, 100000, kv, 0, P, 0x2000, 1 << 60)) == binding.MN_EUNSUPPORTED
