@@ -180,7 +180,7 @@ __device__ __forceinline__ bool own_item(const TileArgs& a, int t, Item& it) {
   }
   const Share s = lane_share(a.batch);
   const int incl = wave_scan_i(s.ranges * s.tiles), first = incl - s.ranges * s.tiles;
-  if (t == 0 && threadIdx.x < 64 && blockIdx.x == 0 && s.flags && a.status) atomicOr(a.status, s.flags);
+  if (t == 0 && threadIdx.x < 64 && (int)blockIdx.x == a.B && s.flags && a.status) atomicOr(a.status, s.flags);
   const uint64_t mine = __ballot(t >= first && t < incl);
   if (mine == 0) return false;
   const int b = __ffsll((unsigned long long)mine) - 1;
@@ -228,18 +228,20 @@ __device__ __forceinline__ int first_sharer(const TileArgs& a) {
   return all ? __ffsll((unsigned long long)all) - 1 : 0;
 }
 
-// A sequence's table row, looked at by one workgroup of its items: every block id in range, and the prefix's entries those that the call
-// reads for all of them.  Rows of a sequence that fails are zeros (prefix_merge_kernel).
-__device__ __forceinline__ void check_table(const TileArgs& a, const Item& it, int kvh) {
-  if (it.slot != a.prefix_slots || it.rbase != 0 || kvh != 0) return;
-  const int32_t *first = a.kv.block_tables + (size_t)first_sharer(a) * a.kv.max_blocks_per_seq;
-  const int32_t* row = a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq;
-  const int shared = a.batch.prefix_len / a.kv.block_size, all = (int)(((long)it.ctx + it.R / (a.H / a.Hkv) + a.kv.block_size - 1) / a.kv.block_size);
+// Sequence b's table row, looked at by a workgroup of its own (ahead of an item's keys it was 1 to 2 us of that item): every block id in
+// range, and the prefix's entries those that the call reads for all of them.  Rows of a sequence that fails are zeros
+// (prefix_merge_kernel).
+__device__ __forceinline__ void check_table(const TileArgs& a, int b) {
+  const int ctx = scalar(a.batch.ctx_lens)[b], k = scalar(a.batch.spec_len)[b];
+  if (ctx < a.batch.prefix_len || k < 0 || (long)ctx + k + 1 > a.batch.max_ctx) return;  // (takes no part)
+  const int32_t* first = a.kv.block_tables + (size_t)first_sharer(a) * a.kv.max_blocks_per_seq;
+  const int32_t* row = a.kv.block_tables + (size_t)b * a.kv.max_blocks_per_seq;
+  const int shared = a.batch.prefix_len / a.kv.block_size, all = (ctx + k) / a.kv.block_size + 1;
   bool bad = false;
   for (int i = threadIdx.x; i < all; i += blockDim.x) bad |= (uint32_t)row[i] >= (uint32_t)a.kv.num_blocks || (i < shared && row[i] != first[i]);
   bad = __syncthreads_or(bad);
   if (threadIdx.x == 0) {
-    a.seq_bad[it.seq] = bad;
+    a.seq_bad[b] = bad;
     if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
   }
 }
@@ -331,21 +333,24 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const Divide by(a.H / a.Hkv);                                  // (query heads per KV head)
   const int G = by.d;
-  int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
+  int kvh = 0, stream = 0, unit = 0;
   Item it;
   bool more = false;
   if constexpr (PAGED) {
-    const int own = a.n_tiles * a.Hkv;                           // workgroups of the sequences' own keys; the streams come behind
-    if ((int)blockIdx.x < own) {
-      if (!own_item(a, blockIdx.x / a.Hkv, it)) return;
-      check_table(a, it, kvh);
+    // a workgroup per table row, those of the sequences' own keys, the streams
+    const int own = a.n_tiles * a.Hkv, wg = (int)blockIdx.x - a.B;
+    if (wg < 0) return check_table(a, blockIdx.x);
+    if (wg < own) {
+      kvh = wg % a.Hkv;
+      if (!own_item(a, wg / a.Hkv, it)) return;
     } else {
-      stream = stream_of(a, blockIdx.x - own);
+      stream = stream_of(a, wg - own);
       unit = stream * a.share;
       if (!stream_item(a, stream, unit, kvh, it)) return;
       more = true;
     }
   } else {
+    kvh = blockIdx.x % a.Hkv;
     if (!prompt_item<ROWS>(a, blockIdx.x / a.Hkv, by, reinterpret_cast<int32_t*>(smem), it)) return;
   }
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -747,21 +752,24 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const Divide by(a.H / a.Hkv);                                  // (query heads per KV head)
   const int G = by.d;
-  int kvh = blockIdx.x % a.Hkv, stream = 0, unit = 0;
+  int kvh = 0, stream = 0, unit = 0;
   Item it;
   bool more = false;
   if constexpr (PAGED) {
-    const int own = a.n_tiles * a.Hkv;                           // workgroups of the sequences' own keys; the streams come behind
-    if ((int)blockIdx.x < own) {
-      if (!own_item(a, blockIdx.x / a.Hkv, it)) return;
-      check_table(a, it, kvh);
+    // a workgroup per table row, those of the sequences' own keys, the streams
+    const int own = a.n_tiles * a.Hkv, wg = (int)blockIdx.x - a.B;
+    if (wg < 0) return check_table(a, blockIdx.x);
+    if (wg < own) {
+      kvh = wg % a.Hkv;
+      if (!own_item(a, wg / a.Hkv, it)) return;
     } else {
-      stream = stream_of(a, blockIdx.x - own);
+      stream = stream_of(a, wg - own);
       unit = stream * a.share;
       if (!stream_item(a, stream, unit, kvh, it)) return;
       more = true;
     }
   } else {
+    kvh = blockIdx.x % a.Hkv;
     if (!prompt_item<FROWS>(a, blockIdx.x / a.Hkv, by, reinterpret_cast<int32_t*>(smem), it)) return;
     if (a.kv.k) append_rows<T, FROWS>(a, it, G, kvh);
   }
@@ -1160,7 +1168,7 @@ static hipError_t launch_mfma_as(const TileArgs& a, hipStream_t st) {
   static hipError_t err = hipSuccess;
   std::call_once(once, [] { err = allow_lds(tile_mfma_kernel<HDIM, CT, 4, PAGED>, lds); });
   if (err != hipSuccess) return err;
-  tile_mfma_kernel<HDIM, CT, 4, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (unsigned)a.n_streams, 256, lds, st>>>(a);
+  tile_mfma_kernel<HDIM, CT, 4, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (PAGED ? (unsigned)(a.n_streams + a.B) : 0u), 256, lds, st>>>(a);
   return hipSuccess;
 }
 template <bool PAGED>
@@ -1177,7 +1185,7 @@ static hipError_t launch_f32(const TileArgs& a, hipStream_t st) {
   std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED>, parts); });
   if (err != hipSuccess) return err;
   const size_t list = PAGED || a.B <= 64 ? 0 : (size_t)a.B * 4;  // (the search's numbers)
-  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (unsigned)a.n_streams, 64 * KW, parts > list ? parts : list, st>>>(a);
+  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (PAGED ? (unsigned)(a.n_streams + a.B) : 0u), 64 * KW, parts > list ? parts : list, st>>>(a);
   return hipSuccess;
 }
 
@@ -1243,7 +1251,7 @@ static PrefixShape prefix_shape(const TileArgs& a, int M, int max_ctx) {
 // Workgroups of a call's largest launch.
 long prefix_workgroups(const TileArgs& a) {
   const PrefixShape s = prefix_shape(a, a.M, a.batch.max_ctx);
-  const long tiles = ((long)a.M * (a.H / a.Hkv) / s.tile_rows + a.B) * s.ranges * a.Hkv + s.n_streams, merge = ((long)a.M * a.H * (a.hd / 4) + 255) / 256;
+  const long tiles = ((long)a.M * (a.H / a.Hkv) / s.tile_rows + a.B) * s.ranges * a.Hkv + s.n_streams + a.B, merge = ((long)a.M * a.H * (a.hd / 4) + 255) / 256;
   return tiles > merge ? tiles : merge;
 }
 struct PrefixLayout {
