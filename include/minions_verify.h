@@ -438,7 +438,8 @@ mn_status mn_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, cons
  *            (strides in elements, so that the three may lie side by side in the rows of one QKV projection; addresses and row
  *            strides are multiples of 16 bytes, strides below 2^24)
  *   seq_rows dev [B+1], ascending from 0 or more; h_seq_rows HOST [B+1], the same values: they size the launch.  Sequences without
- *            rows are fine.  Values on the device that do not fit the launch leave the call undone (MN_DEV_SPEC_LEN).
+ *            rows are fine.  Values on the device that do not fit the launch, a sequence longer than the host's longest among them,
+ *            leave the call undone (MN_DEV_SPEC_LEN).
  *   out      dev [h_seq_rows[B]][n_heads * head_dim], same type as q; only rows that belong to a sequence are written
  *   kv       NULL, or the cache that the prompts enter: the rows of k and v are also written into layer `layer`'s pages, token i
  *            of sequence b at position i of table row b (tokens whose block id is out of range are left out: MN_DEV_BLOCK_TABLE).

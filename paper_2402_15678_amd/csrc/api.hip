@@ -791,6 +791,7 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   t.n_tiles = (int)tiles;
   t.tile_rows = rows;
   t.max_tiles = (int)(((long)longest * G + rows - 1) / rows);
+  t.longest = longest;
   hipError_t lerr;
   {
     Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);

@@ -191,7 +191,7 @@ struct TileArgs {
   void* out;              // [M][H * hd]
   int M, H, Hkv, hd, dtype, B;
   int n_tiles;            // workgroups per KV head (shared prefix: for the sequences' own keys)
-  int max_tiles;          // most tiles of a sequence
+  int max_tiles, longest; // most tiles and most rows of a sequence (dense keys)
   int tile_rows;
   const int32_t* seq_rows;  // [B + 1] (dense keys)
   KvView kv;                // pages to read, or (dense keys, k non-null) to write the rows to

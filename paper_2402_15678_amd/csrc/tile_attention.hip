@@ -93,7 +93,8 @@ __device__ __forceinline__ void find_tile_lanes(int t, int B, int max_tiles, int
 }
 
 // The prompt's item of this workgroup.  Lengths come from the device; those that do not fit the launch (which the host's sized)
-// leave the whole call undone.  s_n: room for a number per sequence.
+// leave the whole call undone: rows outside the packed ones, another number of tiles, or a sequence longer than the host's longest,
+// for which neither the search nor the block table's rows have room.  s_n: room for a number per sequence.
 template <int ROWS>
 __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, const Divide& by, int32_t* s_n, Item& it) {
   const int lane = threadIdx.x & 63, G = by.d;
@@ -101,9 +102,8 @@ __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, const Divi
   auto tiles = [&](int b) {                      // -1: does not fit
     r0 = a.seq_rows[b];
     r1 = a.seq_rows[b + 1];
-    if (r0 < 0 || r1 < r0 || r1 > a.M) return -1;
-    const int n = (int)(((long)(r1 - r0) * G + ROWS - 1) / ROWS);
-    return n > a.max_tiles ? -1 : n;
+    if (r0 < 0 || r1 < r0 || r1 > a.M || r1 - r0 > a.longest) return -1;
+    return (int)(((long)(r1 - r0) * G + ROWS - 1) / ROWS);
   };
   int own = 0;
   if (a.B <= 64) {

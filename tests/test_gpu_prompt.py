@@ -196,6 +196,30 @@ def test_lengths_that_do_not_fit_the_launch_leave_the_call_undone(kind, hd):
         assert (out == -7.0).all()
 
 
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f16", 64), ("f32", 32), ("f16", 32)])
+@pytest.mark.parametrize("fill", [0, 70])
+def test_a_sequence_longer_than_the_hosts_longest_leaves_the_call_undone(kind, hd, fill):
+    """Rows that move between sequences within one number of tiles: the table's rows have no entry for the tokens beyond the host's
+    longest sequence, so neither outputs nor pages may change.  (fill: more than 64 sequences, whose numbers are kept elsewhere.)"""
+    from paper_2402_15678_amd import binding, harness
+    bs, tile = (16, 64) if kind == "f16" and hd >= 64 else (4, 16)
+    host = np.array([0, tile // 4, tile // 2] + [tile // 2] * fill, np.int32)
+    moved = host.copy()
+    moved[1] = tile // 2 - 1
+    d, model = _model(4, 4, hd, kind)
+    q, k, v, row0 = _rows(4, 4, hd, kind, np.diff(host).tolist(), 13)
+    n, width = len(host) - 1, -(-(tile // 4) // bs)
+    table = np.arange(n * width, dtype=np.int32).reshape(n, width)
+    kp = torch.full((n * width, 4, hd // 8, bs, 8), -3.0, dtype=DT[kind], device="cuda")
+    vp = torch.full((n * width, 4, hd, bs), -3.0, dtype=DT[kind], device="cuda")
+    for cache in (None, harness.DeviceKV(d, bs, n * width, table, [0] * n, [kp], [vp])):
+        out = torch.full((len(q), 4 * hd), -7.0, dtype=DT[kind], device="cuda")
+        assert _call(model, q, k, v, moved, out, cache, h_row0=host) == binding.MN_DEV_SPEC_LEN
+        assert (out == -7.0).all() and (kp == -3.0).all() and (vp == -3.0).all()
+    assert _call(model, q, k, v, host, out, cache) == 0
+    _compare(q, k, v, row0, out, kind)
+
+
 def test_same_numbers_on_another_stream_and_from_a_graph():
     from paper_2402_15678_amd import harness
     d, model = _model(64, 8, 128, "f16")
