@@ -445,6 +445,7 @@ mn_status mn_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, cons
  *            of sequence b at position i of table row b (tokens whose block id is out of range are left out: MN_DEV_BLOCK_TABLE).
  *            ctx_lens is neither read nor written.
  * An infinity or NaN in q stays with its row and head; in k and v it reaches the rows that see it, and no other.
+ * Scores of any size will do that fp32 holds, those of finite fp16 rows among them.
  * The scores, the statistics and the sums are fp32; fp16 probabilities are rounded to fp16 for the second product, in the sum of
  * the outputs and of the probabilities alike.  No workspace. */
 mn_status mn_prompt_attention(mn_ctx *ctx, const void *q, long q_stride, const void *k, long k_stride, const void *v,

@@ -22,6 +22,10 @@ constexpr int TKEYS = 64;              // ranges of keys begin at multiples of i
 constexpr int PAGE = 16;               // tokens per block that it reads
 constexpr int NO_LIMIT = 1 << 29;      // an item whose rows all see every key of its range
 constexpr float LAZY = 6.f;            // the reference moves when a score exceeds it by 2^6
+// From here on the rounding of c s - m alone would be an exponent of the size that the references are there to keep away (half a unit
+// at 2^24, 32 at 2^29, where a probability leaves the fp16 range).  Such a row's scores are taken less its reference ahead of the
+// exponentials, from the rounded product, so that the largest one is 0, and its reference follows its scores tile by tile.
+constexpr float FAR = 0x1p24f;
 
 // One tile of work: stack rows [rbase, R) (as many as a workgroup holds) of the tokens from m0 on against the keys [key0, key_end).
 // Row r sees the keys up to ctx + r / G.
@@ -535,9 +539,17 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
           t2 = __builtin_fmaxf(__uint_as_float(x), __uint_as_float(y)) * c;
           const float nm = __builtin_fmaxf(run_m[ct], t2);
           const float alpha = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run_m[ct] - nm);
+          const bool far = __builtin_fabsf(nm) >= FAR;
           run_m[ct] = nm;
-          thr[ct] = nm == -INFINITY ? -INFINITY : (nm + LAZY) * inv_c;
-          neg_m[ct] = nm == -INFINITY ? 0.f : -nm;
+          thr[ct] = far ? -INFINITY : (nm + LAZY) * inv_c;
+          neg_m[ct] = far ? 0.f : -nm;
+          if (__any(far && nm != -INFINITY)) {
+            if (far && nm != -INFINITY) {
+#pragma clang fp contract(off)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) S[ct][e >> 2][e & 3] = (S[ct][e >> 2][e & 3] * c - nm) * inv_c;
+            }
+          }
 #pragma unroll
           for (int u = 0; u < NU; ++u) O[ct][u] *= alpha;
           L[ct] *= alpha;

@@ -1,6 +1,7 @@
 """Attention in 64 bits with a bound on what the kernels' roundings may do to every element.  No arithmetic of the library here."""
 import math
 
+import numpy as np
 import torch
 
 
@@ -50,3 +51,35 @@ def check(got, want, bound):
     worst = int(over.argmax())
     assert over.max() <= 0, "row %d column %d: %g instead of %g, off by more than %g" % (
         worst // got.shape[1], worst % got.shape[1], got.flatten()[worst], want.flatten()[worst], bound.flatten()[worst])
+
+
+def ties(q, k, v, limit):
+    """Scores so far apart that a row's weight is all on the keys that attain its largest, in equal shares (or, with a query of zeros, on
+    all).  Equal keys give equal scores whatever the roundings, every other probability is 0: what is left are the sums and the
+    quotient, and the rounding of the result."""
+    rows, H, hd = q.shape
+    G = H // k.shape[1]
+    q, k, v = q.double(), k.double(), v.double()
+    out, bound = [], []
+    for h in range(H):
+        s = (q[:, h] @ k[:, h // G].t().contiguous()) / math.sqrt(hd)
+        s = s.masked_fill(torch.arange(len(k), device=q.device)[None, :] > limit[:, None], -math.inf)
+        top = s.amax(dim=1, keepdim=True)
+        assert ((s == top) | (top - s > 64)).all()
+        p = (s == top).double()
+        p /= p.sum(dim=1, keepdim=True)
+        out.append(p @ v[:, h // G])
+        bound.append((len(k) + 64) * 2.0 ** -23 * (p @ v[:, h // G].abs()))
+    return torch.stack(out, 1).reshape(rows, -1), torch.stack(bound, 1).reshape(rows, -1)
+
+
+def levels(n, shape, seed):
+    g = np.random.default_rng(seed)
+    x = g.integers(1, 9, n)
+    return torch.tensor(np.sort(x) if shape == "rising" else np.sort(x)[::-1].copy() if shape == "falling" else x, device="cuda")
+
+
+def factors(n, kind, seed):
+    """One factor per row: the largest that the type's scores stand, ordinary ones, none, and negative ones."""
+    far = 65504.0 if kind == "f16" else 2.0 ** 53
+    return torch.tensor(np.random.default_rng(seed).choice([far, -far, far / 16, 8.0, -2.0, 0.0], n), device="cuda")

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2402_15678_amd import synth
-from tests.attention_bounds import attend, check
+from tests.attention_bounds import attend, check, factors, levels, ties
 
 pytestmark = pytest.mark.gpu
 DT = {"f16": torch.float16, "f32": torch.float32}
@@ -413,3 +413,20 @@ def test_damaged_sequences_in_a_large_batch():
         spec[at] += by
         out, status = x.run(spec=spec)
         assert status == binding.MN_DEV_SPEC_LEN and (out == 0).all()
+
+
+@pytest.mark.parametrize("kind,hd,P", [("f16", 128, 1024), ("f16", 64, 512), ("f32", 64, 256), ("f16", 256, 128)])
+@pytest.mark.parametrize("far", [True, False], ids=["far", "mixed"])
+def test_prefix_scores_at_the_end_of_the_range(kind, hd, P, far):
+    x = Batch(4, 2, hd, kind, P, [100, 0, 600], [3, 2, 8], 21)
+    nb = len(x.kp)
+    level = levels(nb * x.bs, "any", 5).view(nb, 1, 1, x.bs, 1)
+    x.kp[:] = torch.where(x.kp.isnan(), x.kp, (level * (8188.0 if kind == "f16" else 2.0 ** 50)).to(x.kp.dtype).expand_as(x.kp))
+    f = torch.full((len(x.q),), 65504.0 if kind == "f16" else 2.0 ** 53, device="cuda") if far else factors(len(x.q), kind, 6)
+    x.q[:] = f.view(-1, 1, 1).to(x.q.dtype)
+    out, status = x.run()
+    assert status == 0
+    for b in range(3):
+        r, (k, v) = x.rows(b), x.dense(b)
+        want, bound = ties(x.q[r], k, v, torch.arange(x.ctx[b], x.ctx[b] + x.ks[b] + 1, device="cuda"))
+        check(out[r], want, bound + (2.0 ** -11 if kind == "f16" else 2.0 ** -24) * want.abs() + (2.0 ** -25 if kind == "f16" else 0))

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2402_15678_amd import synth
-from tests.attention_bounds import attend, check
+from tests.attention_bounds import attend, check, factors, levels, ties
 
 pytestmark = pytest.mark.gpu
 DT = {"f16": torch.float16, "f32": torch.float32}
@@ -303,3 +303,20 @@ def test_rows_beyond_four_gigabytes(kind, hd, M, row):
         n = int(rows[-1]) + 1
         want, bound = attend(q[5:][rows], kk[:n], vv[:n], rows, kind == "f16")
         check(out[5:][rows], want, bound)
+
+
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f16", 64), ("f32", 64), ("f16", 256)])
+@pytest.mark.parametrize("shape", ["rising", "falling", "any"])
+@pytest.mark.parametrize("far", [True, False], ids=["far", "mixed"])
+def test_prompt_scores_at_the_end_of_the_range(kind, hd, shape, far):
+    n = 300
+    d, model = _model(4, 2, hd, kind)
+    q, k, v, row0 = _rows(4, 2, hd, kind, [n], 19)
+    f = torch.full((n,), 65504.0 if kind == "f16" else 2.0 ** 53, device="cuda") if far else factors(n, kind, 3)
+    q, k = q.clone(), k.clone()
+    q[:] = f.view(-1, 1, 1).to(q.dtype)
+    k[:] = (levels(n, shape, 4) * (8188.0 if kind == "f16" else 2.0 ** 50)).view(-1, 1, 1).to(k.dtype)
+    out = torch.zeros((n, 4 * hd), dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    want, bound = ties(q, k, v, torch.arange(n, device="cuda"))
+    check(out, want, bound + (2.0 ** -11 if kind == "f16" else 2.0 ** -24) * want.abs() + (2.0 ** -25 if kind == "f16" else 0))
