@@ -336,6 +336,7 @@ long mn_selector_adjustments(const mn_selector *sel); /* decisions taken so far;
  * Decisions follow from this state alone (lowest free block first, in the order of slot and position), so equal calls give equal
  * tables.  Whatever a call cannot do it leaves as it was and reports in *dev_status (or NULL): a damaged row (an id out of
  * range, a context longer than its blocks) is MN_DEV_BLOCK_TABLE.
+ * Pages move in all layers of the context; one without layers has those of layer 0, as in the attention calls.
  * n <= max_seqs <= MN_MAX_BATCH and B <= max_seqs; n = 0 and B = 0 are no-ops. */
 typedef struct {
   int32_t *block_tables, *block_refs, *seq_blocks;

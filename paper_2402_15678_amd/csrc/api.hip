@@ -852,6 +852,9 @@ extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t
 }
 
 // ---- page pool ----------------------------------------------------------------------------------------
+// Layers whose pages move: a context without layers has those of layer 0, which its attention calls read.
+static int page_layers(const mn_ctx* c) { return c->d.n_layers > 0 ? c->d.n_layers : 1; }
+
 static mn_status check_pool(mn_ctx* c, const mn_kv* kv, const mn_pool* pool, int n, int32_t* status, bool pages, const char* who, PoolView* out) {
   if (!kv || !pool) return fail(c, MN_ENULL, "%s: kv or pool is NULL", who);
   if (!kv->block_tables || !kv->ctx_lens || !pool->block_tables || !pool->block_refs || !pool->seq_blocks)
@@ -863,7 +866,7 @@ static mn_status check_pool(mn_ctx* c, const mn_kv* kv, const mn_pool* pool, int
   if (n < 0 || n > pool->max_seqs) return fail(c, MN_EINVAL, "%s: %d sequences of %d slots", who, n, pool->max_seqs);
   if (pages) {
     if (!kv->k_layers || !kv->v_layers) return fail(c, MN_ENULL, "%s: k_layers or v_layers is NULL", who);
-    for (int l = 0; l < c->d.n_layers; ++l)
+    for (int l = 0; l < page_layers(c); ++l)
       if (!kv->k_layers[l] || !kv->v_layers[l]) return fail(c, MN_ENULL, "%s: kv layer %d pointer is NULL", who, l);
     if (((uint64_t)kv->block_size * c->d.n_kv_heads * c->d.head_dim * 4) >> 34) return fail(c, MN_EUNSUPPORTED, "%s: blocks of %d tokens", who, kv->block_size);
   }
@@ -900,7 +903,7 @@ extern "C" mn_status mn_kv_reserve(mn_ctx* c, mn_kv* kv, const mn_pool* pool, co
   if (!tokens) return fail(c, MN_ENULL, "%s: tokens is NULL", who);
   {
     Tap t(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
-    launch_reserve(p, tokens, B, kv->k_layers, kv->v_layers, c->d.n_layers, page_bytes(c, kv), workspace, (hipStream_t)stream);
+    launch_reserve(p, tokens, B, kv->k_layers, kv->v_layers, page_layers(c), page_bytes(c, kv), workspace, (hipStream_t)stream);
   }
   return hip_check(c, who);
 }
@@ -941,7 +944,7 @@ extern "C" mn_status mn_kv_compact(mn_ctx* c, mn_kv* kv, const mn_pool* pool, in
   if (mn_status s = check_pool_workspace(c, p, workspace, workspace_bytes, who)) return s;
   {
     Tap t(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
-    launch_compact(p, n_live, kv->k_layers, kv->v_layers, c->d.n_layers, page_bytes(c, kv), workspace, (hipStream_t)stream);
+    launch_compact(p, n_live, kv->k_layers, kv->v_layers, page_layers(c), page_bytes(c, kv), workspace, (hipStream_t)stream);
   }
   return hip_check(c, who);
 }

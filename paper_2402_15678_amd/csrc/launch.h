@@ -245,7 +245,7 @@ struct LayerPages {
 size_t pool_work_bytes(int num_blocks, int max_seqs);
 void launch_fork(const PoolView& p, const int32_t* src, const int32_t* dst, int n, hipStream_t st);
 void launch_free(const PoolView& p, const int32_t* seqs, int n, hipStream_t st);
-// page_bytes: one K (or V) block of one layer, a multiple of 16
+// page_bytes: one K (or V) block of one layer, a multiple of 16; n_layers >= 1 (the first layer's launch turns the table of a compaction)
 void launch_reserve(const PoolView& p, const int32_t* tokens, int B, void* const* k, void* const* v, int n_layers, size_t page_bytes,
                     void* workspace, hipStream_t st);
 void launch_compact(const PoolView& p, int32_t* n_live, void* const* k, void* const* v, int n_layers, size_t page_bytes, void* workspace,

@@ -197,3 +197,16 @@ def test_captured_pool_calls_replay():
         life()
         torch.cuda.synchronize()
         assert np.array_equal(pool.kv.block_tables.cpu().numpy(), want.table)
+
+
+@pytest.mark.parametrize("name", ["fp32", "fp16"])
+def test_a_context_without_layers_has_the_pages_of_layer_0(name):
+    """A context without layers, whose attention calls read layer 0's pages: these move with the blocks, and the table with them."""
+    from paper_2402_15678_amd import harness
+    pool, want = _setup(_desc(1, 2, 64, DESCS[name].dtype), 16, 30, 6, [40, 23, 0, 0, 50], 12)
+    pool.model = harness.DeviceModel.random_on_device(pool.model.desc.with_layers(0), 1)
+    for call, args in [("fork", ([0, 0], [2, 3])), ("reserve", ([45, 30, 45, 60, 51],)), ("free", ([0, 3],)), ("compact", ()), ("reserve", ([64] * 5,))]:
+        got = getattr(pool, call)(*[_dev(a) for a in args])
+        n = getattr(want, call)(*args)
+        assert call != "compact" or got.item() == n
+        _compare(pool, want)

@@ -87,3 +87,13 @@ def test_counts_lists_and_workspaces(binding, ctx):
     assert _status(E, lambda: E.mn_kv_compact(ctx, _kv(binding, v=None), pool, None, 0x2000, need)) == E.MN_ENULL
     assert E.lib.mn_kv_reserve(None, None, None, None, 0, None, 0, None, None) == E.MN_ENULL
     assert E.lib.mn_kv_compact(None, None, None, None, None, 0, None, None) == E.MN_ENULL
+
+
+def test_a_context_without_layers_needs_the_pages_of_layer_0(binding):
+    w, keep = _weights(binding)
+    c = binding.mn_create(_desc(binding, n_layers=0), w)
+    need, none = binding.mn_kv_workspace_bytes(8, 4), C.cast(binding.ptr_array([None]), C.POINTER(C.c_void_p))
+    for pages in (dict(k=none), dict(v=none)):
+        assert _status(binding, lambda: binding.mn_kv_reserve(c, _kv(binding, **pages), _pool(binding), P, 1, 0x2000, need)) == binding.MN_ENULL
+        assert _status(binding, lambda: binding.mn_kv_compact(c, _kv(binding, **pages), _pool(binding), None, 0x2000, need)) == binding.MN_ENULL
+    binding.mn_destroy(c)
