@@ -1092,7 +1092,8 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __r
   }
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f, top = -INFINITY;
-  if (meta.y > 0 && !p.seq_bad[meta.x]) {
+  const bool takes_part = meta.y > 0 && !p.seq_bad[meta.x];
+  if (takes_part) {
     int shared = 0;                                              // streams that met the row's tile
     if (p.n_units > 0) {
       const int first = (kvh * p.row_tiles + (m * G + h - kvh * G) / p.batch.tile_rows) * p.prefix_units;
@@ -1144,7 +1145,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __r
       o += s_o[g][lane_at] * w;
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = takes_part ? 1.f / l : 0.f;                  // (a row whose scores are all -inf is no number, as without a prefix)
 #pragma unroll
   for (int e = 0; e < 4; ++e) out[4 * i + e] = (T)(o[e] * inv);
 }

@@ -430,3 +430,19 @@ def test_prefix_scores_at_the_end_of_the_range(kind, hd, P, far):
         r, (k, v) = x.rows(b), x.dense(b)
         want, bound = ties(x.q[r], k, v, torch.arange(x.ctx[b], x.ctx[b] + x.ks[b] + 1, device="cuda"))
         check(out[r], want, bound + (2.0 ** -11 if kind == "f16" else 2.0 ** -24) * want.abs() + (2.0 ** -25 if kind == "f16" else 0))
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (12, 12, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 256, "f16")])
+@pytest.mark.parametrize("count", [3, 70])
+def test_prefix_row_whose_scores_are_all_minus_infinity(H, Hkv, hd, kind, count):
+    x = Batch(H, Hkv, hd, kind, 64, [37, 5, 0] + [1] * (count - 3), [2, 24, 4] + [0] * (count - 3), 24)
+    x.kp[:, :, 0, :, 0] = -x.kp[:, :, 0, :, 0].abs() - 1
+    plain, status = x.run()
+    assert status == 0
+    at = x.rows(1).start + 9
+    x.q[at, H - 1, 0] = float("inf")
+    out, status = x.run()
+    assert status == 0
+    want = plain.clone().view(-1, H, hd)
+    want[at, H - 1] = float("nan")
+    _same(out.view_as(want), want)

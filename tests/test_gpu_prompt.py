@@ -320,3 +320,21 @@ def test_prompt_scores_at_the_end_of_the_range(kind, hd, shape, far):
     assert _call(model, q, k, v, row0, out) == 0
     want, bound = ties(q, k, v, torch.arange(n, device="cuda"))
     check(out, want, bound + (2.0 ** -11 if kind == "f16" else 2.0 ** -24) * want.abs() + (2.0 ** -25 if kind == "f16" else 0))
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (12, 12, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 256, "f16")])
+def test_prompt_row_whose_scores_are_all_minus_infinity(H, Hkv, hd, kind):
+    d, model = _model(H, Hkv, hd, kind)
+    q, k, v, row0 = _rows(H, Hkv, hd, kind, [200, 7], 23)
+    k = k.clone()
+    k[:, :, 0] = -k[:, :, 0].abs() - 1
+    plain = torch.empty((len(q), H * hd), dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, plain) == 0
+    for at in (0, 63, 150):
+        q2 = q.clone()
+        q2[at, H - 1, 0] = float("inf")
+        out = torch.empty_like(plain)
+        assert _call(model, q2, k, v, row0, out) == 0
+        want = plain.clone().view(-1, H, hd)
+        want[at, H - 1] = float("nan")
+        _same(out.view_as(want), want)
