@@ -830,8 +830,9 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
       for (int u = 0; u < NU; ++u)
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
-          const int e0 = HDP == 16 ? min(4 * g, hd - 4) : 16 * u + 4 * g;  // (heads of 8: against zeros of the query)
+          const int e0 = HDP == 16 ? min(4 * g, hd - 4) : 16 * u + 4 * g;
           kx[h][u] = *reinterpret_cast<const Four<T>*>(kr[h] + (PAGED ? (e0 >> 3) * (8 * bs) + (e0 & 7) : e0));
+          if (HDP == 16 && 4 * g >= hd) kx[h][u] = Four<T>{};    // (heads of 8: zeros, as of the query; 0 times infinity is none)
         }
       // ---- values: asked for ahead of the products ----
       Four<T> vx[HALVES][NU];

@@ -446,3 +446,23 @@ def test_prefix_row_whose_scores_are_all_minus_infinity(H, Hkv, hd, kind, count)
     want = plain.clone().view(-1, H, hd)
     want[at, H - 1] = float("nan")
     _same(out.view_as(want), want)
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (8, 8, 8, "f32"), (16, 4, 8, "f16"), (8, 2, 256, "f16")])
+@pytest.mark.parametrize("at", [5, 70])
+def test_prefix_key_at_minus_infinity_has_no_weight(H, Hkv, hd, kind, at):
+    """One of the shared keys, or one of a sequence's own, at minus infinity."""
+    e = hd - 3
+    x = Batch(H, Hkv, hd, kind, 64, [37, 15], [2, 4], 26)
+    x.kp[int(x.table[0, at // x.bs]), :, e // 8, at % x.bs, e % 8] = float("inf")
+    out, status = x.run()
+    assert status == 0
+    for b in range(2):
+        r, (k, v) = x.rows(b), x.dense(b)
+        limit = torch.arange(x.ctx[b], x.ctx[b] + x.ks[b] + 1, device="cuda")
+        hit = at < x.P or b == 0
+        rest = torch.arange(len(k), device="cuda") != (at if hit else -1)
+        want, bound = attend(x.q[r], k[rest], v[rest], limit - int(hit), kind == "f16")
+        up = (hit & (x.q[r][:, :, e] > 0))[:, :, None].expand(-1, H, hd).reshape(len(want), -1)
+        assert out[r][up].isnan().all()
+        check(torch.where(up, want.to(out.dtype), out[r]), want, bound + 2.0 ** -11 * want.abs() + 2.0 ** -25)

@@ -338,3 +338,24 @@ def test_prompt_row_whose_scores_are_all_minus_infinity(H, Hkv, hd, kind):
         want = plain.clone().view(-1, H, hd)
         want[at, H - 1] = float("nan")
         _same(out.view_as(want), want)
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (12, 12, 64, "f16"), (8, 8, 8, "f32"), (16, 4, 8, "f16"), (4, 1, 16, "f32"), (8, 2, 128, "f32"),
+                                           (8, 2, 256, "f16")])
+@pytest.mark.parametrize("at", [1, 40, 255])
+def test_prompt_key_at_minus_infinity_has_no_weight(H, Hkv, hd, kind, at):
+    """An infinity in one element of a key: a score of minus infinity, and the result without that key, where the query's element has the other
+    sign; no number where it has the same."""
+    n, e = 300, hd - 3
+    d, model = _model(H, Hkv, hd, kind)
+    q, k, v, row0 = _rows(H, Hkv, hd, kind, [n], 25)
+    k = k.clone()
+    k[at, :, e] = float("inf")
+    out = torch.empty((n, H * hd), dtype=DT[kind], device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    rest = torch.arange(n, device="cuda") != at
+    limit = torch.arange(n, device="cuda")
+    want, bound = attend(q, k[rest], v[rest], limit - (limit >= at).long(), kind == "f16")
+    up = ((limit >= at)[:, None] & (q[:, :, e] > 0))[:, :, None].expand(n, H, hd).reshape(n, -1)
+    assert out[up].isnan().all() and up.any()
+    check(torch.where(up, want.to(out.dtype), out), want, bound + 2.0 ** -11 * want.abs() + 2.0 ** -25)
