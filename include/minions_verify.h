@@ -337,7 +337,8 @@ long mn_selector_adjustments(const mn_selector *sel); /* decisions taken so far;
  * tables.  Whatever a call cannot do it leaves as it was and reports in *dev_status (or NULL): a damaged row (an id out of
  * range, a context longer than its blocks) is MN_DEV_BLOCK_TABLE.
  * Pages move in all layers of the context; one without layers has those of layer 0, as in the attention calls.
- * n <= max_seqs <= MN_MAX_BATCH and B <= max_seqs; n = 0 and B = 0 are no-ops. */
+ * n <= max_seqs <= MN_MAX_BATCH and B <= max_seqs; n = 0 and B = 0 are no-ops.  num_blocks is at most 2^30, and B * max_blocks_per_seq below
+ * 2^31 (MN_EUNSUPPORTED).  ctx may be NULL for mn_kv_fork and mn_kv_free, which touch no page. */
 typedef struct {
   int32_t *block_tables, *block_refs, *seq_blocks;
   int max_seqs;

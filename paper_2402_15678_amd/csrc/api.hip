@@ -852,6 +852,8 @@ extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t
 }
 
 // ---- page pool ----------------------------------------------------------------------------------------
+constexpr int MAX_POOL_BLOCKS = 1 << 30;  // (the plans count ids, and go past their end, in 32 bits)
+
 // Layers whose pages move: a context without layers has those of layer 0, which its attention calls read.
 static int page_layers(const mn_ctx* c) { return c->d.n_layers > 0 ? c->d.n_layers : 1; }
 
@@ -864,6 +866,7 @@ static mn_status check_pool(mn_ctx* c, const mn_kv* kv, const mn_pool* pool, int
     return fail(c, MN_EINVAL, "%s: block_size/num_blocks/max_blocks_per_seq", who);
   if (pool->max_seqs < 1 || pool->max_seqs > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: max_seqs = %d outside [1, %d]", who, pool->max_seqs, MN_MAX_BATCH);
   if (n < 0 || n > pool->max_seqs) return fail(c, MN_EINVAL, "%s: %d sequences of %d slots", who, n, pool->max_seqs);
+  if (kv->num_blocks > MAX_POOL_BLOCKS) return fail(c, MN_EUNSUPPORTED, "%s: %d blocks", who, kv->num_blocks);
   if (pages) {
     if (!kv->k_layers || !kv->v_layers) return fail(c, MN_ENULL, "%s: k_layers or v_layers is NULL", who);
     for (int l = 0; l < page_layers(c); ++l)
@@ -888,7 +891,7 @@ static size_t page_bytes(const mn_ctx* c, const mn_kv* kv) {
 }
 
 extern "C" size_t mn_kv_workspace_bytes(int num_blocks, int max_seqs) {
-  if (num_blocks < 1 || max_seqs < 1 || max_seqs > MN_MAX_BATCH) return 0;
+  if (num_blocks < 1 || num_blocks > MAX_POOL_BLOCKS || max_seqs < 1 || max_seqs > MN_MAX_BATCH) return 0;
   return pool_work_bytes(num_blocks, max_seqs);
 }
 
@@ -901,6 +904,7 @@ extern "C" mn_status mn_kv_reserve(mn_ctx* c, mn_kv* kv, const mn_pool* pool, co
   if (mn_status s = check_pool_workspace(c, p, workspace, workspace_bytes, who)) return s;
   if (B == 0) return MN_OK;
   if (!tokens) return fail(c, MN_ENULL, "%s: tokens is NULL", who);
+  if ((long)B * kv->max_blocks_per_seq >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d blocks", who, B, kv->max_blocks_per_seq);
   {
     Tap t(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
     launch_reserve(p, tokens, B, kv->k_layers, kv->v_layers, page_layers(c), page_bytes(c, kv), workspace, (hipStream_t)stream);

@@ -97,3 +97,14 @@ def test_a_context_without_layers_needs_the_pages_of_layer_0(binding):
         assert _status(binding, lambda: binding.mn_kv_reserve(c, _kv(binding, **pages), _pool(binding), P, 1, 0x2000, need)) == binding.MN_ENULL
         assert _status(binding, lambda: binding.mn_kv_compact(c, _kv(binding, **pages), _pool(binding), None, 0x2000, need)) == binding.MN_ENULL
     binding.mn_destroy(c)
+
+
+def test_numbers_of_blocks_beyond_what_the_plans_count(binding, ctx):
+    E, need, most = binding, 1 << 40, (1 << 31) - 1
+    assert E.mn_kv_workspace_bytes((1 << 30) + 1, 4) == 0 and E.mn_kv_workspace_bytes(most, 4) == 0
+    for nb in ((1 << 30) + 1, most):
+        assert _status(E, lambda: E.mn_kv_reserve(ctx, _kv(E, nb=nb), _pool(E), P, 1, 0x2000, need)) == E.MN_EUNSUPPORTED
+        assert _status(E, lambda: E.mn_kv_compact(ctx, _kv(E, nb=nb), _pool(E), None, 0x2000, need)) == E.MN_EUNSUPPORTED
+    # 4096 rows that may each ask for 2^19 blocks: their sum passes 32 bits
+    wide, slots = _kv(E, nb=1 << 30, width=1 << 19), _pool(E, slots=4096)
+    assert _status(E, lambda: E.mn_kv_reserve(ctx, wide, slots, P, 4096, 0x2000, need)) == E.MN_EUNSUPPORTED
