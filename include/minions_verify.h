@@ -445,7 +445,7 @@ mn_status mn_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, cons
  *   out      dev [h_seq_rows[B]][n_heads * head_dim], same type as q; only rows that belong to a sequence are written
  *   kv       NULL, or the cache that the prompts enter: the rows of k and v are also written into layer `layer`'s pages, token i
  *            of sequence b at position i of table row b (tokens whose block id is out of range are left out: MN_DEV_BLOCK_TABLE).
- *            ctx_lens is neither read nor written.
+ *            ctx_lens is neither read nor written.  head_dim * block_size is below 2^31, as in mn_prefix_attention (MN_EUNSUPPORTED).
  * An infinity or NaN in q stays with its row and head; in k and v it reaches the rows that see it, and no other.
  * Scores of any size will do that fp32 holds, those of finite fp16 rows among them.
  * The scores, the statistics and the sums are fp32; fp16 probabilities are rounded to fp16 for the second product, in the sum of

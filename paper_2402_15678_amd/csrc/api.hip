@@ -747,6 +747,12 @@ extern "C" mn_status mn_attention(mn_ctx* c, const void* q, const int32_t* spec_
   return hip_check(c, who);
 }
 
+// The tile kernels' offsets inside a head's page of a block are 32 bits.
+static mn_status check_page(mn_ctx* c, const mn_kv* kv, const char* who) {
+  if ((long)kv->block_size * c->d.head_dim >= (1l << 31)) return fail(c, MN_EUNSUPPORTED, "%s: blocks of %d tokens", who, kv->block_size);
+  return MN_OK;
+}
+
 // ---- attention over whole prompts -------------------------------------------------------------------
 extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride, const void* k, long k_stride, const void* v,
                                          long v_stride, const int32_t* seq_rows, const int32_t* h_seq_rows, int B, const mn_kv* kv,
@@ -776,6 +782,7 @@ extern "C" mn_status mn_prompt_attention(mn_ctx* c, const void* q, long q_stride
   TileArgs t{};
   if (kv) {
     if (mn_status s = check_kv(c, kv, longest, who)) return s;
+    if (mn_status s = check_page(c, kv, who)) return s;
     if (layer < 0 || layer >= (d.n_layers > 0 ? d.n_layers : 1)) return fail(c, MN_EINVAL, "%s: layer %d", who, layer);
     if (!kv->k_layers[layer] || !kv->v_layers[layer]) return fail(c, MN_ENULL, "%s: kv layer pointer is NULL", who);
     t.kv = KvView{kv->k_layers[layer], kv->v_layers[layer], kv->block_tables, kv->block_size, kv->num_blocks, kv->max_blocks_per_seq};
@@ -818,6 +825,7 @@ extern "C" mn_status mn_prefix_attention(mn_ctx* c, const void* q, const int32_t
   if (!q || !spec_len || !h_spec_len || !out) return fail(c, MN_ENULL, "%s: a required pointer is NULL", who);
   if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(c, MN_EINVAL, "%s: q and out must be 16-byte aligned", who);
   if (mn_status s = check_kv(c, kv, max_ctx, who)) return s;
+  if (mn_status s = check_page(c, kv, who)) return s;
   const mn_model_desc& d = c->d;
   if (layer < 0 || layer >= (d.n_layers > 0 ? d.n_layers : 1)) return fail(c, MN_EINVAL, "%s: layer %d", who, layer);
   if (!kv->k_layers[layer] || !kv->v_layers[layer]) return fail(c, MN_ENULL, "%s: kv layer pointer is NULL", who);

@@ -44,3 +44,10 @@ def test_workspace(binding, ctx):  # noqa: F811
     assert sizes == sorted(sizes)
     sizes = [E.mn_prefix_workspace_bytes(ctx, 8, 72, 4096, c) for c in (4097, 4200, 4353, 5000, 100000)]
     assert sizes == sorted(sizes)
+
+
+def test_blocks_whose_pages_pass_32_bits(binding, ctx):  # noqa: F811
+    from tests.test_prompt_refusals import _call as prompt
+    E, bs = binding, 1 << 24                                        # of heads of 128: 2^31 elements
+    assert _status(E, lambda: _call(E, ctx, prefix=0, kv=_kv(E, bs=bs))) == E.MN_EUNSUPPORTED
+    assert _status(E, lambda: prompt(E, ctx, kv=_kv(E, bs=bs))) == E.MN_EUNSUPPORTED
