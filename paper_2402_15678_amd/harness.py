@@ -201,6 +201,11 @@ class DeviceKV:
         return (self.k_pages[layer].float().cpu().numpy(), self.v_pages[layer].float().cpu().numpy())
 
 
+def activation_type(desc: synth.ModelDesc) -> torch.dtype:
+    """What the attention calls read and write: fp16 in bf16 models."""
+    return torch.float16 if desc.dtype == synth.DT_BF16 else torch.float32
+
+
 class PromptRows:
     """The host's copy of a packed batch's row offsets (they size the launch)."""
 
@@ -214,7 +219,7 @@ def prompt_attention(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: to
     q [M][H][hd], k and v [M][Hkv][hd]: views with any row stride (a QKV projection's rows)."""
     hd = model.desc.head_dim
     qs, ks, vs = q.stride(), k.stride(), v.stride()
-    assert qs[1:] == ks[1:] == vs[1:] == (hd, 1) and out.is_contiguous() and out.dtype == q.dtype
+    assert qs[1:] == ks[1:] == vs[1:] == (hd, 1) and out.is_contiguous() and out.dtype == q.dtype == k.dtype == v.dtype == activation_type(model.desc)
     B.mn_prompt_attention(model.ctx, q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0],
                           seq_rows.data_ptr(), plan.h, plan.B, out.data_ptr(), kv.c if kv is not None else None, layer,
                           dev_status.data_ptr() if dev_status is not None else None, stream_ptr())
@@ -235,7 +240,7 @@ class PrefixSession:
 
     def attention(self, q: torch.Tensor, spec_len: torch.Tensor, h_spec_len: Sequence[int], out: torch.Tensor, layer: int = 0) -> torch.Tensor:
         """q [rows][H][hd] at positions ctx_b .. ctx_b + spec_len[b], whose keys are in the cache; out [rows][H * hd]."""
-        assert q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype
+        assert q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype == activation_type(self.model.desc)
         B.mn_prefix_attention(self.model.ctx, q.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len),
                               self.prefix_len, self.max_ctx, self.kv.c, layer, out.data_ptr(), self.workspace.data_ptr(),
                               self.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
