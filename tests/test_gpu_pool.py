@@ -210,3 +210,43 @@ def test_a_context_without_layers_has_the_pages_of_layer_0(name):
         n = getattr(want, call)(*args)
         assert call != "compact" or got.item() == n
         _compare(pool, want)
+
+
+def test_replayed_pool_calls_move_the_pages():
+    """Branch, grow, retire and pack in one graph: before every replay mapping and pages are put back, after it all of it is compared."""
+    pool, want = _setup(DESCS["fp16"], 16, 40, 6, [40, 23, 0, 0, 0], 13)
+    pages = [*pool.kv.k_pages, *pool.kv.v_pages]
+    saved, bytes_ = pool.state.clone(), [p.clone() for p in pages]
+    src, dst, tokens, gone = _dev([0, 0, 1]), _dev([2, 3, 4]), _dev([45, 30, 45, 60, 24]), _dev([0, 3])
+
+    def back():
+        pool.state.copy_(saved)
+        for p, b in zip(pages, bytes_):
+            p.copy_(b)
+
+    def life():
+        pool.fork(src, dst)
+        pool.reserve(tokens)
+        pool.free(gone)
+        pool.compact()
+
+    want.fork([0, 0, 1], [2, 3, 4])
+    want.reserve([45, 30, 45, 60, 24])
+    want.free([0, 3])
+    n = want.compact()
+    assert any(not np.array_equal(a, b.cpu().numpy()) for a, b in zip(want.pages, bytes_))
+    life()
+    _compare(pool, want)
+    back()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        life()
+    for _ in range(3):
+        back()
+        pool.n_live.zero_()
+        graph.replay()
+        _compare(pool, want)
+        assert pool.n_live.item() == n
+        back()
+        life()
+        _compare(pool, want)

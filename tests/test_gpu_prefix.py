@@ -466,3 +466,31 @@ def test_prefix_key_at_minus_infinity_has_no_weight(H, Hkv, hd, kind, at):
         up = (hit & (x.q[r][:, :, e] > 0))[:, :, None].expand(-1, H, hd).reshape(len(want), -1)
         assert out[r][up].isnan().all()
         check(torch.where(up, want.to(out.dtype), out[r]), want, bound + 2.0 ** -11 * want.abs() + 2.0 ** -25)
+
+
+def test_agrees_with_the_attention_that_reads_the_prefix_for_everybody_within_the_roundings():
+    """Either is within its bound of the definition at the queries that it multiplies: mn_attention rounds them to fp16 once scaled.  What is left
+    shows a mask that is off by one key."""
+    from paper_2402_15678_amd import binding, harness
+    x = Batch(64, 8, 128, "f16", 1024, [50, 600, 0, 333], [8, 8, 8, 8], 9)
+    out, _ = x.run()
+    kv = x.kv()
+    n = binding.mn_workspace_bytes(x.model.ctx, 4, len(x.q), x.max_ctx)
+    ws, st = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    other = torch.zeros_like(out)
+    binding.mn_attention(x.model.ctx, x.q.data_ptr(), torch.tensor(x.ks, dtype=torch.int32, device="cuda").data_ptr(), binding.host_i32(x.ks), 4,
+                         x.max_ctx, kv.c, 0, other.data_ptr(), ws.data_ptr(), n, st.data_ptr(), harness.stream_ptr())
+    torch.cuda.synchronize()
+    scale = 1.4426950408889634 / 128 ** 0.5
+    rounded = (x.q.float() * scale).half().double() / scale
+    for b in range(4):
+        r = x.rows(b)
+        k, v = x.dense(b)
+        limit = torch.arange(x.ctx[b], x.ctx[b] + 9, device="cuda")
+        want, bound = attend(x.q[r], k, v, limit, True)
+        want2, bound2 = attend(rounded[r], k, v, limit, True)
+        check(other[r], want2, bound2)
+        slack = bound + bound2 + (want - want2).abs()
+        assert ((out[r].double() - other[r].double()).abs() <= slack).all()
+        shifted, _ = attend(x.q[r], k, v, limit - 1, True)
+        assert ((shifted - other[r].double()).abs() > slack).any()

@@ -359,3 +359,36 @@ def test_prompt_key_at_minus_infinity_has_no_weight(H, Hkv, hd, kind, at):
     up = ((limit >= at)[:, None] & (q[:, :, e] > 0))[:, :, None].expand(n, H, hd).reshape(n, -1)
     assert out[up].isnan().all() and up.any()
     check(torch.where(up, want.to(out.dtype), out), want, bound + 2.0 ** -11 * want.abs() + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("H,Hkv,hd,lens", [
+    (4, 4, 128, [300, 65, 64, 63, 1, 0, 128]), (12, 12, 64, [300, 65, 64, 63, 1, 0, 128]),                       # tiles of 64 rows
+    (40, 40, 128, [700, 1, 128, 0, 129, 127, 255, 400]), (64, 64, 64, [500, 33, 0, 128, 129, 1, 640]),           # tiles of 128 rows
+    (64, 32, 128, [500, 65, 64, 1, 0, 463]), (48, 16, 128, [900, 43, 42, 1, 513]), (64, 32, 64, [801, 64, 65, 0, 400])], ids=str)
+def test_every_row_of_a_tile_enters_the_cache(H, Hkv, hd, lens):
+    """Heads of their own and small groups, the shapes with the most tokens per tile, at both tile heights, bit for bit."""
+    from paper_2402_15678_amd import harness
+    bs = 16
+    d, model = _model(H, Hkv, hd, "f16")
+    q, k, v, row0 = _rows(H, Hkv, hd, "f16", lens, 27)
+    need = [-(-n // bs) for n in lens]
+    ids = np.random.default_rng(4).permutation(sum(need) + 5).astype(np.int32)
+    table = np.full((len(lens), max(need)), -1, np.int32)
+    for b, n in enumerate(need):
+        table[b, :n] = ids[sum(need[:b]):sum(need[:b + 1])]
+    kp = torch.full((len(ids), Hkv, hd // 8, bs, 8), -3.0, dtype=torch.float16, device="cuda")
+    vp = torch.full((len(ids), Hkv, hd, bs), -3.0, dtype=torch.float16, device="cuda")
+    wk, wv = kp.clone(), vp.clone()
+    for b, n in enumerate(lens):
+        i = np.arange(n)
+        blk, off = torch.from_numpy(table[b, i // bs].astype(np.int64)).cuda(), torch.from_numpy(i % bs).cuda()
+        wk[blk, :, :, off] = k[row0[b]:row0[b + 1]].unflatten(2, (-1, 8))
+        wv[blk, :, :, off] = v[row0[b]:row0[b + 1]]
+    kv = harness.DeviceKV(d, bs, len(ids), table, [0] * len(lens), [kp], [vp])
+    out = torch.full((len(q), H * hd), -7.0, dtype=torch.float16, device="cuda")
+    assert _call(model, q, k, v, row0, out, kv) == 0
+    assert torch.equal(kp, wk) and torch.equal(vp, wv)
+    without = torch.empty_like(out)
+    assert _call(model, q, k, v, row0, without) == 0
+    assert torch.equal(out, without)
+    _compare(q, k, v, row0, out, "f16")
