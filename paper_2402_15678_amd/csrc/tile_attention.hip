@@ -50,9 +50,9 @@ __device__ __forceinline__ int tiles_from(int level, int B, F n) {
 
 // Tile t of a packed batch whose sequence b has n(b) tiles.  Order: last tiles first (a causal tile's work grows with its number),
 // so the longest ones start first and the short ones fill the gaps.  Level `tile` and the sequence are found by counting how
-// many tiles lie at or above a level; `total` is the number of all tiles.
+// many tiles lie at or above a level.  0 <= t < the sum of n(b), and n(b) <= max_tiles.
 template <typename F>
-__device__ __forceinline__ void find_tile(int t, int B, int max_tiles, F n, int total, int& seq, int& tile) {
+__device__ __forceinline__ void find_tile(int t, int B, int max_tiles, F n, int& seq, int& tile) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = max_tiles, above = 0;         // tiles at levels >= lo: more than t; >= hi: `above`, t at most
   while (hi - lo > 1) {
@@ -126,7 +126,7 @@ __device__ __forceinline__ bool prompt_item(const TileArgs& a, int t, const Divi
   }
   int seq, tile;
   if (a.B <= 64) find_tile_lanes(t, a.B, a.max_tiles, own, seq, tile);
-  else find_tile(t, a.B, a.max_tiles, n, total, seq, tile);
+  else find_tile(t, a.B, a.max_tiles, n, seq, tile);
   seq = __builtin_amdgcn_readfirstlane(seq);
   tile = __builtin_amdgcn_readfirstlane(tile);
   int row0, row1;
@@ -685,14 +685,15 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
         }
       }
     }
-    // Rows that enter the cache: those whose first stack row lies in this workgroup's tile, out of the stages (they are the last keys it read:
-    // the last tile is still there, with others they are fetched again).  A lane's piece of K is 8 elements of one token, and of V
+    // Rows that enter the cache: those whose first stack row lies in this workgroup's tile, out of the stages.  They are the last keys it
+    // read; where they lie in the last tile of keys alone that stage is used as it is, else they are fetched once more (the stages before
+    // it are still there as well: nothing is staged past an item's end).  A lane's piece of K is 8 elements of one token, and of V
     // 8 tokens of one element: 16 bytes of a page each way.  7800 rows of 40 KV heads of 128, 161 us without: written as they come
     // by the rows at the start 221 us, by a kernel of its own 253, like this 208 (now 157 and 192), where 160 MB of pages are worth about 35.
     if (!PAGED && a.kv.k) {
       const int put0 = (it.rbase + G - 1) / G, put1 = (min(it.R, it.rbase + ROWS) + G - 1) / G;
       __syncthreads();                                             // (everybody is through with the stages, and the last tile is there)
-      if (put0 / TK < n_tiles - 1) {                               // (at most ROWS / TK stages, and one more if ROWS / G is no multiple of TK)
+      if (put0 / TK < n_tiles - 1) {                               // (at most ROWS / TK stages; one more than ROWS / G / TK if that is not whole)
         static_assert(ROWS / TK <= STAGES && ROWS / 2 / TK + 1 <= STAGES, "the rows of a tile fit the stages");
         base = static_cast<const char*>(k_wave ? a.k : a.v) + ((size_t)(it.m0 + put0 / TK * TK) * stride + (size_t)kvh * HDIM * 2);
         for (int i = put0 / TK; i * TK < put1; ++i) stage(i);
