@@ -13,8 +13,8 @@
 //  * copy_pages      the pages of the (from, to) pairs that a plan wrote, in all layers; as many workgroups as fill the chip
 //    take chunks by index, so a step without a copy is a short launch.
 // A plan is bound by its chain of round trips to memory, a copy by HBM.  16 requests of 100 to 700 tokens that branch into 4 each,
-// 64/8 heads of 128, 8 layers: fork 4.3 us, plan 8.2 (7.7 with the counts read once into bit masks), copy 9.3.  16 of 48 sequences
-// retired, 12 layers of 12 heads of 64: free 4.7, plan 5.5, copy 92 (4.6 TB/s read and written).
+// 64/8 heads of 128, 8 layers: fork 4.2 us, plan 8.6 (half a microsecond less with the counts read once into bit masks), copy 9.2.  16 of 48 sequences
+// retired, 12 layers of 12 heads of 64: free 4.8, plan 5.0, copy 92 (4.6 TB/s read and written).
 #include "launch.h"
 #include "../../include/minions_verify.h"
 

@@ -1067,7 +1067,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
 
 // Four elements of a row of one head per thread; several slots are asked for at once.  GROUPS threads share them where there are few rows
 // and many slots (6 rows of 64 heads, 33 slots: 4.6 us, with one 10).  Bound by
-// HBM where there are many rows: 576 rows of 64 heads of 128, 71 MB of parts, 17 us.
+// HBM where there are many rows: 576 rows of 64 heads of 128, 71 MB of parts, 16 us.
 constexpr int AT_ONCE = 4;
 template <typename T, int GROUPS>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
