@@ -250,3 +250,14 @@ def test_replayed_pool_calls_move_the_pages():
         back()
         life()
         _compare(pool, want)
+
+
+def test_fork_and_free_need_no_context():
+    from paper_2402_15678_amd import binding, harness
+    pool, want = _setup(DESCS["fp32"], 16, 24, 5, [20, 33, 0, 0], 14)
+    src, dst, gone = _dev([0, 1]), _dev([3, 2]), _dev([1, 3])
+    binding.mn_kv_fork(None, pool.kv.c, pool.c, src.data_ptr(), dst.data_ptr(), 2, pool.dev_status.data_ptr(), harness.stream_ptr())
+    binding.mn_kv_free(None, pool.kv.c, pool.c, gone.data_ptr(), 2, pool.dev_status.data_ptr(), harness.stream_ptr())
+    want.fork([0, 1], [3, 2])
+    want.free([1, 3])
+    _compare(pool, want)

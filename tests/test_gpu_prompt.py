@@ -392,3 +392,22 @@ def test_every_row_of_a_tile_enters_the_cache(H, Hkv, hd, lens):
     assert _call(model, q, k, v, row0, without) == 0
     assert torch.equal(out, without)
     _compare(q, k, v, row0, out, "f16")
+
+
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("scale", [60.0, 900.0, 14000.0])
+def test_scores_of_any_size_give_a_mean_of_the_values_seen(hd, scale):
+    """Random rows of up to the fp16 range: no score is known better than to its fp32 sum's rounding, but every output lies between the least
+    and the largest value that its row sees (its own rounding aside)."""
+    n = 300
+    d, model = _model(4, 2, hd, "f16")
+    q, k, v, row0 = _rows(4, 2, hd, "f16", [n], 28)
+    q, k = (q.float() * scale).clamp(-65504, 65504).half(), (k.float() * scale).clamp(-65504, 65504).half()
+    out = torch.zeros((n, 4 * hd), dtype=torch.float16, device="cuda")
+    assert _call(model, q, k, v, row0, out) == 0
+    assert torch.isfinite(out).all()
+    seen = v.float().repeat_interleave(2, dim=1).reshape(n, -1)
+    least, most = seen.cummin(dim=0).values, seen.cummax(dim=0).values
+    # the weights of a row add up to 1 but for (n + 64) 2^-23, and the result is rounded by 2^-11
+    slack = ((n + 64) * 2.0 ** -23 + 2.0 ** -11) * torch.maximum(least.abs(), most.abs()) + 2.0 ** -25
+    assert (out.float() >= least - slack).all() and (out.float() <= most + slack).all()
