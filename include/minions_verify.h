@@ -65,7 +65,8 @@ enum {
                              the affected rows no longer follow the arithmetic stated at mn_verify_forward */
   MN_DEV_CTX = 32,        /* ctx_b + k_b + 1 exceeds the max_ctx the host passed (the sequence is a no-op) */
   MN_DEV_POOL = 64,       /* mn_kv_reserve: not enough free blocks */
-  MN_DEV_SEQ = 128        /* page pool: a slot out of range, a child's slot that is in use, or one filled twice by a call */
+  MN_DEV_SEQ = 128,       /* page pool: a slot out of range, a child's slot that is in use, or one filled twice by a call */
+  MN_DEV_SHARED = 256     /* mn_kv_evict: a block that would be written is in other rows too */
 };
 
 /* Limits (checked; MN_EINVAL / MN_EUNSUPPORTED beyond them). */
@@ -472,6 +473,94 @@ size_t mn_prefix_workspace_bytes(const mn_ctx *ctx, int B, int max_rows, int pre
 mn_status mn_prefix_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, const int32_t *h_spec_len, int B,
                               int prefix_len, int max_ctx, const mn_kv *kv, int layer, void *out, void *workspace,
                               size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* ---- a cache that does not grow with the text -------------------------------------------------------
+ * Rows are put into the cache at positions that the caller gives (mn_qk_norm_rope), and then either attention looks back a window and
+ * at the first few tokens (mn_window_attention), or it sees everything, the weight that it gives to every cached token is added up
+ * (mn_kv_weigh), and the tokens with the least of it are evicted (mn_kv_evict).  A window goes by the order of the slots, which an
+ * eviction gives up: the two are for different sequences. */
+
+/* How a head's rows are made ready.  Gains NULL: not normed.  The first rot_dim elements are turned, in pairs (i, i + rot_dim / 2), by
+ * p * base^(-2i / rot_dim), p the row's position on the pair's axis: the first pairs[0] pairs belong to axis 0, the next pairs[1] to
+ * axis 1, and so on (time, height, width; a text has one axis).  rot_dim is a multiple of 8, 0 to head_dim; the pairs of the axes add
+ * up to rot_dim / 2. */
+#define MN_MAX_AXES 4
+typedef struct {
+  const float *q_gain, *k_gain; /* dev [head_dim] or NULL */
+  float eps;                    /* inside the square root */
+  int rot_dim, n_axes;          /* 1 <= n_axes <= MN_MAX_AXES */
+  int pairs[MN_MAX_AXES];
+  double base;
+} mn_row_rule;
+
+/* The rows of a QKV projection on their way to attention: queries and keys are normed per head (x * gain / sqrt(mean(x^2) + eps)), turned,
+ * and rounded once to the activation type; values are rounded.  Rows are packed as in mn_verify_forward: sequence b has the rows
+ * ctx_b .. ctx_b + k_b of its slots.
+ *   q, k, v    dev, row m at q + m * q_stride: [n_heads][head_dim], [n_kv_heads][head_dim]; fp32 where rows_f32 is set, as
+ *              mn_proj_gemm leaves them, else the activation type (addresses and row strides are multiples of 16 bytes)
+ *   positions  dev [n_axes][M], any int32 (the slot that a row goes to is not looked at; NULL where rot_dim is 0)
+ *   kv         NULL, or the cache that the keys and values enter, layer `layer`.  ctx_lens is read and not written.
+ *   q_out      dev [M][n_heads * head_dim], activation type, or NULL: no queries are made (q is not read then)
+ *   k_out, v_out dev [M][n_kv_heads * head_dim], the keys and values as dense rows, or NULL
+ * Outputs do not overlap the inputs.  Sequences whose slots do not fit the table (MN_DEV_CTX), rows behind a block id out of range
+ * (MN_DEV_BLOCK_TABLE) and a batch whose device lengths are not the host's (MN_DEV_SPEC_LEN) are left out of the cache; what is dense is
+ * written all the same, but for the keys and values of sequences and batches left out.  Values beyond fp16 are saturated (MN_DEV_RANGE).
+ * spec_len may be NULL where kv is. */
+mn_status mn_qk_norm_rope(mn_ctx *ctx, const void *q, long q_stride, const void *k, long k_stride, const void *v, long v_stride,
+                          int rows_f32, const mn_row_rule *rule, const int32_t *positions, const int32_t *spec_len,
+                          const int32_t *h_spec_len, int B, const mn_kv *kv, int layer, void *q_out, void *k_out, void *v_out,
+                          int32_t *dev_status, void *stream);
+
+/* Multi-token paged attention of one layer with a window: the row in slot p sees the keys i <= p with i > p - window or i < sinks.
+ * Rows, q, out and the cache as in mn_attention; any number of rows per sequence, so that a prompt (no tokens cached yet but its own, put
+ * there by mn_qk_norm_rope), a chunk of one and a single token are all this call.  window >= 1; one of max_ctx and more is
+ * attention over everything.  Of a table row only the entries of blocks that hold a visible key are read: the others may be anything.
+ *   stats  dev [M][n_heads][2] fp32 (out) or NULL: per row and head a reference m and the sum l, such that key i has the weight
+ *          2^(s_i log2(e) / sqrt(head_dim) - m) / l, s_i its product with the query (mn_kv_weigh goes by them)
+ * A sequence that is damaged (MN_DEV_BLOCK_TABLE) or does not fit max_ctx (MN_DEV_CTX) gets zeros, in out and stats, and so do all
+ * rows when the device's lengths are not the host's (MN_DEV_SPEC_LEN).  An infinity or NaN goes as far as in mn_prompt_attention; slots
+ * that hold no token may hold anything.  Arithmetic and choice of instruction as there.
+ * workspace: mn_window_workspace_bytes(ctx, B, sum_b q_b or more) bytes, 256-byte aligned. */
+size_t mn_window_workspace_bytes(const mn_ctx *ctx, int B, int max_rows);
+mn_status mn_window_attention(mn_ctx *ctx, const void *q, const int32_t *spec_len, const int32_t *h_spec_len, int B, int window,
+                              int sinks, int max_ctx, const mn_kv *kv, int layer, void *out, float *stats, void *workspace,
+                              size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* What is known of every cached token, per layer, slot and KV head: the attention weight that it has been given, and the number that it
+ * has in its text (which its slot stops telling with the first eviction). */
+typedef struct {
+  float *mass;   /* dev [n_layers][max_seqs][n_kv_heads][width] */
+  int32_t *born; /* dev, likewise */
+  int max_seqs, width; /* width: slots of a line, at least the longest context */
+} mn_ledger;
+
+/* Adds up the weights that a step's rows gave (one layer): mass[b][h][i] += the sum over the rows that see slot i, and the query heads of
+ * KV head h, of the softmax weight of key i, from the queries and the stats that mn_window_attention left for them without a window.
+ *   n_out dev [B], or NULL.  NULL: all k_b + 1 rows count, in the slots from ctx_b on (ahead of the commit).  Otherwise the first n_out[b]
+ *         of them, in the last n_out[b] slots of the context (behind mn_accept_and_commit, whose n_out it is); a sequence with 0 or
+ *         less is left alone.
+ *   seen  dev [B], tokens that the text had before the first row, or NULL: as many as the row's slot says (nothing evicted yet)
+ * The counting rows' own slots are new: their mass is set, not added to, and born[b][h][slot of row j] = seen[b] + j.  max_ctx bounds the
+ * slots in use, theirs included, and is at most width.  Rows whose stats are no numbers (or zeros) give nothing; slots behind a block id
+ * out of range are left as they were (MN_DEV_BLOCK_TABLE), sequences that do not fit max_ctx (MN_DEV_CTX) or have more rows in n_out than
+ * in spec_len, and batches whose device lengths are not the host's (MN_DEV_SPEC_LEN), likewise.  Sums are fp32, in one order. */
+mn_status mn_kv_weigh(mn_ctx *ctx, const void *q, const float *stats, const int32_t *spec_len, const int32_t *h_spec_len, int B,
+                      const int32_t *n_out, const int32_t *seen, int max_ctx, const mn_kv *kv, int layer, const mn_ledger *ledger,
+                      int32_t *dev_status, void *stream);
+
+/* Cuts the contexts of the slots b < B back to keep[b] tokens, in every layer and KV head for itself: the first `sinks` slots and the
+ * tokens born last, `recent` of the newest's numbers, stay ahead of all others, those by their mass (no numbers last, among
+ * equals the lowest slot first).  Tokens that stay from slot keep[b] on move, with their mass and born, into the slots below that
+ * are left, both in ascending order; nothing else moves.  Afterwards ctx_lens[b] = keep[b], and the blocks behind are let go as by
+ * mn_kv_free.  A slot with keep[b] negative or not below its context is left alone.
+ * So is one whose table row is damaged (MN_DEV_BLOCK_TABLE), whose context is longer than the ledger's lines (MN_DEV_CTX), or that
+ * shares a block behind the first sinks / block_size and below keep[b] (MN_DEV_SHARED: others read what would be moved).
+ * mn_verify_forward turns its rows by their slot: behind an eviction rows are made with mn_qk_norm_rope, whose positions are the caller's.
+ *   keep dev [B]
+ * workspace: mn_evict_workspace_bytes(ctx, B or more, ledger->width or more) bytes, 256-byte aligned. */
+size_t mn_evict_workspace_bytes(const mn_ctx *ctx, int B, int width);
+mn_status mn_kv_evict(mn_ctx *ctx, mn_kv *kv, const mn_pool *pool, const int32_t *keep, int B, int sinks, int recent,
+                      const mn_ledger *ledger, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
 
 /* ---- timing taps (for benchmarks; off by default) --------------------------------------------- */
 

@@ -18,9 +18,10 @@ MN_ARCH_OPT, MN_ARCH_LLAMA = 0, 1
 MN_DT_F32, MN_DT_BF16 = 0, 1
 MN_VOTE_TREE, MN_VOTE_COLUMN = 0, 1
 MN_DEV_BLOCK_TABLE, MN_DEV_SPEC_LEN, MN_DEV_TOKEN, MN_DEV_DRAFTS, MN_DEV_RANGE, MN_DEV_CTX = 1, 2, 4, 8, 16, 32
-MN_DEV_POOL, MN_DEV_SEQ = 64, 128
+MN_DEV_POOL, MN_DEV_SEQ, MN_DEV_SHARED = 64, 128, 256
 MN_MAX_DRAFTS, MN_MAX_BATCH, MN_MAX_SPLIT_K = 64, 4096, 16
 MN_NOALLOC_SCRATCH_BYTES = 32 << 20
+MN_MAX_AXES = 4
 
 
 EXPORTS = ("mn_create", "mn_destroy", "mn_last_error", "mn_status_str", "mn_workspace_bytes", "mn_mv_vote",
@@ -30,6 +31,7 @@ EXPORTS = ("mn_create", "mn_destroy", "mn_last_error", "mn_status_str", "mn_work
            "mn_selector_create", "mn_selector_destroy", "mn_selector_observe", "mn_selector_current",
            "mn_prompt_attention", "mn_prefix_workspace_bytes", "mn_prefix_attention",
            "mn_kv_workspace_bytes", "mn_kv_reserve", "mn_kv_fork", "mn_kv_free", "mn_kv_compact",
+           "mn_qk_norm_rope", "mn_window_workspace_bytes", "mn_window_attention", "mn_kv_weigh", "mn_evict_workspace_bytes", "mn_kv_evict",
            "mn_selector_adjustments", "mn_probe_stream_read", "mn_probe_mfma", "mn_probe_mfma_data")
 PROF_KINDS = ("prepare", "norm", "gemm", "rope_append", "attention", "act", "argmax", "vote", "accept")
 
@@ -57,6 +59,15 @@ class KV(C.Structure):
 
 class Pool(C.Structure):
     _fields_ = [("block_tables", C.c_void_p), ("block_refs", C.c_void_p), ("seq_blocks", C.c_void_p), ("max_seqs", C.c_int)]
+
+
+class RowRule(C.Structure):
+    _fields_ = [("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float), ("rot_dim", C.c_int), ("n_axes", C.c_int),
+                ("pairs", C.c_int * MN_MAX_AXES), ("base", C.c_double)]
+
+
+class Ledger(C.Structure):
+    _fields_ = [("mass", C.c_void_p), ("born", C.c_void_p), ("max_seqs", C.c_int), ("width", C.c_int)]
 
 
 def _load() -> C.CDLL:
@@ -116,6 +127,19 @@ def _load() -> C.CDLL:
     lib.mn_kv_free.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, i32, vp, vp]
     lib.mn_kv_compact.restype = i32
     lib.mn_kv_compact.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, vp, sz, vp, vp]
+    lib.mn_qk_norm_rope.restype = i32
+    lib.mn_qk_norm_rope.argtypes = [vp, vp, C.c_long, vp, C.c_long, vp, C.c_long, i32, C.POINTER(RowRule), vp, vp, C.POINTER(C.c_int32),
+                                    i32, C.POINTER(KV), i32, vp, vp, vp, vp, vp]
+    lib.mn_window_workspace_bytes.restype = sz
+    lib.mn_window_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.mn_window_attention.restype = i32
+    lib.mn_window_attention.argtypes = [vp, vp, vp, C.POINTER(C.c_int32), i32, i32, i32, i32, C.POINTER(KV), i32, vp, vp, vp, sz, vp, vp]
+    lib.mn_kv_weigh.restype = i32
+    lib.mn_kv_weigh.argtypes = [vp, vp, vp, vp, C.POINTER(C.c_int32), i32, vp, vp, i32, C.POINTER(KV), i32, C.POINTER(Ledger), vp, vp]
+    lib.mn_evict_workspace_bytes.restype = sz
+    lib.mn_evict_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.mn_kv_evict.restype = i32
+    lib.mn_kv_evict.argtypes = [vp, C.POINTER(KV), C.POINTER(Pool), vp, i32, i32, i32, C.POINTER(Ledger), vp, sz, vp, vp]
     lib.mn_selector_create.restype = i32
     lib.mn_selector_create.argtypes = [C.POINTER(vp), i32, i32, i32, i32, i32, i32]
     lib.mn_selector_destroy.restype = None
@@ -285,6 +309,39 @@ def mn_kv_free(ctx, kv: KV, pool: Pool, seqs, n, dev_status=None, stream=None) -
 
 def mn_kv_compact(ctx, kv: KV, pool: Pool, n_live, workspace, workspace_bytes, dev_status=None, stream=None) -> None:
     _check(lib.mn_kv_compact(ctx, C.byref(kv), C.byref(pool), n_live, workspace, workspace_bytes, dev_status, stream), ctx)
+
+
+def mn_qk_norm_rope(ctx, q, q_stride, k, k_stride, v, v_stride, rows_f32, rule: Optional[RowRule], positions, spec_len, h_spec_len, B,
+                    kv: Optional[KV], layer, q_out, k_out=None, v_out=None, dev_status=None, stream=None) -> None:
+    _check(lib.mn_qk_norm_rope(ctx, q, q_stride, k, k_stride, v, v_stride, rows_f32, C.byref(rule) if rule is not None else None, positions,
+                               spec_len, h_spec_len, B, C.byref(kv) if kv is not None else None, layer, q_out, k_out, v_out, dev_status,
+                               stream), ctx)
+
+
+def mn_window_workspace_bytes(ctx, B: int, max_rows: int) -> int:
+    return int(lib.mn_window_workspace_bytes(ctx, B, max_rows))
+
+
+def mn_window_attention(ctx, q, spec_len, h_spec_len, B, window, sinks, max_ctx, kv: KV, layer, out, stats, workspace, workspace_bytes,
+                        dev_status=None, stream=None) -> None:
+    _check(lib.mn_window_attention(ctx, q, spec_len, h_spec_len, B, window, sinks, max_ctx, C.byref(kv), layer, out, stats, workspace,
+                                   workspace_bytes, dev_status, stream), ctx)
+
+
+def mn_kv_weigh(ctx, q, stats, spec_len, h_spec_len, B, n_out, seen, max_ctx, kv: KV, layer, ledger: Optional[Ledger], dev_status=None,
+                stream=None) -> None:
+    _check(lib.mn_kv_weigh(ctx, q, stats, spec_len, h_spec_len, B, n_out, seen, max_ctx, C.byref(kv), layer,
+                           C.byref(ledger) if ledger is not None else None, dev_status, stream), ctx)
+
+
+def mn_evict_workspace_bytes(ctx, B: int, width: int) -> int:
+    return int(lib.mn_evict_workspace_bytes(ctx, B, width))
+
+
+def mn_kv_evict(ctx, kv: KV, pool: Pool, keep, B, sinks, recent, ledger: Optional[Ledger], workspace, workspace_bytes, dev_status=None,
+                stream=None) -> None:
+    _check(lib.mn_kv_evict(ctx, C.byref(kv), C.byref(pool), keep, B, sinks, recent, C.byref(ledger) if ledger is not None else None, workspace,
+                           workspace_bytes, dev_status, stream), ctx)
 
 
 def mn_selector_create(s_init: int, s_min: int, s_max: int, decision_threshold: int, s_penalty: int,

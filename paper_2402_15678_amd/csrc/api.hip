@@ -4,6 +4,7 @@
 #include "../../include/minions_verify.h"
 #include "launch.h"
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -957,6 +958,214 @@ extern "C" mn_status mn_kv_compact(mn_ctx* c, mn_kv* kv, const mn_pool* pool, in
   {
     Tap t(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
     launch_compact(p, n_live, kv->k_layers, kv->v_layers, page_layers(c), page_bytes(c, kv), workspace, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
+// ---- a cache that does not grow with the text -----------------------------------------------------------
+static mn_status check_layer(mn_ctx* c, const mn_kv* kv, int layer, bool values, const char* who) {
+  if (layer < 0 || layer >= page_layers(c)) return fail(c, MN_EINVAL, "%s: layer %d", who, layer);
+  if (!kv->k_layers[layer] || (values && !kv->v_layers[layer])) return fail(c, MN_ENULL, "%s: kv layer pointer is NULL", who);
+  return MN_OK;
+}
+static KvView layer_view(const mn_kv* kv, int layer) {
+  return KvView{kv->k_layers[layer], kv->v_layers[layer], kv->block_tables, kv->block_size, kv->num_blocks, kv->max_blocks_per_seq};
+}
+// Rows of a packed batch from the host's lengths.
+static mn_status batch_rows(mn_ctx* c, const int32_t* h_spec_len, int B, int* M, int* max_q, const char* who) {
+  int k_max = 0;
+  for (int b = 0; b < B; ++b) if (h_spec_len[b] > k_max) k_max = h_spec_len[b];
+  if (mn_status s = count_rows(c, h_spec_len, B, k_max, M, max_q, who)) return s;
+  const mn_model_desc& d = c->d;
+  if ((long)*M * (d.n_heads / d.n_kv_heads) >= (1l << 29)) return fail(c, MN_EUNSUPPORTED, "%s: %d rows of %d heads", who, *M, d.n_heads);
+  return MN_OK;
+}
+
+extern "C" mn_status mn_qk_norm_rope(mn_ctx* c, const void* q, long q_stride, const void* k, long k_stride, const void* v, long v_stride,
+                                     int rows_f32, const mn_row_rule* rule, const int32_t* positions, const int32_t* spec_len,
+                                     const int32_t* h_spec_len, int B, const mn_kv* kv, int layer, void* q_out, void* k_out, void* v_out,
+                                     int32_t* dev_status, void* stream) {
+  const char* who = "mn_qk_norm_rope";
+  if (!c) return MN_ENULL;
+  if (B < 0 || B > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: B = %d outside [0, %d]", who, B, MN_MAX_BATCH);
+  if (B == 0) return MN_OK;
+  const mn_model_desc& d = c->d;
+  const bool keys = kv || k_out || v_out;
+  if (!rule || !h_spec_len || (q_out && !q) || (keys && (!k || !v)) || (kv && !spec_len)) return fail(c, MN_ENULL, "%s: a required pointer is NULL", who);
+  if (rule->rot_dim < 0 || rule->rot_dim > d.head_dim || rule->rot_dim % 8)
+    return fail(c, MN_EINVAL, "%s: rot_dim %d is no multiple of 8 up to head_dim %d", who, rule->rot_dim, d.head_dim);
+  if (rule->n_axes < 1 || rule->n_axes > MN_MAX_AXES) return fail(c, MN_EINVAL, "%s: %d axes", who, rule->n_axes);
+  long pairs = 0;
+  for (int a = 0; a < rule->n_axes; ++a) {
+    if (rule->pairs[a] < 0) return fail(c, MN_EINVAL, "%s: axis %d has %d pairs", who, a, rule->pairs[a]);
+    pairs += rule->pairs[a];
+  }
+  if (pairs != rule->rot_dim / 2) return fail(c, MN_ESHAPE, "%s: the axes have %ld pairs, rot_dim %d has %d", who, pairs, rule->rot_dim, rule->rot_dim / 2);
+  if (rule->rot_dim > 0 && !positions) return fail(c, MN_ENULL, "%s: positions is NULL", who);
+  if (rule->rot_dim > 0 && !(rule->base > 0.0 && rule->base < INFINITY)) return fail(c, MN_EINVAL, "%s: base", who);
+  if ((rule->q_gain || rule->k_gain) && !(rule->eps >= 0.f && rule->eps < INFINITY)) return fail(c, MN_EINVAL, "%s: eps", who);
+  const int es = rows_f32 || d.dtype == MN_DT_F32 ? 4 : 2;
+  if ((q_out && q_stride < (long)d.n_heads * d.head_dim) || (keys && (k_stride < (long)d.n_kv_heads * d.head_dim || v_stride < (long)d.n_kv_heads * d.head_dim)))
+    return fail(c, MN_EINVAL, "%s: a row stride is shorter than its row", who);
+  if (q_out && (((uintptr_t)q | (uintptr_t)q_out | (uintptr_t)(q_stride * es)) & 15)) return fail(c, MN_EINVAL, "%s: addresses and row strides must be multiples of 16 bytes", who);
+  if (keys && (((uintptr_t)k | (uintptr_t)v | (uintptr_t)k_out | (uintptr_t)v_out | (uintptr_t)(k_stride * es) | (uintptr_t)(v_stride * es)) & 15))
+    return fail(c, MN_EINVAL, "%s: addresses and row strides must be multiples of 16 bytes", who);
+  int M = 0, max_q = 0;
+  if (mn_status s = batch_rows(c, h_spec_len, B, &M, &max_q, who)) return s;
+  CacheRows t{};
+  if (kv) {
+    if (mn_status s = check_kv(c, kv, max_q, who)) return s;
+    if (mn_status s = check_page(c, kv, who)) return s;
+    if (mn_status s = check_layer(c, kv, layer, true, who)) return s;
+    if ((long)kv->max_blocks_per_seq * kv->block_size >= (1l << 30)) return fail(c, MN_EUNSUPPORTED, "%s: table rows of %d blocks of %d tokens", who, kv->max_blocks_per_seq, kv->block_size);
+    t.kv = layer_view(kv, layer);
+    t.ctx_lens = kv->ctx_lens;
+  }
+  t.q = q; t.k = k; t.v = v; t.q_stride = q_stride; t.k_stride = k_stride; t.v_stride = v_stride;
+  t.q_out = q_out; t.k_out = k_out; t.v_out = v_out; t.q_gain = rule->q_gain; t.k_gain = rule->k_gain;
+  t.positions = positions; t.spec_len = spec_len; t.status = dev_status;
+  t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.rot = rule->rot_dim; t.dtype = d.dtype; t.rows_f32 = rows_f32; t.B = B; t.max_q = max_q;
+  t.eps = rule->eps;
+  for (int a = 0, end = 0; a < 3; ++a) {
+    end += a < rule->n_axes ? rule->pairs[a] : 0;
+    t.axis_end[a] = a < rule->n_axes - 1 ? end : 1 << 30;
+  }
+  // turns per position, base^(-2i / rot) / 2 pi: a product per pair, in more bits than are kept
+  const long double step = rule->rot_dim > 0 ? powl((long double)rule->base, -2.0L / rule->rot_dim) : 1.0L;
+  long double f = 1.0L / 6.283185307179586476925286766559L;
+  for (int i = 0; i < rule->rot_dim / 2; ++i, f *= step) t.freq[i] = (double)f;
+  const long units = keys ? cache_row_units(h_spec_len, B, M, kv != nullptr) : 0;
+  t.n_units = (int)units;
+  const long wgs = cache_rows_shape(t);
+  if (wgs > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %d rows take %ld workgroups", who, M, wgs);
+  if (wgs == 0) return MN_OK;
+  {
+    Tap tp(&c->prof, MN_PROF_ROPE_APPEND, (hipStream_t)stream);
+    launch_cache_rows(t, wgs, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
+extern "C" size_t mn_window_workspace_bytes(const mn_ctx* c, int B, int max_rows) {
+  if (!c || B < 0 || B > MN_MAX_BATCH || max_rows < 0 || max_rows > (1 << 20)) return 0;
+  return window_workspace_bytes(B > 0 ? B : 1, max_rows > 0 ? max_rows : 1, c->d.n_heads, c->d.n_kv_heads, c->d.head_dim);
+}
+
+extern "C" mn_status mn_window_attention(mn_ctx* c, const void* q, const int32_t* spec_len, const int32_t* h_spec_len, int B, int window,
+                                         int sinks, int max_ctx, const mn_kv* kv, int layer, void* out, float* stats, void* workspace,
+                                         size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  const char* who = "mn_window_attention";
+  if (!c) return MN_ENULL;
+  if (B < 0 || B > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: B = %d outside [0, %d]", who, B, MN_MAX_BATCH);
+  if (window < 1 || sinks < 0) return fail(c, MN_EINVAL, "%s: a window of %d and %d first tokens", who, window, sinks);
+  if (max_ctx < 0) return fail(c, MN_EINVAL, "%s: max_ctx = %d", who, max_ctx);
+  if (B == 0) return MN_OK;
+  if (!q || !spec_len || !h_spec_len || !out) return fail(c, MN_ENULL, "%s: a required pointer is NULL", who);
+  if (((uintptr_t)q | (uintptr_t)out) & 15) return fail(c, MN_EINVAL, "%s: q and out must be 16-byte aligned", who);
+  if ((uintptr_t)stats & 7) return fail(c, MN_EINVAL, "%s: stats must be 8-byte aligned", who);
+  if (mn_status s = check_kv(c, kv, max_ctx, who)) return s;
+  if (mn_status s = check_page(c, kv, who)) return s;
+  if (mn_status s = check_layer(c, kv, layer, true, who)) return s;
+  if (max_ctx >= (1 << 28)) return fail(c, MN_EUNSUPPORTED, "%s: max_ctx = %d", who, max_ctx);
+  int M = 0, max_q = 0;
+  if (mn_status s = batch_rows(c, h_spec_len, B, &M, &max_q, who)) return s;
+  if (max_ctx < max_q) return fail(c, MN_EINVAL, "%s: max_ctx %d smaller than the longest scored run %d", who, max_ctx, max_q);
+  const mn_model_desc& d = c->d;
+  TileArgs t{};
+  t.kv = layer_view(kv, layer);
+  t.q = q; t.q_stride = (long)d.n_heads * d.head_dim; t.out = out; t.stats = stats;
+  t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.B = B;
+  t.status = dev_status;
+  t.batch.spec_len = spec_len; t.batch.ctx_lens = kv->ctx_lens; t.batch.max_q = max_q; t.batch.max_ctx = max_ctx;
+  t.window = window < max_ctx ? window : max_ctx; t.sinks = sinks < max_ctx ? sinks : max_ctx;
+  t.tile_rows = window_tile_rows(t);
+  long tiles = 0;
+  for (int b = 0; b < B; ++b) tiles += ((long)(h_spec_len[b] + 1) * (d.n_heads / d.n_kv_heads) + t.tile_rows - 1) / t.tile_rows;
+  if (tiles * d.n_kv_heads > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %ld tiles of %d KV heads", who, tiles, d.n_kv_heads);
+  t.n_tiles = (int)tiles;
+  if (const long wgs = window_workgroups(t); wgs > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %d rows take %ld workgroups", who, M, wgs);
+  if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
+  if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
+  const size_t need = window_workspace_bytes(B, M, d.n_heads, d.n_kv_heads, d.head_dim);
+  if (workspace_bytes < need) return fail(c, MN_EWORKSPACE, "%s: workspace %zu bytes, need %zu", who, workspace_bytes, need);
+  hipError_t lerr;
+  {
+    Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);
+    lerr = launch_window(t, workspace, (hipStream_t)stream);
+  }
+  if (lerr != hipSuccess) return fail(c, MN_EHIP, "%s: kernel attribute: %s", who, hipGetErrorString(lerr));
+  return hip_check(c, who);
+}
+
+static mn_status check_ledger(mn_ctx* c, const mn_ledger* l, int B, const char* who) {
+  if (!l || !l->mass || !l->born) return fail(c, MN_ENULL, "%s: ledger or a member of it is NULL", who);
+  if (l->width < 1 || l->width >= (1 << 28)) return fail(c, MN_EINVAL, "%s: ledger lines of %d slots", who, l->width);
+  if (l->max_seqs < 1 || l->max_seqs > MN_MAX_BATCH || B > l->max_seqs) return fail(c, MN_EINVAL, "%s: a ledger of %d slots for %d sequences", who, l->max_seqs, B);
+  return MN_OK;
+}
+
+extern "C" mn_status mn_kv_weigh(mn_ctx* c, const void* q, const float* stats, const int32_t* spec_len, const int32_t* h_spec_len, int B,
+                                 const int32_t* n_out, const int32_t* seen, int max_ctx, const mn_kv* kv, int layer,
+                                 const mn_ledger* ledger, int32_t* dev_status, void* stream) {
+  const char* who = "mn_kv_weigh";
+  if (!c) return MN_ENULL;
+  if (B < 0 || B > MN_MAX_BATCH) return fail(c, MN_EINVAL, "%s: B = %d outside [0, %d]", who, B, MN_MAX_BATCH);
+  if (max_ctx < 0) return fail(c, MN_EINVAL, "%s: max_ctx = %d", who, max_ctx);
+  if (B == 0) return MN_OK;
+  if (!q || !stats || !spec_len || !h_spec_len) return fail(c, MN_ENULL, "%s: a required pointer is NULL", who);
+  if (((uintptr_t)q & 15) || ((uintptr_t)stats & 7)) return fail(c, MN_EINVAL, "%s: q must be 16-byte aligned, stats 8-byte", who);
+  if (mn_status s = check_kv(c, kv, max_ctx, who)) return s;
+  if (mn_status s = check_page(c, kv, who)) return s;
+  if (mn_status s = check_layer(c, kv, layer, false, who)) return s;
+  if (mn_status s = check_ledger(c, ledger, B, who)) return s;
+  if (max_ctx > ledger->width) return fail(c, MN_ECAPACITY, "%s: max_ctx %d exceeds the ledger's %d slots", who, max_ctx, ledger->width);
+  int M = 0, max_q = 0;
+  if (mn_status s = batch_rows(c, h_spec_len, B, &M, &max_q, who)) return s;
+  const mn_model_desc& d = c->d;
+  WeighArgs t{};
+  t.q = q; t.stats = stats; t.spec_len = spec_len; t.n_out = n_out; t.seen = seen; t.ctx_lens = kv->ctx_lens;
+  t.kv = layer_view(kv, layer);
+  const size_t line = (size_t)layer * ledger->max_seqs * d.n_kv_heads * ledger->width;
+  t.mass = ledger->mass + line; t.born = ledger->born + line; t.status = dev_status;
+  t.B = B; t.M = M; t.H = d.n_heads; t.Hkv = d.n_kv_heads; t.hd = d.head_dim; t.dtype = d.dtype; t.max_q = max_q; t.max_ctx = max_ctx; t.width = ledger->width;
+  const long wgs = weigh_workgroups(t);
+  if (wgs > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %d sequences of up to %d tokens take %ld workgroups", who, B, max_ctx, wgs);
+  if (wgs == 0) return MN_OK;
+  {
+    Tap tp(&c->prof, MN_PROF_ATTENTION, (hipStream_t)stream);
+    launch_weigh(t, (hipStream_t)stream);
+  }
+  return hip_check(c, who);
+}
+
+extern "C" size_t mn_evict_workspace_bytes(const mn_ctx* c, int B, int width) {
+  if (!c || B < 0 || B > MN_MAX_BATCH || width < 1 || width >= (1 << 28)) return 0;
+  return evict_work_bytes(B > 0 ? B : 1, page_layers(c), c->d.n_kv_heads, width);
+}
+
+extern "C" mn_status mn_kv_evict(mn_ctx* c, mn_kv* kv, const mn_pool* pool, const int32_t* keep, int B, int sinks, int recent,
+                                 const mn_ledger* ledger, void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  const char* who = "mn_kv_evict";
+  if (!c) return MN_ENULL;
+  PoolView p;
+  if (mn_status s = check_pool(c, kv, pool, B, dev_status, true, who, &p)) return s;
+  if (mn_status s = check_ledger(c, ledger, B, who)) return s;
+  if (ledger->max_seqs != pool->max_seqs) return fail(c, MN_EINVAL, "%s: a ledger of %d slots for a pool of %d", who, ledger->max_seqs, pool->max_seqs);
+  if (sinks < 0 || recent < 0) return fail(c, MN_EINVAL, "%s: %d first and %d recent tokens", who, sinks, recent);
+  if (B == 0) return MN_OK;
+  if (!keep) return fail(c, MN_ENULL, "%s: keep is NULL", who);
+  const long rows = (long)page_layers(c) * B * c->d.n_kv_heads;
+  if (rows > MAX_WORKGROUPS) return fail(c, MN_EUNSUPPORTED, "%s: %ld lines of the ledger", who, rows);
+  if (!workspace) return fail(c, MN_ENULL, "%s: workspace is NULL", who);
+  if ((uintptr_t)workspace & 255) return fail(c, MN_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
+  const size_t need = evict_work_bytes(B, page_layers(c), c->d.n_kv_heads, ledger->width);
+  if (workspace_bytes < need) return fail(c, MN_EWORKSPACE, "%s: workspace %zu bytes, need %zu", who, workspace_bytes, need);
+  EvictArgs t{};
+  t.pool = p; t.keep = keep; t.mass = ledger->mass; t.born = ledger->born;
+  t.B = B; t.Hkv = c->d.n_kv_heads; t.hd = c->d.head_dim; t.dtype = c->d.dtype; t.width = ledger->width; t.sinks = sinks; t.recent = recent;
+  {
+    Tap tp(&c->prof, MN_PROF_ACCEPT, (hipStream_t)stream);
+    launch_evict(t, kv->k_layers, kv->v_layers, page_layers(c), workspace, (hipStream_t)stream);
   }
   return hip_check(c, who);
 }

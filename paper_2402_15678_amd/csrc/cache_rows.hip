@@ -1,0 +1,298 @@
+// Rows of a projection made ready for the cache: every query and key head normed, turned to its token's position, and rounded once;
+// queries to where the attention reads them, keys and values into the pages of their sequences.
+//
+//   y = g x / sqrt(mean(x^2) + eps) over a head;  pair (i, i + rot / 2) of y is turned by the angle p_a(i) base^(-2i / rot),
+// p_a the token's position on the axis that pair i belongs to.  An angle is a fraction of a turn in 64 bits (a far position times a
+// frequency has no correct digit of its angle left in 32), its sine and cosine and everything else are 32 bits.
+//
+// A lane holds eight elements of a head: four, and the four that they are paired with, so that neither the norm's sum (over hd / 8 lanes)
+// nor the rotation goes through the LDS.  Elements behind `rot` are paired likewise and turned by nothing.
+//  * Queries: a wave takes a row, or a share of its heads where there are few rows; a lane's angles serve all of them.
+//  * Keys and values: a workgroup takes the 16 slots of the cache that a page of 16 tokens is, writes them as the page lies into the LDS, and
+//    copies whole pieces of 16 bytes out.  Straight from the rows a value is two bytes of a 32-byte sector.
+#include "launch.h"
+#include "../../include/minions_verify.h"
+
+namespace mn {
+
+constexpr int SLOTS = 16;              // of a workgroup that fills pages
+
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {  // over groups of a power of two of lanes, up to 32
+  if (lanes > 1) v += __uint_as_float(lane_swap<LANE_1>(__float_as_uint(v)));
+  if (lanes > 2) v += __uint_as_float(lane_swap<LANE_2>(__float_as_uint(v)));
+  if (lanes > 4) v += __uint_as_float(lane_swap<LANE_4>(__float_as_uint(v)));
+  if (lanes > 8) v += __uint_as_float(lane_swap<LANE_8>(__float_as_uint(v)));
+  if (lanes > 16) {
+    uint32_t x, y;
+    lane_pair<16>(__float_as_uint(v), x, y);
+    v = __uint_as_float(x) + __uint_as_float(y);
+  }
+  return v;
+}
+
+template <typename T> struct __attribute__((aligned(4 * sizeof(T)))) Quad { T x[4]; };
+
+// The lane's place in a head, and its angles there.
+struct Place {
+  int a, b;                            // its elements a .. a + 3 and b .. b + 3
+  int pair;                            // the first of its pairs, or -1: not turned
+};
+__device__ __forceinline__ Place place_of(int t, int hd, int rot) {
+  const int half = rot / 2;
+  if (4 * t < half) return Place{4 * t, half + 4 * t, 4 * t};
+  const int e = rot + 4 * t - half;
+  return Place{e, e + (hd - rot) / 2, -1};
+}
+__device__ __forceinline__ void angles(const CacheRows& a, int m, int pair, float (&c)[4], float (&s)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { c[e] = 1.f; s[e] = 0.f; }
+  if (pair < 0) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int i = pair + e, axis = (i >= a.axis_end[0]) + (i >= a.axis_end[1]) + (i >= a.axis_end[2]);
+    double turns = (double)a.positions[(size_t)axis * a.M + m] * a.freq[i];
+    turns -= rint(turns);
+    sincospif(2.f * (float)turns, &s[e], &c[e]);
+  }
+}
+
+// Norm and rotation of the lane's elements x of a head (`lanes` lanes hold one).
+__device__ __forceinline__ void ready(float (&x)[8], const float* gain, float eps, int hd, int lanes, const Place& at, const float (&c)[4], const float (&s)[4]) {
+  if (gain) {
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+    const float r = 1.f / sqrtf(lanes_sum(ss, lanes) / (float)hd + eps);
+    const f32x4 ga = *reinterpret_cast<const f32x4_u*>(gain + at.a), gb = *reinterpret_cast<const f32x4_u*>(gain + at.b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[e] *= r * ga[e]; x[4 + e] *= r * gb[e]; }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float u = x[e], v = x[4 + e];
+    x[e] = u * c[e] - v * s[e];
+    x[4 + e] = v * c[e] + u * s[e];
+  }
+}
+template <typename In>
+__device__ __forceinline__ void load8(const In* row, const Place& at, float (&x)[8]) {
+  const Quad<In> u = *reinterpret_cast<const Quad<In>*>(row + at.a), v = *reinterpret_cast<const Quad<In>*>(row + at.b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { x[e] = (float)u.x[e]; x[4 + e] = (float)v.x[e]; }
+}
+template <typename T>
+__device__ __forceinline__ Quad<T> round4(const float* x, bool& bad) {
+  Quad<T> q;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) q.x[e] = sizeof(T) == 2 ? (T)sat_h(x[e], bad) : (T)x[e];
+  return q;
+}
+
+// The sequence of unit u, and which of its units that is: sequence b has (k_b + 1 + 14) / 16 + 1 of them, as many pages as its rows can
+// touch wherever they begin.  Lengths that do not add up to the host's rows and units are reported, and nothing is written.
+__device__ __forceinline__ bool unit_of(const CacheRows& a, int u, int& seq, int& nth, int& row0, int& q) {
+  __shared__ int s_units[4], s_rows[4], s_hit[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int units_at = 0, rows_at = 0;
+  bool off = false;
+  if (tid == 0) s_hit[0] = -1;
+  for (int b0 = 0; b0 < a.B; b0 += 256) {
+    const int b = b0 + tid;
+    int n = 0, units = 0;
+    if (b < a.B) {
+      const int k = a.spec_len[b];
+      off |= k < 0 || k >= a.max_q;
+      n = off ? 0 : k + 1;
+      units = off ? 0 : (n + 14) / SLOTS + 1;
+    }
+    const int ui = wave_scan_i(units), ri = wave_scan_i(n);
+    __syncthreads();
+    if (lane == 63) { s_units[wave] = ui; s_rows[wave] = ri; }
+    __syncthreads();
+    int before = units_at + ui - units, r = rows_at + ri - n;
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) { before += s_units[w]; r += s_rows[w]; }
+      units_at += s_units[w];
+      rows_at += s_rows[w];
+    }
+    if (u >= before && u < before + units) { s_hit[0] = b; s_hit[1] = u - before; s_hit[2] = r; s_hit[3] = n; }
+  }
+  off = __syncthreads_or(off) || units_at != a.n_units || rows_at != a.M;
+  if (off) {
+    if (tid == 0 && u == 0 && a.status) atomicOr(a.status, MN_DEV_SPEC_LEN);
+    return false;
+  }
+  seq = s_hit[0]; nth = s_hit[1]; row0 = s_hit[2]; q = s_hit[3];
+  return seq >= 0;
+}
+
+template <typename In, typename T>
+__global__ void __launch_bounds__(256) cache_rows_kernel(CacheRows a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int tid = threadIdx.x, hd = a.hd, lanes = hd / 8, t = tid & (lanes - 1);
+  const Place at = place_of(t, hd, a.rot);
+  float c[4], s[4];
+  bool bad = false;
+  const int fills = a.n_units * a.unit_splits;
+  if ((int)blockIdx.x >= fills) {
+    // ---- queries ----
+    const int w = ((int)blockIdx.x - fills) * 4 + (tid >> 6), m = w / a.q_splits, part = w - m * a.q_splits;
+    if (m < a.M) {
+      angles(a, m, at.pair, c, s);
+      const int per = 64 / lanes, h0 = part * a.q_heads, h1 = min(a.H, h0 + a.q_heads);
+      const In* row = static_cast<const In*>(a.q) + (size_t)m * a.q_stride;
+      T* out = static_cast<T*>(a.q_out) + (size_t)m * a.H * hd;
+      for (int hw = h0; hw < h1; hw += per) {                        // (whole waves: the sums go across lanes)
+        const int h = hw + (tid & 63) / lanes;
+        float x[8];
+        load8(row + (size_t)min(h, a.H - 1) * hd, at, x);
+        ready(x, a.q_gain, a.eps, hd, lanes, at, c, s);
+        if (h >= h1) continue;
+        *reinterpret_cast<Quad<T>*>(out + (size_t)h * hd + at.a) = round4<T>(x, bad);
+        *reinterpret_cast<Quad<T>*>(out + (size_t)h * hd + at.b) = round4<T>(x + 4, bad);
+      }
+    }
+  } else {
+    // ---- keys and values of up to 16 slots ----
+    const int u = blockIdx.x / a.unit_splits, part = blockIdx.x - u * a.unit_splits;
+    const int bs = a.kv.block_size;
+    int seq = 0, nth = 0, row0 = 0, q = a.M, ctx = 0;
+    if (a.kv.k) {
+      if (!unit_of(a, u, seq, nth, row0, q)) return;
+      ctx = a.ctx_lens[seq];
+      if (ctx < 0 || (long)ctx + q > (long)a.kv.max_blocks_per_seq * bs) {
+        if (tid == 0 && nth == 0 && part == 0 && a.status) atomicOr(a.status, MN_DEV_CTX);
+        return;
+      }
+    } else {
+      nth = u;
+    }
+    const int slot0 = (ctx / SLOTS + nth) * SLOTS, from = max(slot0, ctx), to = min(slot0 + SLOTS, ctx + q);
+    if (from >= to) return;
+    const bool whole = a.kv.k && bs % SLOTS == 0;                  // the slots lie side by side in one block
+    const int32_t* bt = a.kv.k ? a.kv.block_tables + (size_t)seq * a.kv.max_blocks_per_seq : nullptr;
+    const size_t head_page = (size_t)hd * bs;
+    bool lost = false;                                             // a block id out of range
+    uint32_t id = 0;
+    if (whole) {
+      id = (uint32_t)bt[slot0 / bs];
+      lost = id >= (uint32_t)a.kv.num_blocks;
+    }
+    const int off0 = a.kv.k ? slot0 % bs : 0;
+    T* img_k = reinterpret_cast<T*>(smem);                         // [hd / 8][16][8], [hd][16]
+    T* img_v = img_k + hd * SLOTS;
+    const int at_once = 256 / lanes;                               // rows side by side: 8 (heads of 256), 16 and more
+    const int h1 = min(a.Hkv, (part + 1) * a.unit_heads);
+    // (heads of 256: the two halves of the slots have angles of their own)
+    for (int s0 = 0; s0 < SLOTS; s0 += at_once) {
+      const int in = s0 + tid / lanes, slot = slot0 + in, m = row0 + slot - ctx;
+      const bool mine = in < SLOTS && slot >= from && slot < to;
+      const int mm = mine ? m : row0 + from - ctx;
+      angles(a, mm, at.pair, c, s);
+      for (int h = part * a.unit_heads; h < h1; ++h) {
+        float x[8], y[8];
+        load8(static_cast<const In*>(a.k) + (size_t)mm * a.k_stride + (size_t)h * hd, at, x);
+        load8(static_cast<const In*>(a.v) + (size_t)mm * a.v_stride + (size_t)h * hd, at, y);
+        ready(x, a.k_gain, a.eps, hd, lanes, at, c, s);
+        Quad<T> k[2], v[2];
+        if (mine) {
+          k[0] = round4<T>(x, bad); k[1] = round4<T>(x + 4, bad);
+          v[0] = round4<T>(y, bad); v[1] = round4<T>(y + 4, bad);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int el = e ? at.b : at.a;
+            if (a.k_out) *reinterpret_cast<Quad<T>*>(static_cast<T*>(a.k_out) + ((size_t)m * a.Hkv + h) * hd + el) = k[e];
+            if (a.v_out) *reinterpret_cast<Quad<T>*>(static_cast<T*>(a.v_out) + ((size_t)m * a.Hkv + h) * hd + el) = v[e];
+          }
+        }
+        if (!a.kv.k) continue;
+        if (!whole) {
+          if (mine) {
+            const uint32_t block = (uint32_t)bt[slot / bs];
+            const int off = slot % bs;
+            if (block >= (uint32_t)a.kv.num_blocks) {
+              lost = true;
+            } else {
+              const size_t page = ((size_t)block * a.Hkv + h) * head_page;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int el = (e < 4 ? at.a : at.b) + (e & 3);
+                static_cast<T*>(a.kv.k)[page + ((size_t)(el >> 3) * bs + off) * 8 + (el & 7)] = k[e >> 2].x[e & 3];
+                static_cast<T*>(a.kv.v)[page + (size_t)el * bs + off] = v[e >> 2].x[e & 3];
+              }
+            }
+          }
+          continue;
+        }
+        __syncthreads();                                           // (the head before has left)
+        if (mine) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int el = e ? at.b : at.a;
+            *reinterpret_cast<Quad<T>*>(img_k + ((el >> 3) * SLOTS + in) * 8 + (el & 7)) = k[e];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) img_v[(el + i) * SLOTS + in] = v[e].x[i];
+          }
+        }
+        __syncthreads();
+        if (lost) continue;
+        const size_t page = ((size_t)id * a.Hkv + h) * head_page;
+        constexpr int PER = 16 / sizeof(T);                        // elements of a piece
+        T* pk = static_cast<T*>(a.kv.k) + page;
+        T* pv = static_cast<T*>(a.kv.v) + page;
+        const int lo = max(from - slot0, s0), hi = min(to - slot0, s0 + at_once);
+        for (int i = tid; i < hd * SLOTS / PER; i += 256) {
+          const int e = i * PER;
+          const int ks = e / 8 % SLOTS;                            // K: a piece is of one token
+          if (ks >= lo && ks < hi) *reinterpret_cast<u32x4*>(pk + ((size_t)(e / (8 * SLOTS)) * bs + off0 + ks) * 8 + e % 8) = *reinterpret_cast<const u32x4*>(img_k + e);
+          const int vs = e % SLOTS;                                // V: of several
+          T* out = pv + (size_t)(e / SLOTS) * bs + off0 + vs;
+          if (vs >= lo && vs + PER <= hi) {
+            *reinterpret_cast<u32x4*>(out) = *reinterpret_cast<const u32x4*>(img_v + e);
+          } else {
+            for (int j = 0; j < PER; ++j)
+              if (vs + j >= lo && vs + j < hi) out[j] = img_v[e + j];
+          }
+        }
+      }
+    }
+    if (lost && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+  }
+  if (sizeof(T) == 2 && bad && a.status) atomicOr(a.status, MN_DEV_RANGE);
+}
+
+long cache_row_units(const int32_t* h_spec_len, int B, int M, bool pages) {
+  if (!pages) return ((long)M + SLOTS - 1) / SLOTS;
+  long n = 0;
+  for (int b = 0; b < B; ++b) n += (h_spec_len[b] + 15) / SLOTS + 1;
+  return n;
+}
+
+// Shares of the heads: whole rows where there are enough of them.
+static void split_heads(int heads, long items, int least, long want, int& splits, int& each) {
+  long n = want / (items > 0 ? items : 1);
+  if (n > heads / least) n = heads / least;
+  if (n < 1) n = 1;
+  each = (int)((heads + n - 1) / n);
+  splits = (heads + each - 1) / each;
+}
+
+long cache_rows_shape(CacheRows& a) {
+  const int per = 64 / (a.hd / 8);                                 // heads that a wave holds at once
+  split_heads(a.H, a.M, per, 2048, a.q_splits, a.q_heads);
+  a.q_heads = (a.q_heads + per - 1) / per * per;
+  a.q_splits = (a.H + a.q_heads - 1) / a.q_heads;
+  split_heads(a.Hkv, a.n_units, 1, 512, a.unit_splits, a.unit_heads);
+  return (long)a.n_units * a.unit_splits + (a.q_out ? ((long)a.M * a.q_splits + 3) / 4 : 0);
+}
+
+hipError_t launch_cache_rows(const CacheRows& a, long workgroups, hipStream_t st) {
+  const bool wide = a.rows_f32 != 0;
+  const size_t lds = a.kv.k ? (size_t)2 * a.hd * SLOTS * (a.dtype == MN_DT_BF16 ? 2 : 4) : 0;
+  if (a.dtype == MN_DT_F32) cache_rows_kernel<float, float><<<(unsigned)workgroups, 256, lds, st>>>(a);
+  else if (wide) cache_rows_kernel<float, f16_t><<<(unsigned)workgroups, 256, lds, st>>>(a);
+  else cache_rows_kernel<f16_t, f16_t><<<(unsigned)workgroups, 256, lds, st>>>(a);
+  return hipSuccess;
+}
+
+}  // namespace mn

@@ -202,6 +202,11 @@ struct TileArgs {
   float *o_part, *ml_part;  // [slot][M][H][hd] and [slot][M][H][2]: outputs, (reference, sum)
   int prefix_units, n_units, share, n_streams, prefix_slots, row_tiles;  // the shared part (stream_item)
   int32_t* seq_bad;         // [B] whether a table row is damaged; behind them the first sharer, if there is a work list
+  // windows
+  int window, sinks;        // keys that a row sees: the last `window` ones, and those below `sinks`
+  int ranges, n_checks;     // ranges of a tile's keys; workgroups that look at table rows
+  int keep_keys;            // whether more than one tile of a sequence reads its keys
+  float* stats;             // [M][H][2] (reference, sum) of the rows, or null
 };
 struct PrefixPlan {
   PrefixBatch batch;
@@ -218,13 +223,44 @@ struct PrefixMerge {
   PrefixBatch batch;
   int M, H, Hkv, hd, prefix_slots, prefix_units, n_units, share, row_tiles;
 };
+struct WindowPlan {
+  PrefixBatch batch;
+  int n_tiles;
+  int32_t* items;
+  int4* row_meta;           // [M] (sequence or -1, context, rows, first row)
+  int32_t* status;
+};
 long prefix_workgroups(const TileArgs& a);
+int window_tile_rows(const TileArgs& a);
+long window_workgroups(const TileArgs& a);
+size_t window_workspace_bytes(int B, int M, int H, int Hkv, int hd);
+hipError_t launch_window(TileArgs a, void* workspace, hipStream_t st);
 bool prefix_fits(int M, int H, int Hkv, int prefix_len);
 size_t prefix_workspace_bytes(int B, int M, int H, int Hkv, int hd, int prefix_len, int max_ctx);
 hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st);
 int prompt_tile_rows(const TileArgs& a, long stack_rows);
 hipError_t launch_prompt(const TileArgs& a, hipStream_t st);
 constexpr long MAX_WORKGROUPS = (1l << 24) - 1;  // of 256 threads: a grid has fewer than 2^32
+
+// ---- cache_rows.hip ----
+struct CacheRows {
+  const void *q, *k, *v;    // rows [M][H][hd], [M][Hkv][hd]: fp32, or the activation type
+  long q_stride, k_stride, v_stride;
+  void *q_out, *k_out, *v_out;  // dense rows of the activation type, or null
+  const float *q_gain, *k_gain;
+  const int32_t *positions;     // [axes][M]
+  const int32_t *spec_len, *ctx_lens;
+  KvView kv;                // k null: no pages are written
+  int32_t* status;
+  int M, H, Hkv, hd, rot, dtype, rows_f32, B, max_q;
+  float eps;
+  int axis_end[3];          // the first pair behind the axis
+  int n_units, unit_splits, unit_heads, q_splits, q_heads;  // workgroups of keys and values, shares of the heads (cache_rows_shape)
+  double freq[128];         // turns of pair i per position
+};
+long cache_row_units(const int32_t* h_spec_len, int B, int M, bool pages);
+long cache_rows_shape(CacheRows& a);  // workgroups
+hipError_t launch_cache_rows(const CacheRows& a, long workgroups, hipStream_t st);
 
 // ---- pool.hip ----
 struct PoolView {
@@ -250,5 +286,30 @@ void launch_reserve(const PoolView& p, const int32_t* tokens, int B, void* const
                     void* workspace, hipStream_t st);
 void launch_compact(const PoolView& p, int32_t* n_live, void* const* k, void* const* v, int n_layers, size_t page_bytes, void* workspace,
                     hipStream_t st);
+
+// ---- evict.hip ----
+struct WeighArgs {
+  const void* q;            // [M][H][hd] activation type
+  const float* stats;       // [M][H][2]
+  const int32_t *spec_len, *n_out, *seen, *ctx_lens;  // [B]; n_out, seen may be null
+  KvView kv;
+  float* mass;              // [B][Hkv][width] of the layer
+  int32_t* born;
+  int32_t* status;
+  int B, M, H, Hkv, hd, dtype, max_q, max_ctx, width;
+};
+long weigh_workgroups(const WeighArgs& a);
+void launch_weigh(const WeighArgs& a, hipStream_t st);
+struct EvictArgs {
+  PoolView pool;
+  const int32_t* keep;      // [B]
+  float* mass;              // [layers][max_seqs][Hkv][width]
+  int32_t* born;
+  int32_t *gone, *n_moves;  // [B], [layers * B * Hkv]
+  int2* moves;              // [layers * B * Hkv][2][width / 2] (slot, block)
+  int B, Hkv, hd, dtype, width, sinks, recent, splits;
+};
+size_t evict_work_bytes(int B, int n_layers, int Hkv, int width);
+void launch_evict(EvictArgs a, void* const* k, void* const* v, int n_layers, void* workspace, hipStream_t st);
 
 }  // namespace mn

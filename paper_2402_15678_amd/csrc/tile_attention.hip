@@ -1,5 +1,5 @@
-// Attention of many query rows over the same keys, as tiles of a dense product: whole prompts (packed rows, causal) and batches whose
-// sequences share a prefix of the paged cache.
+// Attention of many query rows over the same keys, as tiles of a dense product: whole prompts (packed rows, causal), batches whose
+// sequences share a prefix of the paged cache, and rows that see a window of it and its first few tokens.
 //
 // o_r = sum_j p_rj v_j / sum_j p_rj with p_rj = 2^(c s_rj - m_r), s_rj = q_r . k_j, c = log2(e) / sqrt(head_dim), in one pass over the
 // keys with a running reference m_r.  The G query heads of a KV head are stacked: row r of the stack is query head r % G of token
@@ -9,6 +9,7 @@
 //    LDS for all the waves of a workgroup.
 //  * tile_f32_kernel    every other type, head_dim and block size: 16x16x4 fp32 matrix instructions.
 //  * prefix_plan_kernel, prefix_merge_kernel   the work list of a shared-prefix call, and the sum of its parts.
+//  * window_plan_kernel, window_merge_kernel   the same of a windowed call.
 #include "launch.h"
 #include "tune.h"
 #include "../../include/minions_verify.h"
@@ -250,6 +251,142 @@ __device__ __forceinline__ void check_table(const TileArgs& a, int b) {
   }
 }
 
+// ---- windows: the row at position p sees the keys p - window + 1 .. p and those below `sinks` ----
+// A tile's keys in granules of 16 (a page of the fp16 kernel): the first ones, sg of them, then those from sg + jump on, where the window
+// of the tile's first row begins.  Entry i of that list is granule at(i); an item takes the entries [i0, i1).
+struct Look {
+  int sg, jump, i0, i1;
+  __device__ __forceinline__ int at(int i) const { return i + (i >= sg ? jump : 0); }
+  __device__ __forceinline__ int entry(int granule) const { return granule - (granule >= sg + jump ? jump : 0); }  // (of a visible one)
+};
+constexpr int GRAIN = 16;
+// Negative where the row sees the e-th key from here on: it has `ahead` keys in front of it, `back` of them behind its window, and `sink` first
+// ones.  Signs, and no conditions: sixteen of those at once are more than the scalar registers hold.
+__device__ __forceinline__ int in_sight(int e, int ahead, int back, int sink) { return ~(ahead - e) & ((back - e) | (e - sink)); }
+constexpr int NO_KEY = 1 << 30;        // behind every position
+
+// The list of the tile whose first and last rows are at the positions p0 and p1.
+__device__ __forceinline__ Look look_from(const TileArgs& a, int p0, int p1, int& entries) {
+  Look k;
+  const int lo = max(0, p0 - a.window + 1), first = lo / GRAIN;
+  k.sg = min((a.sinks + GRAIN - 1) / GRAIN, first);
+  k.jump = first - k.sg;
+  entries = k.sg + p1 / GRAIN + 1 - first;
+  k.i0 = 0;
+  k.i1 = entries;
+  return k;
+}
+
+// What takes part, for up to 64 sequences: lane b has sequence b's rows, its first row, and its row tiles.  Lengths that do not add up to the
+// host's rows and tiles, or a run longer than its longest one, disable the batch (off); a context outside [0, max_ctx) its sequence, whose
+// tiles are there all the same: somebody has to write its zeros.
+struct WindowShare {
+  int q, row0, ctx, tiles, flags;
+  bool off;
+};
+__device__ __forceinline__ bool window_fits(const PrefixBatch& p, int ctx, int q) { return ctx >= 0 && (long)ctx + q <= p.max_ctx; }
+__device__ __forceinline__ WindowShare lane_window(const PrefixBatch& p, int n_tiles) {
+  const int b = threadIdx.x & 63;
+  WindowShare s{0, 0, 0, 0, 0, false};
+  bool off = false;
+  if (b < p.B) {
+    const int k = p.spec_len[b];
+    s.ctx = p.ctx_lens[b];
+    off = k < 0 || k >= p.max_q;
+    s.q = off ? 0 : k + 1;
+    s.tiles = (int)(((long)p.G * s.q + p.tile_rows - 1) / p.tile_rows);
+    if (!window_fits(p, s.ctx, s.q)) s.flags = MN_DEV_CTX;
+  }
+  const int incl = wave_scan_i(s.q);
+  s.row0 = incl - s.q;
+  s.off = __any(off) || __builtin_amdgcn_readlane(incl, 63) != p.M || __builtin_amdgcn_readfirstlane(wave_sum_i(s.tiles)) != n_tiles;
+  if (s.off) s.flags = MN_DEV_SPEC_LEN;
+  return s;
+}
+
+// Tile t of the batch; false: the batch takes no part.  it.R < 0: the sequence does not (|R| rows of zeros).  The last tiles of a sequence
+// come first: where the window is longer than the context they have the most keys.
+__device__ __forceinline__ bool window_tile(const TileArgs& a, int t, Item& it) {
+  if (a.items) {
+    const int4 x = reinterpret_cast<const int4*>(a.items)[2 * t], y = reinterpret_cast<const int4*>(a.items)[2 * t + 1];
+    it = Item{x.x, x.y, x.z, 0, 0, y.y, y.z, 0};
+    return it.R != 0;
+  }
+  const WindowShare s = lane_window(a.batch, a.n_tiles);
+  if ((int)blockIdx.x == a.n_checks && threadIdx.x < 64 && s.flags && a.status) atomicOr(a.status, s.flags);
+  if (s.off) return false;
+  const int incl = wave_scan_i(s.tiles);
+  const int b = __ffsll((unsigned long long)__ballot(t < incl)) - 1;
+  const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, b); };
+  it.m0 = of(s.row0); it.ctx = of(s.ctx); it.seq = b; it.slot = 0; it.key0 = it.key_end = 0;
+  it.rbase = (of(incl) - 1 - t) * a.batch.tile_rows;
+  it.R = a.batch.G * of(s.q) * (of(s.flags) ? -1 : 1);
+  return true;
+}
+
+// Zeros for the rows of this workgroup's tile and head (R rows of the stack at most), or, of a batch that takes no part, for its share of all.
+template <typename T>
+__device__ __forceinline__ void window_zeros(const TileArgs& a, const Item* it, int kvh, int G) {
+  struct __attribute__((aligned(4 * sizeof(T)))) Four0 { T x[4]; };
+  const int per = a.hd / 4;
+  const auto clear = [&](size_t mh, int e) {
+    reinterpret_cast<Four0*>(a.out)[mh * per + e] = Four0{};
+    if (e == 0 && a.stats) *reinterpret_cast<float2*>(a.stats + 2 * mh) = make_float2(0.f, 0.f);
+  };
+  if (it) {
+    for (int i = threadIdx.x; i < min(-it->R - it->rbase, a.batch.tile_rows) * per; i += blockDim.x) {
+      const int r = it->rbase + i / per, j = r / G;
+      clear((size_t)(it->m0 + j) * a.H + kvh * G + r - j * G, i % per);
+    }
+  } else {
+    const size_t all = (size_t)a.M * a.H * per;
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (size_t)gridDim.x * blockDim.x) clear(i / per, (int)(i % per));
+  }
+}
+
+// The item of workgroup wg (behind those that look at the table rows, if there are any).
+template <typename T>
+__device__ __forceinline__ bool window_item(const TileArgs& a, int wg, int G, int& kvh, Item& it, Look& look) {
+  kvh = wg % a.Hkv;
+  const int at = wg / a.Hkv, t = at / a.ranges, range = at - t * a.ranges;
+  if (!window_tile(a, t, it)) {
+    if (a.ranges == 1) window_zeros<T>(a, nullptr, kvh, G);
+    return false;
+  }
+  if (it.R < 0) {
+    if (a.ranges == 1) window_zeros<T>(a, &it, kvh, G);
+    return false;
+  }
+  const int p1 = it.ctx + (min(it.R, it.rbase + a.batch.tile_rows) - 1) / G;
+  int entries;
+  look = look_from(a, it.ctx + it.rbase / G, p1, entries);
+  look.i0 = range * a.batch.chunk;
+  look.i1 = min(entries, look.i0 + a.batch.chunk);
+  it.key_end = p1 + 1;
+  it.slot = range;
+  return look.i0 < look.i1;
+}
+
+// Whether an entry of sequence `seq`'s table row that its rows look at is out of range (the whole workgroup asks).
+__device__ __forceinline__ bool window_table_bad(const TileArgs& a, int seq, int ctx, int q) {
+  const int bs = a.kv.block_size, end = ctx + q, first = max(0, ctx - a.window + 1) / bs, n_first = min(first, (min(a.sinks, end) + bs - 1) / bs);
+  const int32_t* row = a.kv.block_tables + (size_t)seq * a.kv.max_blocks_per_seq;
+  const int all = n_first + (end - 1) / bs + 1 - first;
+  bool bad = false;
+  for (int i = threadIdx.x; i < all; i += blockDim.x) bad |= (uint32_t)row[i < n_first ? i : i - n_first + first] >= (uint32_t)a.kv.num_blocks;
+  return __syncthreads_or(bad);
+}
+// For the calls whose rows are put together from parts: a workgroup per sequence.
+__device__ __forceinline__ void window_check(const TileArgs& a, int b) {
+  const int ctx = scalar(a.batch.ctx_lens)[b], k = scalar(a.batch.spec_len)[b];
+  if (k < 0 || k >= a.batch.max_q || !window_fits(a.batch, ctx, k + 1)) return;  // (takes no part)
+  const bool bad = window_table_bad(a, b, ctx, k + 1);
+  if (threadIdx.x == 0) {
+    a.seq_bad[b] = bad;
+    if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+  }
+}
+
 // Rows of K and V of the tokens whose first stack row lies in this tile, into the pages (position = token of the sequence).
 template <typename T, int ROWS>
 __device__ __forceinline__ void append_rows(const TileArgs& a, const Item& it, int G, int kvh) {
@@ -325,8 +462,9 @@ __device__ __forceinline__ float top(const f32x4 (&S)[2]) {
   return m(m(m(m(S[0][0], S[0][1]), S[0][2]), m(m(S[0][3], S[1][0]), S[1][1])), m(S[1][2], S[1][3]));
 }
 
-template <int HDIM, int CT, int NW, bool PAGED>
+template <int HDIM, int CT, int NW, bool PAGED, bool WINDOW>
 __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
+  static_assert(PAGED || !WINDOW, "windows are of pages");
   using St = TileStage<HDIM>;
   constexpr int HS = St::HS, NU = St::NU, KP = St::KP, LPW = St::FRAGS / NW, ROWS = 16 * CT * NW;
   static_assert(St::FRAGS % NW == 0, "whole pieces per wave");
@@ -339,8 +477,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
   const int G = by.d;
   int kvh = 0, stream = 0, unit = 0;
   Item it;
+  Look look{};
   bool more = false;
-  if constexpr (PAGED) {
+  if constexpr (WINDOW) {
+    const int wg = (int)blockIdx.x - a.n_checks;
+    if (wg < 0) return window_check(a, blockIdx.x);
+    if (!window_item<f16_t>(a, wg, G, kvh, it, look)) return;
+  } else if constexpr (PAGED) {
     // a workgroup per table row, those of the sequences' own keys, the streams
     const int own = a.n_tiles * a.Hkv, wg = (int)blockIdx.x - a.B;
     if (wg < 0) return check_table(a, blockIdx.x);
@@ -390,7 +533,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // ---- staging: waves 0 and 1 fetch K, 2 and 3 V, each the 16 keys (the block) that its parity names, 1 KB of whole rows or of a whole
     // page per load.  The 16-byte chunks of a row, and of a page, change places inside 256 bytes on the way, so that the reads of
     // the operands meet every bank (`turn`). ----
-    const int n_tiles = (it.key_end - it.key0 + TK - 1) / TK;
+    const int n_tiles = WINDOW ? (look.i1 - look.i0 + 1) / 2 : (it.key_end - it.key0 + TK - 1) / TK;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem);
     const int last_key = it.key_end - 1;
     const bool k_wave = wave < NW / 2;
@@ -400,7 +543,10 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     const const_i32* bt = PAGED ? scalar(a.kv.block_tables + (size_t)it.seq * a.kv.max_blocks_per_seq) : nullptr;
     const uint32_t blk_bytes = PAGED ? (uint32_t)a.Hkv * (HDIM * PAGE) * 2u : 0u;
     int next_id = 0;
-    const auto ask_id = [&](int tile) { next_id = bt[min((it.key0 + min(tile, n_tiles - 1) * TK) / PAGE + side, last_key / PAGE)]; };
+    const auto ask_id = [&](int tile) {
+      if constexpr (WINDOW) next_id = bt[look.at(min(look.i0 + 2 * tile + side, look.i1 - 1))];
+      else next_id = bt[min((it.key0 + min(tile, n_tiles - 1) * TK) / PAGE + side, last_key / PAGE)];
+    };
     // dense rows
     constexpr int CH = HDIM / 8, KPP = 64 / CH;                    // 16-byte chunks per row, rows per piece
     const uint32_t stride = (uint32_t)(k_wave ? a.k_stride : a.v_stride) * 2u;
@@ -433,7 +579,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       if constexpr (PAGED) {
         const char* p = base + (uint64_t)min((uint32_t)next_id, (uint32_t)a.kv.num_blocks - 1u) * blk_bytes;
         // (keys that no other tile of rows reads are not kept in the L2)
-        if (more && a.row_tiles > 1) pieces<LPW>([&](auto i) { dma16s<i.value * 1024, false>(p, off0, to + i.value * 1024u); });
+        if (WINDOW ? a.keep_keys : (more && a.row_tiles > 1)) pieces<LPW>([&](auto i) { dma16s<i.value * 1024, false>(p, off0, to + i.value * 1024u); });
         else pieces<LPW>([&](auto i) { dma16s<i.value * 1024, true>(p, off0, to + i.value * 1024u); });
         ask_id(tile + 1);
       } else {
@@ -502,15 +648,30 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // the half behind the next and the values of the next are on their way from the LDS: the matrix pipe and the vector unit both
     // have work, and neither waits for the LDS.
     f16x8 kf[2 * HS], vf[NU], P[CT];
-    const auto first = [&](int k0, const unsigned char* next_keys, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2]) {
-      const int keyg = k0 + 8 * g;
-      const bool masked = k0 + 31 > min_lim;                       // (uniform) a key that some row does not see
+    const auto first = [&](int tile, const unsigned char* next_keys, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2]) {
+      int keyg;                                                    // the lane's eight keys
+      bool masked;                                                 // (uniform) a key that some row does not see
+      if constexpr (WINDOW) {
+        const int i = look.i0 + 2 * tile + (g >> 1);
+        keyg = i < look.i1 ? look.at(i) * PAGE + 8 * (g & 1) : NO_KEY;
+        masked = __any((keyg + 7 > min_lim) | ((keyg <= max_lim - a.window) & (keyg + 7 >= a.sinks)));
+      } else {
+        const int k0 = it.key0 + tile * TK;
+        keyg = k0 + 8 * g;
+        masked = k0 + 31 > min_lim;
+      }
       if (masked) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
+          if constexpr (WINDOW) {
+            const int ahead = lim[ct] - keyg, back = ahead - a.window, sink = a.sinks - keyg;
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (keyg + e > lim[ct]) S[ct][e >> 2][e & 3] = -INFINITY;
+            for (int e = 0; e < 8; ++e) S[ct][e >> 2][e & 3] = in_sight(e, ahead, back, sink) < 0 ? S[ct][e >> 2][e & 3] : -INFINITY;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (keyg + e > lim[ct]) S[ct][e >> 2][e & 3] = -INFINITY;
+          }
           tm[ct] = top(S[ct]);
         }
         if constexpr (PAGED) {
@@ -577,11 +738,21 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
               }
 #pragma unroll
               for (int ct = 0; ct < CT; ++ct) {
-                int ahead = lim[ct] - keyg;
-                asm volatile("" : "+v"(ahead));                    // (worked out anew each time: registers)
                 f16x8 sees;
+                if constexpr (WINDOW) {
+                  // (worked out anew each time: registers)
+                  int ahead = lim[ct] - keyg, sink = a.sinks - keyg;
+                  asm volatile("" : "+v"(ahead), "+v"(sink));
+                  const int back = ahead - a.window;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sees[e] = e <= ahead ? (f16_t)1.f : (f16_t)0.f;
+                  for (int e = 0; e < 8; ++e)
+                    sees[e] = __builtin_bit_cast(f16_t, (uint16_t)(in_sight(e, ahead, back, sink) >> 31 & 0x3c00));  // 1.0 or 0
+                } else {
+                  int ahead = lim[ct] - keyg;
+                  asm volatile("" : "+v"(ahead));
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) sees[e] = e <= ahead ? (f16_t)1.f : (f16_t)0.f;
+                }
                 const f32x4 met = __builtin_amdgcn_mfma_f32_16x16x32_f16(at.v, sees, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -625,7 +796,14 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       __builtin_amdgcn_sched_barrier(0);
     };
 
-    const int n_wave = min(n_tiles, max(0, max_lim + TK - it.key0) / TK);  // tiles that a row of the wave sees
+    // (what only the end asks for waits in vector registers: of the scalar ones there are not enough)
+    const auto aside = [](int v) {
+      if constexpr (WINDOW) asm volatile("" : "+v"(v));
+      return v;
+    };
+    const int end_m0 = aside(it.m0), end_seq = aside(it.seq), end_ctx = aside(it.ctx), end_slot = aside(it.slot), end_kvh = aside(kvh);
+    // tiles that a row of the wave sees
+    const int n_wave = WINDOW ? (rows ? min(n_tiles, max(0, look.entry(max_lim / PAGE) - look.i0 + 2) / 2) : 0) : min(n_tiles, max(0, max_lim + TK - it.key0) / TK);
     __syncthreads();                                               // (the search, or the piece before, is through with the LDS)
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
@@ -645,7 +823,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     // (its values are in the registers), and its place, or that of tile i - 1, is filled again.
     const auto tile = [&](int i, f32x4 (&S)[CT][2], float (&tm)[CT], f32x4 (&Sn)[CT][2], float (&tn)[CT]) {
       const bool on = i < n_wave;                                  // (uniform)
-      if (on) first(it.key0 + i * TK, slot(i + 1), S, tm, Sn);
+      if (on) first(i, slot(i + 1), S, tm, Sn);
       if (AHEAD > 3 && i + 3 < n_tiles) wait_vm<(AHEAD - 3) * LPW>();
       else wait_vm<0>();
       __syncthreads();
@@ -659,6 +837,16 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     wait_vm<0>();                                                  // (of a dense item's first stages, any past its end)
 
     // ---- output: lane holds O^T[16u + 4g + i][row l16], and its row's sum ----
+    if constexpr (WINDOW) {
+      it.m0 = __builtin_amdgcn_readfirstlane(end_m0); it.seq = __builtin_amdgcn_readfirstlane(end_seq); it.ctx = __builtin_amdgcn_readfirstlane(end_ctx);
+      it.slot = __builtin_amdgcn_readfirstlane(end_slot); kvh = __builtin_amdgcn_readfirstlane(end_kvh);
+      if (a.ranges == 1 && window_table_bad(a, it.seq, it.ctx, it.R / G)) {
+        if (tid == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+        it.R = -it.R;
+        window_zeros<f16_t>(a, &it, kvh, G);
+        return;
+      }
+    }
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
       uint32_t x, y;                                               // the row's sum over the four lane groups
@@ -670,12 +858,13 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       if (r >= it.R) continue;
       const int j = by(r), m = it.m0 + j, h = kvh * G + r - j * G;
       const float l = L[ct];
-      if constexpr (PAGED) {
+      if (PAGED && !(WINDOW && a.ranges == 1)) {
         float* o = a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * HDIM + 4 * g;
 #pragma unroll
         for (int u = 0; u < NU; ++u) *reinterpret_cast<f32x4*>(o + 16 * u) = O[ct][u];
         if (g == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(run_m[ct], l);
       } else {
+        if (WINDOW && a.stats && g == 0) *reinterpret_cast<float2*>(a.stats + ((size_t)m * a.H + h) * 2) = make_float2(run_m[ct], l);
         const float inv = 1.f / l;
         f16_t* o = static_cast<f16_t*>(a.out) + ((size_t)m * a.H + h) * HDIM + 4 * g;
 #pragma unroll
@@ -738,7 +927,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
       }
       if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
     }
-  } while (more && stream_item(a, stream, unit, kvh, it));
+  } while (!WINDOW && more && stream_item(a, stream, unit, kvh, it));
 }
 
 // ------------------------------------------------------------------------------------------
@@ -757,7 +946,7 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
 constexpr int FROWS = 16, KW = 4;                                // rows of a workgroup, its waves
 template <typename T> struct __attribute__((aligned(4 * sizeof(T)))) Four { T x[4]; };
 
-template <typename T, int HDP, bool PAGED>
+template <typename T, int HDP, bool PAGED, bool WINDOW>
 __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_kernel(TileArgs a) {
   constexpr int NU = HDP / 16, LD = HDP + 4, HALVES = HDP == 256 ? 1 : 2;  // (16 keys at a time: registers)
   constexpr int KEYS = 16 * HALVES;
@@ -767,8 +956,13 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
   const int G = by.d;
   int kvh = 0, stream = 0, unit = 0;
   Item it;
+  Look look{};
   bool more = false;
-  if constexpr (PAGED) {
+  if constexpr (WINDOW) {
+    const int wg = (int)blockIdx.x - a.n_checks;
+    if (wg < 0) return window_check(a, blockIdx.x);
+    if (!window_item<T>(a, wg, G, kvh, it, look)) return;
+  } else if constexpr (PAGED) {
     // a workgroup per table row, those of the sequences' own keys, the streams
     const int own = a.n_tiles * a.Hkv, wg = (int)blockIdx.x - a.B;
     if (wg < 0) return check_table(a, blockIdx.x);
@@ -814,15 +1008,26 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
     const int shift = (bs & (bs - 1)) == 0 ? 31 - __clz(bs) : -1;
     const auto block_of = [&](int key) { return shift >= 0 ? key >> shift : key / bs; };
     const auto page_of = [&](int key) { return ((size_t)min((uint32_t)bt[block_of(key)], (uint32_t)a.kv.num_blocks - 1u) * a.Hkv + kvh) * (size_t)(hd * bs); };
-    for (int k0 = it.key0 + part * KEYS; k0 <= max_lim; k0 += KW * KEYS) {
+    // (windows: from entry to entry of the list, up to the last that a row sees)
+    const int from = WINDOW ? look.i0 + part * HALVES : it.key0 + part * KEYS;
+    const int upto = WINDOW ? min(look.i1 - 1, look.entry(max_lim / GRAIN)) : max_lim;
+    for (int at = from; at <= upto; at += WINDOW ? KW * HALVES : KW * KEYS) {
       const int last = it.key_end - 1;
+      const auto half_key = [&](int h) {                         // the first key of half h
+        if constexpr (WINDOW) return at + h < look.i1 ? look.at(at + h) * GRAIN : NO_KEY;
+        else return at + 16 * h;
+      };
+      const auto hidden = [&](int key) {
+        if constexpr (WINDOW) return (key > lim) | ((key <= lim - a.window) & (key >= a.sinks));  // (without branches)
+        else return key > lim;
+      };
       // ---- scores ----
       f32x4 S[HALVES];
       const T* kr[HALVES];
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
         S[h] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        const int key = min(k0 + 16 * h + l16, last);
+        const int key = min(half_key(h) + l16, last);
         if constexpr (PAGED) kr[h] = static_cast<const T*>(a.kv.k) + page_of(key) + (size_t)(key - block_of(key) * bs) * 8;
         else kr[h] = static_cast<const T*>(a.k) + (size_t)(it.m0 + key) * a.k_stride + (size_t)kvh * hd;
       }
@@ -840,7 +1045,7 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
         if constexpr (PAGED) {
-          const int key = k0 + 16 * h + 4 * g;
+          const int key = half_key(h) + 4 * g;
           const size_t page = page_of(min(key, last));
 #pragma unroll
           for (int u = 0; u < NU; ++u) {
@@ -864,7 +1069,7 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
           // four keys: four instructions of VEC elements for each of the NU / VEC groups
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const T* v = static_cast<const T*>(a.v) + (size_t)(it.m0 + min(k0 + 16 * h + 4 * g + e, last)) * a.v_stride + (size_t)kvh * hd;
+            const T* v = static_cast<const T*>(a.v) + (size_t)(it.m0 + min(half_key(h) + 4 * g + e, last)) * a.v_stride + (size_t)kvh * hd;
 #pragma unroll
             for (int n = 0; n < NU / VEC; ++n) {
               struct __attribute__((aligned(VEC * sizeof(T)))) Some { T x[VEC]; };
@@ -887,7 +1092,7 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
       for (int h = 0; h < HALVES; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (k0 + 16 * h + 4 * g + e > lim) S[h][e] = -INFINITY;
+          S[h][e] = hidden(half_key(h) + 4 * g + e) ? -INFINITY : S[h][e];
           tm = fmaxf(tm, S[h][e]);
         }
       if (__any(tm > run_m)) {
@@ -902,7 +1107,15 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
 #pragma unroll
         for (int u = 0; u < NU; ++u) O[u] *= alpha;
       }
-      if (k0 + KEYS - 1 > min_lim) {                             // values that are not finite, as above
+      bool masked;                                               // (uniform) a key that some row does not see
+      if constexpr (WINDOW) {
+        masked = false;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) masked |= half_key(h) + 15 > min_lim || !(half_key(h) > max_lim - a.window || half_key(h) + 15 < a.sinks);
+      } else {
+        masked = at + KEYS - 1 > min_lim;
+      }
+      if (masked) {                                              // values that are not finite, as above
         float odd = 0.f;
 #pragma unroll
         for (int h = 0; h < HALVES; ++h)
@@ -917,7 +1130,7 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
             for (int u = 0; u < NU; ++u)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const float v = (float)vx[h][u].x[e], sees = k0 + 16 * h + 4 * g + e <= lim ? 1.f : 0.f;
+                const float v = (float)vx[h][u].x[e], sees = hidden(half_key(h) + 4 * g + e) ? 0.f : 1.f;
                 const bool up = !(v < INFINITY), down = !(v > -INFINITY);
                 const f32x4 a = __builtin_amdgcn_mfma_f32_16x16x4f32(up ? 1.f : 0.f, sees, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
                 const f32x4 b = __builtin_amdgcn_mfma_f32_16x16x4f32(down ? 1.f : 0.f, sees, (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
@@ -949,6 +1162,14 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
     lane_pair<32>(__float_as_uint(run_l), x, y);
     run_l = __uint_as_float(x) + __uint_as_float(y);
     // element of O[u][i] in this lane
+    if constexpr (WINDOW) {
+      if (a.ranges == 1 && window_table_bad(a, it.seq, it.ctx, it.R / G)) {
+        if (tid == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+        it.R = -it.R;
+        window_zeros<T>(a, &it, kvh, G);
+        return;
+      }
+    }
     const auto element = [&](int u, int i) { return u / VEC * (16 * VEC) + VEC * (4 * g + i) + u % VEC; };
     float* s_o = reinterpret_cast<float*>(smem);               // [KW][16][LD]
     float2* s_ml = reinterpret_cast<float2*>(smem + KW * 16 * LD * 4);
@@ -975,17 +1196,18 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
         o += *reinterpret_cast<const f32x4*>(s_o + (w * 16 + row) * LD + e0) * f;
       }
       const int jj = by(rr), m = it.m0 + jj, h = kvh * G + rr - jj * G;
-      if constexpr (PAGED) {
+      if (PAGED && !(WINDOW && a.ranges == 1)) {
         *reinterpret_cast<f32x4*>(a.o_part + (((size_t)it.slot * a.M + m) * a.H + h) * hd + e0) = o;
         if (e0 == 0) *reinterpret_cast<float2*>(a.ml_part + (((size_t)it.slot * a.M + m) * a.H + h) * 2) = make_float2(top, l);
       } else {
+        if (WINDOW && a.stats && e0 == 0) *reinterpret_cast<float2*>(a.stats + ((size_t)m * a.H + h) * 2) = make_float2(top, l);
         Four<T> w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w.x[e] = (T)(o[e] / l);
         *reinterpret_cast<Four<T>*>(static_cast<T*>(a.out) + ((size_t)m * a.H + h) * hd + e0) = w;
       }
     }
-  } while (more && stream_item(a, stream, unit, kvh, it));
+  } while (!WINDOW && more && stream_item(a, stream, unit, kvh, it));
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1069,14 +1291,72 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlan p) {
 // and many slots (6 rows of 64 heads, 33 slots: 4.6 us, with one 10).  Bound by
 // HBM where there are many rows: 576 rows of 64 heads of 128, 71 MB of parts, 16 us.
 constexpr int AT_ONCE = 4;
-template <typename T, int GROUPS>
-__global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
+// The parts of row-head mh in the slots at(0) .. at(n - 1), put together (o, l, top: its output, its sum and their reference).  False: a
+// thread of another group than the first, which has no more to do.
+template <int GROUPS, typename F>
+__device__ __forceinline__ bool sum_slots(const float* o_part, const float* ml_part, size_t heads, int hd, size_t i, size_t mh, int n, F at_slot, f32x4& o,
+                                          float& l, float& top) {
   constexpr int WIDE = 256 / GROUPS;
   __shared__ float s_top[GROUPS][WIDE], s_l[GROUPS][WIDE];
   __shared__ f32x4 s_o[GROUPS][WIDE];
+  const int group = threadIdx.x / WIDE, lane_at = threadIdx.x % WIDE;
+  o = (f32x4){0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+  top = -INFINITY;
+  for (int s0 = group; s0 < n; s0 += AT_ONCE * GROUPS) {
+    float2 ml[AT_ONCE];
+    f32x4 v[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int at = at_slot(min(s0 + u * GROUPS, n - 1));
+      ml[u] = *reinterpret_cast<const float2*>(ml_part + (at * heads + mh) * 2);
+      v[u] = *reinterpret_cast<const f32x4*>(o_part + at * heads * hd + 4 * i);
+    }
+    float nm = top;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) nm = fmaxf(nm, ml[u].x);
+    const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const bool in = s0 + u * GROUPS < n;                       // (what is not finite counts once, and not at all times 0)
+      const float w = in ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
+      l += ml[u].y * w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += in ? v[u][e] * w : 0.f;
+    }
+    top = nm;
+  }
+  if constexpr (GROUPS > 1) {
+    s_top[group][lane_at] = top;
+    s_l[group][lane_at] = l;
+    s_o[group][lane_at] = o;
+    __syncthreads();
+    if (group > 0) return false;
+    float nm = top;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) nm = fmaxf(nm, s_top[g][lane_at]);
+    const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+      const float w = __builtin_amdgcn_exp2f(s_top[g][lane_at] - ref);
+      l += s_l[g][lane_at] * w;
+      o += s_o[g][lane_at] * w;
+    }
+    top = nm;
+  }
+  return true;
+}
+
+template <typename T, int GROUPS>
+__global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __restrict__ out) {
+  constexpr int WIDE = 256 / GROUPS;
   const size_t heads = (size_t)p.M * p.H;
-  const int group = threadIdx.x / WIDE, lane_at = threadIdx.x % WIDE, per = p.hd / 4;
-  const size_t i = min((size_t)blockIdx.x * WIDE + lane_at, heads * per - 1), mh = i / per;  // (past the end: the last ones once more)
+  const int per = p.hd / 4;
+  const size_t i = min((size_t)blockIdx.x * WIDE + threadIdx.x % WIDE, heads * per - 1), mh = i / per;  // (past the end: the last ones once more)
   const int m = (int)(mh / p.H), h = (int)(mh - (size_t)m * p.H), G = p.H / p.Hkv, kvh = h / G;
   int2 meta = make_int2(0, 0);                                   // sequence, ranges of its own keys
   if (p.row_meta) {
@@ -1092,64 +1372,126 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __r
       if (m == r) meta = make_int2(b, ranges);
     }
   }
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f, top = -INFINITY;
   const bool takes_part = meta.y > 0 && !p.seq_bad[meta.x];
-  if (takes_part) {
-    int shared = 0;                                              // streams that met the row's tile
-    if (p.n_units > 0) {
-      const int first = (kvh * p.row_tiles + (m * G + h - kvh * G) / p.batch.tile_rows) * p.prefix_units;
-      shared = (first + p.prefix_units - 1) / p.share - first / p.share + 1;
-    }
-    const int n = shared + meta.y;
-    for (int s0 = group; s0 < n; s0 += AT_ONCE * GROUPS) {
-      float2 ml[AT_ONCE];
-      f32x4 v[AT_ONCE];
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const int s = min(s0 + u * GROUPS, n - 1), at = s < shared ? s : p.prefix_slots + s - shared;
-        ml[u] = *reinterpret_cast<const float2*>(p.ml_part + (at * heads + mh) * 2);
-        v[u] = *reinterpret_cast<const f32x4*>(p.o_part + at * heads * p.hd + 4 * i);
-      }
-      float nm = top;
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) nm = fmaxf(nm, ml[u].x);
-      const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
-      l *= keep;
-      o *= keep;
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const bool in = s0 + u * GROUPS < n;                     // (what is not finite counts once, and not at all times 0)
-        const float w = in ? __builtin_amdgcn_exp2f(ml[u].x - ref) : 0.f;
-        l += ml[u].y * w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += in ? v[u][e] * w : 0.f;
-      }
-      top = nm;
-    }
+  int shared = 0;                                                // streams that met the row's tile
+  if (takes_part && p.n_units > 0) {
+    const int first = (kvh * p.row_tiles + (m * G + h - kvh * G) / p.batch.tile_rows) * p.prefix_units;
+    shared = (first + p.prefix_units - 1) / p.share - first / p.share + 1;
   }
-  if constexpr (GROUPS > 1) {
-    s_top[group][lane_at] = top;
-    s_l[group][lane_at] = l;
-    s_o[group][lane_at] = o;
-    __syncthreads();
-    if (group > 0) return;
-    float nm = top;
-#pragma unroll
-    for (int g = 1; g < GROUPS; ++g) nm = fmaxf(nm, s_top[g][lane_at]);
-    const float ref = nm == -INFINITY ? 0.f : nm, keep = __builtin_amdgcn_exp2f(top - ref);
-    l *= keep;
-    o *= keep;
-#pragma unroll
-    for (int g = 1; g < GROUPS; ++g) {
-      const float w = __builtin_amdgcn_exp2f(s_top[g][lane_at] - ref);
-      l += s_l[g][lane_at] * w;
-      o += s_o[g][lane_at] * w;
-    }
-  }
+  f32x4 o;
+  float l, top;
+  if (!sum_slots<GROUPS>(p.o_part, p.ml_part, heads, p.hd, i, mh, takes_part ? shared + meta.y : 0,
+                         [&](int s) { return s < shared ? s : p.prefix_slots + s - shared; }, o, l, top))
+    return;
   const float inv = takes_part ? 1.f / l : 0.f;                  // (a row whose scores are all -inf is no number, as without a prefix)
 #pragma unroll
   for (int e = 0; e < 4; ++e) out[4 * i + e] = (T)(o[e] * inv);
+}
+
+// ------------------------------------------------------------------------------------------
+// windows
+// ------------------------------------------------------------------------------------------
+// A row tile's keys are a list of granules (Look), in one range where the tiles fill the chip by themselves: the workgroup then writes
+// the rows' outputs, and there is no second launch.  Otherwise in several, whose parts window_merge_kernel puts together.
+//
+// window_plan_kernel (one workgroup; more than 64 sequences): the tiles' records (window_tile), and per row its sequence (-1: takes no part),
+// context, rows and first row.
+__global__ void __launch_bounds__(1024) window_plan_kernel(WindowPlan p) {
+  __shared__ int s_rows[16], s_tiles[16], s_bad;
+  const PrefixBatch& c = p.batch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  const auto length = [&](int b) {
+    const int k = c.spec_len[b];
+    return k >= 0 && k < c.max_q ? k + 1 : -1;
+  };
+  const auto tiles_of = [&](int q) { return (int)(((long)c.G * q + c.tile_rows - 1) / c.tile_rows); };
+  // lengths first: rows or tiles that do not add up to the host's, or a run longer than its longest, disable the batch
+  int rows = 0, tiles = 0;
+  bool off = false;
+  for (int b = tid; b < c.B; b += 1024) {
+    const int q = length(b);
+    off |= q < 0;
+    rows += max(q, 0);
+    tiles += tiles_of(max(q, 0));
+  }
+  rows = wave_sum_i(rows);
+  tiles = wave_sum_i(tiles);
+  if (lane == 0) { s_rows[wave] = rows; s_tiles[wave] = tiles; }
+  if (off) s_bad = 1;
+  __syncthreads();
+  int total = 0, total_tiles = 0;
+  for (int w = 0; w < 16; ++w) { total += s_rows[w]; total_tiles += s_tiles[w]; }
+  const bool batch = s_bad == 0 && total == c.M && total_tiles == p.n_tiles;
+  int flags = batch ? 0 : MN_DEV_SPEC_LEN;
+  int4* items = reinterpret_cast<int4*>(p.items);
+  if (!batch) {
+    for (int m = tid; m < c.M; m += 1024) p.row_meta[m] = make_int4(-1, 0, 0, 0);
+    for (int i = tid; i < p.n_tiles; i += 1024) items[2 * i] = items[2 * i + 1] = make_int4(0, 0, 0, 0);
+  }
+  int row_at = 0, item_at = 0;
+  for (int b0 = 0; batch && b0 < c.B; b0 += 1024) {
+    const int b = b0 + tid, q = b < c.B ? length(b) : 0, n = tiles_of(q);
+    const int rows_incl = wave_scan_i(q), tiles_incl = wave_scan_i(n);
+    __syncthreads();
+    if (lane == 63) { s_rows[wave] = rows_incl; s_tiles[wave] = tiles_incl; }
+    __syncthreads();
+    int row0 = row_at + rows_incl - q, at = item_at + tiles_incl - n;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) { row0 += s_rows[w]; at += s_tiles[w]; }
+      row_at += s_rows[w];
+      item_at += s_tiles[w];
+    }
+    if (b >= c.B) continue;
+    const int ctx = c.ctx_lens[b];
+    const bool fits = window_fits(c, ctx, q);
+    if (!fits) flags |= MN_DEV_CTX;
+    for (int j = 0; j < q; ++j) p.row_meta[row0 + j] = make_int4(fits ? b : -1, ctx, q, row0);
+    for (int i = 0; i < n; ++i) {
+      items[2 * (at + i)] = make_int4(row0, c.G * q * (fits ? 1 : -1), (n - 1 - i) * c.tile_rows, 0);
+      items[2 * (at + i) + 1] = make_int4(0, ctx, b, 0);
+    }
+  }
+  if (flags && p.status) atomicOr(p.status, flags);
+}
+
+template <typename T, int GROUPS>
+__global__ void __launch_bounds__(256) window_merge_kernel(TileArgs a, const int4* __restrict__ row_meta, T* __restrict__ out) {
+  constexpr int WIDE = 256 / GROUPS;
+  const size_t heads = (size_t)a.M * a.H;
+  const int per = a.hd / 4;
+  const size_t i = min((size_t)blockIdx.x * WIDE + threadIdx.x % WIDE, heads * per - 1), mh = i / per;  // (past the end: the last ones once more)
+  const int m = (int)(mh / a.H), h = (int)(mh - (size_t)m * a.H), G = a.H / a.Hkv;
+  int4 meta = make_int4(-1, 0, 0, 0);                            // sequence, context, rows, first row
+  if (row_meta) {
+    meta = row_meta[m];
+  } else {
+    const WindowShare s = lane_window(a.batch, a.n_tiles);
+    const int m0 = __builtin_amdgcn_readfirstlane(m), m1 = __builtin_amdgcn_readlane(m, 63);
+    for (int r = m0; r <= m1; ++r) {
+      const uint64_t has = __ballot(!s.off && s.flags == 0 && r >= s.row0 && r < s.row0 + s.q);
+      if (has == 0) continue;
+      const int b = __ffsll((unsigned long long)has) - 1;
+      const int4 x = make_int4(b, __builtin_amdgcn_readlane(s.ctx, b), __builtin_amdgcn_readlane(s.q, b), __builtin_amdgcn_readlane(s.row0, b));
+      if (m == r) meta = x;
+    }
+  }
+  const bool takes_part = meta.x >= 0 && !a.seq_bad[meta.x];
+  int ranges = 0;
+  if (takes_part) {
+    const int R = G * meta.z, rbase = ((m - meta.w) * G + h % G) / a.batch.tile_rows * a.batch.tile_rows;
+    int entries;
+    look_from(a, meta.y + rbase / G, meta.y + (min(R, rbase + a.batch.tile_rows) - 1) / G, entries);
+    ranges = (entries + a.batch.chunk - 1) / a.batch.chunk;
+  }
+  f32x4 o;
+  float l, top;
+  if (!sum_slots<GROUPS>(a.o_part, a.ml_part, heads, a.hd, i, mh, ranges, [](int s) { return s; }, o, l, top)) return;
+  const float inv = takes_part ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[4 * i + e] = (T)(o[e] * inv);
+  if (a.stats && i % per == 0) *reinterpret_cast<float2*>(a.stats + 2 * mh) = takes_part ? make_float2(top, l) : make_float2(0.f, 0.f);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1176,42 +1518,48 @@ static hipError_t allow_lds(K kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <int HDIM, int CT, bool PAGED>
+template <bool PAGED, bool WINDOW>
+static unsigned tile_workgroups(const TileArgs& a) {
+  const unsigned tiles = (unsigned)a.n_tiles * (unsigned)a.Hkv;
+  return WINDOW ? tiles * (unsigned)a.ranges + (unsigned)a.n_checks : tiles + (PAGED ? (unsigned)(a.n_streams + a.B) : 0u);
+}
+
+template <int HDIM, int CT, bool PAGED, bool WINDOW>
 static hipError_t launch_mfma_as(const TileArgs& a, hipStream_t st) {
   constexpr size_t lds = STAGES * TileStage<HDIM>::BYTES;
   static std::once_flag once;
   static hipError_t err = hipSuccess;
-  std::call_once(once, [] { err = allow_lds(tile_mfma_kernel<HDIM, CT, 4, PAGED>, lds); });
+  std::call_once(once, [] { err = allow_lds(tile_mfma_kernel<HDIM, CT, 4, PAGED, WINDOW>, lds); });
   if (err != hipSuccess) return err;
-  tile_mfma_kernel<HDIM, CT, 4, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (PAGED ? (unsigned)(a.n_streams + a.B) : 0u), 256, lds, st>>>(a);
+  tile_mfma_kernel<HDIM, CT, 4, PAGED, WINDOW><<<tile_workgroups<PAGED, WINDOW>(a), 256, lds, st>>>(a);
   return hipSuccess;
 }
-template <bool PAGED>
+template <bool PAGED, bool WINDOW = false>
 static hipError_t launch_mfma(const TileArgs& a, int tile_rows, hipStream_t st) {
-  if (a.hd == 128) return tile_rows == 128 ? launch_mfma_as<128, 2, PAGED>(a, st) : launch_mfma_as<128, 1, PAGED>(a, st);
-  return tile_rows == 128 ? launch_mfma_as<64, 2, PAGED>(a, st) : launch_mfma_as<64, 1, PAGED>(a, st);
+  if (a.hd == 128) return tile_rows == 128 ? launch_mfma_as<128, 2, PAGED, WINDOW>(a, st) : launch_mfma_as<128, 1, PAGED, WINDOW>(a, st);
+  return tile_rows == 128 ? launch_mfma_as<64, 2, PAGED, WINDOW>(a, st) : launch_mfma_as<64, 1, PAGED, WINDOW>(a, st);
 }
 
-template <typename T, int HDP, bool PAGED>
+template <typename T, int HDP, bool PAGED, bool WINDOW>
 static hipError_t launch_f32(const TileArgs& a, hipStream_t st) {
   constexpr size_t parts = (size_t)KW * 16 * ((HDP + 4) * 4 + 8);
   static std::once_flag once;
   static hipError_t err = hipSuccess;
-  std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED>, parts); });
+  std::call_once(once, [] { err = allow_lds(tile_f32_kernel<T, HDP, PAGED, WINDOW>, parts); });
   if (err != hipSuccess) return err;
   const size_t list = PAGED || a.B <= 64 ? 0 : (size_t)a.B * 4;  // (the search's numbers)
-  tile_f32_kernel<T, HDP, PAGED><<<(unsigned)a.n_tiles * (unsigned)a.Hkv + (PAGED ? (unsigned)(a.n_streams + a.B) : 0u), 64 * KW, parts > list ? parts : list, st>>>(a);
+  tile_f32_kernel<T, HDP, PAGED, WINDOW><<<tile_workgroups<PAGED, WINDOW>(a), 64 * KW, parts > list ? parts : list, st>>>(a);
   return hipSuccess;
 }
 
-template <typename T, bool PAGED>
+template <typename T, bool PAGED, bool WINDOW = false>
 static hipError_t launch_f32_hd(const TileArgs& a, hipStream_t st) {
   switch (a.hd) {
-    case 8: case 16: return launch_f32<T, 16, PAGED>(a, st);
-    case 32: return launch_f32<T, 32, PAGED>(a, st);
-    case 64: return launch_f32<T, 64, PAGED>(a, st);
-    case 128: return launch_f32<T, 128, PAGED>(a, st);
-    default: return launch_f32<T, 256, PAGED>(a, st);
+    case 8: case 16: return launch_f32<T, 16, PAGED, WINDOW>(a, st);
+    case 32: return launch_f32<T, 32, PAGED, WINDOW>(a, st);
+    case 64: return launch_f32<T, 64, PAGED, WINDOW>(a, st);
+    case 128: return launch_f32<T, 128, PAGED, WINDOW>(a, st);
+    default: return launch_f32<T, 256, PAGED, WINDOW>(a, st);
   }
 }
 
@@ -1330,6 +1678,95 @@ hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st) {
   const PrefixMerge g{a.o_part, a.ml_part, meta, a.seq_bad, a.batch, a.M, a.H, a.Hkv, a.hd, s.slots, s.units, s.n_units, s.share, s.row_tiles};
   if (a.dtype == MN_DT_BF16) launch_prefix_merge(g, static_cast<f16_t*>(a.out), st);
   else launch_prefix_merge(g, static_cast<float*>(a.out), st);
+  return hipSuccess;
+}
+
+// Shape of a windowed launch.  Rows of a tile: 128 where a sequence's run fills most of them, as behind a prefix.
+constexpr int WINDOW_RANGES = 16;      // of a tile's keys at most
+constexpr int MIN_GRAINS = 16;         // granules of a range at least
+int window_tile_rows(const TileArgs& a) {
+  if (!tile_mfma(a, true)) return FROWS;
+  if (const int f = MN_TUNE("MN_TILE", 0)) return f;
+  return (long)(a.H / a.Hkv) * a.batch.max_q >= 96 ? 128 : 64;
+}
+struct WindowShape {
+  int ranges, chunk;
+};
+static WindowShape window_shape(const TileArgs& a) {
+  const long tokens = (a.tile_rows + a.H / a.Hkv - 1) / (a.H / a.Hkv) + 1;
+  // granules that the longest tile meets
+  long seen = a.window < a.batch.max_ctx ? a.window : a.batch.max_ctx;
+  seen = (seen + tokens + a.sinks) / GRAIN + 3;
+  const long all = (a.batch.max_ctx + GRAIN - 1) / GRAIN;
+  if (seen > all) seen = all;
+  const int target = MN_TUNE("MN_WGS", STREAMS);
+  long ranges = target / ((long)a.n_tiles * a.Hkv);
+  const long by_keys = seen / MIN_GRAINS;
+  if (ranges > by_keys) ranges = by_keys;
+  if (ranges > WINDOW_RANGES) ranges = WINDOW_RANGES;
+  if (ranges < 1) ranges = 1;
+  const int chunk = (int)((seen + ranges - 1) / ranges + 1) / 2 * 2;
+  return WindowShape{(int)((seen + chunk - 1) / chunk), chunk};
+}
+struct WindowLayout {
+  size_t bad, meta, items, ml_part, o_part, total;
+};
+// (everything here grows with B and M: a workspace for the largest batch serves every smaller one)
+static WindowLayout window_layout(int B, int M, int H, int Hkv, int hd) {
+  WindowLayout L;
+  const long G = H / Hkv;
+  // ranges * tiles * KV heads <= STREAMS where there is more than one, and a tile has 128 rows at most
+  const long a = (long)WINDOW_RANGES * M * H, b = (long)STREAMS * 128;
+  const size_t rows = (size_t)(a < b ? a : b);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 4095) & ~(size_t)4095; return o; };
+  L.bad = take((size_t)B * 4);
+  L.meta = take(B > 64 ? (size_t)M * 16 : 0);
+  L.items = take(B > 64 ? ((size_t)((G * M + 15) / 16) + B) * 32 : 0);
+  L.ml_part = take(rows * 8);
+  L.o_part = take(rows * hd * 4);
+  L.total = at;
+  return L;
+}
+size_t window_workspace_bytes(int B, int M, int H, int Hkv, int hd) { return window_layout(B, M, H, Hkv, hd).total; }
+// Workgroups of a call's largest launch (a.n_tiles, a.tile_rows set).
+long window_workgroups(const TileArgs& a) {
+  const WindowShape s = window_shape(a);
+  const long tiles = (long)a.n_tiles * a.Hkv * s.ranges + a.B, merge = s.ranges > 1 ? ((long)a.M * a.H * (a.hd / 4) + 31) / 32 : 0;
+  return tiles > merge ? tiles : merge;
+}
+
+template <typename T>
+static void launch_window_merge(const TileArgs& a, const int4* meta, hipStream_t st) {
+  const size_t threads = (size_t)a.M * a.H * (a.hd / 4);
+  if (a.ranges >= 8 && threads * 8 <= 512 * 256) window_merge_kernel<T, 8><<<(unsigned)((threads + 31) / 32), 256, 0, st>>>(a, meta, static_cast<T*>(a.out));
+  else window_merge_kernel<T, 1><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(a, meta, static_cast<T*>(a.out));
+}
+
+// a.batch: spec_len, ctx_lens, max_q and max_ctx are the caller's, as are tile_rows and n_tiles (by window_tile_rows)
+hipError_t launch_window(TileArgs a, void* workspace, hipStream_t st) {
+  const WindowLayout L = window_layout(a.B, a.M, a.H, a.Hkv, a.hd);
+  const WindowShape s = window_shape(a);
+  unsigned char* w = static_cast<unsigned char*>(workspace);
+  a.batch.B = a.B; a.batch.M = a.M; a.batch.G = a.H / a.Hkv; a.batch.tile_rows = a.tile_rows; a.batch.chunk = s.chunk;
+  a.ranges = s.ranges;
+  a.n_checks = s.ranges > 1 ? a.B : 0;
+  a.keep_keys = a.n_tiles > a.B;                                 // (other tiles of the sequence read them as well)
+  a.seq_bad = reinterpret_cast<int32_t*>(w + L.bad);
+  a.o_part = reinterpret_cast<float*>(w + L.o_part); a.ml_part = reinterpret_cast<float*>(w + L.ml_part);
+  int4* meta = nullptr;
+  if (a.B > 64) {
+    meta = reinterpret_cast<int4*>(w + L.meta);
+    int32_t* items = reinterpret_cast<int32_t*>(w + L.items);
+    a.items = items;
+    window_plan_kernel<<<1, 1024, 0, st>>>(WindowPlan{a.batch, a.n_tiles, items, meta, a.status});
+  }
+  hipError_t e;
+  if (!tile_mfma(a, true)) e = a.dtype == MN_DT_BF16 ? launch_f32_hd<f16_t, true, true>(a, st) : launch_f32_hd<float, true, true>(a, st);
+  else e = launch_mfma<true, true>(a, a.tile_rows, st);
+  if (e != hipSuccess || a.ranges == 1) return e;
+  if (a.dtype == MN_DT_BF16) launch_window_merge<f16_t>(a, meta, st);
+  else launch_window_merge<float>(a, meta, st);
   return hipSuccess;
 }
 

@@ -247,6 +247,92 @@ class PrefixSession:
         return out
 
 
+class RowRule:
+    """How projected rows are made ready: rot_dim elements of a head turned, pairs[a] of their pairs by the position on axis a, and norms
+    per head where there are gains."""
+
+    def __init__(self, rot_dim: int, pairs: Sequence[int], base: float = 10000.0, q_gain: Optional[torch.Tensor] = None,
+                 k_gain: Optional[torch.Tensor] = None, eps: float = 1e-5):
+        assert 1 <= len(pairs) <= B.MN_MAX_AXES
+        for g in (q_gain, k_gain):
+            assert g is None or (g.dtype == torch.float32 and g.is_contiguous())
+        self.gains, self.n_axes = (q_gain, k_gain), len(pairs)      # (keeps the tensors alive)
+        self.c = B.RowRule(q_gain.data_ptr() if q_gain is not None else None, k_gain.data_ptr() if k_gain is not None else None, eps, rot_dim,
+                           len(pairs), (C.c_int * B.MN_MAX_AXES)(*pairs), base)
+
+
+def qk_norm_rope(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rule: RowRule, positions: Optional[torch.Tensor],
+                 spec_len: Optional[torch.Tensor], h_spec_len: Sequence[int], q_out: Optional[torch.Tensor], kv: Optional[DeviceKV] = None,
+                 layer: int = 0, k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                 dev_status: Optional[torch.Tensor] = None) -> None:
+    """Projected rows (fp32 or the activation type; views with any row stride) normed per head, turned to positions [axes][M] and rounded:
+    queries into q_out, keys and values into the cache behind ctx_lens and, where given, into dense rows."""
+    d = model.desc
+    M, p = sum(h_spec_len) + len(h_spec_len), lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    assert q.dtype == k.dtype == v.dtype and q.dtype in (torch.float32, activation_type(d))
+    assert q.shape == (M, d.n_heads, d.head_dim) and k.shape == v.shape == (M, d.n_kv_heads, d.head_dim)
+    assert q.stride()[1:] == k.stride()[1:] == v.stride()[1:] == (d.head_dim, 1)
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == rule.n_axes * M)
+    for t, heads in ((q_out, d.n_heads), (k_out, d.n_kv_heads), (v_out, d.n_kv_heads)):
+        assert t is None or (t.is_contiguous() and t.dtype == activation_type(d) and t.numel() == M * heads * d.head_dim)
+    B.mn_qk_norm_rope(model.ctx, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                      1 if q.dtype == torch.float32 else 0, rule.c, p(positions), p(spec_len), B.host_i32(h_spec_len), len(h_spec_len),
+                      kv.c if kv is not None else None, layer, p(q_out), p(k_out), p(v_out), p(dev_status), stream_ptr())
+
+
+class WindowSession:
+    """Workspace for attention that looks back `window` tokens and at the first `sinks`, of batches of up to B sequences / max_rows rows,
+    max_q of one sequence."""
+
+    def __init__(self, model: DeviceModel, kv: DeviceKV, B_: int, max_rows: int, max_q: int, max_ctx: int, window: int, sinks: int):
+        self.model, self.kv, self.max_q, self.max_ctx, self.window, self.sinks = model, kv, max_q, max_ctx, window, sinks
+        self.ws_bytes = B.mn_window_workspace_bytes(model.ctx, B_, max_rows)
+        if self.ws_bytes == 0:
+            raise RuntimeError("mn_window_workspace_bytes rejected the shape")
+        dev = kv.block_tables.device
+        self.workspace = torch.empty((self.ws_bytes,), dtype=torch.uint8, device=dev)
+        self.dev_status = torch.zeros((1,), dtype=torch.int32, device=dev)
+
+    def attention(self, q: torch.Tensor, spec_len: torch.Tensor, h_spec_len: Sequence[int], out: torch.Tensor, layer: int = 0,
+                  stats: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """q [rows][H][hd] in the slots ctx_b .. ctx_b + spec_len[b], whose keys are in the cache; out [rows][H * hd]; stats
+        [rows][H][2], for KVLedger.weigh."""
+        assert q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype == activation_type(self.model.desc)
+        assert stats is None or (stats.is_contiguous() and stats.dtype == torch.float32)
+        assert len(h_spec_len) == 0 or max(h_spec_len) < self.max_q
+        B.mn_window_attention(self.model.ctx, q.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len), self.window,
+                              self.sinks, self.max_ctx, self.kv.c, layer, out.data_ptr(), stats.data_ptr() if stats is not None else None,
+                              self.workspace.data_ptr(), self.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
+        return out
+
+
+class KVLedger:
+    """What is known of the cached tokens: the attention weight that each has been given, and its number in the text, [layers][slots]
+    [Hkv][width] both."""
+
+    def __init__(self, model: DeviceModel, kv: DeviceKV, mass: torch.Tensor, born: torch.Tensor):
+        assert mass.dtype == torch.float32 and born.dtype == torch.int32 and mass.is_contiguous() and born.is_contiguous()
+        assert mass.shape == born.shape and mass.shape[0] == max(1, model.desc.n_layers) and mass.shape[2] == model.desc.n_kv_heads
+        self.model, self.kv, self.mass, self.born = model, kv, mass, born
+        self.c = B.Ledger(mass.data_ptr(), born.data_ptr(), mass.shape[1], mass.shape[3])
+        self.dev_status = torch.zeros((1,), dtype=torch.int32, device=mass.device)
+
+    @classmethod
+    def empty(cls, model: DeviceModel, kv: DeviceKV, max_seqs: int, width: int) -> "KVLedger":
+        shape = (max(1, model.desc.n_layers), max_seqs, model.desc.n_kv_heads, width)
+        dev = kv.block_tables.device
+        return cls(model, kv, torch.zeros(shape, dtype=torch.float32, device=dev), torch.zeros(shape, dtype=torch.int32, device=dev))
+
+    def weigh(self, q: torch.Tensor, stats: torch.Tensor, spec_len: torch.Tensor, h_spec_len: Sequence[int], layer: int, max_ctx: int,
+              n_out: Optional[torch.Tensor] = None, seen: Optional[torch.Tensor] = None) -> None:
+        """Adds up the weights that the rows gave (stats: as WindowSession.attention left them without a window); n_out: behind the commit,
+        the rows that it accepted; seen: the texts' tokens before the rows."""
+        assert q.is_contiguous() and q.dtype == activation_type(self.model.desc) and stats.is_contiguous() and stats.dtype == torch.float32
+        B.mn_kv_weigh(self.model.ctx, q.data_ptr(), stats.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len),
+                      n_out.data_ptr() if n_out is not None else None, seen.data_ptr() if seen is not None else None, max_ctx, self.kv.c,
+                      layer, self.c, self.dev_status.data_ptr(), stream_ptr())
+
+
 class KVPool:
     """Which slot of a DeviceKV's table holds which blocks (mn_kv_*): forked requests share pages, every slot gets room ahead of
     its next tokens, finished ones give their blocks back, and the pool can be packed.  The whole mapping (table, references,
@@ -296,6 +382,19 @@ class KVPool:
         B.mn_kv_compact(self.model.ctx, self.kv.c, self.c, self.n_live.data_ptr(), self.workspace.data_ptr(), self.ws_bytes,
                         self.dev_status.data_ptr(), stream_ptr())
         return self.n_live
+
+    def evict(self, keep: torch.Tensor, sinks: int, recent: int, ledger: KVLedger) -> None:
+        """Slots 0 .. len(keep) - 1 are cut back to keep[b] tokens: the first `sinks`, the `recent` newest, and those with the most weight
+        in the ledger."""
+        n, width = keep.numel(), int(ledger.mass.shape[3])
+        if getattr(self, "_evict_for", (0, 0)) < (n, width) or self._evict_for[1] < width:
+            self.evict_bytes = B.mn_evict_workspace_bytes(self.model.ctx, n, width)
+            if self.evict_bytes == 0:
+                raise RuntimeError("mn_evict_workspace_bytes rejected the shape")
+            self.evict_workspace = torch.empty((self.evict_bytes,), dtype=torch.uint8, device=self.state.device)
+            self._evict_for = (n, width)
+        B.mn_kv_evict(self.model.ctx, self.kv.c, self.c, keep.data_ptr(), n, sinks, recent, ledger.c, self.evict_workspace.data_ptr(),
+                      self.evict_bytes, self.dev_status.data_ptr(), stream_ptr())
 
 
 class VerifySession:

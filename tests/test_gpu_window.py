@@ -1,0 +1,328 @@
+"""Windowed attention over the paged cache (mn_window_attention) against the definition in 64 bits, every element within the bound of
+attention_bounds.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2402_15678_amd import synth
+from tests.attention_bounds import attend, check
+
+pytestmark = pytest.mark.gpu
+DT = {"f16": torch.float16, "f32": torch.float32}
+LOG2E = 1.4426950408889634
+
+
+class Batch:
+    """Sequences with ctx[b] cached tokens and ks[b] + 1 query rows behind them.  Slots that hold no token are not a number; table
+    entries that no row looks at are out of range."""
+
+    def __init__(self, H, Hkv, hd, kind, ctx, ks, window, sinks, seed, bs=16, scale=1.0, blind=True, spare=0):
+        from paper_2402_15678_amd import harness
+        self.kind, self.ctx, self.ks, self.H, self.Hkv, self.hd, self.bs, self.window, self.sinks = kind, list(ctx), list(ks), H, Hkv, hd, bs, window, sinks
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        self.tot = [c + k + 1 for c, k in zip(ctx, ks)]
+        need = [-(-t // bs) for t in self.tot]
+        nb = sum(need) + spare
+        ids = np.random.default_rng(seed).permutation(nb).astype(np.int32)
+        self.full = np.full((len(ks), max(need)), -1, np.int32)
+        self.kp = torch.full((nb, Hkv, hd // 8, bs, 8), float("nan"), dtype=DT[kind], device="cuda")
+        self.vp = torch.full((nb, Hkv, hd, bs), float("nan"), dtype=DT[kind], device="cuda")
+        at = 0
+        for b, m in enumerate(need):
+            self.full[b, :m] = ids[at:at + m]
+            at += m
+            n = self.tot[b]
+            k = torch.randn((m * bs, Hkv, hd), generator=g, device="cuda").to(DT[kind])
+            v = torch.randn((m * bs, Hkv, hd), generator=g, device="cuda").to(DT[kind])
+            k[n:], v[n:] = float("nan"), float("nan")
+            blk = torch.from_numpy(self.full[b, :m].astype(np.int64)).cuda()
+            self.kp[blk] = k.view(m, bs, Hkv, hd // 8, 8).permute(0, 2, 3, 1, 4).contiguous()
+            self.vp[blk] = v.view(m, bs, Hkv, hd).permute(0, 2, 3, 1).contiguous()
+        self.table = self.full.copy()
+        if blind:
+            for b, c in enumerate(ctx):
+                first = max(0, c - window + 1) // bs
+                self.table[b, min(first, -(-min(sinks, self.tot[b]) // bs)):first] = 1 << 30
+                self.table[b, need[b]:] = -7
+        self.q = (torch.randn((sum(ks) + len(ks), H, hd), generator=g, device="cuda") * scale).to(DT[kind])
+        self.d = synth.ModelDesc(synth.ARCH_LLAMA, synth.DT_BF16 if kind == "f16" else synth.DT_F32, 1, 128, H, Hkv, hd, 128, 8, 1 << 20)
+        self.model = harness.DeviceModel.random_on_device(self.d, 1)
+        self.max_ctx = max(self.tot)
+
+    def kv(self):
+        from paper_2402_15678_amd import harness
+        return harness.DeviceKV(self.d, self.bs, self.kp.shape[0], self.table, self.ctx, [self.kp], [self.vp])
+
+    def run(self, kv=None, spec=None, max_ctx=None, stats=None):
+        from paper_2402_15678_amd import harness
+        ses = harness.WindowSession(self.model, kv or self.kv(), len(self.ks), len(self.q), max(self.ks) + 1, max_ctx or self.max_ctx, self.window, self.sinks)
+        out = torch.full((len(self.q), self.H * self.hd), -7.0, dtype=DT[self.kind], device="cuda")
+        ses.attention(self.q, torch.tensor(self.ks if spec is None else spec, dtype=torch.int32, device="cuda"), self.ks, out, stats=stats)
+        torch.cuda.synchronize()
+        return out, ses.dev_status.item()
+
+    def rows(self, b):
+        a = sum(self.ks[:b]) + b
+        return slice(a, a + self.ks[b] + 1)
+
+    def dense(self, b):
+        n = self.tot[b]
+        ids = torch.from_numpy(self.full[b, :-(-n // self.bs)].astype(np.int64)).cuda()
+        return (self.kp[ids].permute(0, 3, 1, 2, 4).reshape(-1, self.Hkv, self.hd)[:n], self.vp[ids].permute(0, 3, 1, 2).reshape(-1, self.Hkv, self.hd)[:n])
+
+    def visible(self, b):
+        at = torch.arange(self.tot[b], device="cuda")
+        p = torch.arange(self.ctx[b], self.tot[b], device="cuda")[:, None]
+        return (at <= p) & ((at > p - self.window) | (at < self.sinks))
+
+    def want(self, b, rows=None):
+        """(out, bound) of sequence b's rows, each row on the keys that it sees alone."""
+        k, v = self.dense(b)
+        seen = self.visible(b)
+        out, bound = [], []
+        q = self.q[self.rows(b)]
+        for j in range(len(q)) if rows is None else rows:
+            kk, vv = k[seen[j]], v[seen[j]]
+            o, e = attend(q[j:j + 1], kk, vv, torch.full((1,), len(kk), device="cuda"), self.kind == "f16")
+            out.append(o)
+            bound.append(e)
+        return torch.cat(out), torch.cat(bound)
+
+    def check(self, out, seqs=None, rows=None):
+        for b in range(len(self.ks)) if seqs is None else seqs:
+            o = out[self.rows(b)]
+            check(o if rows is None else o[list(rows)], *self.want(b, rows))
+
+
+GEOMETRIES = [(64, 8, 128, "f16"), (4, 4, 128, "f16"), (12, 12, 64, "f16"), (6, 2, 64, "f16"), (128, 2, 64, "f16"), (4, 4, 64, "f32"),
+              (8, 2, 128, "f32"), (6, 2, 32, "f32"), (8, 8, 8, "f32"), (2, 2, 256, "f32"), (8, 8, 32, "f16"), (8, 2, 256, "f16")]
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", GEOMETRIES)
+@pytest.mark.parametrize("window,sinks,ctx,ks", [(1, 0, [0, 30, 7], [4, 0, 2]), (16, 1, [0, 63, 64, 5, 47], [0, 8, 1, 3, 0]), (33, 20, [200, 33, 0], [5, 0, 40]),
+                                                 (48, 4, [100, 17, 49, 51], [4, 4, 0, 1]), (1000, 64, [300, 1], [2, 0])], ids=str)
+def test_window_matches_the_definition(H, Hkv, hd, kind, window, sinks, ctx, ks):
+    x = Batch(H, Hkv, hd, kind, ctx, ks, window, sinks, H + hd + window)
+    out, status = x.run()
+    assert status == 0
+    x.check(out)
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind,window,sinks,ctx,ks,some", [
+    (64, 8, 128, "f16", 4096, 4, [30000, 100, 5000, 4095], [0, 0, 3, 8], None), (64, 8, 128, "f16", 1024, 16, [0, 700], [2999, 1500], 9),
+    (40, 40, 128, "f16", 300, 50, [0, 5], [1000, 900], 9), (12, 12, 64, "f16", 777, 1, [3000, 0, 9], [200, 1333, 0], 9),
+    (8, 1, 64, "f16", 100000, 0, [20000, 3], [2, 0], None), (4, 4, 64, "f32", 500, 4, [4000, 0], [3, 1200], 9),
+    (8, 2, 256, "f16", 200, 33, [2500, 100], [0, 60], 9), (64, 8, 128, "f16", 2048, 64, [9000], [0], None), (4, 4, 64, "f32", 2000, 4, [2500], [0], None)])
+def test_long_contexts_prompts_and_chunks(H, Hkv, hd, kind, window, sinks, ctx, ks, some):
+    x = Batch(H, Hkv, hd, kind, ctx, ks, window, sinks, 5)
+    out, status = x.run()
+    assert status == 0
+    for b, k in enumerate(ks):
+        x.check(out, [b], None if some is None or k < 2 * some else np.unique(np.linspace(0, k, some).astype(int)).tolist())
+    again, status = x.run(max_ctx=min(x.table.shape[1] * x.bs, x.max_ctx + 11))   # a longer bound on the contexts
+    assert status == 0
+    for b, k in enumerate(ks):
+        x.check(again, [b], None if some is None or k < 2 * some else [0, k // 2, k])
+    assert not (out == -7.0).all(dim=1).any()
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind,bs", [(4, 2, 128, "f16", 8), (6, 2, 32, "f32", 5), (12, 12, 64, "f16", 32), (8, 8, 8, "f32", 1), (4, 4, 64, "f32", 3)])
+def test_other_block_sizes(H, Hkv, hd, kind, bs):
+    x = Batch(H, Hkv, hd, kind, [0, 2 * bs + 1, 150, 333], [3, 0, 5, 20], 37, 6, 6, bs=bs)
+    out, status = x.run()
+    assert status == 0
+    x.check(out)
+
+
+@pytest.mark.parametrize("kind,hd", [("f16", 128), ("f32", 16)])
+@pytest.mark.parametrize("count", [64, 65, 1100])
+def test_many_sequences(kind, hd, count):
+    g = np.random.default_rng(count)
+    x = Batch(4, 2, hd, kind, g.integers(0, 140, count).tolist(), g.integers(0, 4, count).tolist(), 50, 5, 7)
+    out, status = x.run()
+    assert status == 0
+    x.check(out, sorted(set(g.integers(0, count, 40).tolist())))
+    assert not (out == -7.0).all(dim=1).any()
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (12, 12, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 256, "f16")])
+@pytest.mark.parametrize("ctx,ks", [([100, 0, 17], [3, 0, 40]), ([9000, 2000], [0, 2])], ids=str)
+def test_statistics_are_those_of_the_scores(H, Hkv, hd, kind, ctx, ks):
+    """m + log2 l is the logarithm of the sum of the row's 2^(scaled score)."""
+    x = Batch(H, Hkv, hd, kind, ctx, ks, 600, 4, 8)
+    stats = torch.full((len(x.q), H, 2), float("nan"), device="cuda")
+    out, status = x.run(stats=stats)
+    assert status == 0
+    x.check(out)
+    assert torch.equal(out, x.run()[0])                             # with and without them
+    for b in range(len(ks)):
+        k, _ = x.dense(b)
+        seen, q = x.visible(b), x.q[x.rows(b)]
+        for h in range(0, H, max(1, H // 6)):
+            kh = k[:, h // (H // Hkv)].double()
+            s = q[:, h].double() @ kh.t().contiguous() / math.sqrt(hd)
+            mag = (q[:, h].double().abs() @ kh.abs().t().contiguous() / math.sqrt(hd)).amax()
+            want = torch.logsumexp(s.masked_fill(~seen, -math.inf), dim=1) * LOG2E
+            st = stats[x.rows(b)][:, h].double()
+            # the scores' own error, the sum's, and of fp16 probabilities half a step each, or of 2^-24 where they are subnormal
+            n = seen.sum(dim=1).max().item()
+            tol = LOG2E * (hd * 2.0 ** -24 * mag + 2.0 ** -21 * s.abs().amax() + n * 2.0 ** -23 + (2.0 ** -11 + n * 2.0 ** -25 if kind == "f16" else 0))
+            assert ((st[:, 0] + torch.log2(st[:, 1]) - want).abs() <= tol).all()
+
+
+def test_agrees_with_the_attention_that_sees_everything():
+    """A window of the whole context: mn_prefix_attention without a prefix computes the same."""
+    from paper_2402_15678_amd import harness
+    x = Batch(64, 8, 128, "f16", [1050, 600, 0, 333], [8, 8, 8, 8], 1 << 20, 0, 9, blind=False)
+    out, _ = x.run()
+    ses = harness.PrefixSession(x.model, x.kv(), 4, len(x.q), 0, x.max_ctx)
+    want = torch.zeros_like(out)
+    ses.attention(x.q, torch.tensor(x.ks, dtype=torch.int32, device="cuda"), x.ks, want)
+    torch.cuda.synchronize()
+    for b in range(4):
+        _, bound = x.want(b)
+        assert ((out[x.rows(b)].double() - want[x.rows(b)].double()).abs() <= 2 * bound).all()
+
+
+@pytest.mark.parametrize("ctx,ks", [([20, 40, 60, 5, 330, 17], [2, 0, 5, 1, 3, 4]), ([20, 40, 4000, 5, 2500, 17], [2, 0, 5, 1, 3, 4])], ids=str)
+def test_damaged_sequences_get_zeros_and_the_others_their_results(ctx, ks):
+    """Rows that are written by one workgroup, and rows that are put together from ranges."""
+    from paper_2402_15678_amd import binding
+    x = Batch(8, 2, 128, "f16", ctx, ks, 3000, 4, 10, spare=2)
+    stats = torch.zeros((len(x.q), 8, 2), device="cuda")
+    good = x.table.copy()
+    whole, status = x.run(stats=stats)
+    assert status == 0
+    full = stats.clone()
+    cases = [("a wild id", lambda t, c: t.__setitem__((4, 3), 1 << 30), 4, binding.MN_DEV_BLOCK_TABLE),
+             ("a negative id", lambda t, c: t.__setitem__((2, 0), -1), 2, binding.MN_DEV_BLOCK_TABLE),
+             ("a negative context", lambda t, c: c.__setitem__(1, -1), 1, binding.MN_DEV_CTX),
+             ("a context beyond the bound", lambda t, c: c.__setitem__(3, x.max_ctx), 3, binding.MN_DEV_CTX)]
+    for name, damage, b, flag in cases:
+        before = list(x.ctx)
+        x.table = good.copy()
+        damage(x.table, x.ctx)
+        stats.fill_(float("nan"))
+        out, status = x.run(kv=x.kv(), stats=stats)
+        x.table, x.ctx = good, before
+        assert status == flag, name
+        r = x.rows(b)
+        assert (out[r] == 0).all() and (stats[r] == 0).all(), name
+        rest = torch.ones(len(out), dtype=torch.bool, device="cuda")
+        rest[r] = False
+        assert torch.equal(out[rest], whole[rest]) and torch.equal(stats[rest], full[rest]), name
+    for spec in ([2, 0, 5, 1, 3, 5], [3, 0, 5, 1, 2, -1], [2, 0, 6, 0, 3, 4]):
+        out, status = x.run(spec=spec, stats=stats)
+        assert status == binding.MN_DEV_SPEC_LEN and (out == 0).all() and (stats == 0).all()
+
+
+@pytest.mark.parametrize("count", [5, 70])
+@pytest.mark.parametrize("hd,kind", [(128, "f16"), (64, "f32")])
+def test_a_batch_that_does_not_add_up(count, hd, kind):
+    from paper_2402_15678_amd import binding
+    x = Batch(4, 2, hd, kind, [30] * count, [1] * count, 20, 4, 10)
+    good, status = x.run()
+    assert status == 0
+    out, status = x.run(spec=[0] + [1] * (count - 1))
+    assert status == binding.MN_DEV_SPEC_LEN and (out == 0).all()
+    x.ctx[count - 1] = 1 << 29
+    out, status = x.run(kv=x.kv())
+    r = x.rows(count - 1)
+    assert status == binding.MN_DEV_CTX and (out[r] == 0).all() and torch.equal(out[:r.start], good[:r.start])
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (4, 4, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 128, "f32")])
+@pytest.mark.parametrize("ctx,ks", [([70, 0], [2, 90]), ([3000], [1])], ids=str)
+def test_what_is_not_finite_reaches_the_rows_that_see_it(H, Hkv, hd, kind, ctx, ks):
+    window, sinks = 40, 3
+    x = Batch(H, Hkv, hd, kind, ctx, ks, window, sinks, 11)
+    clean, _ = x.run()
+    b = len(ctx) - 1
+    hurt = [1, x.ctx[b] + ks[b] // 2] + ([x.ctx[b] - window - 1] if x.ctx[b] > 100 else [])   # a first token, one of the rows', one out of sight
+    at = [(int(x.full[b, p // 16]), p % 16) for p in hurt]
+    for (blk, off), val in zip(at, (float("inf"), float("nan"), float("nan"))):
+        x.vp[blk, 0, 5, off] = val
+    out, _ = x.run()
+    seen = x.visible(b)
+    G = H // Hkv
+    r = x.rows(b)
+    o, c = out[r].view(-1, H, hd), clean[r].view(-1, H, hd)
+    inf, nan = seen[:, hurt[0]], seen[:, hurt[1]]
+    assert torch.isnan(o[nan][:, :G, 5]).all() and torch.isposinf(o[inf & ~nan][:, :G, 5]).all()
+    same = torch.ones_like(o, dtype=torch.bool)
+    same[:, :G, 5] = ~(inf | nan)[:, None]
+    assert torch.equal(o[same], c[same])
+    if b:
+        assert torch.equal(out[:r.start], clean[:r.start])
+    # a query that is not a number: its row and head alone
+    x.q[r.start, H - 1, 0] = float("nan")
+    again, _ = x.run()
+    a = again[r].view(-1, H, hd)
+    assert torch.isnan(a[0, H - 1]).all()
+    a[0, H - 1] = o[0, H - 1]
+    assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(o))
+
+
+def test_scores_far_apart():
+    for kind, hd in (("f16", 128), ("f16", 64), ("f32", 64)):
+        x = Batch(4, 2, hd, kind, [900, 30], [3, 60], 100, 20, 8, scale=15.0)
+        x.kp[:] = torch.where(torch.isnan(x.kp), x.kp, x.kp * 4)
+        out, status = x.run()
+        assert status == 0
+        x.check(out)
+
+
+def test_pages_beyond_four_gigabytes():
+    from paper_2402_15678_amd import harness
+    x = Batch(16, 8, 128, "f16", [900, 7], [1, 0], 200, 4, 11)
+    nb = 140000
+    far = {int(i): nb - 1 - int(i) * 7 for i in x.full[x.full >= 0].tolist()}
+    want, _ = x.run()
+    kp = torch.zeros((nb, 8, 16, 16, 8), dtype=torch.float16, device="cuda")
+    vp = torch.zeros((nb, 8, 128, 16), dtype=torch.float16, device="cuda")
+    for a, b in far.items():
+        kp[b], vp[b] = x.kp[a], x.vp[a]
+    x.table = np.vectorize(lambda i: far.get(int(i), -1))(x.table).astype(np.int32)
+    x.kp, x.vp = kp, vp
+    out, status = x.run(kv=harness.DeviceKV(x.d, 16, nb, x.table, x.ctx, [kp], [vp]))
+    assert status == 0 and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("ctx", [[200, 31, 0, 64], [5000, 31, 0, 4000]], ids=str)
+def test_captured_and_replayed_on_another_stream(ctx):
+    """Two graphs of one workspace, replayed in turn between eager calls: contexts are read at the replay."""
+    from paper_2402_15678_amd import harness
+    x = Batch(64, 8, 128, "f16", ctx, [2, 0, 5, 1], 1000, 4, 12, blind=False)
+    kv = x.kv()
+    ses = harness.WindowSession(x.model, kv, 4, len(x.q), 6, x.max_ctx, 1000, 4)
+    spec = torch.tensor(x.ks, dtype=torch.int32, device="cuda")
+    outs, graphs = [torch.zeros((len(x.q), 64 * 128), dtype=torch.float16, device="cuda") for _ in range(3)], []
+    stats = torch.zeros((len(x.q), 64, 2), device="cuda")
+    want, _ = x.run()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        ses.attention(x.q, spec, x.ks, outs[2], stats=stats)
+        for i in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                ses.attention(x.q, spec, x.ks, outs[i], stats=stats)
+            graphs.append(g)
+        for n in range(6):
+            outs[n % 2].fill_(-3.0)
+            graphs[n % 2].replay()
+            if n == 3:
+                ses.attention(x.q, spec, x.ks, outs[2], stats=stats)
+            stream.synchronize()
+            assert torch.equal(outs[n % 2], want)
+    torch.cuda.current_stream().wait_stream(stream)
+    assert torch.equal(outs[2], want) and ses.dev_status.item() == 0
+    short = [c // 2 for c in ctx]
+    kv.ctx_lens.copy_(torch.tensor(short, dtype=torch.int32))
+    x.ctx, x.tot = short, [c + k + 1 for c, k in zip(short, x.ks)]
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    x.check(outs[0])
