@@ -11,6 +11,7 @@
 //  * evict_plan_kernel  a workgroup per layer, slot and head: who stays, and who goes where.
 //  * evict_move_kernel  the tokens' keys and values; a workgroup per slot lets the blocks go.
 #include "launch.h"
+#include "tune.h"
 #include "../../include/minions_verify.h"
 
 namespace mn {
@@ -221,11 +222,9 @@ __device__ __forceinline__ uint32_t rank_of(float mass, bool always) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sequence b of the call: whether it loses tokens, and may (asked by the whole workgroup).
-__device__ __forceinline__ bool evicted(const EvictArgs& a, int b, int& n, int& keep, bool report) {
+// Sequence b of the call, of n tokens: whether it loses some, and may (asked by the whole workgroup).
+__device__ __forceinline__ bool evicted(const EvictArgs& a, int b, int n, int keep, bool report) {
   const PoolView& p = a.pool;
-  n = p.ctx_lens[b];
-  keep = a.keep[b];
   if (keep < 0 || n <= keep) return false;
   const int bs = p.block_size, held = p.seq_blocks[b];
   int flags = 0;
@@ -247,103 +246,167 @@ __device__ __forceinline__ bool evicted(const EvictArgs& a, int b, int& n, int& 
   return flags == 0;
 }
 
-constexpr int EVICT_WAVES = 4;
-// Sum of a wave's number over the workgroup, and of the waves before it.
-__device__ __forceinline__ int waves_sum(int v, int* s, int& before) {
+// Sums of N numbers of a wave over the workgroup's WAVES waves, and (of the first) over the waves before it.  Two buffers in turn: one
+// barrier each.
+template <int WAVES, int N>
+__device__ __forceinline__ void waves_sum(int (&v)[N], int (*s)[WAVES][4], int& turn, int& before) {
+  int (*t)[4] = s[turn ^= 1];
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int k = 0; k < N; ++k) t[threadIdx.x >> 6][k] = v[k];
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  int total = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = 0;
   before = 0;
-  for (int w = 0; w < EVICT_WAVES; ++w) {
-    if (w == (int)(threadIdx.x >> 6)) before = total;
-    total += s[w];
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    if (w == (int)(threadIdx.x >> 6)) before = v[0];
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] += t[w][k];
   }
-  return total;
 }
 
-// A wave has a contiguous piece of the slots, a lane every 64th of it.  The keep-th rank is found bit by bit, counting by ballots; among
-// the tokens of that very rank the lowest slots stay.  Then the slots below `keep` that are left, in ascending order, take the tokens that
-// stay from `keep` on, in ascending order: there are as many of either.
-__global__ void __launch_bounds__(64 * EVICT_WAVES) evict_plan_kernel(EvictArgs a) {
-  __shared__ int s_count[EVICT_WAVES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// A wave has a contiguous piece of the slots, a lane every 64th of it: PER of them, as ranks in registers (PER 0: any number, read again each
+// time).  The keep-th rank is found digit by digit, counting in the LDS; among the tokens of that very rank the lowest slots stay.
+// Then the slots below `keep` that are left, in ascending order, take the tokens that stay from `keep` on, in ascending order: there are
+// as many of either.
+template <int WAVES, int PER>
+__global__ void __launch_bounds__(64 * WAVES) evict_plan_kernel(EvictArgs a) {
+  __shared__ int s_count[2][WAVES][4], s_bins[4][256], s_digit[2];
+  constexpr int THREADS = 64 * WAVES;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x, h = row % a.Hkv, b = row / a.Hkv % a.B, layer = row / a.Hkv / a.B;
-  int n, keep;
+  const size_t line = (((size_t)layer * a.pool.max_seqs + b) * a.Hkv + h) * a.width;
+  float* mass = a.mass + line;
+  int32_t* born = a.born + line;
+  const int n = a.pool.ctx_lens[b], keep = a.keep[b];
+  // (asked for ahead of the table row; a context that is longer than the line is none)
+  const int m = n > a.width ? 0 : max(n, 0);
+  const int per = (m + THREADS - 1) / THREADS, lo = min(m, wave * per * 64), hi = min(m, lo + per * 64);
+  float mine[PER > 0 ? PER : 1];
+  int32_t age[PER > 0 ? PER : 1];
+  int last = INT32_MIN;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (lo + 64 * i < hi) {                                      // (uniform)
+      const int at = min(lo + 64 * i + lane, hi - 1);
+      mine[i] = mass[at];
+      age[i] = born[at];
+    }
+  for (int i = tid; i < 4 * 256; i += THREADS) s_bins[0][i] = 0;
   const bool go = evicted(a, b, n, keep, layer == 0 && h == 0);
   if (tid == 0 && layer == 0 && h == 0) a.gone[b] = go ? 1 : 0;
   if (!go) {
     if (tid == 0) a.n_moves[row] = 0;
     return;
   }
-  const size_t line = (((size_t)layer * a.pool.max_seqs + b) * a.Hkv + h) * a.width;
-  float* mass = a.mass + line;
-  int32_t* born = a.born + line;
-  int last = INT32_MIN;
-  for (int i = tid; i < n; i += 64 * EVICT_WAVES) last = max(last, born[i]);
-  for (int d = 32; d; d >>= 1) last = max(last, __shfl_xor(last, d));
-  __syncthreads();
-  if (lane == 0) s_count[wave] = last;
-  __syncthreads();
-  for (int w = 0; w < EVICT_WAVES; ++w) last = max(last, s_count[w]);
-  const long young = (long)last - a.recent;                      // born behind it: recent
-  const auto rank = [&](int i) {
-    const int o = born[i];
-    return rank_of(mass[i], i < a.sinks || o > young);
-  };
-  const int per = (n + 64 * EVICT_WAVES - 1) / (64 * EVICT_WAVES) * 64, lo = min(n, wave * per), hi = min(n, lo + per);
-  const auto count = [&](auto pred) {
-    int c = 0;
-    for (int i = lo; i < hi; i += 64) c += __popcll(__ballot(i + lane < hi && pred(rank(min(i + lane, n - 1)))));
-    return c;
-  };
-  int before;
-  uint32_t T = 0;                                                // the largest number that `keep` ranks reach
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t t = T | 1u << bit;
-    if (waves_sum(count([&](uint32_t r) { return r >= t; }), s_count, before) >= keep) T = t;
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (lo + 64 * i < hi) last = max(last, age[i]);
+  } else {
+    for (int i = tid; i < n; i += THREADS) last = max(last, born[i]);
   }
-  const int above = waves_sum(count([&](uint32_t r) { return r > T; }), s_count, before);
-  waves_sum(count([&](uint32_t r) { return r == T; }), s_count, before);
-  const int ties = keep - above;                                 // of the rank itself stay
-  // f(slot, stays) over the wave's slots
+  for (int d = 32; d; d >>= 1) last = max(last, __shfl_xor(last, d));
+  int turn = 0, before;
+  if (lane == 0) s_count[0][wave][0] = last;                     // (the sums' second buffer)
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) last = max(last, s_count[0][w][0]);
+  const long young = (long)last - a.recent;                      // born behind it: recent
+  uint32_t rank[PER > 0 ? PER : 1];
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (lo + 64 * i < hi) rank[i] = lo + 64 * i + lane < hi ? rank_of(mine[i], lo + 64 * i + lane < a.sinks || age[i] > young) : 0u;
+  // f(slot, whether it is one, its rank) over the wave's slots
   const auto each = [&](auto f) {
-    int at = before;
-    for (int i = lo; i < hi; i += 64) {
-      const bool in = i + lane < hi;
-      const uint32_t r = in ? rank(i + lane) : 0u;
-      const uint64_t same = __ballot(in && r == T);
-      const bool stays = in && (r > T || (r == T && at + __popcll(same & ((1ull << lane) - 1)) < ties));
-      at += __popcll(same);
-      f(i + lane, in, stays);
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (lo + 64 * i < hi) f(lo + 64 * i + lane, lo + 64 * i + lane < hi, rank[i]);
+    } else {
+      for (int i = lo; i < hi; i += 64) {
+        const int at = i + lane;
+        f(at, at < hi, at < hi ? rank_of(mass[at], at < a.sinks || born[at] > young) : 0u);
+      }
     }
   };
-  int holes = 0, movers = 0, holes_at, movers_at;
-  each([&](int i, bool in, bool stays) {
-    holes += __popcll(__ballot(in && !stays && i < keep));
-    movers += __popcll(__ballot(stays && i >= keep));
+  // eight bits at a time, from the top: how many ranks of those that agree with T so far have which digit
+  uint32_t T = 0;
+  int ties = keep;                                               // of the ranks that agree with T stay
+#pragma unroll
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (keep == 0) {                                             // (nobody: no rank is above this one)
+      T = ~0u;
+      break;
+    }
+    int* bins = s_bins[shift / 8];
+    each([&](int, bool in, uint32_t r) {
+      if (in & (shift == 24 || r >> (shift + 8 & 31) == T >> (shift + 8 & 31))) atomicAdd(bins + (r >> shift & 255), 1);
+    });
+    __syncthreads();
+    if (wave == 0) {                                             // lane 0 has the four highest digits
+      int c[4], sum = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum += c[k] = bins[255 - 4 * lane - k];
+      const int incl = wave_scan_i(sum);
+      if (incl >= ties && incl - sum < ties) {
+        int above = incl - sum, k = 0;
+        while (above + c[k] < ties) above += c[k++];
+        s_digit[0] = 255 - 4 * lane - k;
+        s_digit[1] = ties - above;
+      }
+    }
+    __syncthreads();
+    T |= (uint32_t)s_digit[0] << shift;
+    ties = s_digit[1];
+  }
+  int same[1] = {0}, ties_at;
+  each([&](int, bool in, uint32_t r) { same[0] += __popcll(__ballot(in & (r == T))); });
+  waves_sum<WAVES>(same, s_count, turn, ties_at);
+  const uint64_t below = (1ull << lane) - 1;
+  // f(slot, whether it is left for another, whether it moves)
+  const auto decide = [&](auto f) {
+    int at = ties_at;
+    each([&](int i, bool in, uint32_t r) {
+      const uint64_t equal = __ballot(in & (r == T));
+      const bool stays = in & ((r > T) | ((r == T) & (at + __popcll(equal & below) < ties)));
+      at += __popcll(equal);
+      f(i, in & !stays & (i < keep), stays & (i >= keep));
+    });
+  };
+  int holes[1] = {0}, movers[1] = {0}, holes_at, movers_at;
+  decide([&](int, bool hole, bool mover) {
+    holes[0] += __popcll(__ballot(hole));
+    movers[0] += __popcll(__ballot(mover));
   });
-  const int moves = waves_sum(holes, s_count, holes_at);
-  waves_sum(movers, s_count, movers_at);
-  int2* to = a.moves + (size_t)row * a.width;                    // (block, offset) of either side, width / 2 of them at most
+  waves_sum<WAVES>(holes, s_count, turn, holes_at);
+  waves_sum<WAVES>(movers, s_count, turn, movers_at);
+  int2* to = a.moves + (size_t)row * a.width;                    // (slot, block) of either side, width / 2 of them at most
   int2* from = to + a.width / 2;
+  int32_t* firsts = a.firsts + (size_t)row * (a.width / a.pool.block_size + 2);  // per block, the first of its places in the list
   const int32_t* bt = a.pool.tables + (size_t)b * a.pool.width;
-  const int bs = a.pool.block_size;
-  each([&](int i, bool in, bool stays) {
-    const bool hole = in && !stays && i < keep, mover = stays && i >= keep;
-    const uint64_t hb = __ballot(hole), mb = __ballot(mover), below = (1ull << lane) - 1;
-    if (hole) to[holes_at + __popcll(hb & below)] = make_int2(i, bt[i / bs]);
-    if (mover) from[movers_at + __popcll(mb & below)] = make_int2(i, bt[i / bs]);
+  const int bs = a.pool.block_size, shift = (bs & (bs - 1)) == 0 ? 31 - __clz(bs) : -1;
+  const auto block_of = [&](int i) { return shift >= 0 ? i >> shift : i / bs; };
+  decide([&](int i, bool hole, bool mover) {
+    const uint64_t hb = __ballot(hole), mb = __ballot(mover);
+    const int at = holes_at + __popcll(hb & below);
+    if (hole) to[at] = make_int2(i, bt[block_of(i)]);
+    if (mover) from[movers_at + __popcll(mb & below)] = make_int2(i, bt[block_of(i)]);
+    if (i < keep && block_of(i) * bs == i) firsts[block_of(i)] = at;
     holes_at += __popcll(hb);
     movers_at += __popcll(mb);
   });
   __syncthreads();
-  for (int i = tid; i < moves; i += 64 * EVICT_WAVES) {
+  for (int i = tid; i < holes[0]; i += THREADS) {
     const int s = from[i].x, d = to[i].x;
     mass[d] = mass[s];
     born[d] = born[s];
   }
-  if (tid == 0) a.n_moves[row] = moves;
+  if (tid == 0) {
+    a.n_moves[row] = holes[0];
+    firsts[(keep + bs - 1) / bs] = holes[0];
+  }
 }
 
 // The blocks behind the tokens that stay are let go, as when a slot is emptied.
@@ -369,27 +432,119 @@ __device__ __forceinline__ void let_go(const EvictArgs& a, int b) {
 
 // 16 moves of a row at a time: a K token is pieces of 8 elements in as many places, a V token as many places as it has elements.
 template <typename T>
-__global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a, LayerPages pages, int layer0, int release) {
-  const int wg = (int)blockIdx.x - release;
-  if (wg < 0) return let_go(a, blockIdx.x);
+__device__ __forceinline__ void move_tokens(const EvictArgs& a, T* kp, T* vp, int h, const int2* to, const int2* from, int begin, int end) {
   struct __attribute__((aligned(16))) Eight { T x[8]; };
-  const int r = wg / a.splits, split = wg - r * a.splits, per_layer = a.B * a.Hkv;
-  const int h = r % a.Hkv, layer = r / per_layer;
-  const size_t row = (size_t)layer0 * per_layer + r;
-  const int moves = a.n_moves[row], bs = a.pool.block_size, hd = a.hd;
-  const int2* to = a.moves + row * a.width;
-  const int2* from = to + a.width / 2;
-  T* kp = static_cast<T*>(pages.k[layer]);
-  T* vp = static_cast<T*>(pages.v[layer]);
-  for (int i0 = split * 16; i0 < moves; i0 += a.splits * 16) {
-    const int m = min(16, moves - i0);
-    const int2 d = to[i0 + min((int)threadIdx.x % 16, m - 1)], s = from[i0 + min((int)threadIdx.x % 16, m - 1)];
-    if ((int)threadIdx.x % 16 >= m) continue;
+  const int bs = a.pool.block_size, hd = a.hd, nth = threadIdx.x % 16;
+  for (int i0 = begin; i0 < end; i0 += 16) {
+    if (i0 + nth >= end) continue;
+    const int2 d = to[i0 + nth], s = from[i0 + nth];
     const size_t dp = ((size_t)d.y * a.Hkv + h) * ((size_t)hd * bs), sp = ((size_t)s.y * a.Hkv + h) * ((size_t)hd * bs);
     const int dof = d.x % bs, sof = s.x % bs;
     for (int c = threadIdx.x / 16; c < hd / 8; c += 16)
       *reinterpret_cast<Eight*>(kp + dp + ((size_t)c * bs + dof) * 8) = *reinterpret_cast<const Eight*>(kp + sp + ((size_t)c * bs + sof) * 8);
+#pragma unroll 8
     for (int e = threadIdx.x / 16; e < hd; e += 16) vp[dp + (size_t)e * bs + dof] = vp[sp + (size_t)e * bs + sof];
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a, LayerPages pages, int layer0, int release) {
+  const int wg = (int)blockIdx.x - release;
+  if (wg < 0) return let_go(a, blockIdx.x);
+  const int r = wg / a.splits, split = wg - r * a.splits, per_layer = a.B * a.Hkv;
+  const int h = r % a.Hkv, layer = r / per_layer;
+  const size_t row = (size_t)layer0 * per_layer + r;
+  const int moves = a.n_moves[row];
+  const int2* to = a.moves + row * a.width;
+  const int each = (moves + 16 * a.splits - 1) / (16 * a.splits) * 16;
+  move_tokens(a, static_cast<T*>(pages.k[layer]), static_cast<T*>(pages.v[layer]), h, to, to + a.width / 2, split * each, min(moves, (split + 1) * each));
+}
+
+// Blocks of 16 tokens: a wave takes a page at a time, the tokens that stay in it read as well, so that it is written in whole lines.  (Into the
+// places alone the writes were parts of lines: 16 sequences of 1000 to 4000 tokens cut to 1024, 8 layers of 8 heads of 128, 505 us.)  A piece of 16
+// bytes is (part of) one token of K, or PER tokens of one element of V; NU of them per lane.  What is next is looked up meanwhile.
+template <typename T, int NU>
+__global__ void __launch_bounds__(256) evict_pages_kernel(EvictArgs a, LayerPages pages, int layer0, int release) {
+  constexpr int PER = 16 / sizeof(T), BS = 16, AT_ONCE = NU < 4 ? NU : 4;
+  typedef u32x4 Piece;
+  __shared__ __attribute__((aligned(16))) T s_pages[4][2][AT_ONCE * 64 * PER];
+  const int wg = (int)blockIdx.x - release;
+  if (wg < 0) return let_go(a, blockIdx.x);
+  const int r = wg / a.splits, split = wg - r * a.splits, per_layer = a.B * a.Hkv;
+  const int h = r % a.Hkv, layer = r / per_layer, lane = threadIdx.x & 63, nth = lane & (BS - 1);
+  T* image = s_pages[threadIdx.x >> 6][0];
+  T* source = s_pages[threadIdx.x >> 6][1];
+  const size_t row = (size_t)layer0 * per_layer + r;
+  if (a.n_moves[row] == 0) return;
+  const int2* to = a.moves + row * a.width;
+  const int2* from = to + a.width / 2;
+  const int32_t* firsts = a.firsts + row * (a.width / BS + 2);
+  T* kp = static_cast<T*>(pages.k[layer]);
+  T* vp = static_cast<T*>(pages.v[layer]);
+  const int hd = a.hd, page = hd * BS, step = 4 * a.splits;
+  const int blocks = (a.keep[r / a.Hkv % a.B] + BS - 1) / BS;
+  const auto at = [&](int id) { return ((size_t)id * a.Hkv + h) * page; };
+  // places of the block p: [x, y) of the list
+  const auto ask = [&](int p) { return p < blocks ? make_int2(firsts[p], firsts[p + 1]) : make_int2(0, 0); };
+  int p = split * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int2 now = ask(p);
+  for (; p < blocks; p += step) {
+    const int2 next = ask(p + step);
+    const int n = now.y - now.x;
+    if (n > 0) {
+      // lane i < 16: the token that slot i gets
+      const int2 d = to[now.x + min(nth, n - 1)], s = from[now.x + min(nth, n - 1)];
+      const int block = __builtin_amdgcn_readfirstlane(d.y);
+      int id = block, off = nth;
+#pragma unroll
+      for (int i = 0; i < BS; ++i) {
+        const int slot = __builtin_amdgcn_readlane(d.x, i) & (BS - 1), sx = __builtin_amdgcn_readlane(s.x, i), sy = __builtin_amdgcn_readlane(s.y, i);
+        if (i < n && slot == nth) { id = sy; off = sx & (BS - 1); }
+      }
+      // K: a lane's pieces are all of one slot
+      const int k_slot = lane * PER / 8 & (BS - 1);
+      const T* ks = kp + at(__shfl(id, k_slot)) + __shfl(off, k_slot) * 8 + lane * PER % 8;
+      T* kd = kp + at(block);
+      T* vd = vp + at(block);
+#pragma unroll
+      for (int u0 = 0; u0 < NU; u0 += AT_ONCE) {
+        const auto inside = [&](int u) { return (lane + 64 * (u0 + u)) * PER < page; };
+        const auto load = [&](const T* from_page, Piece (&v)[AT_ONCE]) {
+#pragma unroll
+          for (int u = 0; u < AT_ONCE; ++u)
+            if (inside(u)) v[u] = *reinterpret_cast<const Piece*>(from_page + (lane + 64 * (u0 + u)) * PER);
+        };
+        Piece k[AT_ONCE], v[AT_ONCE], w[AT_ONCE];
+        load(vd, v);
+        load(vp + at(__builtin_amdgcn_readlane(s.y, 0)), w);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+          if (inside(u)) k[u] = *reinterpret_cast<const Piece*>(ks + (lane + 64 * (u0 + u)) * PER / (8 * BS) * (8 * BS));
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) *reinterpret_cast<Piece*>(image + (lane + 64 * u) * PER) = v[u];
+        // V: the tokens that come, source page after source page
+        for (int i = 0; i < n;) {
+          const int from_block = __builtin_amdgcn_readlane(s.y, i);
+#pragma unroll
+          for (int u = 0; u < AT_ONCE; ++u) *reinterpret_cast<Piece*>(source + (lane + 64 * u) * PER) = w[u];
+          int last = i + 1;
+          while (last < n && __builtin_amdgcn_readlane(s.y, last) == from_block) ++last;
+          if (last < n) load(vp + at(__builtin_amdgcn_readlane(s.y, last)), w);
+          for (; i < last; ++i) {
+            const int slot = __builtin_amdgcn_readlane(d.x, i) & (BS - 1), of = __builtin_amdgcn_readlane(s.x, i) & (BS - 1);
+#pragma unroll
+            for (int e = lane; e < AT_ONCE * 64 * PER / BS; e += 64) image[e * BS + slot] = source[e * BS + of];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+          if (inside(u)) {
+            *reinterpret_cast<Piece*>(kd + (lane + 64 * (u0 + u)) * PER) = k[u];
+            *reinterpret_cast<Piece*>(vd + (lane + 64 * (u0 + u)) * PER) = *reinterpret_cast<const Piece*>(image + (lane + 64 * u) * PER);
+          }
+      }
+    }
+    now = next;
   }
 }
 
@@ -425,31 +580,54 @@ void launch_weigh(const WeighArgs& a, hipStream_t st) {
   }
 }
 
+template <typename T>
+static void launch_pages(const EvictArgs& a, const LayerPages& pages, int l0, int release, unsigned wgs, hipStream_t st) {
+  const int pieces = a.hd * (int)sizeof(T);                        // 16 bytes each, of a page of K and of one of V
+  if (pieces <= 64) evict_pages_kernel<T, 1><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+  else if (pieces <= 128) evict_pages_kernel<T, 2><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+  else if (pieces <= 256) evict_pages_kernel<T, 4><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+  else if (pieces <= 512) evict_pages_kernel<T, 8><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+  else evict_pages_kernel<T, 16><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+}
+
+static size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 size_t evict_work_bytes(int B, int n_layers, int Hkv, int width) {
   const size_t rows = (size_t)n_layers * B * Hkv;
-  return 4096 + ((size_t)B * 4 + 255) / 256 * 256 + (rows * 4 + 255) / 256 * 256 + rows * (size_t)width * 8;
+  return padded((size_t)B * 4) + padded(rows * 4) + padded(rows * ((size_t)width + 2) * 4) + padded(rows * (size_t)width * 8);
 }
 
 void launch_evict(EvictArgs a, void* const* k, void* const* v, int n_layers, void* workspace, hipStream_t st) {
   unsigned char* w = static_cast<unsigned char*>(workspace);
   const size_t rows = (size_t)n_layers * a.B * a.Hkv;
-  a.gone = reinterpret_cast<int32_t*>(w);
-  w += ((size_t)a.B * 4 + 255) / 256 * 256;
-  a.n_moves = reinterpret_cast<int32_t*>(w);
-  w += (rows * 4 + 255) / 256 * 256;
-  a.moves = reinterpret_cast<int2*>(w);
-  evict_plan_kernel<<<(unsigned)rows, 64 * EVICT_WAVES, 0, st>>>(a);
+  const auto take = [&](size_t bytes) { unsigned char* p = w; w += padded(bytes); return p; };
+  a.gone = reinterpret_cast<int32_t*>(take((size_t)a.B * 4));
+  a.n_moves = reinterpret_cast<int32_t*>(take(rows * 4));
+  a.firsts = reinterpret_cast<int32_t*>(take(rows * ((size_t)a.width + 2) * 4));
+  a.moves = reinterpret_cast<int2*>(take(rows * (size_t)a.width * 8));
+  // (ranks per lane: as few as hold the ledger's lines)
+  if (a.width <= 256) evict_plan_kernel<4, 1><<<(unsigned)rows, 256, 0, st>>>(a);
+  else if (a.width <= 1024) evict_plan_kernel<4, 4><<<(unsigned)rows, 256, 0, st>>>(a);
+  else if (a.width <= 4096) evict_plan_kernel<4, 16><<<(unsigned)rows, 256, 0, st>>>(a);
+  else if (a.width <= 16384) evict_plan_kernel<16, 16><<<(unsigned)rows, 1024, 0, st>>>(a);
+  else evict_plan_kernel<16, 0><<<(unsigned)rows, 1024, 0, st>>>(a);
   for (int l0 = 0; l0 < n_layers; l0 += LAYERS_PER_LAUNCH) {
     LayerPages pages{};
     const int layers = n_layers - l0 < LAYERS_PER_LAUNCH ? n_layers - l0 : LAYERS_PER_LAUNCH;
     for (int l = 0; l < layers; ++l) { pages.k[l] = k[l0 + l]; pages.v[l] = v[l0 + l]; }
     const int release = l0 + layers == n_layers ? a.B : 0;
     const long r = (long)layers * a.B * a.Hkv;
-    a.splits = r >= 2048 ? 1 : (int)((2048 + r - 1) / r);
-    if (a.splits > (a.width + 31) / 32) a.splits = (a.width + 31) / 32;
+    const int want = MN_TUNE("MN_EVICT_WGS", 8192), most = (a.width + 127) / 128;
+    a.splits = r >= want ? 1 : (int)((want + r - 1) / r);
+    if (a.splits > most) a.splits = most;
     const unsigned wgs = (unsigned)(r * a.splits + release);
-    if (a.dtype == MN_DT_BF16) evict_move_kernel<f16_t><<<wgs, 256, 0, st>>>(a, pages, l0, release);
-    else evict_move_kernel<float><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+    if (a.pool.block_size == 16) {
+      if (a.dtype == MN_DT_BF16) launch_pages<f16_t>(a, pages, l0, release, wgs, st);
+      else launch_pages<float>(a, pages, l0, release, wgs, st);
+    } else if (a.dtype == MN_DT_BF16) {
+      evict_move_kernel<f16_t><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+    } else {
+      evict_move_kernel<float><<<wgs, 256, 0, st>>>(a, pages, l0, release);
+    }
   }
 }
 

@@ -306,6 +306,7 @@ struct EvictArgs {
   float* mass;              // [layers][max_seqs][Hkv][width]
   int32_t* born;
   int32_t *gone, *n_moves;  // [B], [layers * B * Hkv]
+  int32_t* firsts;          // [layers * B * Hkv][width / block_size + 2]
   int2* moves;              // [layers * B * Hkv][2][width / 2] (slot, block)
   int B, Hkv, hd, dtype, width, sinks, recent, splits;
 };
