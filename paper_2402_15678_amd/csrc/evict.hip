@@ -52,6 +52,9 @@ __device__ __forceinline__ bool weighed_rows(const WeighArgs& a, int b, Weighed&
     if (tid == 0 && a.status) atomicOr(a.status, w.count > q ? MN_DEV_SPEC_LEN : MN_DEV_CTX);
     return false;
   }
+  w.row0 = __builtin_amdgcn_readfirstlane(w.row0);
+  w.count = __builtin_amdgcn_readfirstlane(w.count);
+  w.base = __builtin_amdgcn_readfirstlane(w.base);
   return true;
 }
 
@@ -83,19 +86,28 @@ __device__ __forceinline__ void put_weight(const WeighArgs& a, const Weighed& w,
 }
 
 constexpr int WPAGE = 16;
-// A wave takes the keys of PAGES pages into registers, as they lie there (a page is the operand of the product: 16 keys by 8 elements in
-// 256 bytes), and the rows that see them in tiles of 16.
-template <int HDIM, int PAGES>
-__global__ void __launch_bounds__(256) weigh_mfma_kernel(WeighArgs a) {
+// Exponent that a row's scores start from, -(m + log2 l), and whether its weights need more care than 2^(c s + that): statistics that are
+// no numbers (its scores may be none either), and far references.
+__device__ __forceinline__ float row_start(float2 st, bool& careful) {
+  careful |= !(st.y >= 0x1p-120f) | !(st.y < INFINITY) | !(__builtin_fabsf(st.x) < FAR_W);
+  return -st.x - __builtin_amdgcn_logf(st.y);
+}
+
+// Many rows (prompts).  A wave takes the keys of PAGES pages into registers, as they lie there (a page is the operand of the product: 16
+// keys by 8 elements in 256 bytes), and the rows that see them in tiles of 16, the next one on its way meanwhile.  ROWS: the four waves have the
+// same keys and every fourth tile, for calls whose keys alone would not fill the chip.
+template <int HDIM, int PAGES, bool ROWS>
+__global__ void __launch_bounds__(256, HDIM == 64 ? 3 : 2) weigh_mfma_kernel(WeighArgs a) {
   constexpr int HS = HDIM / 32;
+  __shared__ float s_sum[4][PAGES * WPAGE];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.B, chunk = rest / a.B;
   Weighed w;
   if (!weighed_rows(a, b, w)) return;
-  const int end = w.base + w.count, key0 = (chunk * 4 + wave) * (PAGES * WPAGE);
+  const int end = w.base + w.count, key0 = (ROWS ? chunk : chunk * 4 + wave) * (PAGES * WPAGE);
   if (key0 >= end) return;
-  const int G = a.H / a.Hkv, R = w.count * G;
+  const int G = a.H / a.Hkv, R = w.count * G, shift = (G & (G - 1)) == 0 ? 31 - __clz(G) : -1;
   const int32_t* bt = a.kv.block_tables + (size_t)b * a.kv.max_blocks_per_seq;
   f16x8 kf[PAGES][HS];
   bool lost[PAGES];
@@ -111,27 +123,58 @@ __global__ void __launch_bounds__(256) weigh_mfma_kernel(WeighArgs a) {
 #pragma unroll
   for (int p = 0; p < PAGES; ++p) sum[p] = (f32x4){0.f, 0.f, 0.f, 0.f};
   const float c = rsqrtf((float)HDIM) * LOG2E_W;
+  struct Tile {
+    f16x8 q[HS];
+    float2 st;
+    int lim;
+  };
+  const auto load = [&](int r0, Tile& t) {                          // (past the last row: that one once more)
+    const int r = min(r0 + l16, R - 1), j = shift >= 0 ? r >> shift : (int)((uint32_t)r / (uint32_t)G);
+    const size_t mh = (size_t)(w.row0 + j) * a.H + kvh * G + r - j * G;
+    const f16_t* q = static_cast<const f16_t*>(a.q) + mh * HDIM;
+#pragma unroll
+    for (int s = 0; s < HS; ++s) t.q[s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
+    t.st = *reinterpret_cast<const float2*>(a.stats + mh * 2);
+    t.lim = w.base + j;
+  };
   // rows before this key's own see none of them
-  for (int r0 = max(0, key0 - w.base) * G / 16 * 16; r0 < R; r0 += 16) {
-    const int r = min(r0 + l16, R - 1), j = r / G, m = w.row0 + j, h = kvh * G + r - j * G;
-    const f16_t* q = static_cast<const f16_t*>(a.q) + ((size_t)m * a.H + h) * HDIM;
-    f16x8 qf[HS];
+  constexpr int STEP = ROWS ? 64 : 16;
+  int r0 = max(0, key0 - w.base) * G / 16 * 16 + (ROWS ? 16 * wave : 0);
+  Tile now, next;
+  const auto work = [&](const Tile& t, int r0) {
+    bool careful = false;
+    float start = row_start(t.st, careful);
+    if (r0 + l16 >= R) start = -INFINITY;
+    const bool all = !__any(t.lim < key0 + PAGES * WPAGE - 1);
+    f32x4 S[PAGES];
 #pragma unroll
-    for (int s = 0; s < HS; ++s) qf[s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
-    const float2 st = *reinterpret_cast<const float2*>(a.stats + ((size_t)m * a.H + h) * 2);
-    const float share = r0 + l16 < R ? row_share(st) : 0.f;
-    const int lim = w.base + j;
+    for (int p = 0; p < PAGES; ++p) S[p] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int p = 0; p < PAGES; ++p) {
-      f32x4 S = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < HS; ++s)
 #pragma unroll
-      for (int s = 0; s < HS; ++s) S = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[p][s], qf[s], S, 0, 0, 0);
+      for (int p = 0; p < PAGES; ++p) S[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[p][s], t.q[s], S[p], 0, 0, 0);
+    if (all && !__any(careful)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = weight(S[e], c, st.x, share);
-        sum[p][e] += key0 + p * WPAGE + 4 * g + e <= lim ? x : 0.f;
-      }
+      for (int p = 0; p < PAGES; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[p][e] += __builtin_amdgcn_exp2f(fmaf(S[p][e], c, start));
+    } else {
+      const float share = r0 + l16 < R ? row_share(t.st) : 0.f;
+#pragma unroll
+      for (int p = 0; p < PAGES; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = weight(S[p][e], c, t.st.x, share);
+          sum[p][e] += key0 + p * WPAGE + 4 * g + e <= t.lim ? x : 0.f;
+        }
     }
+  };
+  load(r0, now);                                                   // (unconditionally, so that waits stay counted)
+  for (; r0 < R; r0 += 2 * STEP) {
+    load(r0 + STEP, next);
+    work(now, r0);
+    load(r0 + 2 * STEP, now);
+    if (r0 + STEP < R) work(next, r0 + STEP);
   }
 #pragma unroll
   for (int p = 0; p < PAGES; ++p) {
@@ -142,10 +185,139 @@ __global__ void __launch_bounds__(256) weigh_mfma_kernel(WeighArgs a) {
       v += __uint_as_float(lane_swap<LANE_2>(__float_as_uint(v)));
       v += __uint_as_float(lane_swap<LANE_4>(__float_as_uint(v)));
       v += __uint_as_float(lane_swap<LANE_8>(__float_as_uint(v)));
-      if (l16 == 0 && !lost[p]) put_weight(a, w, b, kvh, key0 + p * WPAGE + 4 * g + e, v);
+      if (l16 == 0) s_sum[wave][p * WPAGE + 4 * g + e] = v;
     }
+  }
+  if constexpr (ROWS) {
+    __syncthreads();
+    if (wave > 0) return;
+  }
+  static_assert(PAGES * WPAGE == 64, "a key per lane");
+  const float v = ROWS ? s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane] : s_sum[wave][lane];
+#pragma unroll
+  for (int p = 0; p < PAGES; ++p) {
+    if (lane >> 4 == p && !lost[p]) put_weight(a, w, b, kvh, key0 + lane, v);
     if (lost[p] && lane == 0 && key0 + p * WPAGE < end && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
   }
+}
+
+// Few rows (steps).  The rows of a KV head, STREAM_ROWS at most, wait in the LDS, and the keys go by: a wave takes two pages at a time, the next two on
+// their way, the row as the first index of the product (a lane then has one key's weights, of four rows each time).  Bound by HBM.
+constexpr int STREAM_ROWS = 160;
+template <int HDIM>
+__global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
+  constexpr int HS = HDIM / 32, CH = HDIM / 8;                     // 16-byte chunks of a row
+  __shared__ __attribute__((aligned(16))) f16_t s_q[STREAM_ROWS * HDIM];
+  __shared__ __attribute__((aligned(16))) float s_start[STREAM_ROWS], s_m[STREAM_ROWS], s_share[STREAM_ROWS];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.B, range = rest / a.B;
+  Weighed w;
+  if (!weighed_rows(a, b, w)) return;
+  const int end = w.base + w.count, last = min(end, (range + 1) * a.range_keys);
+  int key0 = range * a.range_keys + wave * (2 * WPAGE);
+  if (range * a.range_keys >= end) return;
+  const int G = a.H / a.Hkv, R = w.count * G, tiles = (R + 15) / 16, shift = (G & (G - 1)) == 0 ? 31 - __clz(G) : -1;
+  const auto token_of = [&](int r) { return shift >= 0 ? r >> shift : (int)((uint32_t)r / (uint32_t)G); };
+  const int32_t* bt = a.kv.block_tables + (size_t)b * a.kv.max_blocks_per_seq;
+  const size_t line = ((size_t)b * a.Hkv + kvh) * a.width;
+  struct Keys {
+    f16x8 k[2][HS];
+    float old;                                                     // the weight so far (of the lane's key, lanes 0 .. 31)
+    uint32_t id[2];
+  };
+  const auto load = [&](int key, Keys& t) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      t.id[p] = (uint32_t)bt[min(key / WPAGE + p, (end - 1) / WPAGE)];
+      const f16_t* page = static_cast<const f16_t*>(a.kv.k) + ((size_t)min(t.id[p], (uint32_t)a.kv.num_blocks - 1u) * a.Hkv + kvh) * (HDIM * WPAGE);
+#pragma unroll
+      for (int s = 0; s < HS; ++s)
+        t.k[p][s] = __builtin_bit_cast(f16x8, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(page + ((4 * s + g) * WPAGE + l16) * 8)));
+    }
+    t.old = a.mass[line + min(key + (lane & 31), end - 1)];
+  };
+  Keys ka, kb;
+  load(key0, ka);                                                  // (unconditionally: past the end the last page once more, and waits stay counted)
+  bool careful = false;
+  for (int i = tid; i < tiles * 16 * CH; i += 256) {               // chunks of a row change places, so that 16 rows' meet every bank
+    const int r = i / CH, ch = i % CH, at = r * CH + (ch ^ (HDIM == 128 ? r & 15 : (r >> 1 & 7)));
+    u32x4 x = {0, 0, 0, 0};
+    if (r < R) {
+      const int j = token_of(r);
+      const size_t mh = (size_t)(w.row0 + j) * a.H + kvh * G + r - j * G;
+      x = *reinterpret_cast<const u32x4*>(static_cast<const f16_t*>(a.q) + mh * HDIM + ch * 8);
+      if (ch == 0) {
+        const float2 st = *reinterpret_cast<const float2*>(a.stats + mh * 2);
+        s_start[r] = row_start(st, careful);
+        s_m[r] = st.x;
+        s_share[r] = row_share(st);
+      }
+    } else if (ch == 0) {
+      s_start[r] = -INFINITY;
+      s_m[r] = s_share[r] = 0.f;
+    }
+    *reinterpret_cast<u32x4*>(s_q + at * 8) = x;
+  }
+  const bool slow = __syncthreads_or(careful);
+  const float c = rsqrtf((float)HDIM) * LOG2E_W;
+  bool lost = false;
+  const auto work = [&](const Keys& t, int key0) {
+    float sum[2] = {0.f, 0.f};
+    const bool all = key0 + 2 * WPAGE - 1 <= w.base;               // (the first row sees up to its own slot)
+    for (int i = 0; i < tiles; ++i) {
+      f16x8 q[HS];
+#pragma unroll
+      for (int s = 0; s < HS; ++s) {
+        const int r = 16 * i + l16, ch = 4 * s + g;
+        q[s] = *reinterpret_cast<const f16x8*>(s_q + (r * CH + (ch ^ (HDIM == 128 ? r & 15 : (r >> 1 & 7)))) * 8);
+      }
+      const f32x4 start = *reinterpret_cast<const f32x4*>(s_start + 16 * i + 4 * g);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        f32x4 S = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < HS; ++s) S = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[s], t.k[p][s], S, 0, 0, 0);
+        f32x4 x;
+        if (!slow) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(S[e], c, start[e]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = weight(S[e], c, s_m[16 * i + 4 * g + e], s_share[16 * i + 4 * g + e]);
+        }
+        if (!all) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = key0 + p * WPAGE + l16 <= w.base + token_of(16 * i + 4 * g + e) ? x[e] : 0.f;
+        }
+        sum[p] += (x[0] + x[1]) + (x[2] + x[3]);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {                                  // over the four lane groups
+      uint32_t x, y;
+      lane_pair<16>(__float_as_uint(sum[p]), x, y);
+      sum[p] = __uint_as_float(x) + __uint_as_float(y);
+      lane_pair<32>(__float_as_uint(sum[p]), x, y);
+      sum[p] = __uint_as_float(x) + __uint_as_float(y);
+    }
+    const int key = key0 + lane;
+    const bool gone = (g & 1 ? t.id[1] : t.id[0]) >= (uint32_t)a.kv.num_blocks;
+    lost |= gone && key < end;
+    if (lane < 32 && key < end && !gone) {
+      const float v = g & 1 ? sum[1] : sum[0];
+      a.mass[line + key] = key < w.base ? t.old + v : v;
+      if (key >= w.base) a.born[line + key] = (a.seen ? a.seen[b] : w.base) + key - w.base;
+    }
+  };
+  constexpr int STEP = 4 * 2 * WPAGE;
+  for (; key0 < last; key0 += 2 * STEP) {
+    load(key0 + STEP, kb);
+    work(ka, key0);
+    load(key0 + 2 * STEP, ka);
+    if (key0 + STEP < last) work(kb, key0 + STEP);
+  }
+  if (__any(lost && lane < 32) && lane == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
 }
 
 // A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction.
@@ -553,9 +725,30 @@ __global__ void __launch_bounds__(256) evict_pages_kernel(EvictArgs a, LayerPage
 // ------------------------------------------------------------------------------------------
 static bool weigh_mfma(const WeighArgs& a) { return a.dtype == MN_DT_BF16 && (a.hd == 64 || a.hd == 128) && a.kv.block_size == WPAGE; }
 constexpr int WEIGH_PAGES = 4;
+constexpr int WEIGH_WGS = 1024;        // to aim for
 
-static int weigh_keys(const WeighArgs& a) { return weigh_mfma(a) ? 4 * WEIGH_PAGES * WPAGE : 64; }  // of a workgroup
-long weigh_workgroups(const WeighArgs& a) { return (long)a.B * a.Hkv * ((a.max_ctx + weigh_keys(a) - 1) / weigh_keys(a)); }
+struct WeighShape {
+  int keys;                            // of a workgroup
+  bool stream, rows;                   // few rows; many, that the waves share out
+};
+static WeighShape weigh_shape(const WeighArgs& a) {
+  if (!weigh_mfma(a)) return WeighShape{64, false, false};
+  const long heads = (long)a.B * a.Hkv, R = (long)a.max_q * (a.H / a.Hkv);
+  if (R <= STREAM_ROWS) {
+    // ranges of 128 keys (two pages for each wave) and more
+    long keys = (long)a.max_ctx * heads / MN_TUNE("MN_WEIGH_WGS", WEIGH_WGS) / 128 * 128;
+    if (keys < 128) keys = 128;
+    if (keys > 4096) keys = 4096;
+    return WeighShape{(int)keys, true, false};
+  }
+  const int each = WEIGH_PAGES * WPAGE;
+  const bool rows = heads * ((a.max_ctx + 4 * each - 1) / (4 * each)) < MN_TUNE("MN_WEIGH_ROWS", 1024);
+  return WeighShape{rows ? each : 4 * each, false, rows};
+}
+long weigh_workgroups(const WeighArgs& a) {
+  const int keys = weigh_shape(a).keys;
+  return (long)a.B * a.Hkv * ((a.max_ctx + keys - 1) / keys);
+}
 
 template <typename T>
 static void launch_weigh_f32(const WeighArgs& a, unsigned wgs, hipStream_t st) {
@@ -567,16 +760,24 @@ static void launch_weigh_f32(const WeighArgs& a, unsigned wgs, hipStream_t st) {
     default: weigh_f32_kernel<T, 256><<<wgs, 256, 0, st>>>(a); break;
   }
 }
+template <int HDIM>
+static void launch_weigh_mfma(const WeighArgs& a, const WeighShape& s, unsigned wgs, hipStream_t st) {
+  if (s.stream) weigh_stream_kernel<HDIM><<<wgs, 256, 0, st>>>(a);
+  else if (s.rows) weigh_mfma_kernel<HDIM, WEIGH_PAGES, true><<<wgs, 256, 0, st>>>(a);
+  else weigh_mfma_kernel<HDIM, WEIGH_PAGES, false><<<wgs, 256, 0, st>>>(a);
+}
 
-void launch_weigh(const WeighArgs& a, hipStream_t st) {
+void launch_weigh(WeighArgs a, hipStream_t st) {
   const unsigned wgs = (unsigned)weigh_workgroups(a);
+  const WeighShape s = weigh_shape(a);
+  a.range_keys = s.keys;
   if (!weigh_mfma(a)) {
     if (a.dtype == MN_DT_BF16) launch_weigh_f32<f16_t>(a, wgs, st);
     else launch_weigh_f32<float>(a, wgs, st);
   } else if (a.hd == 128) {
-    weigh_mfma_kernel<128, WEIGH_PAGES><<<wgs, 256, 0, st>>>(a);
+    launch_weigh_mfma<128>(a, s, wgs, st);
   } else {
-    weigh_mfma_kernel<64, WEIGH_PAGES><<<wgs, 256, 0, st>>>(a);
+    launch_weigh_mfma<64>(a, s, wgs, st);
   }
 }
 

@@ -297,9 +297,10 @@ struct WeighArgs {
   int32_t* born;
   int32_t* status;
   int B, M, H, Hkv, hd, dtype, max_q, max_ctx, width;
+  int range_keys;           // of a workgroup
 };
 long weigh_workgroups(const WeighArgs& a);
-void launch_weigh(const WeighArgs& a, hipStream_t st);
+void launch_weigh(WeighArgs a, hipStream_t st);
 struct EvictArgs {
   PoolView pool;
   const int32_t* keep;      // [B]
