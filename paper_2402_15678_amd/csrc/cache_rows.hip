@@ -11,6 +11,7 @@
 //  * Keys and values: a workgroup takes the 16 slots of the cache that a page of 16 tokens is, writes them as the page lies into the LDS, and
 //    copies whole pieces of 16 bytes out.  Straight from the rows a value is two bytes of a 32-byte sector.
 #include "launch.h"
+#include "tune.h"
 #include "../../include/minions_verify.h"
 
 namespace mn {
@@ -88,42 +89,56 @@ __device__ __forceinline__ Quad<T> round4(const float* x, bool& bad) {
   return q;
 }
 
-// The sequence of unit u, and which of its units that is: sequence b has (k_b + 1 + 14) / 16 + 1 of them, as many pages as its rows can
-// touch wherever they begin.  Lengths that do not add up to the host's rows and units are reported, and nothing is written.
-__device__ __forceinline__ bool unit_of(const CacheRows& a, int u, int& seq, int& nth, int& row0, int& q) {
-  __shared__ int s_units[4], s_rows[4], s_hit[4];
+// The sequence of unit u, which of its units that is, its rows and its context: sequence b has (k_b + 1 + 14) / 16 + 1 units, as many pages as
+// its rows can touch wherever they begin.  Lengths that do not add up to the host's rows and units are reported, and nothing is written.
+struct Unit {
+  int seq, nth, row0, q, ctx;
+};
+__device__ __forceinline__ bool unit_of(const CacheRows& a, int u, Unit& x) {
+  __shared__ int s_units[4], s_rows[4], s_hit[5];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int units_at = 0, rows_at = 0;
   bool off = false;
-  if (tid == 0) s_hit[0] = -1;
-  for (int b0 = 0; b0 < a.B; b0 += 256) {
-    const int b = b0 + tid;
-    int n = 0, units = 0;
-    if (b < a.B) {
-      const int k = a.spec_len[b];
-      off |= k < 0 || k >= a.max_q;
-      n = off ? 0 : k + 1;
-      units = off ? 0 : (n + 14) / SLOTS + 1;
+  const auto length = [&](int b) {
+    const int k = a.spec_len[b];
+    off |= k < 0 || k >= a.max_q;
+    return k < 0 || k >= a.max_q ? 0 : k + 1;
+  };
+  const auto units_of = [](int n) { return n > 0 ? (n + 14) / SLOTS + 1 : 0; };
+  if (a.B <= 64) {                                                 // (every wave by itself)
+    int n = 0, ctx = 0;
+    if (lane < a.B) { n = length(lane); ctx = a.ctx_lens[lane]; }
+    const int units = units_of(n), ui = wave_scan_i(units), ri = wave_scan_i(n);
+    off = __any(off) || __builtin_amdgcn_readlane(ui, 63) != a.n_units || __builtin_amdgcn_readlane(ri, 63) != a.M;
+    if (!off) {
+      const int b = __ffsll((unsigned long long)__ballot(u < ui)) - 1;
+      const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, b); };
+      x = Unit{b, u - of(ui) + of(units), of(ri) - of(n), of(n), of(ctx)};
+      return true;
     }
-    const int ui = wave_scan_i(units), ri = wave_scan_i(n);
-    __syncthreads();
-    if (lane == 63) { s_units[wave] = ui; s_rows[wave] = ri; }
-    __syncthreads();
-    int before = units_at + ui - units, r = rows_at + ri - n;
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) { before += s_units[w]; r += s_rows[w]; }
-      units_at += s_units[w];
-      rows_at += s_rows[w];
+  } else {
+    int units_at = 0, rows_at = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 256) {
+      const int b = b0 + tid, n = b < a.B ? length(b) : 0, units = units_of(n);
+      const int ui = wave_scan_i(units), ri = wave_scan_i(n);
+      __syncthreads();
+      if (lane == 63) { s_units[wave] = ui; s_rows[wave] = ri; }
+      __syncthreads();
+      int before = units_at + ui - units, r = rows_at + ri - n;
+      for (int w = 0; w < 4; ++w) {
+        if (w < wave) { before += s_units[w]; r += s_rows[w]; }
+        units_at += s_units[w];
+        rows_at += s_rows[w];
+      }
+      if (u >= before && u < before + units) { s_hit[0] = b; s_hit[1] = u - before; s_hit[2] = r; s_hit[3] = n; s_hit[4] = a.ctx_lens[b]; }
     }
-    if (u >= before && u < before + units) { s_hit[0] = b; s_hit[1] = u - before; s_hit[2] = r; s_hit[3] = n; }
+    off = __syncthreads_or(off) || units_at != a.n_units || rows_at != a.M;
+    if (!off) {
+      x = Unit{s_hit[0], s_hit[1], s_hit[2], s_hit[3], s_hit[4]};
+      return true;
+    }
   }
-  off = __syncthreads_or(off) || units_at != a.n_units || rows_at != a.M;
-  if (off) {
-    if (tid == 0 && u == 0 && a.status) atomicOr(a.status, MN_DEV_SPEC_LEN);
-    return false;
-  }
-  seq = s_hit[0]; nth = s_hit[1]; row0 = s_hit[2]; q = s_hit[3];
-  return seq >= 0;
+  if (tid == 0 && u == 0 && a.status) atomicOr(a.status, MN_DEV_SPEC_LEN);
+  return false;
 }
 
 template <typename In, typename T>
@@ -131,132 +146,145 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(CacheRows a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, hd = a.hd, lanes = hd / 8, t = tid & (lanes - 1);
   const Place at = place_of(t, hd, a.rot);
-  float c[4], s[4];
   bool bad = false;
-  const int fills = a.n_units * a.unit_splits;
-  if ((int)blockIdx.x >= fills) {
-    // ---- queries ----
-    const int w = ((int)blockIdx.x - fills) * 4 + (tid >> 6), m = w / a.q_splits, part = w - m * a.q_splits;
-    if (m < a.M) {
-      angles(a, m, at.pair, c, s);
-      const int per = 64 / lanes, h0 = part * a.q_heads, h1 = min(a.H, h0 + a.q_heads);
-      const In* row = static_cast<const In*>(a.q) + (size_t)m * a.q_stride;
-      T* out = static_cast<T*>(a.q_out) + (size_t)m * a.H * hd;
-      for (int hw = h0; hw < h1; hw += per) {                        // (whole waves: the sums go across lanes)
-        const int h = hw + (tid & 63) / lanes;
-        float x[8];
-        load8(row + (size_t)min(h, a.H - 1) * hd, at, x);
-        ready(x, a.q_gain, a.eps, hd, lanes, at, c, s);
-        if (h >= h1) continue;
-        *reinterpret_cast<Quad<T>*>(out + (size_t)h * hd + at.a) = round4<T>(x, bad);
-        *reinterpret_cast<Quad<T>*>(out + (size_t)h * hd + at.b) = round4<T>(x + 4, bad);
-      }
-    }
+  const int fills = a.n_units * a.unit_parts * a.unit_splits;
+  const bool queries = (int)blockIdx.x >= fills;
+  // the row of this thread, and its share of the heads: of queries a wave's, of keys and values the workgroup's
+  int m, part, in = 0, from = 0, to = 0, slot0 = 0;
+  Unit x{0, 0, 0, a.M, 0};
+  bool mine;
+  if (queries) {
+    const int w = ((int)blockIdx.x - fills) * 4 + (tid >> 6);
+    m = w / a.q_splits;
+    part = w - m * a.q_splits;
+    mine = m < a.M;
+    m = min(m, a.M - 1);
   } else {
-    // ---- keys and values of up to 16 slots ----
-    const int u = blockIdx.x / a.unit_splits, part = blockIdx.x - u * a.unit_splits;
-    const int bs = a.kv.block_size;
-    int seq = 0, nth = 0, row0 = 0, q = a.M, ctx = 0;
+    const int at_once = min(SLOTS, 256 / lanes);                   // slots side by side (heads of 256: 8)
+    const int up = blockIdx.x / a.unit_splits, u = up / a.unit_parts;
+    part = blockIdx.x - up * a.unit_splits;
+    in = (up - u * a.unit_parts) * at_once + tid / lanes;
     if (a.kv.k) {
-      if (!unit_of(a, u, seq, nth, row0, q)) return;
-      ctx = a.ctx_lens[seq];
-      if (ctx < 0 || (long)ctx + q > (long)a.kv.max_blocks_per_seq * bs) {
-        if (tid == 0 && nth == 0 && part == 0 && a.status) atomicOr(a.status, MN_DEV_CTX);
+      if (!unit_of(a, u, x)) return;
+      if (x.ctx < 0 || (long)x.ctx + x.q > (long)a.kv.max_blocks_per_seq * a.kv.block_size) {
+        if (tid == 0 && x.nth == 0 && part == 0 && a.status) atomicOr(a.status, MN_DEV_CTX);
         return;
       }
     } else {
-      nth = u;
+      x.nth = u;
     }
-    const int slot0 = (ctx / SLOTS + nth) * SLOTS, from = max(slot0, ctx), to = min(slot0 + SLOTS, ctx + q);
+    slot0 = (x.ctx / SLOTS + x.nth) * SLOTS;
+    from = max(slot0 + (up - u * a.unit_parts) * at_once, x.ctx);
+    to = min(slot0 + min(SLOTS, (up - u * a.unit_parts + 1) * at_once), x.ctx + x.q);
     if (from >= to) return;
+    mine = slot0 + in >= from && slot0 + in < to;
+    m = x.row0 + (mine ? slot0 + in : from) - x.ctx;
+  }
+  float c[4], s[4];
+  if (queries) {
+    const int per = 64 / lanes, h0 = part * a.q_heads, h1 = mine ? min(a.H, h0 + a.q_heads) : 0;
+    const In* row = static_cast<const In*>(a.q) + (size_t)m * a.q_stride;
+    T* out = static_cast<T*>(a.q_out) + (size_t)m * a.H * hd;
+    constexpr int AT_ONCE = 4;                                     // heads of a lane asked for together
+    for (int hw = h0; hw < h1; hw += AT_ONCE * per) {              // (whole waves: the sums go across lanes)
+      float y[AT_ONCE][8];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) load8(row + (size_t)min(hw + u * per + (tid & 63) / lanes, a.H - 1) * hd, at, y[u]);
+      if (hw == h0) angles(a, m, at.pair, c, s);
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int h = hw + u * per + (tid & 63) / lanes;
+        ready(y[u], a.q_gain, a.eps, hd, lanes, at, c, s);
+        if (h >= h1) continue;
+        *reinterpret_cast<Quad<T>*>(out + (size_t)h * hd + at.a) = round4<T>(y[u], bad);
+        *reinterpret_cast<Quad<T>*>(out + (size_t)h * hd + at.b) = round4<T>(y[u] + 4, bad);
+      }
+    }
+  } else {
+    const int bs = a.kv.block_size, slot = slot0 + in;
     const bool whole = a.kv.k && bs % SLOTS == 0;                  // the slots lie side by side in one block
-    const int32_t* bt = a.kv.k ? a.kv.block_tables + (size_t)seq * a.kv.max_blocks_per_seq : nullptr;
     const size_t head_page = (size_t)hd * bs;
     bool lost = false;                                             // a block id out of range
     uint32_t id = 0;
-    if (whole) {
-      id = (uint32_t)bt[slot0 / bs];
+    if (a.kv.k) {
+      id = (uint32_t)a.kv.block_tables[(size_t)x.seq * a.kv.max_blocks_per_seq + (whole ? slot0 : mine ? slot : from) / bs];
       lost = id >= (uint32_t)a.kv.num_blocks;
     }
-    const int off0 = a.kv.k ? slot0 % bs : 0;
+    const int off0 = whole ? slot0 % bs : 0, off = a.kv.k ? slot % bs : 0;
     T* img_k = reinterpret_cast<T*>(smem);                         // [hd / 8][16][8], [hd][16]
     T* img_v = img_k + hd * SLOTS;
-    const int at_once = 256 / lanes;                               // rows side by side: 8 (heads of 256), 16 and more
-    const int h1 = min(a.Hkv, (part + 1) * a.unit_heads);
-    // (heads of 256: the two halves of the slots have angles of their own)
-    for (int s0 = 0; s0 < SLOTS; s0 += at_once) {
-      const int in = s0 + tid / lanes, slot = slot0 + in, m = row0 + slot - ctx;
-      const bool mine = in < SLOTS && slot >= from && slot < to;
-      const int mm = mine ? m : row0 + from - ctx;
-      angles(a, mm, at.pair, c, s);
-      for (int h = part * a.unit_heads; h < h1; ++h) {
-        float x[8], y[8];
-        load8(static_cast<const In*>(a.k) + (size_t)mm * a.k_stride + (size_t)h * hd, at, x);
-        load8(static_cast<const In*>(a.v) + (size_t)mm * a.v_stride + (size_t)h * hd, at, y);
-        ready(x, a.k_gain, a.eps, hd, lanes, at, c, s);
-        Quad<T> k[2], v[2];
-        if (mine) {
-          k[0] = round4<T>(x, bad); k[1] = round4<T>(x + 4, bad);
-          v[0] = round4<T>(y, bad); v[1] = round4<T>(y + 4, bad);
+    const int h0 = part * a.unit_heads, h1 = min(a.Hkv, h0 + a.unit_heads);
+    const In* k_row = static_cast<const In*>(a.k) + (size_t)m * a.k_stride;
+    const In* v_row = static_cast<const In*>(a.v) + (size_t)m * a.v_stride;
+    float kx[8], vx[8];
+    load8(k_row + (size_t)h0 * hd, at, kx);
+    load8(v_row + (size_t)h0 * hd, at, vx);
+    angles(a, m, at.pair, c, s);
+    for (int h = h0; h < h1; ++h) {
+      Quad<T> k[2], v[2];
+      ready(kx, a.k_gain, a.eps, hd, lanes, at, c, s);
+      bool over = false;
+      k[0] = round4<T>(kx, over); k[1] = round4<T>(kx + 4, over);
+      v[0] = round4<T>(vx, over); v[1] = round4<T>(vx + 4, over);
+      bad |= over && mine;
+      if (h + 1 < h1) {                                            // (the next head's on their way)
+        load8(k_row + (size_t)(h + 1) * hd, at, kx);
+        load8(v_row + (size_t)(h + 1) * hd, at, vx);
+      }
+      if (mine) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int el = e ? at.b : at.a;
-            if (a.k_out) *reinterpret_cast<Quad<T>*>(static_cast<T*>(a.k_out) + ((size_t)m * a.Hkv + h) * hd + el) = k[e];
-            if (a.v_out) *reinterpret_cast<Quad<T>*>(static_cast<T*>(a.v_out) + ((size_t)m * a.Hkv + h) * hd + el) = v[e];
+        for (int e = 0; e < 2; ++e) {
+          const int el = e ? at.b : at.a;
+          if (a.k_out) *reinterpret_cast<Quad<T>*>(static_cast<T*>(a.k_out) + ((size_t)m * a.Hkv + h) * hd + el) = k[e];
+          if (a.v_out) *reinterpret_cast<Quad<T>*>(static_cast<T*>(a.v_out) + ((size_t)m * a.Hkv + h) * hd + el) = v[e];
+        }
+      }
+      if (!a.kv.k) continue;
+      const size_t page = ((size_t)id * a.Hkv + h) * head_page;
+      T* pk = static_cast<T*>(a.kv.k) + page;
+      T* pv = static_cast<T*>(a.kv.v) + page;
+      if (!whole) {
+        if (mine && !lost) {
+          int there = off, el_a = at.a, el_b = at.b;
+          asm volatile("" : "+v"(there), "+v"(el_a), "+v"(el_b));  // (sixteen addresses worked out anew for every head: registers)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int el = (e < 4 ? el_a : el_b) + (e & 3);
+            pk[((size_t)(el >> 3) * bs + there) * 8 + (el & 7)] = k[e >> 2].x[e & 3];
+            pv[(size_t)el * bs + there] = v[e >> 2].x[e & 3];
           }
         }
-        if (!a.kv.k) continue;
-        if (!whole) {
-          if (mine) {
-            const uint32_t block = (uint32_t)bt[slot / bs];
-            const int off = slot % bs;
-            if (block >= (uint32_t)a.kv.num_blocks) {
-              lost = true;
-            } else {
-              const size_t page = ((size_t)block * a.Hkv + h) * head_page;
+        continue;
+      }
+      if (h > h0) __syncthreads();                                 // (the head before has left)
+      if (mine) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int el = (e < 4 ? at.a : at.b) + (e & 3);
-                static_cast<T*>(a.kv.k)[page + ((size_t)(el >> 3) * bs + off) * 8 + (el & 7)] = k[e >> 2].x[e & 3];
-                static_cast<T*>(a.kv.v)[page + (size_t)el * bs + off] = v[e >> 2].x[e & 3];
-              }
-            }
-          }
-          continue;
+        for (int e = 0; e < 2; ++e) {
+          const int el = e ? at.b : at.a;
+          *reinterpret_cast<Quad<T>*>(img_k + ((el >> 3) * SLOTS + in) * 8 + (el & 7)) = k[e];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) img_v[(el + i) * SLOTS + in] = v[e].x[i];
         }
-        __syncthreads();                                           // (the head before has left)
-        if (mine) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int el = e ? at.b : at.a;
-            *reinterpret_cast<Quad<T>*>(img_k + ((el >> 3) * SLOTS + in) * 8 + (el & 7)) = k[e];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) img_v[(el + i) * SLOTS + in] = v[e].x[i];
-          }
-        }
-        __syncthreads();
-        if (lost) continue;
-        const size_t page = ((size_t)id * a.Hkv + h) * head_page;
-        constexpr int PER = 16 / sizeof(T);                        // elements of a piece
-        T* pk = static_cast<T*>(a.kv.k) + page;
-        T* pv = static_cast<T*>(a.kv.v) + page;
-        const int lo = max(from - slot0, s0), hi = min(to - slot0, s0 + at_once);
-        for (int i = tid; i < hd * SLOTS / PER; i += 256) {
-          const int e = i * PER;
-          const int ks = e / 8 % SLOTS;                            // K: a piece is of one token
-          if (ks >= lo && ks < hi) *reinterpret_cast<u32x4*>(pk + ((size_t)(e / (8 * SLOTS)) * bs + off0 + ks) * 8 + e % 8) = *reinterpret_cast<const u32x4*>(img_k + e);
-          const int vs = e % SLOTS;                                // V: of several
-          T* out = pv + (size_t)(e / SLOTS) * bs + off0 + vs;
-          if (vs >= lo && vs + PER <= hi) {
-            *reinterpret_cast<u32x4*>(out) = *reinterpret_cast<const u32x4*>(img_v + e);
-          } else {
-            for (int j = 0; j < PER; ++j)
-              if (vs + j >= lo && vs + j < hi) out[j] = img_v[e + j];
-          }
+      }
+      __syncthreads();
+      if (lost) continue;
+      constexpr int PER = 16 / sizeof(T);                          // elements of a piece
+      const int lo = from - slot0, hi = to - slot0;
+      for (int i = tid; i < hd * SLOTS / PER; i += 256) {
+        const int e = i * PER;
+        const int ks = e / 8 % SLOTS;                              // K: a piece is of one token
+        if (ks >= lo && ks < hi) *reinterpret_cast<u32x4*>(pk + ((size_t)(e / (8 * SLOTS)) * bs + off0 + ks) * 8 + e % 8) = *reinterpret_cast<const u32x4*>(img_k + e);
+        const int vs = e % SLOTS;                                  // V: of several
+        T* out = pv + (size_t)(e / SLOTS) * bs + off0 + vs;
+        if (vs >= lo && vs + PER <= hi) {
+          *reinterpret_cast<u32x4*>(out) = *reinterpret_cast<const u32x4*>(img_v + e);
+        } else {
+          for (int j = 0; j < PER; ++j)
+            if (vs + j >= lo && vs + j < hi) out[j] = img_v[e + j];
         }
       }
     }
-    if (lost && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+    if (lost && mine && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
   }
   if (sizeof(T) == 2 && bad && a.status) atomicOr(a.status, MN_DEV_RANGE);
 }
@@ -278,12 +306,13 @@ static void split_heads(int heads, long items, int least, long want, int& splits
 }
 
 long cache_rows_shape(CacheRows& a) {
-  const int per = 64 / (a.hd / 8);                                 // heads that a wave holds at once
-  split_heads(a.H, a.M, per, 2048, a.q_splits, a.q_heads);
+  const int lanes = a.hd / 8, per = 64 / lanes;                    // heads that a wave holds at once
+  split_heads(a.H, a.M, per, MN_TUNE("MN_ROWS_Q", 4096), a.q_splits, a.q_heads);
   a.q_heads = (a.q_heads + per - 1) / per * per;
   a.q_splits = (a.H + a.q_heads - 1) / a.q_heads;
-  split_heads(a.Hkv, a.n_units, 1, 512, a.unit_splits, a.unit_heads);
-  return (long)a.n_units * a.unit_splits + (a.q_out ? ((long)a.M * a.q_splits + 3) / 4 : 0);
+  a.unit_parts = lanes > 16 ? lanes / 16 : 1;
+  split_heads(a.Hkv, (long)a.n_units * a.unit_parts, 1, MN_TUNE("MN_ROWS_KV", 512), a.unit_splits, a.unit_heads);
+  return (long)a.n_units * a.unit_parts * a.unit_splits + (a.q_out ? ((long)a.M * a.q_splits + 3) / 4 : 0);
 }
 
 hipError_t launch_cache_rows(const CacheRows& a, long workgroups, hipStream_t st) {

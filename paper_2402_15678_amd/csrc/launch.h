@@ -255,7 +255,7 @@ struct CacheRows {
   int M, H, Hkv, hd, rot, dtype, rows_f32, B, max_q;
   float eps;
   int axis_end[3];          // the first pair behind the axis
-  int n_units, unit_splits, unit_heads, q_splits, q_heads;  // workgroups of keys and values, shares of the heads (cache_rows_shape)
+  int n_units, unit_parts, unit_splits, unit_heads, q_splits, q_heads;  // pages to fill, shares of their slots and heads, of a row's heads (cache_rows_shape)
   double freq[128];         // turns of pair i per position
 };
 long cache_row_units(const int32_t* h_spec_len, int B, int M, bool pages);

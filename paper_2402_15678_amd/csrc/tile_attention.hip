@@ -367,20 +367,26 @@ __device__ __forceinline__ bool window_item(const TileArgs& a, int wg, int G, in
   return look.i0 < look.i1;
 }
 
-// Whether an entry of sequence `seq`'s table row that its rows look at is out of range (the whole workgroup asks).
-__device__ __forceinline__ bool window_table_bad(const TileArgs& a, int seq, int ctx, int q) {
+// Whether an entry of sequence `seq`'s table row that its rows look at is out of range (this thread's share of them).  The last one that it
+// looks at is left in `entry`: a caller with something to ask for meanwhile looks at it later.
+__device__ __forceinline__ bool window_table_bad(const TileArgs& a, int seq, int ctx, int q, int& entry) {
   const int bs = a.kv.block_size, end = ctx + q, first = max(0, ctx - a.window + 1) / bs, n_first = min(first, (min(a.sinks, end) + bs - 1) / bs);
   const int32_t* row = a.kv.block_tables + (size_t)seq * a.kv.max_blocks_per_seq;
   const int all = n_first + (end - 1) / bs + 1 - first;
   bool bad = false;
-  for (int i = threadIdx.x; i < all; i += blockDim.x) bad |= (uint32_t)row[i < n_first ? i : i - n_first + first] >= (uint32_t)a.kv.num_blocks;
-  return __syncthreads_or(bad);
+  int i = threadIdx.x;
+  for (; i + (int)blockDim.x < all; i += blockDim.x) bad |= (uint32_t)row[i < n_first ? i : i - n_first + first] >= (uint32_t)a.kv.num_blocks;
+  i = min(i, all - 1);
+  entry = row[i < n_first ? i : i - n_first + first];
+  return bad;
 }
 // For the calls whose rows are put together from parts: a workgroup per sequence.
 __device__ __forceinline__ void window_check(const TileArgs& a, int b) {
   const int ctx = scalar(a.batch.ctx_lens)[b], k = scalar(a.batch.spec_len)[b];
   if (k < 0 || k >= a.batch.max_q || !window_fits(a.batch, ctx, k + 1)) return;  // (takes no part)
-  const bool bad = window_table_bad(a, b, ctx, k + 1);
+  int entry;
+  bool bad = window_table_bad(a, b, ctx, k + 1, entry);
+  bad = __syncthreads_or(bad | ((uint32_t)entry >= (uint32_t)a.kv.num_blocks));
   if (threadIdx.x == 0) {
     a.seq_bad[b] = bad;
     if (bad && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
@@ -804,13 +810,29 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     const int end_m0 = aside(it.m0), end_seq = aside(it.seq), end_ctx = aside(it.ctx), end_slot = aside(it.slot), end_kvh = aside(kvh);
     // tiles that a row of the wave sees
     const int n_wave = WINDOW ? (rows ? min(n_tiles, max(0, look.entry(max_lim / PAGE) - look.i0 + 2) / 2) : 0) : min(n_tiles, max(0, max_lim + TK - it.key0) / TK);
+    bool lost = false;                                             // a damaged table row, looked at while the first tiles are on their way
+    int entry = 0;
+    if constexpr (WINDOW) {
+      if (a.ranges == 1) lost = window_table_bad(a, it.seq, it.ctx, it.R / G, entry);
+    }
     __syncthreads();                                               // (the search, or the piece before, is through with the LDS)
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
       if (!PAGED || i < n_tiles) stage(i);                         // (dense rows: short ones are rare, and the test cost as much)
     if (!PAGED || n_tiles >= AHEAD) wait_vm<(AHEAD - 2) * LPW>();  // (tiles 0 and 1 are there)
     else wait_vm<0>();
-    __syncthreads();
+    if constexpr (WINDOW) {
+      asm volatile("" : "+v"(entry));
+      if (__syncthreads_or(lost | ((uint32_t)entry >= (uint32_t)a.kv.num_blocks))) {
+        wait_vm<0>();
+        if (tid == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+        it.R = -it.R;
+        window_zeros<f16_t>(a, &it, kvh, G);
+        return;
+      }
+    } else {
+      __syncthreads();
+    }
     f32x4 Sa[CT][2], Sb[CT][2];
     float ta[CT], tb[CT];
     load_k(slot(0), kf);
@@ -840,12 +862,6 @@ __global__ void __launch_bounds__(NW * 64, 2) tile_mfma_kernel(TileArgs a) {
     if constexpr (WINDOW) {
       it.m0 = __builtin_amdgcn_readfirstlane(end_m0); it.seq = __builtin_amdgcn_readfirstlane(end_seq); it.ctx = __builtin_amdgcn_readfirstlane(end_ctx);
       it.slot = __builtin_amdgcn_readfirstlane(end_slot); kvh = __builtin_amdgcn_readfirstlane(end_kvh);
-      if (a.ranges == 1 && window_table_bad(a, it.seq, it.ctx, it.R / G)) {
-        if (tid == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
-        it.R = -it.R;
-        window_zeros<f16_t>(a, &it, kvh, G);
-        return;
-      }
     }
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -1163,7 +1179,10 @@ __global__ void __launch_bounds__(256, PAGED && HDP >= 128 ? 1 : 2) tile_f32_ker
     run_l = __uint_as_float(x) + __uint_as_float(y);
     // element of O[u][i] in this lane
     if constexpr (WINDOW) {
-      if (a.ranges == 1 && window_table_bad(a, it.seq, it.ctx, it.R / G)) {
+      int entry = 0;
+      bool lost = false;
+      if (a.ranges == 1) lost = window_table_bad(a, it.seq, it.ctx, it.R / G, entry);
+      if (__syncthreads_or(lost | ((uint32_t)entry >= (uint32_t)a.kv.num_blocks))) {
         if (tid == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
         it.R = -it.R;
         window_zeros<T>(a, &it, kvh, G);
