@@ -24,12 +24,13 @@ constexpr float FAR_W = 0x1p24f;       // references from here on: see the atten
 struct Weighed {
   int row0, count, base;
 };
+template <int NW>
 __device__ __forceinline__ bool weighed_rows(const WeighArgs& a, int b, Weighed& w) {
-  __shared__ int s_before[4], s_all[4];
+  __shared__ int s_before[NW], s_all[NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int before = 0, all = 0;
   bool off = false;
-  for (int i = tid; i < a.B; i += 256) {
+  for (int i = tid; i < a.B; i += 64 * NW) {
     const int k = a.spec_len[i];
     off |= k < 0 || k >= a.max_q;
     if (i < b) before += k + 1;
@@ -39,8 +40,10 @@ __device__ __forceinline__ bool weighed_rows(const WeighArgs& a, int b, Weighed&
   all = wave_sum_i(all);
   if (lane == 0) { s_before[wave] = before; s_all[wave] = all; }
   off = __syncthreads_or(off);
-  w.row0 = s_before[0] + s_before[1] + s_before[2] + s_before[3];
-  if (off || s_all[0] + s_all[1] + s_all[2] + s_all[3] != a.M) {
+  w.row0 = all = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) { w.row0 += s_before[i]; all += s_all[i]; }
+  if (off || all != a.M) {
     if (tid == 0 && b == 0 && a.status) atomicOr(a.status, MN_DEV_SPEC_LEN);
     return false;
   }
@@ -94,18 +97,18 @@ __device__ __forceinline__ float row_start(float2 st, bool& careful) {
 }
 
 // Many rows (prompts).  A wave takes the keys of PAGES pages into registers, as they lie there (a page is the operand of the product: 16
-// keys by 8 elements in 256 bytes), and the rows that see them in tiles of 16, the next one on its way meanwhile.  ROWS: the four waves have the
-// same keys and every fourth tile, for calls whose keys alone would not fill the chip.
-template <int HDIM, int PAGES, bool ROWS>
-__global__ void __launch_bounds__(256, HDIM == 64 ? 3 : 2) weigh_mfma_kernel(WeighArgs a) {
+// keys by 8 elements in 256 bytes), and the rows that see them in tiles of 16, the next one on its way meanwhile.  ROWS: the NW waves have the
+// same keys and every NW-th tile, for calls whose keys alone would not fill the chip.
+template <int HDIM, int PAGES, int NW, bool ROWS>
+__global__ void __launch_bounds__(64 * NW, HDIM == 64 ? 3 : 2) weigh_mfma_kernel(WeighArgs a) {
   constexpr int HS = HDIM / 32;
-  __shared__ float s_sum[4][PAGES * WPAGE];
+  __shared__ float s_sum[NW][PAGES * WPAGE];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.B, chunk = rest / a.B;
   Weighed w;
-  if (!weighed_rows(a, b, w)) return;
-  const int end = w.base + w.count, key0 = (ROWS ? chunk : chunk * 4 + wave) * (PAGES * WPAGE);
+  if (!weighed_rows<NW>(a, b, w)) return;
+  const int end = w.base + w.count, key0 = (ROWS ? chunk : chunk * NW + wave) * (PAGES * WPAGE);
   if (key0 >= end) return;
   const int G = a.H / a.Hkv, R = w.count * G, shift = (G & (G - 1)) == 0 ? 31 - __clz(G) : -1;
   const int32_t* bt = a.kv.block_tables + (size_t)b * a.kv.max_blocks_per_seq;
@@ -138,7 +141,7 @@ __global__ void __launch_bounds__(256, HDIM == 64 ? 3 : 2) weigh_mfma_kernel(Wei
     t.lim = w.base + j;
   };
   // rows before this key's own see none of them
-  constexpr int STEP = ROWS ? 64 : 16;
+  constexpr int STEP = ROWS ? 16 * NW : 16;
   int r0 = max(0, key0 - w.base) * G / 16 * 16 + (ROWS ? 16 * wave : 0);
   Tile now, next;
   const auto work = [&](const Tile& t, int r0) {
@@ -193,7 +196,10 @@ __global__ void __launch_bounds__(256, HDIM == 64 ? 3 : 2) weigh_mfma_kernel(Wei
     if (wave > 0) return;
   }
   static_assert(PAGES * WPAGE == 64, "a key per lane");
-  const float v = ROWS ? s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane] : s_sum[wave][lane];
+  float v = s_sum[wave][lane];
+  if constexpr (ROWS)
+#pragma unroll
+    for (int i = 1; i < NW; ++i) v += s_sum[i][lane];
 #pragma unroll
   for (int p = 0; p < PAGES; ++p) {
     if (lane >> 4 == p && !lost[p]) put_weight(a, w, b, kvh, key0 + lane, v);
@@ -213,7 +219,7 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.B, range = rest / a.B;
   Weighed w;
-  if (!weighed_rows(a, b, w)) return;
+  if (!weighed_rows<4>(a, b, w)) return;
   const int end = w.base + w.count, last = min(end, (range + 1) * a.range_keys);
   int key0 = range * a.range_keys + wave * (2 * WPAGE);
   if (range * a.range_keys >= end) return;
@@ -320,17 +326,18 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
   if (__any(lost && lane < 32) && lane == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
 }
 
-// A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction.
-template <typename T, int HDP>
+// A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction; ROWS: all waves the same keys and every fourth tile.
+template <typename T, int HDP, bool ROWS>
 __global__ void __launch_bounds__(256) weigh_f32_kernel(WeighArgs a) {
   constexpr int NU = HDP / 16;
   struct __attribute__((aligned(4 * sizeof(T)))) Four { T x[4]; };
+  __shared__ float s_sum[4][16];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, hd = a.hd, bs = a.kv.block_size;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.B, chunk = rest / a.B;
   Weighed w;
-  if (!weighed_rows(a, b, w)) return;
-  const int end = w.base + w.count, key0 = (chunk * 4 + wave) * 16;
+  if (!weighed_rows<4>(a, b, w)) return;
+  const int end = w.base + w.count, key0 = (ROWS ? chunk : chunk * 4 + wave) * 16;
   if (key0 >= end) return;
   const int G = a.H / a.Hkv, R = w.count * G;
   const int key = min(key0 + l16, end - 1);
@@ -349,28 +356,48 @@ __global__ void __launch_bounds__(256) weigh_f32_kernel(WeighArgs a) {
       for (int e = 0; e < 4; ++e) k[u][e] = (float)x.x[e];
     }
   }
+  struct Tile {
+    Four q[NU];
+    float2 st;
+    int lim;
+  };
+  const auto load = [&](int r0, Tile& t) {                          // (past the last row: that one once more)
+    const int r = min(r0 + l16, R - 1), j = (int)((uint32_t)r / (uint32_t)G);
+    const size_t mh = (size_t)(w.row0 + j) * a.H + kvh * G + r - j * G;
+    const T* q = static_cast<const T*>(a.q) + mh * hd;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) t.q[u] = *reinterpret_cast<const Four*>(q + (HDP == 16 ? min(4 * g, hd - 4) : 16 * u + 4 * g));  // (heads of 8: keys of zeros behind)
+    t.st = *reinterpret_cast<const float2*>(a.stats + mh * 2);
+    t.lim = w.base + j;
+  };
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int r0 = max(0, key0 - w.base) * G / 16 * 16; r0 < R; r0 += 16) {
-    const int r = min(r0 + l16, R - 1), j = r / G, m = w.row0 + j, h = kvh * G + r - j * G;
-    const T* q = static_cast<const T*>(a.q) + ((size_t)m * a.H + h) * hd;
-    f32x4 S = {0.f, 0.f, 0.f, 0.f};
+  const auto work = [&](const Tile& t, int r0) {
+    f32x4 S = {0.f, 0.f, 0.f, 0.f}, S2 = S;                         // (two sums: neither waits for itself)
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      const int e0 = 16 * u + 4 * g;
-      Four x{};
-      if (e0 < hd) x = *reinterpret_cast<const Four*>(q + e0);
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u][e], (float)x.x[e], S, 0, 0, 0);
-    }
-    const float2 st = *reinterpret_cast<const float2*>(a.stats + ((size_t)m * a.H + h) * 2);
-    const float share = r0 + l16 < R ? row_share(st) : 0.f;
+      for (int e = 0; e < 4; ++e) {
+        f32x4& to = e & 1 ? S2 : S;
+        to = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u][e], HDP == 16 && 4 * g >= hd ? 0.f : (float)t.q[u].x[e], to, 0, 0, 0);
+      }
+    S += S2;
+    const float share = r0 + l16 < R ? row_share(t.st) : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float x = weight(S[e], c, st.x, share);
-      sum[e] += key0 + 4 * g + e <= w.base + j ? x : 0.f;
+      const float x = weight(S[e], c, t.st.x, share);
+      sum[e] += key0 + 4 * g + e <= t.lim ? x : 0.f;
     }
+  };
+  constexpr int STEP = ROWS ? 64 : 16;
+  int r0 = max(0, key0 - w.base) * G / 16 * 16 + (ROWS ? 16 * wave : 0);
+  Tile now, next;
+  load(r0, now);
+  for (; r0 < R; r0 += 2 * STEP) {
+    load(r0 + STEP, next);
+    work(now, r0);
+    load(r0 + 2 * STEP, now);
+    if (r0 + STEP < R) work(next, r0 + STEP);
   }
-  const uint64_t gone = __ballot(lost);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     float v = sum[e];
@@ -378,9 +405,15 @@ __global__ void __launch_bounds__(256) weigh_f32_kernel(WeighArgs a) {
     v += __uint_as_float(lane_swap<LANE_2>(__float_as_uint(v)));
     v += __uint_as_float(lane_swap<LANE_4>(__float_as_uint(v)));
     v += __uint_as_float(lane_swap<LANE_8>(__float_as_uint(v)));
-    if (l16 == 0 && !(gone >> (4 * g + e) & 1)) put_weight(a, w, b, kvh, key0 + 4 * g + e, v);
+    if (l16 == 0) s_sum[wave][4 * g + e] = v;
   }
-  if (gone && lane == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
+  if constexpr (ROWS) {
+    __syncthreads();
+    if (wave > 0) return;
+  }
+  const float v = ROWS ? s_sum[0][l16] + s_sum[1][l16] + s_sum[2][l16] + s_sum[3][l16] : s_sum[wave][l16];
+  if (lane < 16 && !lost) put_weight(a, w, b, kvh, key0 + l16, v);
+  if (__any(lost) && lane == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -730,41 +763,49 @@ constexpr int WEIGH_WGS = 1024;        // to aim for
 struct WeighShape {
   int keys;                            // of a workgroup
   bool stream, rows;                   // few rows; many, that the waves share out
+  int waves;
 };
 static WeighShape weigh_shape(const WeighArgs& a) {
-  if (!weigh_mfma(a)) return WeighShape{64, false, false};
   const long heads = (long)a.B * a.Hkv, R = (long)a.max_q * (a.H / a.Hkv);
+  if (!weigh_mfma(a)) return R > 64 ? WeighShape{16, false, true, 4} : WeighShape{64, false, false, 4};
   if (R <= STREAM_ROWS) {
     // ranges of 128 keys (two pages for each wave) and more
     long keys = (long)a.max_ctx * heads / MN_TUNE("MN_WEIGH_WGS", WEIGH_WGS) / 128 * 128;
     if (keys < 128) keys = 128;
     if (keys > 4096) keys = 4096;
-    return WeighShape{(int)keys, true, false};
+    return WeighShape{(int)keys, true, false, 4};
   }
   const int each = WEIGH_PAGES * WPAGE;
-  const bool rows = heads * ((a.max_ctx + 4 * each - 1) / (4 * each)) < MN_TUNE("MN_WEIGH_ROWS", 1024);
-  return WeighShape{rows ? each : 4 * each, false, rows};
+  const long chunks = heads * ((a.max_ctx + each - 1) / each);
+  if (chunks >= 4 * MN_TUNE("MN_WEIGH_ROWS", WEIGH_WGS)) return WeighShape{4 * each, false, false, 4};
+  return WeighShape{each, false, true, chunks < MN_TUNE("MN_WEIGH_EIGHT", 512) ? 8 : 4};
 }
 long weigh_workgroups(const WeighArgs& a) {
   const int keys = weigh_shape(a).keys;
   return (long)a.B * a.Hkv * ((a.max_ctx + keys - 1) / keys);
 }
 
+template <typename T, int HDP>
+static void launch_weigh_f32_as(const WeighArgs& a, bool rows, unsigned wgs, hipStream_t st) {
+  if (rows) weigh_f32_kernel<T, HDP, true><<<wgs, 256, 0, st>>>(a);
+  else weigh_f32_kernel<T, HDP, false><<<wgs, 256, 0, st>>>(a);
+}
 template <typename T>
-static void launch_weigh_f32(const WeighArgs& a, unsigned wgs, hipStream_t st) {
+static void launch_weigh_f32(const WeighArgs& a, bool rows, unsigned wgs, hipStream_t st) {
   switch (a.hd) {
-    case 8: case 16: weigh_f32_kernel<T, 16><<<wgs, 256, 0, st>>>(a); break;
-    case 32: weigh_f32_kernel<T, 32><<<wgs, 256, 0, st>>>(a); break;
-    case 64: weigh_f32_kernel<T, 64><<<wgs, 256, 0, st>>>(a); break;
-    case 128: weigh_f32_kernel<T, 128><<<wgs, 256, 0, st>>>(a); break;
-    default: weigh_f32_kernel<T, 256><<<wgs, 256, 0, st>>>(a); break;
+    case 8: case 16: launch_weigh_f32_as<T, 16>(a, rows, wgs, st); break;
+    case 32: launch_weigh_f32_as<T, 32>(a, rows, wgs, st); break;
+    case 64: launch_weigh_f32_as<T, 64>(a, rows, wgs, st); break;
+    case 128: launch_weigh_f32_as<T, 128>(a, rows, wgs, st); break;
+    default: launch_weigh_f32_as<T, 256>(a, rows, wgs, st); break;
   }
 }
 template <int HDIM>
 static void launch_weigh_mfma(const WeighArgs& a, const WeighShape& s, unsigned wgs, hipStream_t st) {
   if (s.stream) weigh_stream_kernel<HDIM><<<wgs, 256, 0, st>>>(a);
-  else if (s.rows) weigh_mfma_kernel<HDIM, WEIGH_PAGES, true><<<wgs, 256, 0, st>>>(a);
-  else weigh_mfma_kernel<HDIM, WEIGH_PAGES, false><<<wgs, 256, 0, st>>>(a);
+  else if (!s.rows) weigh_mfma_kernel<HDIM, WEIGH_PAGES, 4, false><<<wgs, 256, 0, st>>>(a);
+  else if (s.waves == 4) weigh_mfma_kernel<HDIM, WEIGH_PAGES, 4, true><<<wgs, 256, 0, st>>>(a);
+  else weigh_mfma_kernel<HDIM, WEIGH_PAGES, 8, true><<<wgs, 512, 0, st>>>(a);
 }
 
 void launch_weigh(WeighArgs a, hipStream_t st) {
@@ -772,8 +813,8 @@ void launch_weigh(WeighArgs a, hipStream_t st) {
   const WeighShape s = weigh_shape(a);
   a.range_keys = s.keys;
   if (!weigh_mfma(a)) {
-    if (a.dtype == MN_DT_BF16) launch_weigh_f32<f16_t>(a, wgs, st);
-    else launch_weigh_f32<float>(a, wgs, st);
+    if (a.dtype == MN_DT_BF16) launch_weigh_f32<f16_t>(a, s.rows, wgs, st);
+    else launch_weigh_f32<float>(a, s.rows, wgs, st);
   } else if (a.hd == 128) {
     launch_weigh_mfma<128>(a, s, wgs, st);
   } else {

@@ -267,17 +267,19 @@ def qk_norm_rope(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: torch.
                  dev_status: Optional[torch.Tensor] = None) -> None:
     """Projected rows (fp32 or the activation type; views with any row stride) normed per head, turned to positions [axes][M] and rounded:
     queries into q_out, keys and values into the cache behind ctx_lens and, where given, into dense rows."""
-    d = model.desc
-    M, p = sum(h_spec_len) + len(h_spec_len), lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    assert q.dtype == k.dtype == v.dtype and q.dtype in (torch.float32, activation_type(d))
-    assert q.shape == (M, d.n_heads, d.head_dim) and k.shape == v.shape == (M, d.n_kv_heads, d.head_dim)
-    assert q.stride()[1:] == k.stride()[1:] == v.stride()[1:] == (d.head_dim, 1)
-    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == rule.n_axes * M)
-    for t, heads in ((q_out, d.n_heads), (k_out, d.n_kv_heads), (v_out, d.n_kv_heads)):
-        assert t is None or (t.is_contiguous() and t.dtype == activation_type(d) and t.numel() == M * heads * d.head_dim)
-    B.mn_qk_norm_rope(model.ctx, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
-                      1 if q.dtype == torch.float32 else 0, rule.c, p(positions), p(spec_len), B.host_i32(h_spec_len), len(h_spec_len),
-                      kv.c if kv is not None else None, layer, p(q_out), p(k_out), p(v_out), p(dev_status), stream_ptr())
+    d, n = model.desc, len(h_spec_len)
+    M, H, Hk, hd, act, kind = sum(h_spec_len) + n, d.n_heads, d.n_kv_heads, d.head_dim, activation_type(d), q.dtype
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    assert (kind is act or kind is torch.float32) and kind is k.dtype and kind is v.dtype
+    assert q.shape == (M, H, hd) and k.shape == (M, Hk, hd) and v.shape == (M, Hk, hd) and qs[1:] == ks[1:] == vs[1:] == (hd, 1)
+    assert positions is None or (positions.dtype is torch.int32 and positions.numel() == rule.n_axes * M and positions.is_contiguous())
+    for t, heads in ((q_out, H), (k_out, Hk), (v_out, Hk)):
+        assert t is None or (t.dtype is act and t.numel() == M * heads * hd and t.is_contiguous())
+    B.mn_qk_norm_rope(model.ctx, q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0], kind is torch.float32, rule.c,
+                      None if positions is None else positions.data_ptr(), None if spec_len is None else spec_len.data_ptr(),
+                      B.host_i32(h_spec_len), n, None if kv is None else kv.c, layer, None if q_out is None else q_out.data_ptr(),
+                      None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(),
+                      None if dev_status is None else dev_status.data_ptr(), stream_ptr())
 
 
 class WindowSession:
@@ -297,8 +299,8 @@ class WindowSession:
                   stats: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [rows][H][hd] in the slots ctx_b .. ctx_b + spec_len[b], whose keys are in the cache; out [rows][H * hd]; stats
         [rows][H][2], for KVLedger.weigh."""
-        assert q.is_contiguous() and out.is_contiguous() and out.dtype == q.dtype == activation_type(self.model.desc)
-        assert stats is None or (stats.is_contiguous() and stats.dtype == torch.float32)
+        assert q.is_contiguous() and out.is_contiguous() and out.dtype is q.dtype is activation_type(self.model.desc)
+        assert stats is None or (stats.dtype is torch.float32 and stats.is_contiguous())
         assert len(h_spec_len) == 0 or max(h_spec_len) < self.max_q
         B.mn_window_attention(self.model.ctx, q.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len), self.window,
                               self.sinks, self.max_ctx, self.kv.c, layer, out.data_ptr(), stats.data_ptr() if stats is not None else None,
