@@ -777,7 +777,7 @@ static WeighShape weigh_shape(const WeighArgs& a) {
   }
   const int each = WEIGH_PAGES * WPAGE;
   const long chunks = heads * ((a.max_ctx + each - 1) / each);
-  if (chunks >= 4 * MN_TUNE("MN_WEIGH_ROWS", WEIGH_WGS)) return WeighShape{4 * each, false, false, 4};
+  if (chunks >= 4 * MN_TUNE("MN_WEIGH_ROWS", WEIGH_WGS) && R <= 4096) return WeighShape{4 * each, false, false, 4};
   return WeighShape{each, false, true, chunks < MN_TUNE("MN_WEIGH_EIGHT", 512) ? 8 : 4};
 }
 long weigh_workgroups(const WeighArgs& a) {
