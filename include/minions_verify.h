@@ -527,7 +527,8 @@ mn_status mn_window_attention(mn_ctx *ctx, const void *q, const int32_t *spec_le
                               size_t workspace_bytes, int32_t *dev_status, void *stream);
 
 /* What is known of every cached token, per layer, slot and KV head: the attention weight that it has been given, and the number that it
- * has in its text (which its slot stops telling with the first eviction). */
+ * has in its text (which its slot stops telling with the first eviction).  Lines belong to slots: mn_kv_compact does not touch them, and
+ * of a fork they are copied by whoever wants the child to go on counting. */
 typedef struct {
   float *mass;   /* dev [n_layers][max_seqs][n_kv_heads][width] */
   int32_t *born; /* dev, likewise */

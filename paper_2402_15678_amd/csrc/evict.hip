@@ -90,9 +90,9 @@ __device__ __forceinline__ void put_weight(const WeighArgs& a, const Weighed& w,
 
 constexpr int WPAGE = 16;
 // Exponent that a row's scores start from, -(m + log2 l), and whether its weights need more care than 2^(c s + that): statistics that are
-// no numbers (its scores may be none either), and far references.
+// no numbers (its scores may be none either), and references from 2^8 on, whose sum with log2 l is rounded by more than 2^-17.
 __device__ __forceinline__ float row_start(float2 st, bool& careful) {
-  careful |= !(st.y >= 0x1p-120f) | !(st.y < INFINITY) | !(__builtin_fabsf(st.x) < FAR_W);
+  careful |= !(st.y >= 0x1p-120f) | !(st.y < INFINITY) | !(__builtin_fabsf(st.x) < 0x1p8f);
   return -st.x - __builtin_amdgcn_logf(st.y);
 }
 
@@ -327,6 +327,8 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
 }
 
 // A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction; ROWS: all waves the same keys and every fourth tile.
+// The products are those of the attention, factor for factor and in its order (as they are in the fp16 kernels): beyond 2^24 a
+// reference is only as good as the very score that it came from.
 template <typename T, int HDP, bool ROWS>
 __global__ void __launch_bounds__(256) weigh_f32_kernel(WeighArgs a) {
   constexpr int NU = HDP / 16;
@@ -372,19 +374,15 @@ __global__ void __launch_bounds__(256) weigh_f32_kernel(WeighArgs a) {
   };
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   const auto work = [&](const Tile& t, int r0) {
-    f32x4 S = {0.f, 0.f, 0.f, 0.f}, S2 = S;                         // (two sums: neither waits for itself)
+    f32x4 S = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f32x4& to = e & 1 ? S2 : S;
-        to = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u][e], HDP == 16 && 4 * g >= hd ? 0.f : (float)t.q[u].x[e], to, 0, 0, 0);
-      }
-    S += S2;
+      for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_16x16x4f32(k[u][e], HDP == 16 && 4 * g >= hd ? 0.f : (float)t.q[u].x[e] * c, S, 0, 0, 0);
     const float share = r0 + l16 < R ? row_share(t.st) : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float x = weight(S[e], c, t.st.x, share);
+      const float x = weight(S[e], 1.f, t.st.x, share);
       sum[e] += key0 + 4 * g + e <= t.lim ? x : 0.f;
     }
   };

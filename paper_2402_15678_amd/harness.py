@@ -310,7 +310,7 @@ class WindowSession:
 
 class KVLedger:
     """What is known of the cached tokens: the attention weight that each has been given, and its number in the text, [layers][slots]
-    [Hkv][width] both."""
+    [Hkv][width] both.  A slot's lines stay with the slot: whoever forks a request copies them."""
 
     def __init__(self, model: DeviceModel, kv: DeviceKV, mass: torch.Tensor, born: torch.Tensor):
         assert mass.dtype == torch.float32 and born.dtype == torch.int32 and mass.is_contiguous() and born.is_contiguous()
@@ -318,6 +318,8 @@ class KVLedger:
         self.model, self.kv, self.mass, self.born = model, kv, mass, born
         self.c = B.Ledger(mass.data_ptr(), born.data_ptr(), mass.shape[1], mass.shape[3])
         self.dev_status = torch.zeros((1,), dtype=torch.int32, device=mass.device)
+        self.ws_bytes = B.mn_evict_workspace_bytes(model.ctx, mass.shape[1], mass.shape[3])   # (of KVPool.evict)
+        self.workspace = torch.empty((self.ws_bytes,), dtype=torch.uint8, device=mass.device)
 
     @classmethod
     def empty(cls, model: DeviceModel, kv: DeviceKV, max_seqs: int, width: int) -> "KVLedger":
@@ -388,15 +390,8 @@ class KVPool:
     def evict(self, keep: torch.Tensor, sinks: int, recent: int, ledger: KVLedger) -> None:
         """Slots 0 .. len(keep) - 1 are cut back to keep[b] tokens: the first `sinks`, the `recent` newest, and those with the most weight
         in the ledger."""
-        n, width = keep.numel(), int(ledger.mass.shape[3])
-        if getattr(self, "_evict_for", (0, 0)) < (n, width) or self._evict_for[1] < width:
-            self.evict_bytes = B.mn_evict_workspace_bytes(self.model.ctx, n, width)
-            if self.evict_bytes == 0:
-                raise RuntimeError("mn_evict_workspace_bytes rejected the shape")
-            self.evict_workspace = torch.empty((self.evict_bytes,), dtype=torch.uint8, device=self.state.device)
-            self._evict_for = (n, width)
-        B.mn_kv_evict(self.model.ctx, self.kv.c, self.c, keep.data_ptr(), n, sinks, recent, ledger.c, self.evict_workspace.data_ptr(),
-                      self.evict_bytes, self.dev_status.data_ptr(), stream_ptr())
+        B.mn_kv_evict(self.model.ctx, self.kv.c, self.c, keep.data_ptr(), keep.numel(), sinks, recent, ledger.c, ledger.workspace.data_ptr(),
+                      ledger.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
 
 
 class VerifySession:

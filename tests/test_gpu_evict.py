@@ -13,7 +13,7 @@ from tests.test_gpu_window import Batch
 pytestmark = pytest.mark.gpu
 DT = {"f16": torch.float16, "f32": torch.float32}
 LOG2E = 1.4426950408889634
-GEOMETRIES = [(64, 8, 128, "f16"), (4, 4, 128, "f16"), (12, 12, 64, "f16"), (6, 2, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 128, "f32"),
+GEOMETRIES = [(64, 8, 128, "f16"), (4, 4, 128, "f16"), (12, 12, 64, "f16"), (6, 2, 64, "f16"), (128, 2, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 128, "f32"),
               (6, 2, 32, "f32"), (8, 8, 8, "f32"), (2, 2, 256, "f32"), (8, 8, 32, "f16"), (8, 2, 256, "f16"), (8, 2, 16, "f32")]
 
 
@@ -125,10 +125,44 @@ def test_weights_of_many_sequences(count):
 
 
 def test_long_contexts_and_prompts():
-    for H, Hkv, hd, kind, ctx, ks in ((16, 2, 128, "f16", [9000], [8]), (4, 2, 128, "f16", [0, 300], [1500, 700]), (2, 2, 64, "f32", [0], [900])):
+    for H, Hkv, hd, kind, ctx, ks in ((16, 2, 128, "f16", [9000], [8]), (4, 2, 128, "f16", [0, 300], [1500, 700]), (2, 2, 64, "f32", [0], [900]),
+                                      (6, 2, 128, "f16", [40, 0], [350, 1]), (40, 40, 128, "f16", [700] * 8, [200] * 8), (12, 12, 64, "f16", [700, 3] * 8, [100, 230] * 8),
+                                      (16, 2, 64, "f16", [0], [5000])):
         x = Weighed(H, Hkv, hd, kind, ctx, ks, 6)
         assert x.weigh() == 0
         x.check_weights()
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind", [(8, 2, 128, "f16"), (4, 4, 64, "f16"), (4, 2, 64, "f32")])
+@pytest.mark.parametrize("ctx,ks", [([300, 40], [3, 0]), ([0], [400])], ids=str)
+@pytest.mark.parametrize("far", [False, True])
+def test_large_references(H, Hkv, hd, kind, ctx, ks, far):
+    """Scores so far apart that a row's weight is all on the keys that attain its largest, in equal shares; the statistics are the attention's own."""
+    x = Weighed(H, Hkv, hd, kind, ctx, ks, 9)
+    g = np.random.default_rng(9)
+    for b in range(len(ks)):
+        n = x.tot[b]
+        k = torch.tensor(g.integers(1, 9, (n, Hkv)) * (4096.0 if far else 1.0), device="cuda")[:, :, None].expand(n, Hkv, hd)
+        p = torch.arange(n, device="cuda")
+        blk = torch.from_numpy(x.full[b].astype(np.int64)).cuda()[p // 16]
+        x.kp[blk, :, :, p % 16] = k.reshape(n, Hkv, hd // 8, 8).to(x.kp.dtype)
+    x.q.fill_(64.0 if not far else 65504.0 if kind == "f16" else 2.0 ** 40)
+    _, status = x.run(stats=x.stats)
+    assert status == 0 and (x.stats[:, :, 0].abs() >= (2.0 ** 24 if far else 500)).all()
+    assert x.weigh() == 0
+    for b in range(len(ks)):
+        k, _ = x.dense(b)
+        seen = x.visible(b)
+        for h in range(Hkv):
+            s = k[:, h, 0].double().expand(len(seen), -1).masked_fill(~seen, -math.inf)
+            p = (s == s.amax(dim=1, keepdim=True)).double()
+            want = (p / p.sum(dim=1, keepdim=True)).sum(dim=0) * (H // Hkv)
+            want[:x.ctx[b]] += x.mass0[0, b, h, :x.ctx[b]].double()
+            # Ties are equal whatever the roundings: what is left are the sums and the quotients.  Below 2^24 the fp16 attention takes c s - m in one
+            # rounding, which of the largest score is the rounding of m = c s and not 0: at most 2^-24 of m < 2^15, so that its probability is within
+            # 2^-9 of 1, and is off by half a step, 2^-11, as the sum l has it (fp16) and as it is here (not rounded).
+            tol = (len(seen) * (H // Hkv) + x.tot[b] + 64) * 2.0 ** -23 + (2.0 ** -11 if kind == "f16" and not far else 0)
+            assert ((x.ledger.mass[0, b, h, :x.tot[b]].double() - want).abs() <= want * tol).all()
 
 
 def test_rows_without_statistics_give_nothing():

@@ -326,3 +326,21 @@ def test_captured_and_replayed_on_another_stream(ctx):
     graphs[0].replay()
     torch.cuda.synchronize()
     x.check(outs[0])
+
+
+@pytest.mark.parametrize("ctx", [[200, 31, 0, 64], [5000, 31, 0, 4000]], ids=str)
+def test_two_calls_at_once(ctx):
+    """Sessions of their own, on streams of their own."""
+    from paper_2402_15678_amd import harness
+    xs = [Batch(64, 8, 128, "f16", ctx, [2, 0, 5, 1], w, 4, 13 + w, blind=False) for w in (700, 1500)]
+    want = [x.run()[0] for x in xs]
+    ses = [harness.WindowSession(x.model, x.kv(), 4, len(x.q), 6, x.max_ctx, x.window, 4) for x in xs]
+    spec = torch.tensor(xs[0].ks, dtype=torch.int32, device="cuda")
+    outs, streams = [torch.zeros_like(o) for o in want], [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, s, o, st in zip(xs, ses, outs, streams):
+            with torch.cuda.stream(st):
+                s.attention(x.q, spec, x.ks, o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
