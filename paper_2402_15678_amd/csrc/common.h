@@ -174,6 +174,18 @@ __device__ __forceinline__ void dma16(const char* g, uint32_t lds_base) {
   else
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off offset:%2" ::"v"(g), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
 }
+// dma16 from a scalar base and a 32-bit offset per lane
+template <int OFFSET, bool STREAM>
+__device__ __forceinline__ void dma16s(const char* base, uint32_t off, uint32_t lds_base) {
+  if constexpr (STREAM)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3 nt" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
+}
+// the same of 4 bytes per lane
+__device__ __forceinline__ void dma4s(const char* base, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds_base) : "memory");
+}
 // wait until at most N of this wave's memory loads are outstanding (they complete in order)
 template <int N>
 __device__ __forceinline__ void wait_vm() {

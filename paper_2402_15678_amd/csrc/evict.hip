@@ -96,19 +96,24 @@ __device__ __forceinline__ float row_start(float2 st, bool& careful) {
   return -st.x - __builtin_amdgcn_logf(st.y);
 }
 
-// Many rows (prompts).  A wave takes the keys of PAGES pages into registers, as they lie there (a page is the operand of the product: 16
-// keys by 8 elements in 256 bytes), and the rows that see them in tiles of 16, the next one on its way meanwhile.  ROWS: the NW waves have the
-// same keys and every NW-th tile, for calls whose keys alone would not fill the chip.
-template <int HDIM, int PAGES, int NW, bool ROWS>
-__global__ void __launch_bounds__(64 * NW, HDIM == 64 ? 3 : 2) weigh_mfma_kernel(WeighArgs a) {
-  constexpr int HS = HDIM / 32;
+// Many rows (prompts).  The NW waves of a workgroup take the keys of PAGES pages into registers, as they lie there (a page is the operand of
+// the product: 16 keys by 8 elements in 256 bytes), and of the rows that see them every NW-th tile of 16 each.  A wave fetches its tiles into
+// places of its own in the LDS, two ahead, by direct loads of whole rows: straight into the operands' registers every lane of a load met
+// another line, and neither the exponentials nor the products were what it waited for (8000 rows of 40 heads of 128 629 us, without either
+// the same, without the loads 418; so 437, 750 TFLOP/s, where a large product reaches 1073: without the exponentials 402, without the fetches
+// 361, without the reads from the LDS 438).  16-byte chunks of a row change places, so that the reads of the operands meet every bank.
+template <int HDIM, int PAGES, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) weigh_mfma_kernel(WeighArgs a) {
+  constexpr int HS = HDIM / 32, CH = HDIM / 8, RPL = 64 / CH, LOADS = 16 / RPL;  // 16-byte chunks of a row, rows of a load, loads of a tile
+  constexpr int SLOTS = 3, BYTES = 16 * HDIM * 2 + 256;            // a tile: its rows, and their statistics
+  __shared__ __attribute__((aligned(1024))) unsigned char s_rows[NW][SLOTS][BYTES];
   __shared__ float s_sum[NW][PAGES * WPAGE];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.B, chunk = rest / a.B;
   Weighed w;
   if (!weighed_rows<NW>(a, b, w)) return;
-  const int end = w.base + w.count, key0 = (ROWS ? chunk : chunk * NW + wave) * (PAGES * WPAGE);
+  const int end = w.base + w.count, key0 = chunk * (PAGES * WPAGE);
   if (key0 >= end) return;
   const int G = a.H / a.Hkv, R = w.count * G, shift = (G & (G - 1)) == 0 ? 31 - __clz(G) : -1;
   const int32_t* bt = a.kv.block_tables + (size_t)b * a.kv.max_blocks_per_seq;
@@ -126,59 +131,83 @@ __global__ void __launch_bounds__(64 * NW, HDIM == 64 ? 3 : 2) weigh_mfma_kernel
 #pragma unroll
   for (int p = 0; p < PAGES; ++p) sum[p] = (f32x4){0.f, 0.f, 0.f, 0.f};
   const float c = rsqrtf((float)HDIM) * LOG2E_W;
-  struct Tile {
-    f16x8 q[HS];
-    float2 st;
-    int lim;
+  const auto token_of = [&](int r) { return shift >= 0 ? r >> shift : (int)((uint32_t)r / (uint32_t)G); };
+  const auto turn = [](int row) { return HDIM == 128 ? row & 15 : row >> 1 & 7; };
+
+  // ---- fetching.  Where G divides 16 all tiles but the last are the same pattern of rows further on. ----
+  const bool regular = shift >= 0 && G <= 16;
+  const int last_tile = (R - 1) / 16 * 16;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)&s_rows[wave][0][0]);
+  const auto place = [&](int i) {                                  // row i from a token's first one on, in rows and heads
+    const int j = token_of(i);
+    return (uint32_t)(j * a.H + i - j * G);
   };
-  const auto load = [&](int r0, Tile& t) {                          // (past the last row: that one once more)
-    const int r = min(r0 + l16, R - 1), j = shift >= 0 ? r >> shift : (int)((uint32_t)r / (uint32_t)G);
-    const size_t mh = (size_t)(w.row0 + j) * a.H + kvh * G + r - j * G;
-    const f16_t* q = static_cast<const f16_t*>(a.q) + mh * HDIM;
+  const auto offset = [&](int load, int r0, int j0) {              // the lane's bytes of a load of the tile at r0 (past the last row: that one once more)
+    const int row = load * RPL + lane / CH;
+    return place(min(r0 + row, R - 1) - j0 * G) * (uint32_t)(HDIM * 2) + 16u * (uint32_t)((lane % CH) ^ turn(row));
+  };
+  const auto stat_offset = [&](int r0, int j0) { return place(min(r0 + (lane >> 1 & 15), R - 1) - j0 * G) * 8u + 4u * (lane & 1); };
+  uint32_t off[LOADS], stat_off = stat_offset(0, 0);
 #pragma unroll
-    for (int s = 0; s < HS; ++s) t.q[s] = *reinterpret_cast<const f16x8*>(q + 32 * s + 8 * g);
-    t.st = *reinterpret_cast<const float2*>(a.stats + mh * 2);
-    t.lim = w.base + j;
+  for (int i = 0; i < LOADS; ++i) off[i] = offset(i, 0, 0);
+  const auto fetch = [&](int r0, int slot) {
+    const int rc = min(r0, last_tile), j0 = __builtin_amdgcn_readfirstlane(token_of(rc));
+    const size_t mh = (size_t)(w.row0 + j0) * a.H + kvh * G;
+    const char* q = reinterpret_cast<const char*>(static_cast<const f16_t*>(a.q) + mh * HDIM);
+    const char* stats = reinterpret_cast<const char*>(a.stats + mh * 2);
+    const uint32_t to = lds0 + (uint32_t)slot * BYTES;
+    const bool same = regular && rc < last_tile;                   // (uniform)
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) dma16s<0, false>(q, same ? off[i] : offset(i, rc, j0), to + 1024u * i);
+    dma4s(stats, same ? stat_off : stat_offset(rc, j0), to + 16 * HDIM * 2);
   };
-  // rows before this key's own see none of them
-  constexpr int STEP = ROWS ? 16 * NW : 16;
-  int r0 = max(0, key0 - w.base) * G / 16 * 16 + (ROWS ? 16 * wave : 0);
-  Tile now, next;
-  const auto work = [&](const Tile& t, int r0) {
-    bool careful = false;
-    float start = row_start(t.st, careful);
-    if (r0 + l16 >= R) start = -INFINITY;
-    const bool all = !__any(t.lim < key0 + PAGES * WPAGE - 1);
+  const auto work = [&](int r0, int slot) {
+    const unsigned char* st = s_rows[wave][slot];
+    f16x8 q[HS];
+#pragma unroll
+    for (int s = 0; s < HS; ++s) q[s] = *reinterpret_cast<const f16x8*>(st + l16 * (2 * HDIM) + 16 * ((4 * s + g) ^ turn(l16)));
+    const float2 stat = *reinterpret_cast<const float2*>(st + 16 * HDIM * 2 + l16 * 8);
+    bool careful = r0 + l16 >= R;
+    const float start = row_start(stat, careful);
+    const bool all = w.base + token_of(r0) >= key0 + PAGES * WPAGE - 1;
     f32x4 S[PAGES];
 #pragma unroll
     for (int p = 0; p < PAGES; ++p) S[p] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < HS; ++s)
 #pragma unroll
-      for (int p = 0; p < PAGES; ++p) S[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[p][s], t.q[s], S[p], 0, 0, 0);
+      for (int p = 0; p < PAGES; ++p) S[p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[p][s], q[s], S[p], 0, 0, 0);
     if (all && !__any(careful)) {
 #pragma unroll
       for (int p = 0; p < PAGES; ++p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[p][e] += __builtin_amdgcn_exp2f(fmaf(S[p][e], c, start));
     } else {
-      const float share = r0 + l16 < R ? row_share(t.st) : 0.f;
+      const float share = r0 + l16 < R ? row_share(stat) : 0.f;
+      const int lim = w.base + token_of(min(r0 + l16, R - 1));
 #pragma unroll
       for (int p = 0; p < PAGES; ++p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = weight(S[p][e], c, t.st.x, share);
-          sum[p][e] += key0 + p * WPAGE + 4 * g + e <= t.lim ? x : 0.f;
+          const float x = weight(S[p][e], c, stat.x, share);
+          sum[p][e] += key0 + p * WPAGE + 4 * g + e <= lim ? x : 0.f;
         }
     }
   };
-  load(r0, now);                                                   // (unconditionally, so that waits stay counted)
-  for (; r0 < R; r0 += 2 * STEP) {
-    load(r0 + STEP, next);
-    work(now, r0);
-    load(r0 + 2 * STEP, now);
-    if (r0 + STEP < R) work(next, r0 + STEP);
+  // rows before this key's own see none of them
+  constexpr int STEP = 16 * NW;
+  int r0 = max(0, key0 - w.base) * G / 16 * 16 + 16 * wave, slot = 0;
+  fetch(r0, 0);
+  fetch(r0 + STEP, 1);
+  for (; r0 < R; r0 += STEP) {
+    const int third = slot == 0 ? 2 : slot - 1;
+    __builtin_amdgcn_s_waitcnt(0xc07f);                            // lgkmcnt(0): the wave has read that place
+    fetch(r0 + 2 * STEP, third);
+    wait_vm<2 * (LOADS + 1)>();                                    // (this tile is there; the two behind it may be on their way)
+    work(r0, slot);
+    slot = slot == SLOTS - 1 ? 0 : slot + 1;
   }
+  wait_vm<0>();
 #pragma unroll
   for (int p = 0; p < PAGES; ++p) {
 #pragma unroll
@@ -191,15 +220,12 @@ __global__ void __launch_bounds__(64 * NW, HDIM == 64 ? 3 : 2) weigh_mfma_kernel
       if (l16 == 0) s_sum[wave][p * WPAGE + 4 * g + e] = v;
     }
   }
-  if constexpr (ROWS) {
-    __syncthreads();
-    if (wave > 0) return;
-  }
+  __syncthreads();
+  if (wave > 0) return;
   static_assert(PAGES * WPAGE == 64, "a key per lane");
-  float v = s_sum[wave][lane];
-  if constexpr (ROWS)
+  float v = s_sum[0][lane];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) v += s_sum[i][lane];
+  for (int i = 1; i < NW; ++i) v += s_sum[i][lane];
 #pragma unroll
   for (int p = 0; p < PAGES; ++p) {
     if (lane >> 4 == p && !lost[p]) put_weight(a, w, b, kvh, key0 + lane, v);
@@ -208,7 +234,8 @@ __global__ void __launch_bounds__(64 * NW, HDIM == 64 ? 3 : 2) weigh_mfma_kernel
 }
 
 // Few rows (steps).  The rows of a KV head, STREAM_ROWS at most, wait in the LDS, and the keys go by: a wave takes two pages at a time, the next two on
-// their way, the row as the first index of the product (a lane then has one key's weights, of four rows each time).  Bound by HBM.
+// their way, the row as the first index of the product (a lane then has one key's weights, of four rows each time).  Bound by HBM: 9 rows of 64/8 heads
+// of 128, 32 sequences of 1000 to 8000 tokens 66 us, 4.2 TB/s (a wave that took its keys once and the rows from HBM 103).
 constexpr int STREAM_ROWS = 160;
 template <int HDIM>
 __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
@@ -326,7 +353,9 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
   if (__any(lost && lane < 32) && lane == 0 && a.status) atomicOr(a.status, MN_DEV_BLOCK_TABLE);
 }
 
-// A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction; ROWS: all waves the same keys and every fourth tile.
+// A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction; ROWS: all waves the same keys and every fourth tile
+// (3 prompts of 600 rows of 8/2 heads of 256: 78 us, keys shared out 488).  Products and their order are the attention's own.  Bound by that
+// instruction, and with few rows by launch.
 // The products are those of the attention, factor for factor and in its order (as they are in the fp16 kernels): beyond 2^24 a
 // reference is only as good as the very score that it came from.
 template <typename T, int HDP, bool ROWS>
@@ -472,7 +501,8 @@ __device__ __forceinline__ void waves_sum(int (&v)[N], int (*s)[WAVES][4], int& 
 // A wave has a contiguous piece of the slots, a lane every 64th of it: PER of them, as ranks in registers (PER 0: any number, read again each
 // time).  The keep-th rank is found digit by digit, counting in the LDS; among the tokens of that very rank the lowest slots stay.
 // Then the slots below `keep` that are left, in ascending order, take the tokens that stay from `keep` on, in ascending order: there are
-// as many of either.
+// as many of either.  A workgroup has one head, and what it waits for is one step after the other: 8 layers of 8 heads of 16 sequences of 1000 to
+// 4000 tokens 37 us, one sequence of the smallest model 7.
 template <int WAVES, int PER>
 __global__ void __launch_bounds__(64 * WAVES) evict_plan_kernel(EvictArgs a) {
   __shared__ int s_count[2][WAVES][4], s_bins[4][256], s_digit[2];
@@ -756,7 +786,7 @@ __global__ void __launch_bounds__(256) evict_pages_kernel(EvictArgs a, LayerPage
 // ------------------------------------------------------------------------------------------
 static bool weigh_mfma(const WeighArgs& a) { return a.dtype == MN_DT_BF16 && (a.hd == 64 || a.hd == 128) && a.kv.block_size == WPAGE; }
 constexpr int WEIGH_PAGES = 4;
-constexpr int WEIGH_WGS = 1024;        // to aim for
+constexpr int WEIGH_WGS = 1024;        // to aim for (512, 1024, 2048: 81, 69, 73 us with 9 rows of 64/8 heads, 32 sequences of 1000 to 8000 tokens)
 
 struct WeighShape {
   int keys;                            // of a workgroup
@@ -766,17 +796,22 @@ struct WeighShape {
 static WeighShape weigh_shape(const WeighArgs& a) {
   const long heads = (long)a.B * a.Hkv, R = (long)a.max_q * (a.H / a.Hkv);
   if (!weigh_mfma(a)) return R > 64 ? WeighShape{16, false, true, 4} : WeighShape{64, false, false, 4};
-  if (R <= STREAM_ROWS) {
+  // The rows stay and the keys go by, or the other way round.  Over 64 rows the first pays where keys are many: 128 rows of 64/8 heads, 32
+  // sequences of 4000 tokens 76 us (rows going by: 116), of 40 heads, 4 of 2000 tokens 36 (43), 8 of 500 tokens 38 (29); of 64/8 heads, 8 of
+  // 2000 tokens 26 (21), their 64 rows 18 (17).
+  if (R <= 64 || (R <= STREAM_ROWS && heads * a.max_ctx >= 256 * WEIGH_WGS)) {
     // ranges of 128 keys (two pages for each wave) and more
-    long keys = (long)a.max_ctx * heads / MN_TUNE("MN_WEIGH_WGS", WEIGH_WGS) / 128 * 128;
+    long keys = (long)a.max_ctx * heads / WEIGH_WGS / 128 * 128;
     if (keys < 128) keys = 128;
     if (keys > 4096) keys = 4096;
     return WeighShape{(int)keys, true, false, 4};
   }
   const int each = WEIGH_PAGES * WPAGE;
-  const long chunks = heads * ((a.max_ctx + each - 1) / each);
-  if (chunks >= 4 * MN_TUNE("MN_WEIGH_ROWS", WEIGH_WGS) && R <= 4096) return WeighShape{4 * each, false, false, 4};
-  return WeighShape{each, false, true, chunks < MN_TUNE("MN_WEIGH_EIGHT", 512) ? 8 : 4};
+  // Eight waves where workgroups are few (1500 rows of 64/8 heads: 73 us, with four 121; 1000 rows of 40 heads, 640 workgroups: 27, with four
+  // 19), two where they are many and each has little to do (8 prompts of 1000 rows of 40 heads 93 us, with four 117, with one 98; 2 of 3000
+  // rows 166, with four 161).
+  const long wgs = heads * ((a.max_ctx + each - 1) / each);
+  return WeighShape{each, false, true, wgs < 512 ? 8 : wgs >= 2048 && R <= 2048 ? 2 : 4};
 }
 long weigh_workgroups(const WeighArgs& a) {
   const int keys = weigh_shape(a).keys;
@@ -801,9 +836,9 @@ static void launch_weigh_f32(const WeighArgs& a, bool rows, unsigned wgs, hipStr
 template <int HDIM>
 static void launch_weigh_mfma(const WeighArgs& a, const WeighShape& s, unsigned wgs, hipStream_t st) {
   if (s.stream) weigh_stream_kernel<HDIM><<<wgs, 256, 0, st>>>(a);
-  else if (!s.rows) weigh_mfma_kernel<HDIM, WEIGH_PAGES, 4, false><<<wgs, 256, 0, st>>>(a);
-  else if (s.waves == 4) weigh_mfma_kernel<HDIM, WEIGH_PAGES, 4, true><<<wgs, 256, 0, st>>>(a);
-  else weigh_mfma_kernel<HDIM, WEIGH_PAGES, 8, true><<<wgs, 512, 0, st>>>(a);
+  else if (s.waves == 2) weigh_mfma_kernel<HDIM, WEIGH_PAGES, 2><<<wgs, 128, 0, st>>>(a);
+  else if (s.waves == 4) weigh_mfma_kernel<HDIM, WEIGH_PAGES, 4><<<wgs, 256, 0, st>>>(a);
+  else weigh_mfma_kernel<HDIM, WEIGH_PAGES, 8><<<wgs, 512, 0, st>>>(a);
 }
 
 void launch_weigh(WeighArgs a, hipStream_t st) {

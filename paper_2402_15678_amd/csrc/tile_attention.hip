@@ -453,15 +453,6 @@ __device__ __forceinline__ void pieces(F f) {
   }
 }
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-// dma16 from a scalar base and a 32-bit offset per lane
-template <int OFFSET, bool STREAM>
-__device__ __forceinline__ void dma16s(const char* base, uint32_t off, uint32_t lds_base) {
-  if constexpr (STREAM)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3 nt" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3" ::"v"(off), "s"(base), "s"(lds_base - (uint32_t)OFFSET), "n"(OFFSET) : "memory");
-}
-
 // the largest of a lane's eight scores (`maximum` takes a NaN as it is, and so needs no instruction to quiet one first)
 __device__ __forceinline__ float top(const f32x4 (&S)[2]) {
   const auto m = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
