@@ -1691,13 +1691,17 @@ hipError_t launch_prefix(TileArgs a, void* workspace, hipStream_t st) {
   return hipSuccess;
 }
 
-// Shape of a windowed launch.  Rows of a tile: 128 where a sequence's run fills most of them, as behind a prefix.
+// Shape of a windowed launch.  Rows of a tile: 128 (each key is staged half as often) where tiles of 64 would be more than the chip holds at
+// once.  8 runs of 80 rows behind windows of 1024, 40 heads of 128: 45 us, tiles of 64 62; of 128 rows 52 and 56; but 8 runs of 112 rows behind
+// windows of 4096, 64/8 heads: 42 and 38; 2 prompts of 80 rows, 40 heads: 10 and 7.5.  Ranges are as many as workgroups fit: halved, 4 sequences
+// of one row behind 4096, 64/8 heads 17.9 -> 19.0, 8 of 96 rows 37 -> 40; quartered 25 and 61.
 constexpr int WINDOW_RANGES = 16;      // of a tile's keys at most
 constexpr int MIN_GRAINS = 16;         // granules of a range at least
 int window_tile_rows(const TileArgs& a) {
   if (!tile_mfma(a, true)) return FROWS;
   if (const int f = MN_TUNE("MN_TILE", 0)) return f;
-  return (long)(a.H / a.Hkv) * a.batch.max_q >= 96 ? 128 : 64;
+  const long rows = (long)(a.H / a.Hkv) * a.batch.max_q;
+  return rows > 64 && (rows + 63) / 64 * a.B * a.Hkv > STREAMS ? 128 : 64;
 }
 struct WindowShape {
   int ranges, chunk;

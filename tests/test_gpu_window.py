@@ -129,6 +129,19 @@ def test_long_contexts_prompts_and_chunks(H, Hkv, hd, kind, window, sinks, ctx, 
     assert not (out == -7.0).all(dim=1).any()
 
 
+@pytest.mark.parametrize("H,Hkv,hd,window,sinks,ctx,ks", [
+    (64, 8, 128, 33, 20, [0, 200, 63, 5, 130] * 8, [12, 0, 20, 7, 1] * 8), (12, 12, 64, 48, 4, [100, 0, 17, 49] * 15, [70, 64, 0, 33] * 15),
+    (128, 2, 64, 16, 1, [0, 40, 333] * 24, [8, 0, 3] * 24), (4, 4, 128, 1000, 64, [300, 0, 1500] * 23, [99, 64, 65] * 23),
+    (6, 2, 128, 70, 0, [31, 700] * 50, [40, 41] * 50)], ids=str)
+def test_tiles_of_many_rows(H, Hkv, hd, window, sinks, ctx, ks):
+    """Runs of which tiles of 64 rows would be more than the chip holds at once."""
+    x = Batch(H, Hkv, hd, "f16", ctx, ks, window, sinks, 21)
+    out, status = x.run()
+    assert status == 0
+    x.check(out, list(range(5)) + [len(ks) - 2, len(ks) - 1])
+    x.check(out, None, [0])
+
+
 @pytest.mark.parametrize("H,Hkv,hd,kind,bs", [(4, 2, 128, "f16", 8), (6, 2, 32, "f32", 5), (12, 12, 64, "f16", 32), (8, 8, 8, "f32", 1), (4, 4, 64, "f32", 3)])
 def test_other_block_sizes(H, Hkv, hd, kind, bs):
     x = Batch(H, Hkv, hd, kind, [0, 2 * bs + 1, 150, 333], [3, 0, 5, 20], 37, 6, 6, bs=bs)
@@ -187,12 +200,13 @@ def test_agrees_with_the_attention_that_sees_everything():
         assert ((out[x.rows(b)].double() - want[x.rows(b)].double()).abs() <= 2 * bound).all()
 
 
+@pytest.mark.parametrize("H,Hkv,more", [(8, 2, 0), (128, 8, 54), (128, 8, 62)])
 @pytest.mark.parametrize("ctx,ks", [([20, 40, 60, 5, 330, 17], [2, 0, 5, 1, 3, 4]), ([20, 40, 4000, 5, 2500, 17], [2, 0, 5, 1, 3, 4])], ids=str)
-def test_damaged_sequences_get_zeros_and_the_others_their_results(ctx, ks):
-    """Rows that are written by one workgroup, and rows that are put together from ranges."""
+def test_damaged_sequences_get_zeros_and_the_others_their_results(ctx, ks, H, Hkv, more):
+    """Rows that are written by one workgroup (of both tile sizes), and rows that are put together from ranges."""
     from paper_2402_15678_amd import binding
-    x = Batch(8, 2, 128, "f16", ctx, ks, 3000, 4, 10, spare=2)
-    stats = torch.zeros((len(x.q), 8, 2), device="cuda")
+    x = Batch(H, Hkv, 128, "f16", ctx + [9] * more, ks + [0] * more, 3000, 4, 10, spare=2)
+    stats = torch.zeros((len(x.q), H, 2), device="cuda")
     good = x.table.copy()
     whole, status = x.run(stats=stats)
     assert status == 0
@@ -215,7 +229,7 @@ def test_damaged_sequences_get_zeros_and_the_others_their_results(ctx, ks):
         rest[r] = False
         assert torch.equal(out[rest], whole[rest]) and torch.equal(stats[rest], full[rest]), name
     for spec in ([2, 0, 5, 1, 3, 5], [3, 0, 5, 1, 2, -1], [2, 0, 6, 0, 3, 4]):
-        out, status = x.run(spec=spec, stats=stats)
+        out, status = x.run(spec=spec + [0] * more, stats=stats)
         assert status == binding.MN_DEV_SPEC_LEN and (out == 0).all() and (stats == 0).all()
 
 
@@ -235,7 +249,7 @@ def test_a_batch_that_does_not_add_up(count, hd, kind):
 
 
 @pytest.mark.parametrize("H,Hkv,hd,kind", [(64, 8, 128, "f16"), (4, 4, 64, "f16"), (4, 4, 64, "f32"), (8, 2, 128, "f32")])
-@pytest.mark.parametrize("ctx,ks", [([70, 0], [2, 90]), ([3000], [1])], ids=str)
+@pytest.mark.parametrize("ctx,ks", [([70, 0], [2, 90]), ([3000], [1]), ([11] * 70 + [70, 0], [20] * 70 + [2, 90])], ids=lambda v: f"{len(v)}-{v[-1]}")
 def test_what_is_not_finite_reaches_the_rows_that_see_it(H, Hkv, hd, kind, ctx, ks):
     window, sinks = 40, 3
     x = Batch(H, Hkv, hd, kind, ctx, ks, window, sinks, 11)
