@@ -6,10 +6,10 @@
 // token's key may stand in any slot of its sequence, each head's in another, since its rotation is in it and attention asks for no
 // order: so a head that loses tokens fills their slots with those that it keeps from behind the new end, and nothing else moves.
 //
-//  * weigh_mfma_kernel  fp16, head_dim 64 or 128, blocks of 16 tokens.
+//  * weigh_mfma_kernel, weigh_stream_kernel  fp16, head_dim 64 or 128, blocks of 16 tokens: many rows, few rows.
 //  * weigh_f32_kernel   every other type, head_dim and block size.
 //  * evict_plan_kernel  a workgroup per layer, slot and head: who stays, and who goes where.
-//  * evict_move_kernel  the tokens' keys and values; a workgroup per slot lets the blocks go.
+//  * evict_pages_kernel, evict_move_kernel  the tokens' keys and values (blocks of 16 tokens; others); a workgroup per slot lets the blocks go.
 #include "launch.h"
 #include "tune.h"
 #include "../../include/minions_verify.h"
@@ -694,8 +694,10 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a, LayerPages
 }
 
 // Blocks of 16 tokens: a wave takes a page at a time, the tokens that stay in it read as well, so that it is written in whole lines.  (Into the
-// places alone the writes were parts of lines: 16 sequences of 1000 to 4000 tokens cut to 1024, 8 layers of 8 heads of 128, 505 us.)  A piece of 16
-// bytes is (part of) one token of K, or PER tokens of one element of V; NU of them per lane.  What is next is looked up meanwhile.
+// places alone the writes were parts of lines: 16 sequences of 1000 to 4000 tokens cut to 1024, 8 layers of 8 heads of 128, 505 us; now
+// 391.)  A piece of 16 bytes is (part of) one token of K, or PER tokens of one element of V; NU of them per lane.  What is next is looked up
+// meanwhile.  Bound by HBM: a page's lines hold pieces of 4 to 8 of its tokens, so nearly every line of the pages that tokens come from and go to
+// passes, 1.8 GB at 4.6 TB/s, which is what a copy reaches; the tokens that move alone would be 0.66 GB.
 template <typename T, int NU>
 __global__ void __launch_bounds__(256) evict_pages_kernel(EvictArgs a, LayerPages pages, int layer0, int release) {
   constexpr int PER = 16 / sizeof(T), BS = 16, AT_ONCE = NU < 4 ? NU : 4;
@@ -891,6 +893,7 @@ void launch_evict(EvictArgs a, void* const* k, void* const* v, int n_layers, voi
     for (int l = 0; l < layers; ++l) { pages.k[l] = k[l0 + l]; pages.v[l] = v[l0 + l]; }
     const int release = l0 + layers == n_layers ? a.B : 0;
     const long r = (long)layers * a.B * a.Hkv;
+    // 1024, 2048, 4096, 8192, 16384 workgroups: 499, 493, 481, 471, 467 us (16 sequences cut to 1024 tokens, 8 layers of 8 heads, plan included)
     const int want = MN_TUNE("MN_EVICT_WGS", 8192), most = (a.width + 127) / 128;
     a.splits = r >= want ? 1 : (int)((want + r - 1) / r);
     if (a.splits > most) a.splits = most;
