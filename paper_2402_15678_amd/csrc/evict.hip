@@ -235,8 +235,9 @@ __global__ void __launch_bounds__(64 * NW, 2) weigh_mfma_kernel(WeighArgs a) {
 
 // Few rows (steps).  The rows of a KV head, STREAM_ROWS at most, wait in the LDS, and the keys go by: a wave takes two pages at a time, the next two on
 // their way, the row as the first index of the product (a lane then has one key's weights, of four rows each time).  Bound by HBM: 9 rows of 64/8 heads
-// of 128, 32 sequences of 1000 to 8000 tokens 66 us, 4.2 TB/s (a wave that took its keys once and the rows from HBM 103).
-constexpr int STREAM_ROWS = 160;
+// of 128, 32 sequences of 1000 to 8000 tokens 59 us, 4.7 TB/s (a wave that took its keys once and the rows from HBM 103; with a look into the
+// table at every step 66; pieces of 128 keys to the workgroups in turn, for the sake of the shorter sequences, nothing).
+constexpr int STREAM_ROWS = 160, STREAM_KEYS = 4096;               // rows that fit; keys of a workgroup at most
 template <int HDIM>
 __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
   constexpr int HS = HDIM / 32, CH = HDIM / 8;                     // 16-byte chunks of a row
@@ -259,10 +260,16 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
     float old;                                                     // the weight so far (of the lane's key, lanes 0 .. 31)
     uint32_t id[2];
   };
+  // all blocks that the wave will ask for, two of a step to a pair of lanes: looked up step by step, each would be waited for
+  constexpr int STEP = 4 * 2 * WPAGE;
+  static_assert(STREAM_KEYS <= 32 * STEP, "a lane's block each");
+  const int32_t blocks = bt[min((key0 + (lane >> 1) * STEP) / WPAGE + (lane & 1), (end - 1) / WPAGE)];
+  const int first = key0;
   const auto load = [&](int key, Keys& t) {
+    const int at = min((key - first) / STEP, 31) * 2;              // (past the range: another page of it, that nobody uses)
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      t.id[p] = (uint32_t)bt[min(key / WPAGE + p, (end - 1) / WPAGE)];
+      t.id[p] = (uint32_t)__builtin_amdgcn_readlane(blocks, at + p);
       const f16_t* page = static_cast<const f16_t*>(a.kv.k) + ((size_t)min(t.id[p], (uint32_t)a.kv.num_blocks - 1u) * a.Hkv + kvh) * (HDIM * WPAGE);
 #pragma unroll
       for (int s = 0; s < HS; ++s)
@@ -343,7 +350,6 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
       if (key >= w.base) a.born[line + key] = (a.seen ? a.seen[b] : w.base) + key - w.base;
     }
   };
-  constexpr int STEP = 4 * 2 * WPAGE;
   for (; key0 < last; key0 += 2 * STEP) {
     load(key0 + STEP, kb);
     work(ka, key0);
@@ -788,7 +794,7 @@ __global__ void __launch_bounds__(256) evict_pages_kernel(EvictArgs a, LayerPage
 // ------------------------------------------------------------------------------------------
 static bool weigh_mfma(const WeighArgs& a) { return a.dtype == MN_DT_BF16 && (a.hd == 64 || a.hd == 128) && a.kv.block_size == WPAGE; }
 constexpr int WEIGH_PAGES = 4;
-constexpr int WEIGH_WGS = 1024;        // to aim for (512, 1024, 2048: 81, 69, 73 us with 9 rows of 64/8 heads, 32 sequences of 1000 to 8000 tokens)
+constexpr int WEIGH_WGS = 512;         // to aim for: two a CU.  40 heads, 4 sequences of 2000 tokens, 64 rows: 21.6 us, 1024: 27.2, 2048: 41.9
 
 struct WeighShape {
   int keys;                            // of a workgroup
@@ -799,13 +805,13 @@ static WeighShape weigh_shape(const WeighArgs& a) {
   const long heads = (long)a.B * a.Hkv, R = (long)a.max_q * (a.H / a.Hkv);
   if (!weigh_mfma(a)) return R > 64 ? WeighShape{16, false, true, 4} : WeighShape{64, false, false, 4};
   // The rows stay and the keys go by, or the other way round.  Over 64 rows the first pays where keys are many: 128 rows of 64/8 heads, 32
-  // sequences of 4000 tokens 76 us (rows going by: 116), of 40 heads, 4 of 2000 tokens 36 (43), 8 of 500 tokens 38 (29); of 64/8 heads, 8 of
-  // 2000 tokens 26 (21), their 64 rows 18 (17).
-  if (R <= 64 || (R <= STREAM_ROWS && heads * a.max_ctx >= 256 * WEIGH_WGS)) {
+  // sequences of 4000 tokens 63 us (rows going by: 116), of 40 heads, 4 of 2000 tokens 28 (43), 8 of 500 tokens 25 (29); of 64/8 heads, 8 of
+  // 2000 tokens 25 (21), their 64 rows 17 (17).
+  if (R <= 64 || (R <= STREAM_ROWS && heads * a.max_ctx >= 288 * WEIGH_WGS)) {
     // ranges of 128 keys (two pages for each wave) and more
     long keys = (long)a.max_ctx * heads / WEIGH_WGS / 128 * 128;
     if (keys < 128) keys = 128;
-    if (keys > 4096) keys = 4096;
+    if (keys > STREAM_KEYS) keys = STREAM_KEYS;
     return WeighShape{(int)keys, true, false, 4};
   }
   const int each = WEIGH_PAGES * WPAGE;

@@ -127,7 +127,8 @@ def test_weights_of_many_sequences(count):
 def test_long_contexts_and_prompts():
     for H, Hkv, hd, kind, ctx, ks in ((16, 2, 128, "f16", [9000], [8]), (4, 2, 128, "f16", [0, 300], [1500, 700]), (2, 2, 64, "f32", [0], [900]),
                                       (6, 2, 128, "f16", [40, 0], [350, 1]), (40, 40, 128, "f16", [700] * 8, [200] * 8), (12, 12, 64, "f16", [700, 3] * 8, [100, 230] * 8),
-                                      (16, 2, 64, "f16", [0], [5000]), (40, 40, 128, "f16", [900, 11] * 4, [120, 150] * 4), (8, 8, 64, "f16", [0], [1100])):
+                                      (16, 2, 64, "f16", [0], [5000]), (40, 40, 128, "f16", [900, 11] * 4, [120, 150] * 4), (8, 8, 64, "f16", [0], [1100]),
+                                      (8, 8, 64, "f16", [9000] * 14 + [8200, 17] + [9100] * 16, [1] * 31 + [0])):
         x = Weighed(H, Hkv, hd, kind, ctx, ks, 6)
         assert x.weigh() == 0
         x.check_weights()
