@@ -282,20 +282,20 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
   bool careful = false;
   for (int i = tid; i < tiles * 16 * CH; i += 256) {               // chunks of a row change places, so that 16 rows' meet every bank
     const int r = i / CH, ch = i % CH, at = r * CH + (ch ^ (HDIM == 128 ? r & 15 : (r >> 1 & 7)));
-    u32x4 x = {0, 0, 0, 0};
-    if (r < R) {
-      const int j = token_of(r);
-      const size_t mh = (size_t)(w.row0 + j) * a.H + kvh * G + r - j * G;
-      x = *reinterpret_cast<const u32x4*>(static_cast<const f16_t*>(a.q) + mh * HDIM + ch * 8);
-      if (ch == 0) {
+    // (past the last row that one once more, of no weight: zeros for a query would make no number of an infinity in a key)
+    const int rr = min(r, R - 1), j = token_of(rr);
+    const size_t mh = (size_t)(w.row0 + j) * a.H + kvh * G + rr - j * G;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const f16_t*>(a.q) + mh * HDIM + ch * 8);
+    if (ch == 0) {
+      if (r < R) {
         const float2 st = *reinterpret_cast<const float2*>(a.stats + mh * 2);
         s_start[r] = row_start(st, careful);
         s_m[r] = st.x;
         s_share[r] = row_share(st);
+      } else {
+        s_start[r] = -INFINITY;
+        s_m[r] = s_share[r] = 0.f;
       }
-    } else if (ch == 0) {
-      s_start[r] = -INFINITY;
-      s_m[r] = s_share[r] = 0.f;
     }
     *reinterpret_cast<u32x4*>(s_q + at * 8) = x;
   }

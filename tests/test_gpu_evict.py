@@ -184,6 +184,35 @@ def test_rows_without_statistics_give_nothing():
     assert odd.sum() <= 1 and torch.equal(x.ledger.mass[~odd & (torch.arange(x.width, device="cuda") != 36)], whole[~odd & (torch.arange(x.width, device="cuda") != 36)])
 
 
+@pytest.mark.parametrize("H,Hkv,hd,kind,ctx,ks", [
+    (64, 8, 128, "f16", [300, 40, 5], [0, 1, 2]), (40, 40, 128, "f16", [100, 33], [0, 15]), (12, 12, 64, "f16", [70, 64], [0, 4]), (6, 2, 64, "f16", [50, 9], [3, 19]),
+    (16, 2, 128, "f16", [9000], [8]), (8, 2, 128, "f16", [60, 5], [100, 15]), (12, 12, 64, "f16", [20, 100], [79, 128]), (40, 40, 128, "f16", [700] * 8, [200] * 8),
+    (64, 8, 64, "f16", [900, 9] * 20, [150, 11] * 20), (4, 2, 64, "f32", [40, 7], [2, 9]), (8, 2, 128, "f32", [100], [50]), (8, 8, 8, "f32", [33, 4], [0, 90]),
+    (8, 2, 256, "f16", [50, 60], [0, 30]), (8, 8, 32, "f16", [64], [3])], ids=str)
+def test_infinite_keys_that_no_row_looks_at_weigh_nothing(H, Hkv, hd, kind, ctx, ks):
+    """An infinity in a key whose every score is minus infinity is a key with a score of -10^4: no weight, and the others as they were, whatever the number
+    of rows (multiples of 16 and others, of a KV head, in every kernel)."""
+    x = Weighed(H, Hkv, hd, kind, ctx, ks, 12)
+    low, high = 3, hd - 2                                           # elements that all queries have below -1, above 1
+    x.q[:, :, low], x.q[:, :, high] = -1 - x.q[:, :, low].abs(), 1 + x.q[:, :, high].abs()
+
+    def plant(value):
+        for b, c in enumerate(ctx):
+            for slot, e, v in ((1, low, value), (c, high, -value), (x.tot[b] - 1, low, value)):   # behind all rows, the first row's, the last row's
+                x.kp[int(x.full[b, slot // 16]), :, e // 8, slot % 16, e % 8] = v
+    plant(60000.0)
+    _, status = x.run(stats=x.stats)
+    assert status == 0 and x.weigh() == 0
+    mass, born, stats = x.ledger.mass.clone(), x.ledger.born.clone(), x.stats.clone()
+    plant(math.inf)
+    _, status = x.run(stats=x.stats)
+    assert status == 0 and torch.equal(x.stats, stats)
+    assert x.weigh() == 0
+    assert torch.isfinite(x.ledger.mass).all() and torch.equal(x.ledger.mass, mass) and torch.equal(x.ledger.born, born)
+    for b, c in enumerate(ctx):
+        assert torch.equal(x.ledger.mass[0, b, :, 1], x.mass0[0, b, :, 1]) and (x.ledger.mass[0, b, :, [c, x.tot[b] - 1]] == 0).all()
+
+
 def test_damage_is_left_out_of_the_weights():
     from paper_2402_15678_amd import binding, harness
     x = Weighed(8, 2, 128, "f16", [100, 20, 40], [3, 2, 0], 8)
