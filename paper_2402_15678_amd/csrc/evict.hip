@@ -471,7 +471,7 @@ __device__ __forceinline__ bool evicted(const EvictArgs& a, int b, int n, int ke
   bool bad = false, shared = false;
   if (flags == 0) {
     const int32_t* row = p.tables + (size_t)b * p.width;
-    const int first = min(a.sinks, keep) / bs, last = (keep + bs - 1) / bs;   // blocks that may be written
+    const int first = a.sinks / bs, last = (int)(((long)keep + bs - 1) / bs);   // blocks that may be written, if any
     for (int i = threadIdx.x; i < held; i += blockDim.x) {
       const uint32_t id = (uint32_t)row[i];
       if (id >= (uint32_t)p.num_blocks) bad = true;

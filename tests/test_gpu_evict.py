@@ -375,6 +375,21 @@ def test_sharers_and_damage_are_left_alone():
         x.kv.block_tables[2], x.pool.seq_blocks[2], x.kv.ctx_lens[2] = good[2], held[2], ctx[2]
 
 
+def test_a_shared_block_among_the_first_tokens_is_no_hindrance():
+    """All that stays are first tokens: nothing moves, and who shares their blocks goes on reading them; the next token gets a block of its own."""
+    x = Cache(2, 64, "f16", 2, [200, 0], 13)
+    x.pool.fork(torch.tensor([0], dtype=torch.int32, device="cuda"), torch.tensor([1], dtype=torch.int32, device="cuda"))
+    x.mass[:, 1], x.born[:, 1] = x.mass[:, 0], x.born[:, 0]
+    s = x.snapshot()
+    assert x.evict([90, -1], 100, 3) == 0                           # blocks 0 .. 5 stay, the last with 10 tokens; the first 100 tokens are in blocks 0 .. 6
+    x.check(x.want(s, [90, -1], 100, 3))
+    x.pool.reserve(torch.tensor([91, 0], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    table = x.kv.block_tables.tolist()
+    assert x.pool.dev_status.item() == 0 and table[0][:5] == table[1][:5] and table[0][5] != table[1][5] and x.pool.block_refs[table[0][5]].item() == 1
+    assert torch.equal(x.k[:, table[0][5]], x.k[:, table[1][5]]) and torch.equal(x.v[:, table[0][5]], x.v[:, table[1][5]])
+
+
 def test_more_layers_than_a_launch_holds():
     x = Cache(1, 16, "f32", 100, [60, 33], 4)
     s = x.snapshot()
