@@ -6,6 +6,7 @@ Importing this module fails loudly if the library has not been built
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -186,7 +187,12 @@ def ptr_array(ptrs: Sequence[Optional[int]]):
 
 
 def host_i32(values: Sequence[int]):
-    return (C.c_int32 * max(1, len(values)))(*[int(v) for v in values])
+    n = len(values)
+    try:
+        # (64 numbers one by one: 7 us of a call's 10)
+        return (C.c_int32 * max(1, n))(*values) if n < 8 else (C.c_int32 * n).from_buffer(array.array("i", values))
+    except (TypeError, OverflowError):                               # numbers of other types
+        return (C.c_int32 * max(1, n))(*[int(v) for v in values])
 
 
 def mn_create(desc: ModelDesc, weights: Weights) -> int:

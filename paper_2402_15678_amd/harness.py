@@ -247,6 +247,11 @@ class PrefixSession:
         return out
 
 
+def _numbers(t: Optional[torch.Tensor], n: int, device: int) -> bool:
+    """Whether t, if it is there, has a number for each of n sequences, as the calls read them."""
+    return t is None or (t.dtype is torch.int32 and t.numel() >= n and t.get_device() == device and t.is_contiguous())
+
+
 class RowRule:
     """How projected rows are made ready: rot_dim elements of a head turned, pairs[a] of their pairs by the position on axis a, and norms
     per head where there are gains."""
@@ -257,6 +262,9 @@ class RowRule:
         for g in (q_gain, k_gain):
             assert g is None or (g.dtype == torch.float32 and g.is_contiguous())
         self.gains, self.n_axes = (q_gain, k_gain), len(pairs)      # (keeps the tensors alive)
+        at = [(g.numel(), g.get_device()) for g in self.gains if g is not None]
+        assert len(set(at)) <= 1
+        self.at = at[0] if at else None                             # the gains' elements, and device
         self.c = B.RowRule(q_gain.data_ptr() if q_gain is not None else None, k_gain.data_ptr() if k_gain is not None else None, eps, rot_dim,
                            len(pairs), (C.c_int * B.MN_MAX_AXES)(*pairs), base)
 
@@ -273,8 +281,11 @@ def qk_norm_rope(model: DeviceModel, q: torch.Tensor, k: torch.Tensor, v: torch.
     assert (kind is act or kind is torch.float32) and kind is k.dtype and kind is v.dtype
     assert q.shape == (M, H, hd) and k.shape == (M, Hk, hd) and v.shape == (M, Hk, hd) and qs[1:] == ks[1:] == vs[1:] == (hd, 1)
     assert positions is None or (positions.dtype is torch.int32 and positions.numel() == rule.n_axes * M and positions.is_contiguous())
+    dev = q.get_device()
+    assert k.get_device() == dev == v.get_device() and (positions is None or positions.get_device() == dev) and _numbers(spec_len, n, dev)
+    assert rule.at is None or rule.at == (hd, dev)
     for t, heads in ((q_out, H), (k_out, Hk), (v_out, Hk)):
-        assert t is None or (t.dtype is act and t.numel() == M * heads * hd and t.is_contiguous())
+        assert t is None or (t.dtype is act and t.numel() == M * heads * hd and t.is_contiguous() and t.get_device() == dev)
     B.mn_qk_norm_rope(model.ctx, q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0], kind is torch.float32, rule.c,
                       None if positions is None else positions.data_ptr(), None if spec_len is None else spec_len.data_ptr(),
                       B.host_i32(h_spec_len), n, None if kv is None else kv.c, layer, None if q_out is None else q_out.data_ptr(),
@@ -301,8 +312,12 @@ class WindowSession:
         [rows][H][2], for KVLedger.weigh."""
         assert q.is_contiguous() and out.is_contiguous() and out.dtype is q.dtype is activation_type(self.model.desc)
         assert stats is None or (stats.dtype is torch.float32 and stats.is_contiguous())
-        assert len(h_spec_len) == 0 or max(h_spec_len) < self.max_q
-        B.mn_window_attention(self.model.ctx, q.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len), self.window,
+        n, d, dev = len(h_spec_len), self.model.desc, self.workspace.get_device()
+        assert n == 0 or max(h_spec_len) < self.max_q
+        heads = (sum(h_spec_len) + n) * d.n_heads                    # of all rows: the calls could not tell if there were fewer
+        assert q.numel() >= heads * d.head_dim <= out.numel() and (stats is None or (stats.numel() >= 2 * heads and stats.get_device() == dev))
+        assert q.get_device() == dev == out.get_device() and _numbers(spec_len, n, dev)
+        B.mn_window_attention(self.model.ctx, q.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), n, self.window,
                               self.sinks, self.max_ctx, self.kv.c, layer, out.data_ptr(), stats.data_ptr() if stats is not None else None,
                               self.workspace.data_ptr(), self.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
         return out
@@ -314,7 +329,7 @@ class KVLedger:
 
     def __init__(self, model: DeviceModel, kv: DeviceKV, mass: torch.Tensor, born: torch.Tensor):
         assert mass.dtype == torch.float32 and born.dtype == torch.int32 and mass.is_contiguous() and born.is_contiguous()
-        assert mass.shape == born.shape and mass.shape[0] == max(1, model.desc.n_layers) and mass.shape[2] == model.desc.n_kv_heads
+        assert mass.device == born.device and mass.shape == born.shape and mass.shape[0] == max(1, model.desc.n_layers) and mass.shape[2] == model.desc.n_kv_heads
         self.model, self.kv, self.mass, self.born = model, kv, mass, born
         self.c = B.Ledger(mass.data_ptr(), born.data_ptr(), mass.shape[1], mass.shape[3])
         self.dev_status = torch.zeros((1,), dtype=torch.int32, device=mass.device)
@@ -332,7 +347,11 @@ class KVLedger:
         """Adds up the weights that the rows gave (stats: as WindowSession.attention left them without a window); n_out: behind the commit,
         the rows that it accepted; seen: the texts' tokens before the rows."""
         assert q.is_contiguous() and q.dtype == activation_type(self.model.desc) and stats.is_contiguous() and stats.dtype == torch.float32
-        B.mn_kv_weigh(self.model.ctx, q.data_ptr(), stats.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), len(h_spec_len),
+        n, d, dev = len(h_spec_len), self.model.desc, self.mass.get_device()
+        heads = (sum(h_spec_len) + n) * d.n_heads
+        assert q.numel() >= heads * d.head_dim and stats.numel() >= 2 * heads and q.get_device() == dev == stats.get_device()
+        assert _numbers(spec_len, n, dev) and _numbers(n_out, n, dev) and _numbers(seen, n, dev)
+        B.mn_kv_weigh(self.model.ctx, q.data_ptr(), stats.data_ptr(), spec_len.data_ptr(), B.host_i32(h_spec_len), n,
                       n_out.data_ptr() if n_out is not None else None, seen.data_ptr() if seen is not None else None, max_ctx, self.kv.c,
                       layer, self.c, self.dev_status.data_ptr(), stream_ptr())
 
@@ -390,6 +409,7 @@ class KVPool:
     def evict(self, keep: torch.Tensor, sinks: int, recent: int, ledger: KVLedger) -> None:
         """Slots 0 .. len(keep) - 1 are cut back to keep[b] tokens: the first `sinks`, the `recent` newest, and those with the most weight
         in the ledger."""
+        assert _numbers(keep, 0, ledger.mass.get_device())
         B.mn_kv_evict(self.model.ctx, self.kv.c, self.c, keep.data_ptr(), keep.numel(), sinks, recent, ledger.c, ledger.workspace.data_ptr(),
                       ledger.ws_bytes, self.dev_status.data_ptr(), stream_ptr())
 

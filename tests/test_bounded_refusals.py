@@ -2,6 +2,7 @@
 import ctypes as C
 from types import SimpleNamespace
 
+import numpy as np
 import pytest
 import torch
 
@@ -175,3 +176,64 @@ def test_rows_of_another_type_or_shape_are_refused(dtype, right, monkeypatch):
                  lambda: harness.KVLedger(model, None, new(torch.float32, 1, 1, 2, 32), new(torch.int32, 1, 1, 2, 31))):
         with pytest.raises(AssertionError):
             call()
+
+
+def test_too_few_rows_and_numbers_of_another_type_or_device_are_refused(monkeypatch):
+    """The library gets addresses: rows that are not there would be read, 64-bit numbers taken as pairs, a host's address as the device's."""
+    d = synth.ModelDesc(synth.ARCH_LLAMA, synth.DT_BF16, 1, 128, 2, 2, 64, 128, 8, 64)
+    model, calls = SimpleNamespace(desc=d, ctx=None), []
+
+    class Far(torch.Tensor):
+        def get_device(self):
+            return 3
+    for name in ("mn_qk_norm_rope", "mn_window_attention", "mn_kv_weigh", "mn_kv_evict"):
+        monkeypatch.setattr(harness.B, name, lambda *a, name=name: calls.append(name))
+    monkeypatch.setattr(harness, "stream_ptr", lambda: 0)
+    half, whole = torch.float16, torch.float32
+    new = lambda t, *s, far=False: torch.zeros(s, dtype=t).as_subclass(Far if far else torch.Tensor)  # noqa: E731
+    i32 = lambda n, t=torch.int32, far=False: torch.zeros(n, dtype=t).as_subclass(Far if far else torch.Tensor)  # noqa: E731
+    ses = harness.WindowSession.__new__(harness.WindowSession)
+    ses.model, ses.kv, ses.max_q, ses.max_ctx, ses.window, ses.sinks, ses.ws_bytes = model, SimpleNamespace(c=None), 3, 32, 8, 0, 0
+    ses.workspace = ses.dev_status = torch.zeros(1, dtype=torch.int32)
+    ledger = harness.KVLedger(model, SimpleNamespace(c=None), new(whole, 1, 2, 2, 32), i32((1, 2, 2, 32)))
+    pool = harness.KVPool.__new__(harness.KVPool)
+    pool.model, pool.kv, pool.c, pool.dev_status = model, SimpleNamespace(c=None), None, i32(1)
+
+    def rows(gain=64, spec=i32(2), pos=i32((1, 5)), k=False, out=False):
+        rule = harness.RowRule(64, [32], 10000.0, new(whole, 64), new(whole, gain))
+        harness.qk_norm_rope(model, new(half, 5, 2, 64), new(half, 5, 2, 64, far=k), new(half, 5, 2, 64), rule, pos, spec, [2, 1], new(half, 5, 128, far=out))
+
+    def window(n=5, m=5, k=5, spec=i32(2), q=False, stats=False):
+        ses.attention(new(half, n, 2, 64, far=q), spec, [2, 1], new(half, m, 128), stats=new(whole, k, 2, 2, far=stats))
+
+    def weigh(n=5, k=5, spec=i32(2), n_out=None, seen=None, q=False, stats=False):
+        ledger.weigh(new(half, n, 2, 64, far=q), new(whole, k, 2, 2, far=stats), spec, [2, 1], 0, 32, n_out, seen)
+
+    def evict(keep):
+        pool.evict(keep, 1, 1, ledger)
+    rows()
+    window()
+    window(n=6, m=7, k=8)                                            # (buffers of a larger batch)
+    weigh(n_out=i32(2), seen=i32(3))
+    evict(i32(2))
+    evict(i32(0))
+    assert calls == ["mn_qk_norm_rope"] + ["mn_window_attention"] * 2 + ["mn_kv_weigh"] + ["mn_kv_evict"] * 2
+    wrong = (i32(1), i32(2, torch.int64), i32(2, whole), i32(4)[::2], i32(2, far=True))
+    bad = [lambda s=s, c=c: c(spec=s) for s in wrong for c in (rows, window, weigh)] + [lambda s=s, k=k: weigh(**{k: s}) for s in wrong for k in ("n_out", "seen")]
+    bad += [lambda s=s: evict(s) for s in wrong[1:]]
+    bad += [lambda kw=kw: rows(**kw) for kw in (dict(gain=32), dict(gain=128), dict(pos=i32((1, 5), far=True)), dict(k=True), dict(out=True))]
+    bad += [lambda kw=kw: window(**kw) for kw in (dict(n=4), dict(m=4), dict(k=4), dict(q=True), dict(stats=True))]
+    bad += [lambda kw=kw: weigh(**kw) for kw in (dict(n=4), dict(k=4), dict(q=True), dict(stats=True))]
+    bad += [lambda: harness.KVLedger(model, None, new(whole, 1, 1, 2, 32), i32((1, 1, 2, 32)).to("meta"))]
+    for call in bad:
+        with pytest.raises(AssertionError):
+            call()
+    assert len(calls) == 6
+
+
+@pytest.mark.parametrize("n", [0, 1, 7, 8, 9, 4096])
+def test_host_numbers_of_every_kind(n, binding):  # noqa: F811
+    want = [i * 7 - 3 for i in range(n)]
+    for values in (want, tuple(want), np.array(want, np.int64), [np.int32(v) for v in want], [float(v) for v in want], np.array(want, np.float32)):
+        got = binding.host_i32(values)
+        assert list(got)[:n] == want and len(got) >= 1
