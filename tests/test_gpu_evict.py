@@ -324,6 +324,16 @@ def test_eviction_matches_the_lists(Hkv, hd, kind, layers, bs, n, keep, sinks, r
     x.check(x.want(s, keep, sinks, recent))
 
 
+@pytest.mark.parametrize("Hkv,hd,kind", [(2, 128, "f32"), (2, 256, "f16"), (3, 32, "f16"), (1, 8, "f16")])
+@pytest.mark.parametrize("n,keep,sinks,recent", [([100, 64, 1, 65], [64, 63, 64, 64], 4, 16), ([300, 17], [16, 1], 0, 0), ([700, 129], [513, 128], 20, 100)], ids=str)
+def test_pages_of_every_size_are_evicted(Hkv, hd, kind, n, keep, sinks, recent):
+    """Pages of 256 bytes, 1 KB and 8 KB: what a wave takes in part of one turn, in one, and in two."""
+    x = Cache(Hkv, hd, kind, 2, n, Hkv + hd)
+    s = x.snapshot()
+    assert x.evict(keep, sinks, recent) == 0
+    x.check(x.want(s, keep, sinks, recent))
+
+
 @pytest.mark.parametrize("n", [1000, 4096, 5000, 9000, 20000])
 def test_long_contexts_are_evicted_again_and_again(n):
     """By half, by one, by a few, and to the last protected one."""
@@ -504,3 +514,77 @@ def test_a_life_in_a_bounded_cache(H, Hkv, hd, kind):
                 held[b][h] = t[:budget]
         assert kv.ctx_lens.tolist() == [len(held[b][0]) for b in range(B)]
         assert pool.seq_blocks.tolist() == [max(-(-len(held[b][0]) // bs), 0) if len(held[b][0]) == budget else pool.seq_blocks[b].item() for b in range(B)]
+
+
+@pytest.mark.parametrize("H,Hkv,hd,kind,lens", [(8, 2, 128, "f16", (3, 0, 8)), (12, 12, 64, "f16", (20, 1, 70)), (4, 2, 64, "f32", (4, 2, 0)), (8, 2, 256, "f16", (9, 0, 1))], ids=str)
+def test_steps_are_captured_and_replayed(H, Hkv, hd, kind, lens):
+    """Room, rows, attention, commit, weights and eviction of a step in one graph: replayed over changing contexts it leaves, bit for bit, what the calls leave
+    that are made one by one."""
+    from paper_2402_15678_amd import harness
+    B, budget, bs, nb, width, steps = len(lens), 90, 16, 40, 12, 5
+    d = synth.ModelDesc(synth.ARCH_LLAMA, synth.DT_BF16 if kind == "f16" else synth.DT_F32, 1, 128, H, Hkv, hd, 128, 8, 1 << 16)
+    model, M = harness.DeviceModel.random_on_device(d, 1), sum(lens) + B
+    ctx0 = [70, 0, 88]
+    table = np.full((B, width), -1, np.int32)
+    for b, c in enumerate(ctx0):
+        table[b, :-(-c // bs)] = np.arange(-(-c // bs)) + 6 * b
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    draw = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    k0, v0 = draw(nb, Hkv, hd // 8, bs, 8).to(DT[kind]), draw(nb, Hkv, hd, bs).to(DT[kind])
+    kv = harness.DeviceKV(d, bs, nb, table, ctx0, [k0.clone()], [v0.clone()])
+    pool = harness.KVPool.from_tables(model, kv)
+    ledger = harness.KVLedger.empty(model, kv, B, width * bs)
+    ledger.mass.copy_(torch.rand(ledger.mass.shape, generator=g, device="cuda"))
+    ledger.born.copy_(torch.arange(width * bs, dtype=torch.int32, device="cuda").expand(ledger.born.shape))
+    rule = harness.RowRule(hd, [hd // 2], 10000.0, 1 + 0.1 * draw(hd), 1 + 0.1 * draw(hd))
+    ses = harness.WindowSession(model, kv, B, M, max(lens) + 1, width * bs, width * bs, 0)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    qkv, place, took, seen, spec, keep = draw(M, H + 2 * Hkv, hd), i32([[0] * M]), i32([0] * B), i32(ctx0), i32(lens), i32([budget] * B)
+    room = i32([0] * B)
+    q, out, stats = (torch.zeros(s, dtype=t, device="cuda") for s, t in (((M, H, hd), DT[kind]), ((M, H * hd), DT[kind]), ((M, H, 2), torch.float32)))
+
+    def step():
+        torch.add(kv.ctx_lens, spec, out=room)
+        room.add_(1)
+        pool.reserve(room)
+        harness.qk_norm_rope(model, qkv[:, :H], qkv[:, H:H + Hkv], qkv[:, H + Hkv:], rule, place, spec, lens, q, kv=kv, dev_status=pool.dev_status)
+        ses.attention(q, spec, lens, out, stats=stats)
+        kv.ctx_lens.add_(took)
+        ledger.weigh(q, stats, spec, lens, 0, width * bs, took, seen)
+        seen.add_(took)
+        pool.evict(keep, 3, 20, ledger)
+    state = (kv.k_pages[0], kv.v_pages[0], ledger.mass, ledger.born, pool.state, seen, q, out, stats)
+    start = [t.clone() for t in state]
+    r = np.random.default_rng(4)
+    inputs = [(draw(M, H + 2 * Hkv, hd), [int(r.integers(0, 5000)) for _ in range(M)], [int(r.integers(1, k + 2)) for k in lens]) for _ in range(steps)]
+
+    def run(go):
+        for t, old in zip(state, start):
+            t.copy_(old)
+        left, ctx = [], list(ctx0)
+        for rows, at, n in inputs:
+            qkv.copy_(rows)
+            place.copy_(i32([at]))
+            took.copy_(i32(n))
+            go()
+            torch.cuda.synchronize()
+            assert pool.dev_status.item() == 0 and ses.dev_status.item() == 0 and ledger.dev_status.item() == 0
+            held = [-(-(c + k + 1) // bs) for c, k in zip(ctx, lens)]  # (a slot keeps the room of rows that were not accepted)
+            held = [max(h, o) for h, o in zip(held, left[-1][1])] if left else held
+            ctx = [c + m for c, m in zip(ctx, n)]
+            held = [-(-budget // bs) if c > budget else h for c, h in zip(ctx, held)]
+            ctx = [min(c, budget) for c in ctx]
+            assert kv.ctx_lens.tolist() == ctx and pool.seq_blocks.tolist() == held
+            left.append(([t.clone() for t in state], held))
+        return left
+    want = run(step)
+    assert max(want[-1][0][5].tolist()) > budget                    # (somebody was cut back)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for a, b in zip(run(graph.replay), want):
+        for x, y in zip(a[0], b[0]):
+            assert torch.equal(x, y)
