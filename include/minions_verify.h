@@ -478,7 +478,7 @@ mn_status mn_prefix_attention(mn_ctx *ctx, const void *q, const int32_t *spec_le
  * Rows are put into the cache at positions that the caller gives (mn_qk_norm_rope), and then either attention looks back a window and
  * at the first few tokens (mn_window_attention), or it sees everything, the weight that it gives to every cached token is added up
  * (mn_kv_weigh), and the tokens with the least of it are evicted (mn_kv_evict).  A window goes by the order of the slots, which an
- * eviction gives up: the two are for different sequences. */
+ * eviction gives up: the two are for different sequences, and no call looks for a mixture. */
 
 /* How a head's rows are made ready.  Gains NULL: not normed.  The first rot_dim elements are turned, in pairs (i, i + rot_dim / 2), by
  * p * base^(-2i / rot_dim), p the row's position on the pair's axis: the first pairs[0] pairs belong to axis 0, the next pairs[1] to

@@ -11,7 +11,8 @@
 //  * Keys and values: a workgroup takes the 16 slots of the cache that a page of 16 tokens is, writes them as the page lies into the LDS, and
 //    copies whole pieces of 16 bytes out.  Straight from the rows a value is two bytes of a 32-byte sector.
 // Bound by HBM where rows are many: prompts of 500 to 3000 tokens of 64/8 heads of 128 70 us, 294 MB at 4.2 TB/s (a copy: 4.6).  9 rows of 64
-// sequences (fp32 rows, 35 MB) 14 us, half of them the way in: the batch's lengths, a row's loads, a head's sum.  4 rows of 12 heads 6 us, that alone.
+// sequences (fp32 rows, 35 MB) 14 us: the way in (the batch's lengths, a row's loads, a head's sum) beside the bytes, and work on heads that are not
+// kept: a wave asks for and norms as many heads as AT_ONCE loads hold, 16 there, whatever its share is, there 12.  4 rows of 12 heads 6 us, the way in alone.
 #include "launch.h"
 #include "tune.h"
 #include "../../include/minions_verify.h"

@@ -90,7 +90,7 @@ __device__ __forceinline__ void put_weight(const WeighArgs& a, const Weighed& w,
 
 constexpr int WPAGE = 16;
 // Exponent that a row's scores start from, -(m + log2 l), and whether its weights need more care than 2^(c s + that): statistics that are
-// no numbers (its scores may be none either), and references from 2^8 on, whose sum with log2 l is rounded by more than 2^-17.
+// no numbers (its scores may be none either), and references from 2^8 on, whose sum with log2 l is rounded by 2^-16 and more.
 __device__ __forceinline__ float row_start(float2 st, bool& careful) {
   careful |= !(st.y >= 0x1p-120f) | !(st.y < INFINITY) | !(__builtin_fabsf(st.x) < 0x1p8f);
   return -st.x - __builtin_amdgcn_logf(st.y);
@@ -360,8 +360,9 @@ __global__ void __launch_bounds__(256, 3) weigh_stream_kernel(WeighArgs a) {
 }
 
 // A wave takes 16 keys, and the rows that see them in tiles of 16, on the fp32 instruction; ROWS: all waves the same keys and every fourth tile
-// (3 prompts of 600 rows of 8/2 heads of 256: 78 us, keys shared out 488).  Products and their order are the attention's own.  Bound by that
-// instruction, and with few rows by launch.
+// (3 prompts of 600 rows of 8/2 heads of 256: 80 us, keys shared out 488).  Products and their order are the attention's own.  Bound by their
+// chain, each product waiting for the one before, and by the workgroups of a sequence's first keys, which walk all its rows (the instruction's rate
+// alone would be 14 us; 8 prompts of 200 rows of 8/2 fp32 heads of 128 19 and 2); with few rows by the chain and launch.
 // The products are those of the attention, factor for factor and in its order (as they are in the fp16 kernels): beyond 2^24 a
 // reference is only as good as the very score that it came from.
 template <typename T, int HDP, bool ROWS>
@@ -703,7 +704,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(EvictArgs a, LayerPages
 // places alone the writes were parts of lines: 16 sequences of 1000 to 4000 tokens cut to 1024, 8 layers of 8 heads of 128, 505 us; now
 // 391.)  A piece of 16 bytes is (part of) one token of K, or PER tokens of one element of V; NU of them per lane.  What is next is looked up
 // meanwhile.  Bound by HBM: a page's lines hold pieces of 4 to 8 of its tokens, so nearly every line of the pages that tokens come from and go to
-// passes, 1.8 GB at 4.6 TB/s, which is what a copy reaches; the tokens that move alone would be 0.66 GB.
+// passes, 1.8 GB at 4.6 TB/s, which is what a copy reaches; the tokens that move alone would be 0.66 GB.  In two turns for pages of 8 KB (2 fp32 heads of 128,
+// fp16 of 256): 213 and 218 us, 0.92 GB at 4.3 TB/s.
 template <typename T, int NU>
 __global__ void __launch_bounds__(256) evict_pages_kernel(EvictArgs a, LayerPages pages, int layer0, int release) {
   constexpr int PER = 16 / sizeof(T), BS = 16, AT_ONCE = NU < 4 ? NU : 4;

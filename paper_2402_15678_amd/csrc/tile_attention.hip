@@ -1404,11 +1404,12 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixMerge p, T* __r
 // A row tile's keys are a list of granules (Look), in one range where the tiles fill the chip by themselves: the workgroup then writes
 // the rows' outputs, and there is no second launch.  Otherwise in several, whose parts window_merge_kernel puts together.
 // One row of 24 sequences behind 4096 tokens of 64/8 heads of 128: 63 us, 385 MB at 6.1 TB/s, and 5 for the merge.  Chunks of 1500 to 2500 tokens
-// behind 8192: 1080 us, 1.02 PFLOP/s, the matrix pipe's.  Four prompts of 1500 to 6000 tokens, 40 heads, a window of 1024: 386 us, 0.66 PFLOP/s: a
-// tile of 128 rows meets 1152 keys of which a row sees 1024, whole granules of the first ones, and pays its way in and out for 18 steps.
+// behind 8192: 1080 us, 1.02 PFLOP/s, the matrix pipe's.  Four prompts of 1500 to 6000 tokens, 40 heads, a window of 1024: 380 us, 0.67 PFLOP/s: the
+// tiles' steps are 278 GFLOP for 256 of visible pairs (273 us at the chunks' rate), and 4480 workgroups pay their way in and out for 18 double steps each.
 //
 // window_plan_kernel (one workgroup; more than 64 sequences): the tiles' records (window_tile), and per row its sequence (-1: takes no part),
-// context, rows and first row.
+// context, rows and first row.  A thread writes its sequence's rows one after the other, and only the merge reads them: 65 prompts of 1000 tokens 44 us
+// ahead of 1120 (40 heads of 128), of 200 tokens 11 ahead of 31 (12 of 64).
 __global__ void __launch_bounds__(1024) window_plan_kernel(WindowPlan p) {
   __shared__ int s_rows[16], s_tiles[16], s_bad;
   const PrefixBatch& c = p.batch;
